@@ -356,6 +356,106 @@ sb_status sb_exchange_step(sb_ctx* ctx, const float* s_up, const float* s_down, 
 sb_status sb_calib_moments_noalloc(void* cuda_stream, const void* X_bf16, int64_t T, int64_t K,
                                    int64_t ldx, float* sumsq, int accumulate, float scale);
 
+/* ---- Microscaled 4-bit floating point -------------------------------------------------------
+ * The formats the tensor cores multiply natively, next to the integer codes of sb_pack_blocks:
+ * e2m1 codes (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) with one scale byte per block of
+ * consecutive columns of a row.
+ *   SB_FP4_MX: blocks of 32, scale e8m0 (2^(byte - 127), 255 = NaN).
+ *   SB_FP4_NV: blocks of 16, scale e4m3 (0x7f = NaN) times one fp32 scale of the whole matrix.
+ * Layout of a matrix [R][C], C' = C rounded up to a multiple of 32:
+ *   codes:  [R][C' / 2] bytes, column 2 i in the low and column 2 i + 1 in the high half of byte
+ *           i of a row; the padding columns hold zeros.  16-byte aligned.
+ *   scales: tiles of 128 rows x 4 blocks, 512 bytes each, row tile by row tile: the scale of
+ *           row r, block j is byte 16 (r % 32) + 4 ((r % 128) / 32) + j % 4 of tile
+ *           (r / 128) * ceil(C' / block / 4) + j / 4; padding rows and blocks hold zeros.
+ *           16-byte aligned, sb_fp4_scale_bytes(R, C, format) bytes.
+ *   tensor_scale: DEVICE fp32 (SB_FP4_NV: NULL = 1; SB_FP4_MX: must be NULL).
+ * Nothing here reads a tensor scale on the host: the calls only enqueue.                      */
+enum { SB_FP4_MX = 0, SB_FP4_NV = 1 };
+int64_t sb_fp4_code_bytes(int64_t R, int64_t C);
+int64_t sb_fp4_scale_bytes(int64_t R, int64_t C, int format);      /* -1: bad arguments       */
+
+/* Quantisation, per block with amax = max |x|:
+ *   SB_FP4_MX: e = clamp(floor(log2 amax) - 2, -127, 127) (amax = 0: -127), d = 2^e;
+ *   SB_FP4_NV: s = e4m3((amax / 6) / g), d = s g  (quotients and product rounded to fp32, e4m3
+ *              round to nearest even, at most 448; g = *tensor_scale);
+ *   code = e2m1(x / d), round to nearest even, at most 6 in magnitude; 0 where d = 0.
+ * A block that holds a NaN or an infinity (or whose scale is not a number: g not positive) gets
+ * the NaN scale and multiplies as NaN.  X: bf16 [R][C], leading dimension ldx (a multiple of 8, at least
+ * C; 16-byte aligned base), C any.  codes and scales are written whole, padding included.    */
+sb_status sb_fp4_quantize(sb_ctx* ctx, const void* X_bf16, int64_t R, int64_t C, int64_t ldx, int format,
+                          const float* tensor_scale, uint8_t* codes, uint8_t* scales);
+/* Y[r][c] = the value the code stands for (code * d as above, rounded once to bf16).
+ * Y: bf16 [R][C], leading dimension ldy >= C, any alignment of its element type.             */
+sb_status sb_fp4_dequantize(sb_ctx* ctx, const uint8_t* codes, const uint8_t* scales, int64_t R, int64_t C,
+                            int format, const float* tensor_scale, void* Y_bf16, int64_t ldy);
+/* Y[m][n] = sum_k A[m][k] B[n][k] on the values both stand for: A [M][K] (activations), B [N][K]
+ * (weights), the same format.  The tensor cores multiply the codes with their block scales
+ * exactly and add in fp32; the tensor scales multiply the sum, which is rounded once.
+ * Y: bf16 (out_f32 = 0) or fp32 (1) [M][N], leading dimension ldy >= N, any alignment of its
+ * element type.  One token (M = 1) to whole prompts; the sums of a call are always taken in the
+ * same order.  A pipeline wait that does not complete within 2 s latches SB_ERR_TIMEOUT.     */
+sb_status sb_fp4_gemm(sb_ctx* ctx, const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale,
+                      int64_t M, const uint8_t* b_codes, const uint8_t* b_scales, const float* b_tensor_scale,
+                      int64_t N, int64_t K, int format, void* Y, int out_f32, int64_t ldy);
+
+/* ---- Key/value cache in 8 bits ----------------------------------------------------------------
+ * A paged cache of int8 or e4m3 codes with one bf16 scale for every SB_KV8_BLOCK tokens and head;
+ * a code stands for code * scale.  All calls take the requests' lengths from device memory and
+ * only enqueue, so a captured graph serves requests that grow.
+ *   starts: device int32 [requests + 1], lens: device int32 [requests].  Request b has lens[b]
+ *   tokens in the cache, of which the last n = starts[b + 1] - starts[b] (0 allowed) are the
+ *   call's own: rows starts[b] .. of its dense arguments.  max_new: at least every n.  Token p of
+ *   request b lives in page table[b][p / page_tokens], slot p % page_tokens.
+ * A request whose numbers do not fit (n < 0 or > max_new, rows outside the dense arguments, lens
+ * < n, more tokens than its table row has pages, a page number outside the cache) is skipped as
+ * far as they do not fit and SB_ERR_INVALID is latched.                                         */
+enum { SB_KV_INT8 = 0, SB_KV_E4M3 = 1, SB_KV8_BLOCK = 16 };
+typedef struct {                /* host struct, read during the call                             */
+    void *k, *v;                /* device codes [pages][heads][page_tokens][dim], 16-byte aligned */
+    void *k_scale, *v_scale;    /* device bf16 [pages][heads][page_tokens / 16]                  */
+    const int32_t* table;       /* device page numbers [requests][table_stride]                  */
+    int64_t table_stride;       /* pages a request may have                                      */
+    int64_t pages;
+    int32_t requests, heads;
+    int32_t page_tokens;        /* a multiple of 16                                              */
+    int32_t dim;                /* a multiple of 16, 16 .. 256                                   */
+    int32_t type;               /* SB_KV_INT8 or SB_KV_E4M3                                      */
+    int32_t reserved;
+} sb_kv8_cache;
+
+/* Writes the new tokens.  Per 16 tokens and head: amax over the new tokens' elements,
+ *   s = max(scale already there (if the block holds earlier tokens of the request),
+ *           amax / qmax rounded to fp32 and then UP to bf16),   qmax = 127 (int8), 448 (e4m3),
+ * codes = x / s rounded to nearest even (0 where s = 0); when s has grown the earlier tokens of
+ * the block are requantised, code = rne((code s_before) / s).  With s on 8 significant bits no
+ * quotient of a bf16 number falls so near a tie that fp32 decides it differently from exact
+ * arithmetic.  NaN is stored as 0, an infinity as the largest code, and SB_ERR_NONFINITE is
+ * latched: the cache never holds a NaN.  Writing the same tokens again changes nothing.
+ * K, V: bf16, element (token, head, d) at token * token_stride + head * head_stride + d; strides
+ * multiples of 8, 16-byte aligned bases.  total: rows of K and V (starts may not pass it).     */
+sb_status sb_kv8_append(sb_ctx* ctx, const sb_kv8_cache* cache, const void* K_bf16, int64_t k_token_stride,
+                        int64_t k_head_stride, const void* V_bf16, int64_t v_token_stride, int64_t v_head_stride,
+                        int64_t total, const int32_t* starts, const int32_t* lens, int64_t max_new);
+/* The values of the last n tokens of every request, rounded to bf16: K, V [total][heads][dim]. */
+sb_status sb_kv8_read(sb_ctx* ctx, const sb_kv8_cache* cache, int64_t total, const int32_t* starts,
+                      const int32_t* lens, int64_t max_new, void* K_bf16, void* V_bf16);
+/* Attention of the new tokens over the cache (which holds them already):
+ *   O[i] = sum_j softmax_j(scale q_i k_j) v_j over the keys j <= p_i (p_i = the query's position,
+ *   lens[b] - n + its index) and, with window > 0, j > p_i - window,
+ * q_heads a multiple of the cache's heads, query head h reads cache head h / (q_heads / heads).
+ * lse[i][h] (or NULL): the natural log of the sum of exp(scale q k); a query that sees no key
+ * gets O = 0 and lse = -inf.  One new token per request (decode), a few (drafts) or whole
+ * prompts; max_len: at least every lens[b] (it decides how the keys are split, nothing else).
+ * Queries are multiplied in fp16 after an exact power-of-two scaling per row, weights of a key
+ * are rounded to fp16, sums and softmax statistics are fp32.
+ * Q, O: bf16, element (token, head, d) at token * token_stride + head * head_stride + d; strides
+ * multiples of 8, 16-byte aligned bases; lse fp32 [total][q_heads].                             */
+sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, const void* Q_bf16, int64_t q_token_stride,
+                           int64_t q_head_stride, int q_heads, int64_t total, const int32_t* starts,
+                           const int32_t* lens, int64_t max_new, int64_t max_len, float scale, int64_t window,
+                           void* O_bf16, int64_t o_token_stride, int64_t o_head_stride, float* lse);
+
 #ifdef __cplusplus
 }
 #endif

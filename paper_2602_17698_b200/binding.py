@@ -20,6 +20,10 @@ SB_OK, SB_ERR_INVALID, SB_ERR_SHAPE, SB_ERR_BUDGET, SB_ERR_SCRATCH, SB_ERR_CUDA,
     SB_ERR_NOCONVERGE, SB_ERR_NONFINITE, SB_ERR_TIMEOUT = range(9)
 SB_ALLOC_SCALEBITS, SB_ALLOC_GREEDY = 0, 1
 SB_ACC_ROW, SB_ACC_COL = 1, 2
+SB_FP4_MX, SB_FP4_NV = 0, 1
+SB_KV_INT8, SB_KV_E4M3 = 0, 1
+SB_KV8_BLOCK = 16
+FP4_FORMATS = {"mx": SB_FP4_MX, "nv": SB_FP4_NV}
 
 EXPORTS = ["sb_create", "sb_destroy", "sb_sync", "sb_last_error", "sb_kernel_launches", "sb_debug_lookback",
            "sb_checked_build",
@@ -28,7 +32,9 @@ EXPORTS = ["sb_create", "sb_destroy", "sb_sync", "sb_last_error", "sb_kernel_lau
            "sb_pack_blocks",
            "sb_calib_moments_noalloc", "sb_first_order_scores", "sb_exchange_step",
            "sb_reorder_channels_first_order", "sb_calib_gram",
-           "sb_block_scores_full", "sb_dequant_gemm"]
+           "sb_block_scores_full", "sb_dequant_gemm",
+           "sb_fp4_code_bytes", "sb_fp4_scale_bytes", "sb_fp4_quantize", "sb_fp4_dequantize", "sb_fp4_gemm",
+           "sb_kv8_append", "sb_kv8_read", "sb_kv8_attention"]
 
 
 class SbError(RuntimeError):
@@ -61,6 +67,13 @@ class StepReport(C.Structure):
 
     def as_dict(self):
         return {k: getattr(self, k) for k, _ in self._fields_}
+
+
+class Kv8CacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("table", C.c_void_p), ("table_stride", C.c_int64), ("pages", C.c_int64),
+                ("requests", C.c_int32), ("heads", C.c_int32), ("page_tokens", C.c_int32), ("dim", C.c_int32),
+                ("type", C.c_int32), ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -112,8 +125,18 @@ def lib() -> C.CDLL:
                                       C.POINTER(C.c_int), i32, vp, i64]
         L.sb_reorder_channels_first_order.argtypes = [vp, vp, vp, i64, i64, i64, i64, i32, i32, vp, vp, i32,
                                                       i64, i64, vp, vp]
+        L.sb_fp4_code_bytes.argtypes = [i64, i64]
+        L.sb_fp4_scale_bytes.argtypes = [i64, i64, i32]
+        L.sb_fp4_quantize.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, vp]
+        L.sb_fp4_dequantize.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp, i64]
+        L.sb_fp4_gemm.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, i32, vp, i32, i64]
+        cp = C.POINTER(Kv8CacheStruct)
+        L.sb_kv8_append.argtypes = [vp, cp, vp, i64, i64, vp, i64, i64, i64, vp, vp, i64]
+        L.sb_kv8_read.argtypes = [vp, cp, i64, vp, vp, i64, vp, vp]
+        L.sb_kv8_attention.argtypes = [vp, cp, vp, i64, i64, i32, i64, vp, vp, i64, i64, f32, i64, vp, i64, i64, vp]
+        L.sb_fp4_code_bytes.restype = L.sb_fp4_scale_bytes.restype = i64
         for name in EXPORTS:
-            if name not in ("sb_last_error", "sb_kernel_launches"):
+            if name not in ("sb_last_error", "sb_kernel_launches", "sb_fp4_code_bytes", "sb_fp4_scale_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -137,6 +160,78 @@ def _mat(W: torch.Tensor):
     if W.dim() != 2 or W.dtype != torch.bfloat16 or W.stride(1) != 1:
         raise ValueError("expected a row-major 2-D bf16 tensor")
     return W.shape[0], W.shape[1], W.stride(0)
+
+
+def fp4_code_bytes(rows: int, cols: int) -> int:
+    """Bytes of the codes of a 4-bit matrix (rows padded to 32 columns)."""
+    return int(lib().sb_fp4_code_bytes(rows, cols))
+
+
+def fp4_scale_bytes(rows: int, cols: int, fmt: str) -> int:
+    """Bytes of its scales (tiles of 128 rows x 4 blocks)."""
+    return int(lib().sb_fp4_scale_bytes(rows, cols, FP4_FORMATS[fmt]))
+
+
+class Fp4Matrix:
+    """A matrix in a microscaled 4-bit format ("mx" or "nv"): codes uint8 [rows][padded cols / 2],
+    scales uint8 (tiles), and for "nv" the fp32 scale of the whole matrix, a tensor of one element
+    on the device (None: 1)."""
+    __slots__ = ("codes", "scales", "rows", "cols", "fmt", "tensor_scale")
+
+    def __init__(self, codes, scales, rows: int, cols: int, fmt: str = "nv", tensor_scale=None):
+        if fmt not in FP4_FORMATS:
+            raise ValueError(f"unknown 4-bit format {fmt!r}")
+        pitch = (cols + 31) // 32 * 16
+        tiles = (rows + 127) // 128 * ((pitch * 2 // (32 if fmt == "mx" else 16) + 3) // 4)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_contiguous() or not scales.is_contiguous():
+            raise TypeError("codes and scales are contiguous uint8 tensors")
+        if codes.numel() != rows * pitch or scales.numel() != tiles * 512:
+            raise ValueError("codes or scales have another size than the format's")
+        if tensor_scale is not None and (tensor_scale.dtype != torch.float32 or tensor_scale.numel() != 1):
+            raise TypeError("tensor_scale is one fp32 element")
+        self.codes, self.scales, self.rows, self.cols, self.fmt, self.tensor_scale = codes, scales, rows, cols, fmt, tensor_scale
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, fmt: str = "nv", tensor_scale=None, device="cuda"):
+        return cls(torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=device),
+                   torch.empty(fp4_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device=device), rows, cols, fmt, tensor_scale)
+
+
+class Kv8Cache:
+    """A paged key/value cache in 8 bits: k, v int8 or float8_e4m3fn [pages][heads][page tokens][dim],
+    k_scale, v_scale bf16 [pages][heads][page tokens / 16], table int32 [requests][pages of a request]."""
+    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "struct")
+
+    def __init__(self, k, v, k_scale, v_scale, table):
+        pages, heads, page_tokens, dim = k.shape
+        if k.dtype not in (torch.int8, torch.float8_e4m3fn) or v.dtype != k.dtype:
+            raise TypeError("keys and values are int8 or float8_e4m3fn")
+        if k_scale.dtype != torch.bfloat16 or v_scale.dtype != torch.bfloat16 or table.dtype != torch.int32:
+            raise TypeError("scales are bf16 and page numbers int32")
+        if v.shape != k.shape or k_scale.numel() * SB_KV8_BLOCK != pages * heads * page_tokens or v_scale.numel() != k_scale.numel() or table.dim() != 2:
+            raise ValueError("keys, values, scales and table do not fit one another")
+        if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()) or table.stride(1) != 1:
+            raise ValueError("the cache's tensors are contiguous")
+        if not k.is_cuda:
+            raise ValueError("expected a CUDA tensor (the library has no CPU path)")
+        self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
+        self.struct = Kv8CacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(),
+                                     table.stride(0) if table.shape[0] > 1 else table.shape[1], pages, table.shape[0], heads,
+                                     page_tokens, dim, SB_KV_INT8 if k.dtype == torch.int8 else SB_KV_E4M3, 0)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_tokens: int, dim: int, table, dtype=torch.int8):
+        kv = torch.zeros((2, pages, heads, page_tokens, dim), dtype=torch.uint8, device=table.device).view(dtype)
+        sc = torch.zeros((2, pages, heads, page_tokens // SB_KV8_BLOCK), dtype=torch.bfloat16, device=table.device)
+        return cls(kv[0], kv[1], sc[0], sc[1], table)
+
+
+def _heads(x: torch.Tensor, what: str):
+    """(address, token stride, head stride) of a bf16 [tokens][heads][dim] tensor."""
+    if x.dim() != 3 or x.dtype != torch.bfloat16 or x.stride(2) != 1 or not x.is_cuda:
+        raise ValueError(f"{what}: expected a bf16 [tokens][heads][dim] CUDA tensor with contiguous rows")
+    # the stride of an axis of one element is never used
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0
 
 
 class Context:
@@ -417,6 +512,92 @@ class Context:
             _ptr(level, torch.uint8), R, Cc, block_rows, block_cols, group, barr, L,
             _ptr(Y, torch.float32), Y.stride(0)))
         return Y
+
+    # ---- microscaled 4-bit matrices ---------------------------------------------------------
+    def fp4_quantize(self, X: torch.Tensor, out: Fp4Matrix) -> Fp4Matrix:
+        """X (bf16 [rows][cols]) into `out`, whose format and tensor scale it takes."""
+        R, Cc, ldx = _mat(X)
+        if (R, Cc) != (out.rows, out.cols):
+            raise ValueError("X and the 4-bit matrix have different sizes")
+        self._check(lib().sb_fp4_quantize(self._h, _ptr(X), R, Cc, ldx if R > 1 else (Cc + 7) // 8 * 8, FP4_FORMATS[out.fmt],
+                                          _ptr(out.tensor_scale), _ptr(out.codes), _ptr(out.scales)))
+        return out
+
+    def fp4_dequantize(self, m: Fp4Matrix, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The bf16 values a 4-bit matrix stands for."""
+        if out is None:
+            out = torch.empty((m.rows, m.cols), dtype=torch.bfloat16, device=m.codes.device)
+        R, Cc, ldy = _mat(out)
+        if (R, Cc) != (m.rows, m.cols):
+            raise ValueError("out and the 4-bit matrix have different sizes")
+        self._check(lib().sb_fp4_dequantize(self._h, _ptr(m.codes), _ptr(m.scales), R, Cc, FP4_FORMATS[m.fmt], _ptr(m.tensor_scale),
+                                            _ptr(out), ldy if R > 1 else Cc))
+        return out
+
+    def fp4_gemm(self, a: Fp4Matrix, b: Fp4Matrix, out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
+        """a [M][K] times the transpose of b [N][K] -> [M][N] in bf16 or fp32 (out's type, or out_dtype)."""
+        if a.cols != b.cols or a.fmt != b.fmt:
+            raise ValueError("the two matrices need the same format and number of columns")
+        if out is None:
+            out = torch.empty((a.rows, b.rows), dtype=out_dtype, device=a.codes.device)
+        if out.dtype not in (torch.bfloat16, torch.float32) or out.shape != (a.rows, b.rows) or out.stride(1) != 1:
+            raise ValueError("out: a row-major bf16 or fp32 [M][N] tensor")
+        self._check(lib().sb_fp4_gemm(self._h, _ptr(a.codes), _ptr(a.scales), _ptr(a.tensor_scale), a.rows, _ptr(b.codes),
+                                      _ptr(b.scales), _ptr(b.tensor_scale), b.rows, a.cols, FP4_FORMATS[a.fmt], _ptr(out),
+                                      int(out.dtype == torch.float32), out.stride(0) if a.rows > 1 else b.rows))
+        return out
+
+    # ---- key/value cache in 8 bits ----------------------------------------------------------
+    def _kv8_rows(self, cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor):
+        n = cache.struct.requests
+        if starts.dtype != torch.int32 or lens.dtype != torch.int32 or starts.numel() != n + 1 or lens.numel() != n:
+            raise ValueError("starts: int32 [requests + 1], lens: int32 [requests]")
+        return _ptr(starts), _ptr(lens)
+
+    def kv8_append(self, cache: Kv8Cache, K: torch.Tensor, V: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int):
+        """Writes the new tokens' keys and values (bf16 [tokens][heads][dim]); request b's rows are
+        starts[b] .. starts[b + 1], its length with them lens[b]."""
+        s, n = self._kv8_rows(cache, starts, lens)
+        if K.shape != V.shape or K.shape[1:] != (cache.struct.heads, cache.struct.dim):
+            raise ValueError("K and V: [tokens][heads][dim] of the cache")
+        (k, kt, kh), (v, vt, vh) = _heads(K, "K"), _heads(V, "V")
+        self._check(lib().sb_kv8_append(self._h, C.byref(cache.struct), k, kt, kh, v, vt, vh, K.shape[0], s, n, int(max_new)))
+
+    def kv8_read(self, cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor, max_new: int, total: Optional[int] = None, out=None):
+        """The values of the last starts[b + 1] - starts[b] tokens of every request, as bf16
+        [tokens][heads][dim] keys and values; `out`, or `total` = starts[-1] to allocate them."""
+        s, n = self._kv8_rows(cache, starts, lens)
+        if out is None:
+            shape = (int(starts[-1]) if total is None else total, cache.struct.heads, cache.struct.dim)
+            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
+        K, V = out
+        if K.shape != V.shape or K.shape[1:] != (cache.struct.heads, cache.struct.dim) or not K.is_contiguous() or not V.is_contiguous():
+            raise ValueError("out: two contiguous [tokens][heads][dim] tensors")
+        self._check(lib().sb_kv8_read(self._h, C.byref(cache.struct), K.shape[0], s, n, int(max_new), _ptr(K, torch.bfloat16), _ptr(V, torch.bfloat16)))
+        return K, V
+
+    def kv8_attention(self, cache: Kv8Cache, Q: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int, max_len: int,
+                      scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, want_lse: bool = False):
+        """Causal attention of the new tokens (Q bf16 [tokens][query heads][dim]) over the cache, which
+        holds them already.  Returns (out, lse); lse is None unless given or asked for."""
+        s, n = self._kv8_rows(cache, starts, lens)
+        if Q.dim() != 3 or Q.shape[2] != cache.struct.dim:
+            raise ValueError("Q: [tokens][query heads][dim of the cache]")
+        q, qt, qh = _heads(Q, "Q")
+        if out is None:
+            out = torch.empty(Q.shape, dtype=torch.bfloat16, device=Q.device)
+        if out.shape != Q.shape:
+            raise ValueError("out: the shape of Q")
+        o, ot, oh = _heads(out, "out")
+        if lse is None and want_lse:
+            lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+        if lse is not None and (lse.shape != Q.shape[:2] or not lse.is_contiguous()):
+            raise ValueError("lse: contiguous fp32 [tokens][query heads]")
+        self._check(lib().sb_kv8_attention(self._h, C.byref(cache.struct), q, qt, qh, Q.shape[1], Q.shape[0], s, n, int(max_new),
+                                           int(max_len), Q.shape[2] ** -0.5 if scale is None else float(scale), int(window), o, ot, oh,
+                                           _ptr(lse, torch.float32)))
+        return out, lse
 
 
 def checked_build() -> bool:

@@ -98,6 +98,7 @@ sb_status sb_destroy(sb_ctx* ctx) {
     if (ctx->lb_mem) cudaFree(ctx->lb_mem);
     if (ctx->moment_done) cudaFree(ctx->moment_done);
     if (ctx->stats_done) cudaFree(ctx->stats_done);
+    if (ctx->kv8_done) cudaFree(ctx->kv8_done);
     if (ctx->pinned) cudaFreeHost(ctx->pinned);
     delete ctx;
     return SB_OK;

@@ -3,6 +3,7 @@
 #include <set>
 #include <vector>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -35,6 +36,8 @@ struct sb_ctx {
     unsigned int* moment_done = nullptr;   // per column chunk: row splits finished (zero between calls)
     int moments_ctas_per_sm = 0;           // resident CTAs per SM of the moments kernel (asked once)
     unsigned int* stats_done = nullptr;    // per tile row / tile column: tiles finished (zero between calls)
+    unsigned int* kv8_done = nullptr;      // attention: splits finished per output tile (zero between calls)
+    size_t kv8_done_n = 0;
     void* lb_mem = nullptr;      // look-back descriptors (context-owned, never in the arena)
     unsigned int lb_max_tiles = 0;
     int64_t launches = 0;
@@ -92,7 +95,7 @@ constexpr int SB_STATS_TILES = 8192;     // 128-wide tiles per axis a reorder ca
 constexpr int SB_MOMENT_CHUNKS = 4096;   // column chunks of 256 a moments call may have (K <= 1M)
 
 enum SbKernelId { SBK_MOMENTS = 1, SBK_STATS, SBK_SCORES, SBK_GATHER, SBK_ARGSORT, SBK_SCAN,
-                  SBK_SORT, SBK_ALLOC, SBK_PACK, SBK_GEMM };
+                  SBK_SORT, SBK_ALLOC, SBK_PACK, SBK_GEMM, SBK_FP4, SBK_KV8 };
 
 // ---- device helpers ----------------------------------------------------------------
 #ifdef __CUDACC__
