@@ -8,10 +8,10 @@ typedef CUresult (*SbEncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_
                                     const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                     CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Rows of `row_bytes` bytes (a multiple of 16), `pitch` bytes apart, as a map of boxes of 128 bytes
-// x box_rows with the 128-byte swizzle; what lies outside reads as zero.
-inline sb_status t5_map_rows(sb_ctx* ctx, CUtensorMap* map, const void* base, int64_t rows, int64_t row_bytes,
-                             int64_t pitch, int box_rows) {
+// Rows of row_elems elements, `pitch` bytes apart (a multiple of 16), as a map of boxes of box_elems x box_rows; what lies
+// outside reads as zero.
+inline sb_status t5_map(sb_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t rows,
+                        int64_t row_elems, int64_t pitch, int box_elems, int box_rows, bool swizzle) {
     static SbEncodeTiledFn encode = nullptr;
     if (!encode) {
         void* fn = nullptr;
@@ -21,15 +21,19 @@ inline sb_status t5_map_rows(sb_ctx* ctx, CUtensorMap* map, const void* base, in
             return sb_fail(ctx, SB_ERR_CUDA, "the driver does not export cuTensorMapEncodeTiled");
         encode = reinterpret_cast<SbEncodeTiledFn>(fn);
     }
-    const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+    const cuuint64_t dims[2] = {(cuuint64_t)row_elems, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+    const cuuint32_t box[2] = {(cuuint32_t)box_elems, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    const CUresult r = encode(map, type, 2, const_cast<void*>(base), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return sb_fail(ctx, SB_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return SB_OK;
+}
+// rows of row_bytes bytes (a multiple of 16) in boxes of 128 bytes x box_rows with the 128-byte swizzle
+inline sb_status t5_map_rows(sb_ctx* ctx, CUtensorMap* map, const void* base, int64_t rows, int64_t row_bytes, int box_rows) {
+    return t5_map(ctx, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, rows, row_bytes, row_bytes, 128, box_rows, true);
 }
 
 #ifdef __CUDACC__
@@ -82,6 +86,14 @@ __device__ __forceinline__ bool t5_bar_wait(unsigned bar, unsigned parity, volat
 static __device__ __noinline__ void t5_bar_drain(unsigned bar, unsigned parity) {
     const unsigned long long t0 = t5_now_ns();
     while (!t5_bar_try(bar, parity) && t5_now_ns() - t0 < T5_WAIT_NS) {}
+}
+// One lane of a converged warp. The warps that issue copies and products run their loops whole, with
+// this predicate on the instructions alone: the operands then stay in uniform registers. In a
+// branch of lane 0 the same thirteen instructions of a ring stage took 1066 cycles to issue.
+__device__ __forceinline__ bool t5_elect() {
+    unsigned p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void t5_load_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
     asm volatile(
