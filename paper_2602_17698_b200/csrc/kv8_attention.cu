@@ -28,10 +28,11 @@
 // Long caches are cut into chunks of keys; a chunk's CTA leaves unnormalised sums, and the last
 // CTA of a row tile to finish (a counter) adds the chunks in their order: the result does not
 // depend on which one that is.
-#include "kv8.cuh"
+#include "kv8_attention.cuh"
 
 namespace {
 
+constexpr int AT_PROMPT_FROM = 64;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
 constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
@@ -62,49 +63,6 @@ __device__ __forceinline__ uint32_t at_transpose(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ float at_exp2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t at_half2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-// Operand words hold e4m3 codes as they are, int8 codes with the sign bits flipped (at_flip).
-template <int TYPE> __device__ __forceinline__ uint32_t at_flip(uint32_t w) { return TYPE == SB_KV_INT8 ? w ^ 0x80808080u : w; }
-// bytes (0, 1) or (2, 3) of a word as two fp16
-template <int TYPE, int HALF>
-__device__ __forceinline__ uint32_t at_pair(uint32_t w) {
-    if (TYPE == SB_KV_INT8) {
-        const uint32_t u = __byte_perm(w, 0x64646464u, HALF ? 0x4342 : 0x4140);
-        const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __float2half2_rn(1152.f));
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-    return e4m3x2_to_f16x2(HALF ? w >> 16 : w);
-}
-
-struct AtArgs {
-    Kv8Geom g;
-    const uint8_t *k, *v;
-    const uint16_t *k_scale, *v_scale;
-    const __nv_bfloat16* q;
-    int64_t q_token_stride, q_head_stride;
-    __nv_bfloat16* o;
-    int64_t o_token_stride, o_head_stride;
-    float* lse;
-    int group;                   // query heads per cache head
-    int row_tiles, splits;       // of the grid
-    int chunk;                   // keys per CTA, a multiple of AT_STEP
-    float scale_log2;            // softmax scale * log2(e)
-    int window;
-    float* part;                 // [tile][splits][8 NR][dim] unnormalised sums
-    float2* part_ml;             // [tile][splits][8 NR] (running maximum, sum)
-    unsigned* done;              // per tile: chunks finished
-    SbDeviceState* st;
-};
-
 template <int DP, int NR>
 struct AtShape {
     static constexpr int STAGES = DP == 64 ? 4 : 3;
@@ -220,8 +178,7 @@ kv8_rows_kernel(const AtArgs a) {
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const int ex = max(14, min(254, (int)(amax >> 7)));          // largest element in 2^(ex - 127) [1, 2)
-        const float up = __uint_as_float((uint32_t)min(254, 267 - ex) << 23);
+        const float up = at_query_scale(amax);
 #pragma unroll
         for (int i = 0; i < DP / 64; ++i)
             *reinterpret_cast<uint32_t*>(qrow + 128 * i + 4 * lane) = at_half2(bf16lo(w[i]) * up, bf16hi(w[i]) * up);
@@ -350,7 +307,7 @@ kv8_rows_kernel(const AtArgs a) {
         // value scales relative to a power of two that only grows
         const float vmax = fmaxf(vsc[0], vsc[1]);
         if (vmax > vref) {
-            const float fresh = __uint_as_float(max((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u, 0x00800000u));
+            const float fresh = at_value_ref(vmax);
             const float f = __fdiv_rn(vref, fresh);
             vref = fresh;
 #pragma unroll
@@ -360,7 +317,7 @@ kv8_rows_kernel(const AtArgs a) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o[i][nr][k] *= f;
         }
-        const float inv = vref > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(vref)) : 0.f;     // 2^-e of 2^e
+        const float inv = at_value_inv(vref);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float vw = vsc[e] * inv;
@@ -441,10 +398,10 @@ kv8_rows_kernel(const AtArgs a) {
         const int row = r0 + r;
         const int64_t tok = rq.row0 + row / a.group;
         const int h = head * a.group + row % a.group;
-        const float f = sum > 0.f ? __fdiv_rn(1.f, sum) : (sum == 0.f ? 0.f : sum);
+        const float f = at_norm(sum);
         const uint2 w = make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
         *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) = w;
-        if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = sum == 0.f ? -INFINITY : (mm + log2f(sum)) * 0.6931471805599453f;
+        if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(mm, sum);
     };
     for (int idx = threadIdx.x; idx < nrow * (D / 4); idx += AT_WARPS * 32) {
         const int r = idx / (D / 4), d = 4 * (idx - r * (D / 4));
@@ -594,5 +551,8 @@ extern "C" sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, co
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;
+    // Many query rows per cache head: a key is converted once for 256 rows and the products run at the
+    // rate of tcgen05; few: the cache's bytes bound the call and 8 to 32 rows per warp are enough.
+    if (max_new * a.group > AT_PROMPT_FROM && cache->dim <= 128) return kv8_prompt(ctx, a, cache->type, max_new, max_len);
     return cache->type == SB_KV_INT8 ? rows_by_dim<SB_KV_INT8>(ctx, a, max_new, max_len) : rows_by_dim<SB_KV_E4M3>(ctx, a, max_new, max_len);
 }

@@ -251,6 +251,19 @@ def test_long_cache_in_many_chunks(ctx, kind, dim):
     _attend(ctx, kind, [9000, 1234], [1, 3], 1, 4, 64, dim, poison=False)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("past,new,heads,group,dim,window", [
+    ([3000], [70], 1, 4, 128, 0), ([2500, 10], [33, 65], 2, 3, 64, 0), ([1500], [257], 1, 1, 96, 0), ([4000, 0], [40, 64], 1, 4, 80, 700),
+    ([0], [129], 1, 2, 128, 0), ([1111, 0, 127], [20, 0, 40], 2, 5, 128, 0)])
+def test_chunks_of_prompts_behind_a_long_past(ctx, kind, past, new, heads, group, dim, window):
+    _attend(ctx, kind, past, new, heads, group, 16, dim, window=window)
+
+
+@pytest.mark.parametrize("max_len", [1, 1500, 10 ** 6])
+def test_max_len_with_many_rows(ctx, max_len):
+    _attend(ctx, "e4m3", [2900, 40], [30, 20], 1, 4, 32, 128, max_len=max_len)
+
+
 @pytest.mark.parametrize("max_len", [1, 100, 2000, 3000])
 def test_max_len_decides_nothing_but_the_chunks(ctx, max_len):
     _attend(ctx, "int8", [2900, 40], [2, 1], 1, 3, 100 // 16 * 16, 128, max_len=max_len, poison=False)
