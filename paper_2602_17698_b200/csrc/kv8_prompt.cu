@@ -10,7 +10,7 @@
 // conversion. Scales never touch K and V: a scale block is 16 columns of S, its key scale goes
 // into the factor of S, its value scale into P.
 //
-// Warps 0-3 and 4-7: softmax of the two tiles; 8-11: conversion; 12: products. While one tile's
+// Warps 0-3 and 4-7: softmax of the two tiles; 8-11: conversion; 12: products; 13: copies. While one tile's
 // softmax runs, the other tile's P V and the next S keep the tensor cores busy. The running
 // maximum of a row is only moved when it is off by more than 2^8 (P stays below 2^8, far from
 // fp16's end), so sums in tensor memory are rarely touched between tiles.
@@ -25,7 +25,10 @@ namespace {
 constexpr int PR_ROWS = 128;             // query rows of a tile; two per CTA
 constexpr int PR_KEYS = 128;             // keys of a tile
 constexpr int PR_BLOCKS = PR_KEYS / SB_KV8_BLOCK;
-constexpr int PR_THREADS = 13 * 32;
+constexpr int PR_THREADS = 16 * 32;       // warps 14 and 15 only lend their registers
+// registers of a softmax, conversion and other warp's thread: 8 x 184 + 4 x 96 + 4 x 48 warps' shares <= 16 x 128
+constexpr int PR_REGS_SOFTMAX = 184, PR_REGS_CONVERT = 96, PR_REGS_REST = 48;
+static_assert(8 * PR_REGS_SOFTMAX + 4 * PR_REGS_CONVERT + 4 * PR_REGS_REST <= 16 * 128, "what the block was launched with");
 constexpr float PR_SLACK = 8.f;          // log2 of how far a row's maximum may run ahead of its reference
 
 template <int DP>
@@ -33,8 +36,10 @@ struct PrShape {
     static constexpr int PANELS = DP / 64;                          // 128-byte columns of an operand row
     static constexpr int PANEL = 128 * 128;                         // bytes: 128 rows x 128
     static constexpr int OPERAND = PANELS * PANEL;
-    static constexpr int Q_AT = 0, K_AT = 2 * OPERAND, V_AT = 4 * OPERAND;      // two of each
-    static constexpr int SC_AT = 6 * OPERAND;                       // scales of four tiles: 8 of K, 8 of V
+    static constexpr int RING = 3, RAW_RING = 4;                    // converted and raw tiles: K, V, K, V, ...
+    static constexpr int RAW = PR_KEYS * DP;
+    static constexpr int Q_AT = 0, T_AT = 2 * OPERAND, RAW_AT = T_AT + RING * OPERAND;
+    static constexpr int SC_AT = RAW_AT + RAW_RING * RAW;           // scales of four tiles: 8 of K, 8 of V
     static constexpr int BAR_AT = SC_AT + 4 * 64;
     static constexpr int SMEM = BAR_AT + 256 + 1024;
     // tensor memory: S (and P) of the two tiles, then O of the two tiles
@@ -84,6 +89,69 @@ __device__ __forceinline__ constexpr unsigned pr_idesc(int n, bool b_mn) {
     return 1u << 4 | (b_mn ? 1u << 16 : 0u) | (unsigned)(n >> 3) << 17 | (unsigned)(PR_ROWS >> 4) << 24;
 }
 
+// Column c of a row's 128 scores is seen if from < c <= upto; EDGE: some are not.
+// Largest score of a row, in units of log2 (kf: factor of each 16 columns, not negative).
+template <bool EDGE>
+__device__ __forceinline__ float pr_max(unsigned ts, unsigned (&s)[2][32], const float (&kf)[PR_BLOCKS], int upto, int from) {
+    float mx = -INFINITY;
+    t5_ld32(ts, s[0]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        t5_wait_ld();
+        if (c < 3) t5_ld32(ts + 32 * (c + 1), s[(c + 1) & 1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float bm[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                float x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    x[u] = __uint_as_float(s[c & 1][16 * h + i + u]);
+                    if (EDGE && (32 * c + 16 * h + i + u > upto || 32 * c + 16 * h + i + u <= from)) x[u] = -INFINITY;
+                }
+                bm[0] = fmaxf(fmaxf(bm[0], x[0]), x[1]);
+                bm[1] = fmaxf(fmaxf(bm[1], x[2]), x[3]);
+            }
+            const float top = fmaxf(bm[0], bm[1]);
+            // a factor of 0 makes 0 of any score, but no NaN of a block that is masked whole
+            mx = fmaxf(mx, EDGE && top == -INFINITY ? -INFINITY : top * kf[2 * c + h]);
+        }
+    }
+    return mx;
+}
+// The row's weights 2^(score - ref), times the value scale of their 16 columns, in fp16 over the
+// columns whose scores have been read; returns the sum of the weights.
+template <bool EDGE>
+__device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[2][32], const float (&kf)[PR_BLOCKS], const float (&vs)[PR_BLOCKS],
+                                            float inv, float ref, int upto, int from) {
+    float sum[2] = {0.f, 0.f};
+    t5_ld32(ts, s[0]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        t5_wait_ld();
+        if (c < 3) t5_ld32(ts + 32 * (c + 1), s[(c + 1) & 1]);
+        uint32_t p[16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float vw = vs[2 * c + h] * inv, kk = kf[2 * c + h];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float e[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    e[u] = at_exp2(fmaf(__uint_as_float(s[c & 1][16 * h + i + u]), kk, -ref));
+                    if (EDGE && (32 * c + 16 * h + i + u > upto || 32 * c + 16 * h + i + u <= from)) e[u] = 0.f;
+                    sum[u] += e[u];
+                }
+                p[8 * h + i / 2] = at_half2(e[0] * vw, e[1] * vw);
+            }
+        }
+        pr_st16(ts + 16 * c, p);
+    }
+    return sum[0] + sum[1];
+}
+
 template <int TYPE, int DP>
 __global__ void __launch_bounds__(PR_THREADS, 1)
 kv8_prompt_kernel(const AtArgs a) {
@@ -92,9 +160,10 @@ kv8_prompt_kernel(const AtArgs a) {
     unsigned char* smem = pr_raw + ((1024u - (t5_smem(pr_raw) & 1023u)) & 1023u);
     float* sc = reinterpret_cast<float*>(smem + S::SC_AT);           // [4][16]
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + S::BAR_AT);
-    unsigned long long *kfull = bars, *kempty = bars + 2, *vfull = bars + 4, *vempty = bars + 6, *sfull = bars + 8,
-                       *pfull = bars + 10, *odone = bars + 12, *scfull = bars + 14, *qready = bars + 18, *last = bars + 19;
-    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 20);
+    // raw tiles: landed, converted; converted tiles: there, multiplied; per row tile: scores, weights, sums
+    unsigned long long *raw_full = bars, *raw_empty = bars + 4, *full = bars + 8, *empty = bars + 11, *sfull = bars + 14,
+                       *pfull = bars + 16, *odone = bars + 18, *scfull = bars + 20, *qready = bars + 24, *last = bars + 25;
+    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 26);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int head = blockIdx.x, b = blockIdx.z;
@@ -125,11 +194,15 @@ kv8_prompt_kernel(const AtArgs a) {
     const int ntiles = (k1 - k0 + PR_KEYS - 1) / PR_KEYS;
 
     if (threadIdx.x == 0) {
+        for (int i = 0; i < S::RAW_RING; ++i) {
+            t5_bar_init(t5_smem(raw_full + i), 1);
+            t5_bar_init(t5_smem(raw_empty + i), 4);
+        }
+        for (int i = 0; i < S::RING; ++i) {
+            t5_bar_init(t5_smem(full + i), 4);
+            t5_bar_init(t5_smem(empty + i), 1);
+        }
         for (int i = 0; i < 2; ++i) {
-            t5_bar_init(t5_smem(kfull + i), 4);
-            t5_bar_init(t5_smem(kempty + i), 1);
-            t5_bar_init(t5_smem(vfull + i), 4);
-            t5_bar_init(t5_smem(vempty + i), 1);
             t5_bar_init(t5_smem(sfull + i), 1);
             t5_bar_init(t5_smem(pfull + i), 4);
             t5_bar_init(t5_smem(odone + i), 1);
@@ -154,6 +227,7 @@ kv8_prompt_kernel(const AtArgs a) {
 
     if (warp < 8) {
         // ---- softmax: one query row per thread ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_REGS_SOFTMAX));
         const int qt = warp >> 2;
         if (qt == 0 || two) {
             const int r = threadIdx.x;                               // row of the CTA
@@ -205,29 +279,9 @@ kv8_prompt_kernel(const AtArgs a) {
                     vs[i] = scj[PR_BLOCKS + i];
                     vmax = fmaxf(vmax, vs[i]);
                 }
-                // what a masked score becomes: bit i of block mask
                 const int upto = min(pos, k1 - 1) - key, from = a.window > 0 ? pos - a.window - key : -1;
-                auto masked = [&](int c) { return c > upto || c <= from; };
-                float mx = -INFINITY;
                 unsigned s[2][32];
-                t5_ld32(ts, s[0]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    t5_wait_ld();
-                    if (c < 3) t5_ld32(ts + 32 * (c + 1), s[(c + 1) & 1]);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float bm = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float x = __uint_as_float(s[c & 1][16 * h + i]);
-                            if (edge && masked(32 * c + 16 * h + i)) x = -INFINITY;
-                            bm = fmaxf(bm, x);
-                        }
-                        const float y = bm * kf[2 * c + h];          // a block without a scale: 0, or NaN if all masked
-                        mx = fmaxf(mx, edge && bm == -INFINITY ? -INFINITY : y);
-                    }
-                }
+                const float mx = edge ? pr_max<true>(ts, s, kf, upto, from) : pr_max<false>(ts, s, kf, upto, from);
                 // move the reference (and the power of two of the value scales) when it is too far off
                 float f = 1.f;
                 if (mx > m + PR_SLACK || (m == -INFINITY && mx > m)) {
@@ -252,31 +306,7 @@ kv8_prompt_kernel(const AtArgs a) {
                     }
                 }
                 const float inv = at_value_inv(vref), ref = m == -INFINITY ? 0.f : m;
-                t5_ld32(ts, s[0]);
-                float sum[2] = {0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    t5_wait_ld();
-                    if (c < 3) t5_ld32(ts + 32 * (c + 1), s[(c + 1) & 1]);
-                    uint32_t p[16];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float vw = vs[2 * c + h] * inv, kk = kf[2 * c + h];
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            float e[2];
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                e[u] = at_exp2(fmaf(__uint_as_float(s[c & 1][16 * h + i + u]), kk, -ref));
-                                if (edge && masked(32 * c + 16 * h + i + u)) e[u] = 0.f;
-                                sum[u] += e[u];
-                            }
-                            p[8 * h + i / 2] = at_half2(e[0] * vw, e[1] * vw);
-                        }
-                    }
-                    pr_st16(ts + 16 * c, p);                         // columns whose scores have been read
-                }
-                l += sum[0] + sum[1];
+                l += edge ? pr_weights<true>(ts, s, kf, vs, inv, ref, upto, from) : pr_weights<false>(ts, s, kf, vs, inv, ref, upto, from);
                 pr_wait_st();
                 t5_fence_before();
                 __syncwarp();
@@ -325,82 +355,114 @@ kv8_prompt_kernel(const AtArgs a) {
         }
     } else if (warp < 12) {
         // ---- conversion: a thread takes one 16-byte piece of every PASS-th row of a tile ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_CONVERT));
         constexpr int PIECES = DP / 16, PASS = 128 / PIECES, NP = PR_KEYS / PASS;
         const int tid = threadIdx.x - 256, piece = tid % PIECES, krow = tid / PIECES;
-        const int per_page = a.g.page_tokens;
-        // page of block lane % 8 of a tile
-        auto load_page = [&](int j) -> int {
-            const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * (lane & 7);
-            if (key >= k1) return -1;
-            int64_t page;
-            return kv8_page(a.g, b, key / per_page, page, a.st) ? (int)page : -1;
-        };
-        auto fetch = [&](const uint8_t* codes, int j, int pages, uint4 (&x)[NP]) {
+        // rows from here on were not copied, or hold nothing of the request: zeros
+        const int limit = min(rq.len, (k1 + SB_KV8_BLOCK - 1) / SB_KV8_BLOCK * SB_KV8_BLOCK) - k0;
+        auto convert = [&](int n) {
+            const unsigned src = t5_smem(smem + S::RAW_AT + n % S::RAW_RING * S::RAW) + (unsigned)(krow * D + 16 * piece);
+            unsigned char* dst = smem + S::T_AT + n % S::RING * S::OPERAND + (piece >> 2) * S::PANEL;
+            const int left = 16 * piece < D ? limit - (n >> 1) * PR_KEYS : 0;
+            uint4 x[NP];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int kk = krow + PASS * i, blk = kk / SB_KV8_BLOCK;
-                const int page = __shfl_sync(0xffffffffu, pages, blk);
-                const int key = k0 + j * PR_KEYS + kk;
                 x[i] = make_uint4(0, 0, 0, 0);
-                if (page >= 0 && key < rq.len && 16 * piece < D)
-                    x[i] = *reinterpret_cast<const uint4*>(codes + (((int64_t)page * a.g.heads + head) * per_page + key % per_page) * D + 16 * piece);
+                if (krow + PASS * i < left) x[i] = at_lds128(src + (unsigned)(PASS * i * D));
             }
-        };
-        auto put = [&](unsigned char* dst, const uint4 (&x)[NP]) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int kk = krow + PASS * i;
                 const uint32_t w[4] = {at_flip<TYPE>(x[i].x), at_flip<TYPE>(x[i].y), at_flip<TYPE>(x[i].z), at_flip<TYPE>(x[i].w)};
                 const uint4 lo4 = make_uint4(at_pair<TYPE, 0>(w[0]), at_pair<TYPE, 1>(w[0]), at_pair<TYPE, 0>(w[1]), at_pair<TYPE, 1>(w[1]));
                 const uint4 hi4 = make_uint4(at_pair<TYPE, 0>(w[2]), at_pair<TYPE, 1>(w[2]), at_pair<TYPE, 0>(w[3]), at_pair<TYPE, 1>(w[3]));
-                unsigned char* row = dst + (piece >> 2) * S::PANEL + kk * 128;
                 const int c = 2 * (piece & 3);
                 // the second panel's lanes store their halves the other way round: no two lanes of a row
                 // on the same banks
                 const bool swap = (piece >> 2) != 0;
-                *reinterpret_cast<uint4*>(row + (((swap ? c + 1 : c) ^ (kk & 7)) << 4)) = swap ? hi4 : lo4;
-                *reinterpret_cast<uint4*>(row + (((swap ? c : c + 1) ^ (kk & 7)) << 4)) = swap ? lo4 : hi4;
+                *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap ? c + 1 : c) ^ (kk & 7)) << 4)) = swap ? hi4 : lo4;
+                *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap ? c : c + 1) ^ (kk & 7)) << 4)) = swap ? lo4 : hi4;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-        };
-        int pages = load_page(0), next_pages = load_page(1);
-        uint4 kx[NP], vx[NP];
-        fetch(a.k, 0, pages, kx);
-        fetch(a.v, 0, pages, vx);
-        for (int j = 0; j < ntiles; ++j) {
-            const int st = j & 1;
-            float scale = 0.f;
-            if (warp == 8 && lane < 2 * PR_BLOCKS) {
-                const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * (lane & 7);
-                if (pages >= 0) {
-                    const int64_t at = ((int64_t)pages * a.g.heads + head) * (per_page / SB_KV8_BLOCK) + key % per_page / SB_KV8_BLOCK;
-                    scale = __uint_as_float((uint32_t)(lane < PR_BLOCKS ? a.k_scale : a.v_scale)[at] << 16);
-                }
+            if (lane == 0) {
+                t5_bar_arrive(t5_smem(full + n % S::RING));
+                t5_bar_arrive(t5_smem(raw_empty + n % S::RAW_RING));
             }
-            if (!wait(kempty + st, (j >> 1) + 1)) break;
-            // the tile four before this one has been through both softmaxes: its scales can go
-            if (warp == 8) {
-                if (lane < 2 * PR_BLOCKS) sc[16 * (j & 3) + lane] = scale;
+        };
+        // The first of these warps brings the scales: lane 8 u + i block i of the keys (u = 0) or values
+        // (u = 1), fetched a tile ahead, its page two tiles ahead.
+        const int sblk = SB_KV8_BLOCK * (lane & 7);
+        const uint16_t* const scales = (lane & 8) ? a.v_scale : a.k_scale;
+        const bool brings = warp == 8 && lane < 2 * PR_BLOCKS;
+        auto entry_of = [&](int j) -> int {
+            const int key = k0 + j * PR_KEYS + sblk;
+            return brings && key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : -1;
+        };
+        auto scale_of = [&](int j, int entry) -> uint16_t {
+            if (entry < 0 || entry >= a.g.pages) return 0;
+            const int slot = (k0 + j * PR_KEYS + sblk) % a.g.page_tokens;
+            return scales[((int64_t)entry * a.g.heads + head) * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK];
+        };
+        uint16_t scale = scale_of(0, entry_of(0));
+        int entry = entry_of(1);
+        for (int n = 0; n < 2 * ntiles; ++n) {
+            if (!wait(empty + n % S::RING, n / S::RING + 1)) break;
+            if (warp == 8 && !(n & 1)) {
+                // whoever read the scales of four tiles ago is done: the slot's last tile came after them
+                const int j = n >> 1;
+                if (brings) sc[16 * (j & 3) + lane] = __uint_as_float((uint32_t)scale << 16);
                 __syncwarp();
                 if (lane == 0) t5_bar_arrive(t5_smem(scfull + (j & 3)));
+                scale = scale_of(j + 1, entry);
+                entry = entry_of(j + 2);
             }
-            put(smem + S::K_AT + st * S::OPERAND, kx);
-            if (lane == 0) t5_bar_arrive(t5_smem(kfull + st));
-            pages = next_pages;
-            next_pages = load_page(j + 2);
-            if (j + 1 < ntiles) fetch(a.k, j + 1, pages, kx);
-            if (!wait(vempty + st, (j >> 1) + 1)) break;
-            put(smem + S::V_AT + st * S::OPERAND, vx);
-            if (lane == 0) t5_bar_arrive(t5_smem(vfull + st));
-            if (j + 1 < ntiles) fetch(a.v, j + 1, pages, vx);
+            if (!wait(raw_full + n % S::RAW_RING, n / S::RAW_RING)) break;
+            convert(n);
         }
     } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_REST));
+    }
+    if (warp == 13) {
+        // ---- copies: a tile is eight scale blocks, each contiguous in its page; lane i brings block i ----
+        const unsigned bytes = (unsigned)(SB_KV8_BLOCK * D);
+        auto entry_of = [&](int j) -> int {
+            const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
+            return lane < PR_BLOCKS && key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : -1;
+        };
+        int entry = entry_of(0), issued = 0;
+        for (int n = 0; n < 2 * ntiles; n += 2) {
+            const int j = n >> 1, key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
+            const int slot = key % a.g.page_tokens;
+            const bool inside = lane < PR_BLOCKS && key < k1, fine = inside && entry >= 0 && entry < a.g.pages;
+            if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
+            const int64_t at = (((int64_t)entry * a.g.heads + head) * a.g.page_tokens + slot) * D;
+            const unsigned count = (unsigned)__popc(__ballot_sync(0xffffffffu, fine));
+            entry = entry_of(j + 1);
+            bool ok = true;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int rs = (n + u) % S::RAW_RING;
+                ok = ok && wait(raw_empty + rs, (n + u) / S::RAW_RING + 1);
+                if (!ok) break;
+                const unsigned bar = t5_smem(raw_full + rs);
+                if (lane == 0) t5_bar_expect(bar, count * bytes);
+                __syncwarp();
+                if (fine) t5_load_bulk(t5_smem(smem + S::RAW_AT + rs * S::RAW) + (unsigned)lane * bytes, (u ? a.v : a.k) + at, bytes, bar);
+                __syncwarp();
+                ++issued;
+            }
+            if (!ok) break;
+        }
+        // copies in flight land before the block leaves
+        for (int i = max(0, issued - S::RAW_RING); i < issued; ++i)
+            t5_bar_drain(t5_smem(raw_full + i % S::RAW_RING), (unsigned)(i / S::RAW_RING) & 1u);
+    } else if (warp == 12) {
         // ---- products ----
         const bool one = t5_elect();
         bool ok = wait(qready, 0);
         auto scores = [&](int qt, int j) {
-            const unsigned q = t5_smem(smem + S::Q_AT + qt * S::OPERAND), k = t5_smem(smem + S::K_AT + (j & 1) * S::OPERAND);
+            const unsigned q = t5_smem(smem + S::Q_AT + qt * S::OPERAND), k = t5_smem(smem + S::T_AT + 2 * j % S::RING * S::OPERAND);
 #pragma unroll
             for (int s = 0; s < DP / 16; ++s)
                 pr_mma_ss(one, tmem + S::S_COL + qt * 128, t5_desc_sw128(q + (s >> 2) * S::PANEL + 32 * (s & 3)),
@@ -408,43 +470,46 @@ kv8_prompt_kernel(const AtArgs a) {
             pr_commit(one, t5_smem(sfull + qt));
         };
         auto values = [&](int qt, int j) {
-            const unsigned v = t5_smem(smem + S::V_AT + (j & 1) * S::OPERAND);
+            const unsigned v = t5_smem(smem + S::T_AT + (2 * j + 1) % S::RING * S::OPERAND);
 #pragma unroll
             for (int s = 0; s < PR_KEYS / 16; ++s)
                 pr_mma_ts(one, tmem + S::O_COL + qt * DP, tmem + S::S_COL + qt * 128 + 8 * s, pr_desc_v<DP>(v + 2048 * s),
                           pr_idesc(DP, true), j > 0 || s > 0);
             if (j == ntiles - 1) pr_commit(one, t5_smem(odone + qt));
         };
-        ok = ok && wait(kfull, 0);
+        auto there = [&](int n) { return wait(full + n % S::RING, n / S::RING); };
+        auto done = [&](int n) { pr_commit(one, t5_smem(empty + n % S::RING)); };
+        ok = ok && there(0);
         if (ok) {
             t5_fence_after();
             scores(0, 0);
             if (two) scores(1, 0);
-            pr_commit(one, t5_smem(kempty));
+            done(0);
         }
         for (int j = 0; ok && j < ntiles; ++j) {
-            const int st = j & 1, ns = (j + 1) & 1;
-            ok = wait(vfull + st, j >> 1) && wait(pfull, j);
+            const int v = 2 * j + 1, k = 2 * j + 2;                  // this tile's values, the next tile's keys
+            const bool more = j + 1 < ntiles;
+            ok = there(v) && wait(pfull, j);
             if (!ok) break;
             t5_fence_after();
             values(0, j);
-            if (!two) pr_commit(one, t5_smem(vempty + st));
-            if (j + 1 < ntiles) {
-                ok = wait(kfull + ns, (j + 1) >> 1);
+            if (!two) done(v);
+            if (more) {
+                ok = there(k);
                 if (!ok) break;
                 t5_fence_after();
                 scores(0, j + 1);
-                if (!two) pr_commit(one, t5_smem(kempty + ns));
+                if (!two) done(k);
             }
             if (two) {
                 ok = wait(pfull + 1, j);
                 if (!ok) break;
                 t5_fence_after();
                 values(1, j);
-                pr_commit(one, t5_smem(vempty + st));
-                if (j + 1 < ntiles) {
+                done(v);
+                if (more) {
                     scores(1, j + 1);
-                    pr_commit(one, t5_smem(kempty + ns));
+                    done(k);
                 }
             }
         }

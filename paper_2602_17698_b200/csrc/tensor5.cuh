@@ -63,7 +63,7 @@ __device__ __forceinline__ bool t5_bar_try(unsigned bar, unsigned parity) {
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-static __device__ __noinline__ bool t5_bar_wait_slow(unsigned bar, unsigned parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool t5_bar_wait_slow(unsigned bar, unsigned parity, volatile int* abort_flag) {
     unsigned long long t0 = 0;
     for (unsigned spins = 0;; ++spins) {
         if (t5_bar_try(bar, parity)) return true;
@@ -83,7 +83,7 @@ __device__ __forceinline__ bool t5_bar_wait(unsigned bar, unsigned parity, volat
 }
 // bounded wait for copies this thread has issued, whatever the other roles did: shared memory is
 // not left while a copy may still land in it
-static __device__ __noinline__ void t5_bar_drain(unsigned bar, unsigned parity) {
+__device__ __forceinline__ void t5_bar_drain(unsigned bar, unsigned parity) {
     const unsigned long long t0 = t5_now_ns();
     while (!t5_bar_try(bar, parity) && t5_now_ns() - t0 < T5_WAIT_NS) {}
 }
