@@ -10,8 +10,9 @@
 // conversion. Scales never touch K and V: a scale block is 16 columns of S, its key scale goes
 // into the factor of S, its value scale into P.
 //
-// Warps 0-3 and 4-7: softmax of the two tiles; 8-11: conversion; 12: products; 13: copies. While one tile's
-// softmax runs, the other tile's P V and the next S keep the tensor cores busy. The running
+// Warps 0-3 and 4-7: softmax of the two tiles; 8-11: conversion; 12 and 14: their products; 13: copies. A softmax
+// step takes half a key tile (64 keys): while it works on one half, the tensor cores multiply the
+// other half's weights and put the next tile's scores in their place. The running
 // maximum of a row is only moved when it is off by more than 2^8 (P stays below 2^8, far from
 // fp16's end), so sums in tensor memory are rarely touched between tiles.
 //
@@ -25,7 +26,9 @@ namespace {
 constexpr int PR_ROWS = 128;             // query rows of a tile; two per CTA
 constexpr int PR_KEYS = 128;             // keys of a tile
 constexpr int PR_BLOCKS = PR_KEYS / SB_KV8_BLOCK;
-constexpr int PR_THREADS = 16 * 32;       // warps 14 and 15 only lend their registers
+constexpr int PR_SUB = 64;               // keys of a softmax step: half a tile
+constexpr int PR_SUBBLOCKS = PR_SUB / SB_KV8_BLOCK;
+constexpr int PR_THREADS = 16 * 32;       // warp 15 only lends its registers
 // registers of a softmax, conversion and other warp's thread: 8 x 184 + 4 x 96 + 4 x 48 warps' shares <= 16 x 128
 constexpr int PR_REGS_SOFTMAX = 184, PR_REGS_CONVERT = 96, PR_REGS_REST = 48;
 static_assert(8 * PR_REGS_SOFTMAX + 4 * PR_REGS_CONVERT + 4 * PR_REGS_REST <= 16 * 128, "what the block was launched with");
@@ -41,7 +44,7 @@ struct PrShape {
     static constexpr int Q_AT = 0, T_AT = 2 * OPERAND, RAW_AT = T_AT + RING * OPERAND;
     static constexpr int SC_AT = RAW_AT + RAW_RING * RAW;           // scales of four tiles: 8 of K, 8 of V
     static constexpr int BAR_AT = SC_AT + 4 * 64;
-    static constexpr int SMEM = BAR_AT + 256 + 1024;
+    static constexpr int SMEM = BAR_AT + 288 + 1024;
     // tensor memory: S (and P) of the two tiles, then O of the two tiles
     static constexpr int S_COL = 0, O_COL = 256, TMEM = DP == 64 ? 512 : 512;
 };
@@ -51,15 +54,6 @@ __device__ __forceinline__ void pr_st16(unsigned taddr, const uint32_t (&r)[16])
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-__device__ __forceinline__ void pr_st32(unsigned taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
 __device__ __forceinline__ void pr_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // fp16 x fp16 -> fp32, M = 128; A from shared memory (a descriptor) or tensor memory
@@ -89,48 +83,40 @@ __device__ __forceinline__ constexpr unsigned pr_idesc(int n, bool b_mn) {
     return 1u << 4 | (b_mn ? 1u << 16 : 0u) | (unsigned)(n >> 3) << 17 | (unsigned)(PR_ROWS >> 4) << 24;
 }
 
-// Column c of a row's 128 scores is seen if from < c <= upto; EDGE: some are not.
+// Column c of a row's 64 scores is seen if from < c <= upto; EDGE: some are not.
 // Largest score of a row, in units of log2 (kf: factor of each 16 columns, not negative).
 template <bool EDGE>
-__device__ __forceinline__ float pr_max(unsigned ts, unsigned (&s)[2][32], const float (&kf)[PR_BLOCKS], int upto, int from) {
+__device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const float (&kf)[PR_SUBBLOCKS], int upto, int from) {
     float mx = -INFINITY;
-    t5_ld32(ts, s[0]);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        t5_wait_ld();
-        if (c < 3) t5_ld32(ts + 32 * (c + 1), s[(c + 1) & 1]);
+    for (int h = 0; h < PR_SUBBLOCKS; ++h) {
+        float bm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float bm[2] = {-INFINITY, -INFINITY};
+        for (int i = 0; i < 16; i += 4) {
+            float x[4];
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                float x[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    x[u] = __uint_as_float(s[c & 1][16 * h + i + u]);
-                    if (EDGE && (32 * c + 16 * h + i + u > upto || 32 * c + 16 * h + i + u <= from)) x[u] = -INFINITY;
-                }
-                bm[0] = fmaxf(fmaxf(bm[0], x[0]), x[1]);
-                bm[1] = fmaxf(fmaxf(bm[1], x[2]), x[3]);
+            for (int u = 0; u < 4; ++u) {
+                const int c = 16 * h + i + u;
+                x[u] = __uint_as_float(s[c >> 5][c & 31]);
+                if (EDGE && (c > upto || c <= from)) x[u] = -INFINITY;
             }
-            const float top = fmaxf(bm[0], bm[1]);
-            // a factor of 0 makes 0 of any score, but no NaN of a block that is masked whole
-            mx = fmaxf(mx, EDGE && top == -INFINITY ? -INFINITY : top * kf[2 * c + h]);
+            bm[0] = fmaxf(fmaxf(bm[0], x[0]), x[1]);
+            bm[1] = fmaxf(fmaxf(bm[1], x[2]), x[3]);
         }
+        const float top = fmaxf(bm[0], bm[1]);
+        // a factor of 0 makes 0 of any score, but no NaN of a block that is masked whole
+        mx = fmaxf(mx, EDGE && top == -INFINITY ? -INFINITY : top * kf[h]);
     }
     return mx;
 }
 // The row's weights 2^(score - ref), times the value scale of their 16 columns, in fp16 over the
-// columns whose scores have been read; returns the sum of the weights.
+// scores; returns the sum of the weights.
 template <bool EDGE>
-__device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[2][32], const float (&kf)[PR_BLOCKS], const float (&vs)[PR_BLOCKS],
-                                            float inv, float ref, int upto, int from) {
+__device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[PR_SUB / 32][32], const float (&kf)[PR_SUBBLOCKS],
+                                            const float (&vs)[PR_SUBBLOCKS], float inv, float ref, int upto, int from) {
     float sum[2] = {0.f, 0.f};
-    t5_ld32(ts, s[0]);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        t5_wait_ld();
-        if (c < 3) t5_ld32(ts + 32 * (c + 1), s[(c + 1) & 1]);
+    for (int c = 0; c < PR_SUB / 32; ++c) {
         uint32_t p[16];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -140,7 +126,7 @@ __device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[2][32], c
                 float e[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    e[u] = at_exp2(fmaf(__uint_as_float(s[c & 1][16 * h + i + u]), kk, -ref));
+                    e[u] = at_exp2(fmaf(__uint_as_float(s[c][16 * h + i + u]), kk, -ref));
                     if (EDGE && (32 * c + 16 * h + i + u > upto || 32 * c + 16 * h + i + u <= from)) e[u] = 0.f;
                     sum[u] += e[u];
                 }
@@ -160,10 +146,11 @@ kv8_prompt_kernel(const AtArgs a) {
     unsigned char* smem = pr_raw + ((1024u - (t5_smem(pr_raw) & 1023u)) & 1023u);
     float* sc = reinterpret_cast<float*>(smem + S::SC_AT);           // [4][16]
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + S::BAR_AT);
-    // raw tiles: landed, converted; converted tiles: there, multiplied; per row tile: scores, weights, sums
-    unsigned long long *raw_full = bars, *raw_empty = bars + 4, *full = bars + 8, *empty = bars + 11, *sfull = bars + 14,
-                       *pfull = bars + 16, *odone = bars + 18, *scfull = bars + 20, *qready = bars + 24, *last = bars + 25;
-    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 26);
+    // raw tiles: landed, converted; converted tiles: there, multiplied; per row tile (and half of a key
+    // tile): scores, weights, sums
+    unsigned long long *raw_full = bars, *raw_empty = bars + 4, *full = bars + 8, *empty = bars + 12, *sfull = bars + 16,
+                       *pfull = bars + 20, *odone = bars + 24, *scfull = bars + 26, *qready = bars + 30, *last = bars + 32;
+    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 34);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int head = blockIdx.x, b = blockIdx.z;
@@ -200,16 +187,18 @@ kv8_prompt_kernel(const AtArgs a) {
         }
         for (int i = 0; i < S::RING; ++i) {
             t5_bar_init(t5_smem(full + i), 4);
-            t5_bar_init(t5_smem(empty + i), 1);
+            t5_bar_init(t5_smem(empty + i), two ? 2 : 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             t5_bar_init(t5_smem(sfull + i), 1);
             t5_bar_init(t5_smem(pfull + i), 4);
-            t5_bar_init(t5_smem(odone + i), 1);
         }
+        for (int i = 0; i < 2; ++i) t5_bar_init(t5_smem(odone + i), 1);
         for (int i = 0; i < 4; ++i) t5_bar_init(t5_smem(scfull + i), 1);
-        t5_bar_init(t5_smem(qready), two ? 8 : 4);
-        t5_bar_init(t5_smem(last), 1);
+        for (int i = 0; i < 2; ++i) {
+            t5_bar_init(t5_smem(qready + i), 4);
+            t5_bar_init(t5_smem(last + i), 1);
+        }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -237,25 +226,25 @@ kv8_prompt_kernel(const AtArgs a) {
             {
                 const int64_t tok = rq.row0 + (real ? row / a.group : 0);
                 const __nv_bfloat16* src = a.q + tok * a.q_token_stride + (int64_t)(head * a.group + (real ? row % a.group : 0)) * a.q_head_stride;
-                uint32_t amax = 0;
-                for (int d = 0; d < D; d += 8) {
-                    const uint4 x = real ? *reinterpret_cast<const uint4*>(src + d) : make_uint4(0, 0, 0, 0);
-                    uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
-                    amax = max(amax, max(m & 0xffffu, m >> 16));
-                }
-                const float up = at_query_scale(amax);
+                uint4 x[DP / 8];
+                uint32_t m = 0;
+#pragma unroll
+                for (int c = 0; c < DP / 8; ++c)
+                    x[c] = real && 8 * c < D ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < DP / 8; ++c)
+                    m = __vmaxu2(m, __vmaxu2(__vmaxu2(x[c].x & 0x7fff7fffu, x[c].y & 0x7fff7fffu), __vmaxu2(x[c].z & 0x7fff7fffu, x[c].w & 0x7fff7fffu)));
+                const float up = at_query_scale(max(m & 0xffffu, m >> 16));
                 fq = __fdiv_rn(a.scale_log2, up);
                 unsigned char* q = smem + S::Q_AT + qt * S::OPERAND + (r & 127) * 128;
 #pragma unroll
-                for (int c = 0; c < DP / 8; ++c) {
-                    const uint4 x = real && 8 * c < D ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
+                for (int c = 0; c < DP / 8; ++c)
                     *reinterpret_cast<uint4*>(q + (c >> 3) * S::PANEL + (((c & 7) ^ (r & 7)) << 4)) =
-                        make_uint4(at_half2(bf16lo(x.x) * up, bf16hi(x.x) * up), at_half2(bf16lo(x.y) * up, bf16hi(x.y) * up),
-                                   at_half2(bf16lo(x.z) * up, bf16hi(x.z) * up), at_half2(bf16lo(x.w) * up, bf16hi(x.w) * up));
-                }
+                        make_uint4(at_half2(bf16lo(x[c].x) * up, bf16hi(x[c].x) * up), at_half2(bf16lo(x[c].y) * up, bf16hi(x[c].y) * up),
+                                   at_half2(bf16lo(x[c].z) * up, bf16hi(x[c].z) * up), at_half2(bf16lo(x[c].w) * up, bf16hi(x[c].w) * up));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) t5_bar_arrive(t5_smem(qready));
+                if (lane == 0) t5_bar_arrive(t5_smem(qready + qt));
             }
             const int pos = real ? rq.past + row / a.group : -1;
             // positions of the tile's first and last row decide which key tiles need a mask
@@ -265,23 +254,27 @@ kv8_prompt_kernel(const AtArgs a) {
             const unsigned ts = tmem + lanes + S::S_COL + qt * 128, to = tmem + lanes + S::O_COL + qt * DP;
             float m = -INFINITY, l = 0.f, vref = 0.f;
             bool ok = true;
-            for (int j = 0; j < ntiles; ++j) {
-                ok = wait(sfull + qt, j) && wait(scfull + (j & 3), j >> 2);
+            for (int n = 0; n < 2 * ntiles; ++n) {                   // halves of the key tiles
+                const int j = n >> 1, u = n & 1;
+                ok = wait(sfull + 2 * qt + u, j) && (u || wait(scfull + (j & 3), j >> 2));
                 if (!ok) break;
                 t5_fence_after();
-                const int key = k0 + j * PR_KEYS;
-                const bool edge = key + PR_KEYS > pos_lo + 1 || key + PR_KEYS > k1 || ragged || (a.window > 0 && key <= pos_hi - a.window);
-                const float* scj = sc + 16 * (j & 3);
-                float kf[PR_BLOCKS], vs[PR_BLOCKS], vmax = 0.f;
+                unsigned s[PR_SUB / 32][32];
+                t5_ld32(ts + PR_SUB * u, s[0]);
+                t5_ld32(ts + PR_SUB * u + 32, s[1]);
+                const int key = k0 + n * PR_SUB;
+                const bool edge = key + PR_SUB > pos_lo + 1 || key + PR_SUB > k1 || ragged || (a.window > 0 && key <= pos_hi - a.window);
+                const float* scj = sc + 16 * (j & 3) + PR_SUBBLOCKS * u;
+                float kf[PR_SUBBLOCKS], vs[PR_SUBBLOCKS], vmax = 0.f;
 #pragma unroll
-                for (int i = 0; i < PR_BLOCKS; ++i) {
+                for (int i = 0; i < PR_SUBBLOCKS; ++i) {
                     kf[i] = scj[i] * fq;
                     vs[i] = scj[PR_BLOCKS + i];
                     vmax = fmaxf(vmax, vs[i]);
                 }
                 const int upto = min(pos, k1 - 1) - key, from = a.window > 0 ? pos - a.window - key : -1;
-                unsigned s[2][32];
-                const float mx = edge ? pr_max<true>(ts, s, kf, upto, from) : pr_max<false>(ts, s, kf, upto, from);
+                t5_wait_ld();
+                const float mx = edge ? pr_max<true>(s, kf, upto, from) : pr_max<false>(s, kf, upto, from);
                 // move the reference (and the power of two of the value scales) when it is too far off
                 float f = 1.f;
                 if (mx > m + PR_SLACK || (m == -INFINITY && mx > m)) {
@@ -294,26 +287,31 @@ kv8_prompt_kernel(const AtArgs a) {
                     f *= __fdiv_rn(vref, fresh);
                     vref = fresh;
                 }
-                if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-#pragma unroll
-                    for (int c = 0; c < DP / 32; ++c) {
-                        unsigned o[32];
-                        t5_ld32(to + 32 * c, o);
+                if (n > 0 && __any_sync(0xffffffffu, f != 1.f)) {
+                    // the sums so far: the products of the half before this one have to be done
+                    ok = wait(odone + qt, n - 1);
+                    if (!ok) break;
+                    t5_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < DP; c += 16) {
+                        unsigned o[16];
+                        t5_ld16(to + c, o);
                         t5_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        pr_st32(to + 32 * c, o);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        pr_st16(to + c, o);
                     }
                 }
                 const float inv = at_value_inv(vref), ref = m == -INFINITY ? 0.f : m;
-                l += edge ? pr_weights<true>(ts, s, kf, vs, inv, ref, upto, from) : pr_weights<false>(ts, s, kf, vs, inv, ref, upto, from);
+                l += edge ? pr_weights<true>(ts + PR_SUB * u, s, kf, vs, inv, ref, upto, from)
+                          : pr_weights<false>(ts + PR_SUB * u, s, kf, vs, inv, ref, upto, from);
                 pr_wait_st();
                 t5_fence_before();
                 __syncwarp();
-                if (lane == 0) t5_bar_arrive(t5_smem(pfull + qt));
+                if (lane == 0) t5_bar_arrive(t5_smem(pfull + 2 * qt + u));
             }
             // ---- results ----
-            if (ok) ok = wait(odone + qt, 0);
+            if (ok) ok = wait(odone + qt, 2 * ntiles - 1);
             if (ok) {
                 t5_fence_after();
                 const int64_t tok = rq.row0 + row / a.group;
@@ -457,65 +455,60 @@ kv8_prompt_kernel(const AtArgs a) {
         // copies in flight land before the block leaves
         for (int i = max(0, issued - S::RAW_RING); i < issued; ++i)
             t5_bar_drain(t5_smem(raw_full + i % S::RAW_RING), (unsigned)(i / S::RAW_RING) & 1u);
-    } else if (warp == 12) {
-        // ---- products ----
+    } else if (warp == 12 || (warp == 14 && two)) {
+        // ---- products of one row tile ----
+        const int qt = warp == 14;
         const bool one = t5_elect();
-        bool ok = wait(qready, 0);
-        auto scores = [&](int qt, int j) {
-            const unsigned q = t5_smem(smem + S::Q_AT + qt * S::OPERAND), k = t5_smem(smem + S::T_AT + 2 * j % S::RING * S::OPERAND);
+        // n: half of a key tile
+        auto scores = [&](int n) {
+            const unsigned q = t5_smem(smem + S::Q_AT + qt * S::OPERAND);
+            const unsigned k = t5_smem(smem + S::T_AT + (n & ~1) % S::RING * S::OPERAND) + (unsigned)((n & 1) * PR_SUB * 128);
 #pragma unroll
             for (int s = 0; s < DP / 16; ++s)
-                pr_mma_ss(one, tmem + S::S_COL + qt * 128, t5_desc_sw128(q + (s >> 2) * S::PANEL + 32 * (s & 3)),
-                          t5_desc_sw128(k + (s >> 2) * S::PANEL + 32 * (s & 3)), pr_idesc(PR_KEYS, false), s > 0);
-            pr_commit(one, t5_smem(sfull + qt));
+                pr_mma_ss(one, tmem + S::S_COL + qt * 128 + (n & 1) * PR_SUB, t5_desc_sw128(q + (s >> 2) * S::PANEL + 32 * (s & 3)),
+                          t5_desc_sw128(k + (s >> 2) * S::PANEL + 32 * (s & 3)), pr_idesc(PR_SUB, false), s > 0);
+            pr_commit(one, t5_smem(sfull + 2 * qt + (n & 1)));
         };
-        auto values = [&](int qt, int j) {
-            const unsigned v = t5_smem(smem + S::T_AT + (2 * j + 1) % S::RING * S::OPERAND);
+        auto values = [&](int n) {
+            const unsigned v = t5_smem(smem + S::T_AT + (n | 1) % S::RING * S::OPERAND) + (unsigned)((n & 1) * PR_SUB * 128);
 #pragma unroll
-            for (int s = 0; s < PR_KEYS / 16; ++s)
-                pr_mma_ts(one, tmem + S::O_COL + qt * DP, tmem + S::S_COL + qt * 128 + 8 * s, pr_desc_v<DP>(v + 2048 * s),
-                          pr_idesc(DP, true), j > 0 || s > 0);
-            if (j == ntiles - 1) pr_commit(one, t5_smem(odone + qt));
+            for (int s = 0; s < PR_SUB / 16; ++s)
+                pr_mma_ts(one, tmem + S::O_COL + qt * DP, tmem + S::S_COL + qt * 128 + (n & 1) * PR_SUB + 8 * s, pr_desc_v<DP>(v + 2048 * s),
+                          pr_idesc(DP, true), n > 0 || s > 0);
+            pr_commit(one, t5_smem(odone + qt));
         };
-        auto there = [&](int n) { return wait(full + n % S::RING, n / S::RING); };
-        auto done = [&](int n) { pr_commit(one, t5_smem(empty + n % S::RING)); };
-        ok = ok && there(0);
+        // converted tiles in the order K 0, V 0, K 1, V 1, ...: the halves 2 j and 2 j + 1 use tiles
+        // 2 j (keys) and 2 j + 1 (values)
+        auto there = [&](int tile) { return wait(full + tile % S::RING, tile / S::RING); };
+        auto done = [&](int tile) { pr_commit(one, t5_smem(empty + tile % S::RING)); };
+        const int halves = 2 * ntiles;
+        bool ok = wait(qready + qt, 0) && there(0);
         if (ok) {
             t5_fence_after();
-            scores(0, 0);
-            if (two) scores(1, 0);
+            scores(0);
+            scores(1);
             done(0);
         }
-        for (int j = 0; ok && j < ntiles; ++j) {
-            const int v = 2 * j + 1, k = 2 * j + 2;                  // this tile's values, the next tile's keys
-            const bool more = j + 1 < ntiles;
-            ok = there(v) && wait(pfull, j);
+        for (int n = 0; ok && n < halves; ++n) {
+            const int tile = n & ~1;
+            ok = ((n & 1) || there(tile + 1)) && wait(pfull + 2 * qt + (n & 1), n >> 1);
             if (!ok) break;
             t5_fence_after();
-            values(0, j);
-            if (!two) done(v);
-            if (more) {
-                ok = there(k);
+            values(n);
+            if (n & 1) done(tile + 1);
+            if (n + 2 < halves) {
+                // The same half of the next tile's scores, into the columns the weights were read from.
+                // Products of different shapes are not ordered by their issue: those have to be done.
+                ok = ((n & 1) || there(tile + 2)) && wait(odone + qt, n);
                 if (!ok) break;
                 t5_fence_after();
-                scores(0, j + 1);
-                if (!two) done(k);
-            }
-            if (two) {
-                ok = wait(pfull + 1, j);
-                if (!ok) break;
-                t5_fence_after();
-                values(1, j);
-                done(v);
-                if (more) {
-                    scores(1, j + 1);
-                    done(k);
-                }
+                scores(n + 2);
+                if (n & 1) done(tile + 2);
             }
         }
         if (!ok) {                                   // what was issued still reads shared memory
-            pr_commit(one, t5_smem(last));
-            t5_bar_drain(t5_smem(last), 0u);
+            pr_commit(one, t5_smem(last + qt));
+            t5_bar_drain(t5_smem(last + qt), 0u);
         }
     }
     __syncwarp();
