@@ -183,7 +183,7 @@ kv8_rows_kernel(const AtArgs a) {
         for (int e = 0; e < 2; ++e) {
             const int r = 8 * nr + 2 * t + e;
             fq[nr][e] = reinterpret_cast<const float*>(smem + S::F_AT)[r];
-            pos[nr][e] = r < nrow ? rq.past + (r0 + r) / a.group : -1;
+            pos[nr][e] = rq.past + (r0 + r) / a.group;          // rows past the last: queries of zeros, dropped at the end
         }
     // B operand of step 4 c + j: d = 64 c + 16 t + 4 j + {0, 1} and + {2, 3} of row g
     const unsigned qlane = at_smem(smem) + S::Q_AT + (unsigned)(g * S::QPITCH + 32 * t);
@@ -257,7 +257,7 @@ kv8_rows_kernel(const AtArgs a) {
                 }
             }
         }
-        const bool edge = key + AT_STEP > rq.past + i0 + 1 || key + AT_STEP > k1 || (a.window > 0 && key <= rq.past + i1 - a.window) || nrow < S::ROWS;
+        const bool edge = key + AT_STEP > rq.past + i0 + 1 || key + AT_STEP > k1 || (a.window > 0 && key <= rq.past + i1 - a.window);
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             float mx[2] = {-INFINITY, -INFINITY};

@@ -13,6 +13,7 @@ struct AtArgs {
     int64_t o_token_stride, o_head_stride;
     float* lse;
     int group;                   // query heads per cache head
+    unsigned group_inverse;      // ceil(2^32 / group), for group > 1
     int row_tiles, splits;       // of the grid
     int chunk;                   // keys per CTA
     float scale_log2;            // softmax scale * log2(e)

@@ -29,9 +29,11 @@ constexpr int PR_BLOCKS = PR_KEYS / SB_KV8_BLOCK;
 constexpr int PR_SUB = 64;               // keys of a softmax step: half a tile
 constexpr int PR_SUBBLOCKS = PR_SUB / SB_KV8_BLOCK;
 constexpr int PR_THREADS = 16 * 32;       // warp 15 only lends its registers
-// registers of a softmax, conversion and other warp's thread: 8 x 184 + 4 x 96 + 4 x 48 warps' shares <= 16 x 128
-constexpr int PR_REGS_SOFTMAX = 184, PR_REGS_CONVERT = 96, PR_REGS_REST = 48;
+// registers of a softmax, conversion and other warp's thread: 8 x 160 + 4 x 96 + 4 x 96 warps' shares <= 16 x 128
+constexpr int PR_REGS_SOFTMAX = 160, PR_REGS_CONVERT = 96, PR_REGS_REST = 96;
 static_assert(8 * PR_REGS_SOFTMAX + 4 * PR_REGS_CONVERT + 4 * PR_REGS_REST <= 16 * 128, "what the block was launched with");
+constexpr int PR_EXTRA = 4;              // what an item costs besides its key tiles, in key tiles
+constexpr int PR_LEAST = 8;              // units of a share at least
 constexpr float PR_SLACK = 8.f;          // log2 of how far a row's maximum may run ahead of its reference
 
 template <int DP>
@@ -43,8 +45,9 @@ struct PrShape {
     static constexpr int RAW = PR_KEYS * DP;
     static constexpr int Q_AT = 0, T_AT = 2 * OPERAND, RAW_AT = T_AT + RING * OPERAND;
     static constexpr int SC_AT = RAW_AT + RAW_RING * RAW;           // scales of four tiles: 8 of K, 8 of V
-    static constexpr int BAR_AT = SC_AT + 4 * 64;
-    static constexpr int SMEM = BAR_AT + 288 + 1024;
+    static constexpr int F_AT = SC_AT + 4 * 64;                      // score factor of a row, fp32
+    static constexpr int BAR_AT = F_AT + 2 * PR_ROWS * 4;
+    static constexpr int SMEM = BAR_AT + 304 + 1024;
     // tensor memory: S (and P) of the two tiles, then O of the two tiles
     static constexpr int S_COL = 0, O_COL = 256, TMEM = DP == 64 ? 512 : 512;
 };
@@ -113,72 +116,184 @@ __device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const fl
 // scores; returns the sum of the weights.
 template <bool EDGE>
 __device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[PR_SUB / 32][32], const float (&kf)[PR_SUBBLOCKS],
-                                            const float (&vs)[PR_SUBBLOCKS], float inv, float ref, int upto, int from) {
-    float sum[2] = {0.f, 0.f};
+                                            const float (&vw)[PR_SUBBLOCKS], float ref, int upto, int from) {
+    f32x2 sum[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
+    const f32x2 off = pk2(-ref, -ref);
 #pragma unroll
     for (int c = 0; c < PR_SUB / 32; ++c) {
         uint32_t p[16];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float vw = vs[2 * c + h] * inv, kk = kf[2 * c + h];
+            const f32x2 w = pk2(vw[2 * c + h], vw[2 * c + h]), kk = pk2(kf[2 * c + h], kf[2 * c + h]);
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 float e[2];
+                upk2(fma2(pk2(__uint_as_float(s[c][16 * h + i]), __uint_as_float(s[c][16 * h + i + 1])), kk, off), e[0], e[1]);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    e[u] = at_exp2(fmaf(__uint_as_float(s[c][16 * h + i + u]), kk, -ref));
+                    e[u] = at_exp2(e[u]);
                     if (EDGE && (32 * c + 16 * h + i + u > upto || 32 * c + 16 * h + i + u <= from)) e[u] = 0.f;
-                    sum[u] += e[u];
                 }
-                p[8 * h + i / 2] = at_half2(e[0] * vw, e[1] * vw);
+                const f32x2 x = pk2(e[0], e[1]);
+                sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], x);
+                upk2(mul2(x, w), e[0], e[1]);
+                p[8 * h + i / 2] = at_half2(e[0], e[1]);
             }
         }
         pr_st16(ts + 16 * c, p);
     }
-    return sum[0] + sum[1];
+    float lo, hi;
+    upk2(add2(sum[0], sum[1]), lo, hi);
+    return lo + hi;
 }
+
+// ---- who does what -------------------------------------------------------------------------------
+// An item is 256 query rows of a request and head; its work, in units, is its key tiles and PR_EXTRA
+// for its queries and results. The units of all items, one after the other (requests, row tiles,
+// heads), are cut into equal shares, one per CTA: the requests' lengths are known on the device only,
+// and a share costs the same whatever they are. An item that a share's border cuts leaves its pieces
+// in scratch, and kv8_prompt_sum_kernel adds them.
+struct PrWork {
+    long long* prefix;           // [items / heads + 1] units of one head before the row tile
+    int4* start;                 // [ctas] (row tile of all requests, head, unit) a share starts with; x < 0: no share
+    long long* share;            // units of a share; units in all
+    int ctas;
+};
+struct PrItem {
+    Kv8Request rq;
+    int b, r0, nrow;             // rows of the request's n * group from r0
+    int lo, hi;                  // keys that some row sees
+    int tiles;
+    __device__ __forceinline__ int units() const { return tiles ? tiles + PR_EXTRA : 0; }
+};
+__device__ __forceinline__ PrItem pr_item(const AtArgs& a, int row_tile, SbDeviceState* st) {
+    PrItem it;
+    it.b = row_tile / a.row_tiles;
+    it.r0 = (row_tile - it.b * a.row_tiles) * 2 * PR_ROWS;
+    it.tiles = 0;
+    if (!kv8_request(a.g, it.b, it.rq, st)) return it;
+    const int rows = it.rq.n * a.group;
+    if (it.r0 >= rows) return it;
+    it.nrow = min(2 * PR_ROWS, rows - it.r0);
+    const int i0 = it.r0 / a.group, i1 = (it.r0 + it.nrow - 1) / a.group;
+    it.hi = it.rq.past + i1 + 1;
+    it.lo = a.window > 0 ? max(0, it.rq.past + i0 - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
+    it.tiles = (it.hi - it.lo + PR_KEYS - 1) / PR_KEYS;
+    return it;
+}
+__global__ void __launch_bounds__(1024)
+kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
+    __shared__ long long warp_sum_at[32], total_at;
+    const int n = a.row_tiles * a.g.requests, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long before = 0;
+    for (int base = 0; base < n; base += 1024) {
+        const int i = base + threadIdx.x;
+        const long long mine = i < n ? pr_item(a, i, a.st).units() : 0;
+        long long x = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) warp_sum_at[warp] = x;
+        __syncthreads();
+        if (warp == 0) {
+            long long t = warp_sum_at[lane];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, t, o);
+                if (lane >= o) t += y;
+            }
+            warp_sum_at[lane] = t;
+            if (lane == 31) total_at = t;
+        }
+        __syncthreads();
+        if (i < n) w.prefix[i] = before + x - mine + (warp ? warp_sum_at[warp - 1] : 0);
+        before += total_at;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) w.prefix[n] = before;
+    __syncthreads();
+    const long long total = before * a.g.heads;
+    const long long share = max((total + w.ctas - 1) / w.ctas, (long long)PR_LEAST);
+    if (threadIdx.x == 0) { w.share[0] = share; w.share[1] = total; }
+    for (int c = threadIdx.x; c < w.ctas; c += 1024) {
+        const long long at = c * share;
+        if (at >= total) { w.start[c] = make_int4(-1, 0, 0, 0); continue; }
+        int lo = 0, hi = n;                                          // the last row tile that starts at or before `at`
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (w.prefix[mid] * a.g.heads <= at) lo = mid; else hi = mid;
+        }
+        const long long rest = at - w.prefix[lo] * a.g.heads, units = w.prefix[lo + 1] - w.prefix[lo];
+        w.start[c] = make_int4(lo, (int)(rest / units), (int)(rest % units), 0);
+    }
+}
+
+// A share as its pieces of items; every warp walks through them by itself.
+struct PrWalk {
+    int row_tile, head, unit;                                        // where the piece starts
+    int tile0, count;                                                // its key tiles: tile0 .. + count of it.tiles
+    long long left;
+    bool first;
+    PrItem it;
+    // the piece from `unit` on; its key tiles may be none (only what an item costs besides)
+    __device__ __forceinline__ void cut() {
+        const int units = (int)min((long long)(it.units() - unit), left);
+        tile0 = max(0, unit - PR_EXTRA);
+        count = max(0, unit + units - PR_EXTRA) - tile0;
+        left -= units;
+    }
+    __device__ __forceinline__ bool step(const AtArgs& a) {
+        while (count == 0) {
+            if (left <= 0) return false;
+            first = false;
+            unit = 0;
+            if (++head >= a.g.heads || it.tiles == 0) {
+                head = 0;
+                if (++row_tile >= a.row_tiles * a.g.requests) return false;
+                it = pr_item(a, row_tile, a.st);
+            }
+            if (it.tiles) cut();
+        }
+        return true;
+    }
+    __device__ __forceinline__ bool begin(const AtArgs& a, const PrWork& w) {
+        const int4 s = w.start[blockIdx.x];
+        if (s.x < 0) return false;
+        left = min(w.share[0], w.share[1] - (long long)blockIdx.x * w.share[0]);
+        row_tile = s.x; head = s.y; unit = s.z;
+        first = true;
+        it = pr_item(a, row_tile, a.st);
+        count = 0;
+        if (it.tiles) cut();
+        return step(a);
+    }
+    __device__ __forceinline__ bool next(const AtArgs& a) {
+        count = 0;
+        return step(a);
+    }
+};
 
 template <int TYPE, int DP>
 __global__ void __launch_bounds__(PR_THREADS, 1)
-kv8_prompt_kernel(const AtArgs a) {
+kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     using S = PrShape<DP>;
     extern __shared__ unsigned char pr_raw[];
     unsigned char* smem = pr_raw + ((1024u - (t5_smem(pr_raw) & 1023u)) & 1023u);
     float* sc = reinterpret_cast<float*>(smem + S::SC_AT);           // [4][16]
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + S::BAR_AT);
     // raw tiles: landed, converted; converted tiles: there, multiplied; per row tile (and half of a key
-    // tile): scores, weights, sums
+    // tile): scores, weights, sums; all sums of a piece.  A wait tells a phase from its neighbours only
+    // (one bit), so every barrier is waited for by someone who cannot be two phases away.
     unsigned long long *raw_full = bars, *raw_empty = bars + 4, *full = bars + 8, *empty = bars + 12, *sfull = bars + 16,
-                       *pfull = bars + 20, *odone = bars + 24, *scfull = bars + 26, *qready = bars + 30, *last = bars + 32;
-    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 34);
+                       *pfull = bars + 20, *odone = bars + 24, *scfull = bars + 26, *qready = bars + 30, *last = bars + 32, *fin = bars + 34;
+    unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 36);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int head = blockIdx.x, b = blockIdx.z;
-    const int split = (int)(blockIdx.y % (unsigned)a.splits);
-    const int rt = a.row_tiles - 1 - (int)(blockIdx.y / (unsigned)a.splits);        // the longest first
     const int D = a.g.dim;
-    Kv8Request rq;
-    if (!kv8_request(a.g, b, rq, a.st)) return;
-    const int rows = rq.n * a.group, r0 = rt * 2 * PR_ROWS;
-    if (r0 >= rows) return;
-    const int nrow = min(2 * PR_ROWS, rows - r0);
-    const bool two = nrow > PR_ROWS;
-    const int i0 = r0 / a.group, i1 = (r0 + nrow - 1) / a.group;
-    const int hi = rq.past + i1 + 1;
-    const int lo = a.window > 0 ? max(0, rq.past + i0 - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
-    int chunk = a.chunk;                                             // max_len may be too small: then the chunks grow
-    if ((int64_t)chunk * a.splits < hi - lo) chunk = ((hi - lo + a.splits - 1) / a.splits + PR_KEYS - 1) / PR_KEYS * PR_KEYS;
-    const int nsplit = (hi - lo + chunk - 1) / chunk;
-    const int64_t tile_id = ((int64_t)b * a.g.heads + head) * a.row_tiles + rt;
-    if (split >= nsplit) {
-        // nothing here: the sum over the chunks skips it
-        if (a.splits > 1)
-            for (int r = threadIdx.x; r < 2 * PR_ROWS; r += PR_THREADS)
-                a.part_ml[(tile_id * a.splits + split) * (2 * PR_ROWS) + r] = make_float2(-INFINITY, 0.f);
-        return;
-    }
-    const int k0 = lo + split * chunk, k1 = min(hi, k0 + chunk);
-    const int ntiles = (k1 - k0 + PR_KEYS - 1) / PR_KEYS;
+    PrWalk wk;
+    if (!wk.begin(a, work)) return;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::RAW_RING; ++i) {
@@ -187,17 +302,18 @@ kv8_prompt_kernel(const AtArgs a) {
         }
         for (int i = 0; i < S::RING; ++i) {
             t5_bar_init(t5_smem(full + i), 4);
-            t5_bar_init(t5_smem(empty + i), two ? 2 : 1);
+            t5_bar_init(t5_smem(empty + i), 2);
         }
         for (int i = 0; i < 4; ++i) {
             t5_bar_init(t5_smem(sfull + i), 1);
             t5_bar_init(t5_smem(pfull + i), 4);
+            t5_bar_init(t5_smem(scfull + i), 1);
         }
-        for (int i = 0; i < 2; ++i) t5_bar_init(t5_smem(odone + i), 1);
-        for (int i = 0; i < 4; ++i) t5_bar_init(t5_smem(scfull + i), 1);
         for (int i = 0; i < 2; ++i) {
+            t5_bar_init(t5_smem(odone + i), 1);
             t5_bar_init(t5_smem(qready + i), 4);
             t5_bar_init(t5_smem(last + i), 1);
+            t5_bar_init(t5_smem(fin + i), 1);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -218,150 +334,189 @@ kv8_prompt_kernel(const AtArgs a) {
         // ---- softmax: one query row per thread ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_REGS_SOFTMAX));
         const int qt = warp >> 2;
-        if (qt == 0 || two) {
-            const int r = threadIdx.x;                               // row of the CTA
-            const int row = r0 + r;
-            const bool real = r < nrow;
-            float fq;
+        const unsigned lanes = (unsigned)((warp & 3) * 32) << 16;
+        const unsigned ts = tmem + lanes + S::S_COL + qt * 128, to = tmem + lanes + S::O_COL + qt * DP;
+        int tiles_all = 0, tiles_mine = 0, pieces = 0;               // key tiles and pieces so far (of this row tile)
+        bool ok = true;
+        for (bool more = true; more && ok; more = wk.next(a), ++tiles_all) {
+            const PrItem& it = wk.it;
+            const int count = wk.count;
+            tiles_all += count - 1;
+            const int base_all = tiles_all - (count - 1);
+            if (it.nrow <= qt * PR_ROWS) {                           // no rows, but no phase of a barrier is left out
+                for (int j = 0; ok && j < count; ++j) ok = wait(scfull + ((base_all + j) & 3), (base_all + j) >> 2);
+                continue;
+            }
+            const int r = threadIdx.x, row = it.r0 + r;              // row of the item, of the request
+            const bool real = r < it.nrow;
             {
-                const int64_t tok = rq.row0 + (real ? row / a.group : 0);
-                const __nv_bfloat16* src = a.q + tok * a.q_token_stride + (int64_t)(head * a.group + (real ? row % a.group : 0)) * a.q_head_stride;
-                uint4 x[DP / 8];
-                uint32_t m = 0;
+                // rows by half warps, 16 bytes a lane: the largest element, the scaling, fp16 into the
+                // swizzled operand
+                constexpr int LANES = DP / 8, RPI = 32 / LANES, NI = 32 / RPI;      // lanes of a row, rows at a time
+                const int c = lane % LANES, sub = lane / LANES;
+                float* factor = reinterpret_cast<float*>(smem + S::F_AT) + qt * PR_ROWS;
+                unsigned char* q0 = smem + S::Q_AT + qt * S::OPERAND + (c >> 3) * S::PANEL;
+                const int tok0 = it.r0 / a.group, head0 = it.r0 - tok0 * a.group;
+                const __nv_bfloat16* src = a.q + (int64_t)(it.rq.row0 + tok0) * a.q_token_stride + (int64_t)wk.head * a.group * a.q_head_stride + 8 * c;
+                uint4 x[NI];
 #pragma unroll
-                for (int c = 0; c < DP / 8; ++c)
-                    x[c] = real && 8 * c < D ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < NI; ++i) {
+                    const int rr = qt * PR_ROWS + (warp & 3) * 32 + i * RPI + sub, at = head0 + rr;
+                    const int tok = a.group > 1 ? (int)__umulhi((unsigned)at, a.group_inverse) : at;
+                    x[i] = make_uint4(0, 0, 0, 0);
+                    if (rr < it.nrow && 8 * c < D)
+                        x[i] = *reinterpret_cast<const uint4*>(src + tok * a.q_token_stride + (at - tok * a.group) * a.q_head_stride);
+                }
 #pragma unroll
-                for (int c = 0; c < DP / 8; ++c)
-                    m = __vmaxu2(m, __vmaxu2(__vmaxu2(x[c].x & 0x7fff7fffu, x[c].y & 0x7fff7fffu), __vmaxu2(x[c].z & 0x7fff7fffu, x[c].w & 0x7fff7fffu)));
-                const float up = at_query_scale(max(m & 0xffffu, m >> 16));
-                fq = __fdiv_rn(a.scale_log2, up);
-                unsigned char* q = smem + S::Q_AT + qt * S::OPERAND + (r & 127) * 128;
+                for (int i = 0; i < NI; ++i) {
+                    uint32_t m = __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
 #pragma unroll
-                for (int c = 0; c < DP / 8; ++c)
-                    *reinterpret_cast<uint4*>(q + (c >> 3) * S::PANEL + (((c & 7) ^ (r & 7)) << 4)) =
-                        make_uint4(at_half2(bf16lo(x[c].x) * up, bf16hi(x[c].x) * up), at_half2(bf16lo(x[c].y) * up, bf16hi(x[c].y) * up),
-                                   at_half2(bf16lo(x[c].z) * up, bf16hi(x[c].z) * up), at_half2(bf16lo(x[c].w) * up, bf16hi(x[c].w) * up));
+                    for (int o = 1; o < LANES; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    const float up = at_query_scale(max(m & 0xffffu, m >> 16));
+                    const int rr = (warp & 3) * 32 + i * RPI + sub;
+                    if (c == 0) factor[rr] = up;
+                    *reinterpret_cast<uint4*>(q0 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
+                        make_uint4(at_half2(bf16lo(x[i].x) * up, bf16hi(x[i].x) * up), at_half2(bf16lo(x[i].y) * up, bf16hi(x[i].y) * up),
+                                   at_half2(bf16lo(x[i].z) * up, bf16hi(x[i].z) * up), at_half2(bf16lo(x[i].w) * up, bf16hi(x[i].w) * up));
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) t5_bar_arrive(t5_smem(qready + qt));
             }
-            const int pos = real ? rq.past + row / a.group : -1;
+            const float fq = __fdiv_rn(a.scale_log2, reinterpret_cast<const float*>(smem + S::F_AT)[r]);
+            // (a thread without a row has queries of zeros, and its results go nowhere)
+            const int pos = it.rq.past + row / a.group;
             // positions of the tile's first and last row decide which key tiles need a mask
-            const int pos_lo = rq.past + (r0 + qt * PR_ROWS) / a.group, pos_hi = rq.past + (r0 + min(nrow, (qt + 1) * PR_ROWS) - 1) / a.group;
-            const bool ragged = nrow < (qt + 1) * PR_ROWS;
-            const unsigned lanes = (unsigned)((warp & 3) * 32) << 16;
-            const unsigned ts = tmem + lanes + S::S_COL + qt * 128, to = tmem + lanes + S::O_COL + qt * DP;
-            float m = -INFINITY, l = 0.f, vref = 0.f;
-            bool ok = true;
-            for (int n = 0; n < 2 * ntiles; ++n) {                   // halves of the key tiles
+            const int pos_lo = it.rq.past + (it.r0 + qt * PR_ROWS) / a.group;
+            const int pos_hi = it.rq.past + (it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1) / a.group;
+            const int k0 = it.lo + wk.tile0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
+            float m = -INFINITY, l = 0.f, vref = 0.f, inv = 0.f;
+            ok = wait(scfull + (base_all & 3), base_all >> 2);
+            for (int n = 0; ok && n < 2 * count; ++n) {              // halves of the key tiles
                 const int j = n >> 1, u = n & 1;
-                ok = wait(sfull + 2 * qt + u, j) && (u || wait(scfull + (j & 3), j >> 2));
+                ok = wait(sfull + 2 * qt + u, tiles_mine + j);
                 if (!ok) break;
                 t5_fence_after();
                 unsigned s[PR_SUB / 32][32];
                 t5_ld32(ts + PR_SUB * u, s[0]);
                 t5_ld32(ts + PR_SUB * u + 32, s[1]);
                 const int key = k0 + n * PR_SUB;
-                const bool edge = key + PR_SUB > pos_lo + 1 || key + PR_SUB > k1 || ragged || (a.window > 0 && key <= pos_hi - a.window);
-                const float* scj = sc + 16 * (j & 3) + PR_SUBBLOCKS * u;
-                float kf[PR_SUBBLOCKS], vs[PR_SUBBLOCKS], vmax = 0.f;
-#pragma unroll
-                for (int i = 0; i < PR_SUBBLOCKS; ++i) {
-                    kf[i] = scj[i] * fq;
-                    vs[i] = scj[PR_BLOCKS + i];
-                    vmax = fmaxf(vmax, vs[i]);
-                }
+                const bool edge = key + PR_SUB > pos_lo + 1 || key + PR_SUB > k1 || (a.window > 0 && key <= pos_hi - a.window);
+                const float4* scj = reinterpret_cast<const float4*>(sc + 16 * ((base_all + j) & 3) + PR_SUBBLOCKS * u);
+                const float4 k4 = scj[0], v4 = scj[PR_BLOCKS / 4];
+                const float kf[PR_SUBBLOCKS] = {k4.x * fq, k4.y * fq, k4.z * fq, k4.w * fq};
+                const float vmax = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
                 const int upto = min(pos, k1 - 1) - key, from = a.window > 0 ? pos - a.window - key : -1;
                 t5_wait_ld();
                 const float mx = edge ? pr_max<true>(s, kf, upto, from) : pr_max<false>(s, kf, upto, from);
-                // move the reference (and the power of two of the value scales) when it is too far off
-                float f = 1.f;
-                if (mx > m + PR_SLACK || (m == -INFINITY && mx > m)) {
-                    f = m == -INFINITY ? 0.f : at_exp2(m - mx);
-                    m = mx;
-                    l *= f;
-                }
-                if (vmax > vref) {
-                    const float fresh = at_value_ref(vmax);
-                    f *= __fdiv_rn(vref, fresh);
-                    vref = fresh;
-                }
-                if (n > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-                    // the sums so far: the products of the half before this one have to be done
-                    ok = wait(odone + qt, n - 1);
-                    if (!ok) break;
-                    t5_fence_after();
+                // the reference (and the power of two of the value scales) moves when it is too far off
+                const bool off = mx > m + PR_SLACK || (m == -INFINITY && mx > m) || vmax > vref;
+                if (__any_sync(0xffffffffu, off)) {
+                    float f = 1.f;
+                    if (mx > m + PR_SLACK || (m == -INFINITY && mx > m)) {
+                        f = m == -INFINITY ? 0.f : at_exp2(m - mx);
+                        m = mx;
+                        l *= f;
+                    }
+                    if (vmax > vref) {
+                        const float fresh = at_value_ref(vmax);
+                        f *= __fdiv_rn(vref, fresh);
+                        vref = fresh;
+                        inv = at_value_inv(vref);
+                    }
+                    if (n > 0) {
+                        // the sums so far: the products of the half before this one have to be done
+                        ok = wait(odone + qt, 2 * tiles_mine + n - 1);
+                        if (!ok) break;
+                        t5_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < DP; c += 16) {
-                        unsigned o[16];
-                        t5_ld16(to + c, o);
-                        t5_wait_ld();
+                        for (int c = 0; c < DP; c += 16) {
+                            unsigned o[16];
+                            t5_ld16(to + c, o);
+                            t5_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        pr_st16(to + c, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            pr_st16(to + c, o);
+                        }
                     }
                 }
-                const float inv = at_value_inv(vref), ref = m == -INFINITY ? 0.f : m;
-                l += edge ? pr_weights<true>(ts + PR_SUB * u, s, kf, vs, inv, ref, upto, from)
-                          : pr_weights<false>(ts + PR_SUB * u, s, kf, vs, inv, ref, upto, from);
+                const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
+                const float ref = m == -INFINITY ? 0.f : m;
+                l += edge ? pr_weights<true>(ts + PR_SUB * u, s, kf, vw, ref, upto, from)
+                          : pr_weights<false>(ts + PR_SUB * u, s, kf, vw, ref, upto, from);
                 pr_wait_st();
                 t5_fence_before();
                 __syncwarp();
                 if (lane == 0) t5_bar_arrive(t5_smem(pfull + 2 * qt + u));
+                if (u && j + 1 < count) ok = wait(scfull + ((base_all + j + 1) & 3), (base_all + j + 1) >> 2);
             }
             // ---- results ----
-            if (ok) ok = wait(odone + qt, 2 * ntiles - 1);
-            if (ok) {
-                t5_fence_after();
-                const int64_t tok = rq.row0 + row / a.group;
-                const int h = head * a.group + row % a.group;
-                const float norm = a.splits > 1 ? vref : at_norm(l) * vref;
-                const int64_t at = (tile_id * a.splits + split) * (2 * PR_ROWS) + r;
+            if (ok) ok = wait(fin + qt, pieces);
+            if (!ok) break;
+            t5_fence_after();
+            tiles_mine += count;
+            ++pieces;
+            const bool whole = count == it.tiles;
+            const int h0 = wk.head * a.group;
+            const int64_t tok = it.rq.row0 + row / a.group;
+            const int h = h0 + row % a.group;
+            const float norm = whole ? at_norm(l) * vref : vref;
+            const int64_t slot = 2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1);
+            // this warp's rows in bf16 where its queries were, in the same order
+            unsigned char* o0 = smem + S::Q_AT + qt * S::OPERAND + (warp & 3) * 32 * 128;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    unsigned o[32];
-                    t5_ld32(to + c, o);
-                    t5_wait_ld();
-                    if (real) {
-                        if (a.splits > 1) {
+            for (int c = 0; c < D; c += 32) {
+                unsigned o[32];
+                t5_ld32(to + c, o);
+                t5_wait_ld();
+                if (!whole) {
 #pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                if (c + i < D)
-                                    *reinterpret_cast<float4*>(a.part + at * D + c + i) =
-                                        make_float4(__uint_as_float(o[i]) * norm, __uint_as_float(o[i + 1]) * norm,
-                                                    __uint_as_float(o[i + 2]) * norm, __uint_as_float(o[i + 3]) * norm);
-                        } else {
-                            __nv_bfloat16* dst = a.o + tok * a.o_token_stride + h * a.o_head_stride + c;
+                    for (int i = 0; i < 32; i += 4)
+                        if (c + i < D)
+                            *reinterpret_cast<float4*>(a.part + ((slot * (D / 4) + (c + i) / 4) * (2 * PR_ROWS) + r) * 4) =
+                                make_float4(__uint_as_float(o[i]) * norm, __uint_as_float(o[i + 1]) * norm,
+                                            __uint_as_float(o[i + 2]) * norm, __uint_as_float(o[i + 3]) * norm);
+                } else {
 #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                uint32_t w[4];
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t w[4];
 #pragma unroll
-                                for (int u = 0; u < 4; ++u)
-                                    w[u] = u32(__floats2bfloat162_rn(__uint_as_float(o[i + 2 * u]) * norm, __uint_as_float(o[i + 2 * u + 1]) * norm));
-                                if (c + i < D) *reinterpret_cast<uint4*>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
-                        }
+                        for (int u = 0; u < 4; ++u)
+                            w[u] = u32(__floats2bfloat162_rn(__uint_as_float(o[i + 2 * u]) * norm, __uint_as_float(o[i + 2 * u + 1]) * norm));
+                        *reinterpret_cast<uint4*>(o0 + ((c + i) >> 6) * S::PANEL + lane * 128 + (((((c + i) >> 3) & 7) ^ (lane & 7)) << 4)) =
+                            make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                    __syncwarp();
                 }
-                if (a.splits > 1) a.part_ml[at] = real ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
-                else if (real && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
             }
-        } else if (a.splits > 1) {
-            a.part_ml[(tile_id * a.splits + split) * (2 * PR_ROWS) + threadIdx.x] = make_float2(-INFINITY, 0.f);
+            if (whole) {
+                __syncwarp();
+                constexpr int LANES = DP / 8, RPI = 32 / LANES;
+                const int c = lane % LANES, sub = lane / LANES;
+                const int tok0 = it.r0 / a.group, head0 = it.r0 - tok0 * a.group;
+                __nv_bfloat16* dst = a.o + (int64_t)(it.rq.row0 + tok0) * a.o_token_stride + (int64_t)h0 * a.o_head_stride + 8 * c;
+#pragma unroll 4
+                for (int i = 0; i < 32; i += RPI) {
+                    const int rl = i + sub, rr = qt * PR_ROWS + (warp & 3) * 32 + rl, at = head0 + rr;
+                    const int tk = a.group > 1 ? (int)__umulhi((unsigned)at, a.group_inverse) : at;
+                    const uint4 v = *reinterpret_cast<const uint4*>(o0 + (c >> 3) * S::PANEL + rl * 128 + (((c & 7) ^ (rl & 7)) << 4));
+                    if (rr < it.nrow && 8 * c < D)
+                        *reinterpret_cast<uint4*>(dst + tk * a.o_token_stride + (at - tk * a.group) * a.o_head_stride) = v;
+                }
+                __syncwarp();
+                if (real && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
+            } else if (real) a.part_ml[slot * (2 * PR_ROWS) + r] = make_float2(m, l);
+            t5_fence_before();                                       // the sums are read before the next piece's products
         }
     } else if (warp < 12) {
         // ---- conversion: a thread takes one 16-byte piece of every PASS-th row of a tile ----
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_CONVERT));
         constexpr int PIECES = DP / 16, PASS = 128 / PIECES, NP = PR_KEYS / PASS;
         const int tid = threadIdx.x - 256, piece = tid % PIECES, krow = tid / PIECES;
-        // rows from here on were not copied, or hold nothing of the request: zeros
-        const int limit = min(rq.len, (k1 + SB_KV8_BLOCK - 1) / SB_KV8_BLOCK * SB_KV8_BLOCK) - k0;
-        auto convert = [&](int n) {
+        // n: converted tile of all, left: rows that were copied and belong to the request (the rest: zeros)
+        auto convert = [&](int n, int left) {
             const unsigned src = t5_smem(smem + S::RAW_AT + n % S::RAW_RING * S::RAW) + (unsigned)(krow * D + 16 * piece);
             unsigned char* dst = smem + S::T_AT + n % S::RING * S::OPERAND + (piece >> 2) * S::PANEL;
-            const int left = 16 * piece < D ? limit - (n >> 1) * PR_KEYS : 0;
+            if (16 * piece >= D) left = 0;
             uint4 x[NP];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
@@ -393,30 +548,38 @@ kv8_prompt_kernel(const AtArgs a) {
         const int sblk = SB_KV8_BLOCK * (lane & 7);
         const uint16_t* const scales = (lane & 8) ? a.v_scale : a.k_scale;
         const bool brings = warp == 8 && lane < 2 * PR_BLOCKS;
-        auto entry_of = [&](int j) -> int {
-            const int key = k0 + j * PR_KEYS + sblk;
-            return brings && key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : -1;
-        };
-        auto scale_of = [&](int j, int entry) -> uint16_t {
-            if (entry < 0 || entry >= a.g.pages) return 0;
-            const int slot = (k0 + j * PR_KEYS + sblk) % a.g.page_tokens;
-            return scales[((int64_t)entry * a.g.heads + head) * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK];
-        };
-        uint16_t scale = scale_of(0, entry_of(0));
-        int entry = entry_of(1);
-        for (int n = 0; n < 2 * ntiles; ++n) {
-            if (!wait(empty + n % S::RING, n / S::RING + 1)) break;
-            if (warp == 8 && !(n & 1)) {
-                // whoever read the scales of four tiles ago is done: the slot's last tile came after them
-                const int j = n >> 1;
-                if (brings) sc[16 * (j & 3) + lane] = __uint_as_float((uint32_t)scale << 16);
-                __syncwarp();
-                if (lane == 0) t5_bar_arrive(t5_smem(scfull + (j & 3)));
-                scale = scale_of(j + 1, entry);
-                entry = entry_of(j + 2);
+        bool ok = true;
+        int n = 0;                                                   // converted tiles so far
+        for (bool more = true; more && ok; more = wk.next(a)) {
+            const int k0 = wk.it.lo + wk.tile0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
+            const int limit = min(wk.it.rq.len, (k1 + SB_KV8_BLOCK - 1) / SB_KV8_BLOCK * SB_KV8_BLOCK) - k0;
+            auto entry_of = [&](int j) -> int {
+                const int key = k0 + j * PR_KEYS + sblk;
+                return brings && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + key / a.g.page_tokens] : -1;
+            };
+            auto scale_of = [&](int j, int entry) -> uint16_t {
+                if (entry < 0 || entry >= a.g.pages) return 0;
+                const int slot = (k0 + j * PR_KEYS + sblk) % a.g.page_tokens;
+                return scales[((int64_t)entry * a.g.heads + wk.head) * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK];
+            };
+            uint16_t scale = scale_of(0, entry_of(0));
+            int entry = entry_of(1);
+            for (int i = 0; i < 2 * wk.count; ++i, ++n) {
+                ok = wait(empty + n % S::RING, n / S::RING + 1);
+                if (!ok) break;
+                if (warp == 8 && !(i & 1)) {
+                    // whoever read the scales of four tiles ago is done: the slot's last tile came after them
+                    const int j = n >> 1;
+                    if (brings) sc[16 * (j & 3) + lane] = __uint_as_float((uint32_t)scale << 16);
+                    __syncwarp();
+                    if (lane == 0) t5_bar_arrive(t5_smem(scfull + (j & 3)));
+                    scale = scale_of((i >> 1) + 1, entry);
+                    entry = entry_of((i >> 1) + 2);
+                }
+                ok = wait(raw_full + n % S::RAW_RING, n / S::RAW_RING);
+                if (!ok) break;
+                convert(n, limit - (i >> 1) * PR_KEYS);
             }
-            if (!wait(raw_full + n % S::RAW_RING, n / S::RAW_RING)) break;
-            convert(n);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_REST));
@@ -424,87 +587,102 @@ kv8_prompt_kernel(const AtArgs a) {
     if (warp == 13) {
         // ---- copies: a tile is eight scale blocks, each contiguous in its page; lane i brings block i ----
         const unsigned bytes = (unsigned)(SB_KV8_BLOCK * D);
-        auto entry_of = [&](int j) -> int {
-            const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
-            return lane < PR_BLOCKS && key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : -1;
-        };
-        int entry = entry_of(0), issued = 0;
-        for (int n = 0; n < 2 * ntiles; n += 2) {
-            const int j = n >> 1, key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
-            const int slot = key % a.g.page_tokens;
-            const bool inside = lane < PR_BLOCKS && key < k1, fine = inside && entry >= 0 && entry < a.g.pages;
-            if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
-            const int64_t at = (((int64_t)entry * a.g.heads + head) * a.g.page_tokens + slot) * D;
-            const unsigned count = (unsigned)__popc(__ballot_sync(0xffffffffu, fine));
-            entry = entry_of(j + 1);
-            bool ok = true;
+        bool ok = true;
+        int issued = 0;
+        for (bool more = true; more && ok; more = wk.next(a)) {
+            const int k0 = wk.it.lo + wk.tile0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
+            auto entry_of = [&](int j) -> int {
+                const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
+                return lane < PR_BLOCKS && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + key / a.g.page_tokens] : -1;
+            };
+            int entry = entry_of(0);
+            for (int j = 0; ok && j < wk.count; ++j) {
+                const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
+                const int slot = key % a.g.page_tokens;
+                const bool inside = lane < PR_BLOCKS && key < k1, fine = inside && entry >= 0 && entry < a.g.pages;
+                if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
+                const int64_t at = (((int64_t)entry * a.g.heads + wk.head) * a.g.page_tokens + slot) * D;
+                const unsigned blocks = (unsigned)__popc(__ballot_sync(0xffffffffu, fine));
+                entry = entry_of(j + 1);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int rs = (n + u) % S::RAW_RING;
-                ok = ok && wait(raw_empty + rs, (n + u) / S::RAW_RING + 1);
-                if (!ok) break;
-                const unsigned bar = t5_smem(raw_full + rs);
-                if (lane == 0) t5_bar_expect(bar, count * bytes);
-                __syncwarp();
-                if (fine) t5_load_bulk(t5_smem(smem + S::RAW_AT + rs * S::RAW) + (unsigned)lane * bytes, (u ? a.v : a.k) + at, bytes, bar);
-                __syncwarp();
-                ++issued;
+                for (int u = 0; u < 2; ++u) {
+                    const int rs = issued % S::RAW_RING;
+                    ok = ok && wait(raw_empty + rs, issued / S::RAW_RING + 1);
+                    if (!ok) break;
+                    const unsigned bar = t5_smem(raw_full + rs);
+                    if (lane == 0) t5_bar_expect(bar, blocks * bytes);
+                    __syncwarp();
+                    if (fine) t5_load_bulk(t5_smem(smem + S::RAW_AT + rs * S::RAW) + (unsigned)lane * bytes, (u ? a.v : a.k) + at, bytes, bar);
+                    __syncwarp();
+                    ++issued;
+                }
             }
-            if (!ok) break;
         }
         // copies in flight land before the block leaves
         for (int i = max(0, issued - S::RAW_RING); i < issued; ++i)
             t5_bar_drain(t5_smem(raw_full + i % S::RAW_RING), (unsigned)(i / S::RAW_RING) & 1u);
-    } else if (warp == 12 || (warp == 14 && two)) {
+    } else if (warp == 12 || warp == 14) {
         // ---- products of one row tile ----
         const int qt = warp == 14;
         const bool one = t5_elect();
-        // n: half of a key tile
-        auto scores = [&](int n) {
+        // h: half of a key tile, of all this row tile's; tile: converted tile of all
+        auto scores = [&](int h, int tile) {
             const unsigned q = t5_smem(smem + S::Q_AT + qt * S::OPERAND);
-            const unsigned k = t5_smem(smem + S::T_AT + (n & ~1) % S::RING * S::OPERAND) + (unsigned)((n & 1) * PR_SUB * 128);
+            const unsigned k = t5_smem(smem + S::T_AT + tile % S::RING * S::OPERAND) + (unsigned)((h & 1) * PR_SUB * 128);
 #pragma unroll
             for (int s = 0; s < DP / 16; ++s)
-                pr_mma_ss(one, tmem + S::S_COL + qt * 128 + (n & 1) * PR_SUB, t5_desc_sw128(q + (s >> 2) * S::PANEL + 32 * (s & 3)),
+                pr_mma_ss(one, tmem + S::S_COL + qt * 128 + (h & 1) * PR_SUB, t5_desc_sw128(q + (s >> 2) * S::PANEL + 32 * (s & 3)),
                           t5_desc_sw128(k + (s >> 2) * S::PANEL + 32 * (s & 3)), pr_idesc(PR_SUB, false), s > 0);
-            pr_commit(one, t5_smem(sfull + 2 * qt + (n & 1)));
+            pr_commit(one, t5_smem(sfull + 2 * qt + (h & 1)));
         };
-        auto values = [&](int n) {
-            const unsigned v = t5_smem(smem + S::T_AT + (n | 1) % S::RING * S::OPERAND) + (unsigned)((n & 1) * PR_SUB * 128);
+        auto values = [&](int h, int tile, bool add) {
+            const unsigned v = t5_smem(smem + S::T_AT + tile % S::RING * S::OPERAND) + (unsigned)((h & 1) * PR_SUB * 128);
 #pragma unroll
             for (int s = 0; s < PR_SUB / 16; ++s)
-                pr_mma_ts(one, tmem + S::O_COL + qt * DP, tmem + S::S_COL + qt * 128 + (n & 1) * PR_SUB + 8 * s, pr_desc_v<DP>(v + 2048 * s),
-                          pr_idesc(DP, true), n > 0 || s > 0);
+                pr_mma_ts(one, tmem + S::O_COL + qt * DP, tmem + S::S_COL + qt * 128 + (h & 1) * PR_SUB + 8 * s, pr_desc_v<DP>(v + 2048 * s),
+                          pr_idesc(DP, true), add || s > 0);
             pr_commit(one, t5_smem(odone + qt));
         };
-        // converted tiles in the order K 0, V 0, K 1, V 1, ...: the halves 2 j and 2 j + 1 use tiles
-        // 2 j (keys) and 2 j + 1 (values)
         auto there = [&](int tile) { return wait(full + tile % S::RING, tile / S::RING); };
         auto done = [&](int tile) { pr_commit(one, t5_smem(empty + tile % S::RING)); };
-        const int halves = 2 * ntiles;
-        bool ok = wait(qready + qt, 0) && there(0);
-        if (ok) {
-            t5_fence_after();
-            scores(0);
-            scores(1);
-            done(0);
-        }
-        for (int n = 0; ok && n < halves; ++n) {
-            const int tile = n & ~1;
-            ok = ((n & 1) || there(tile + 1)) && wait(pfull + 2 * qt + (n & 1), n >> 1);
-            if (!ok) break;
-            t5_fence_after();
-            values(n);
-            if (n & 1) done(tile + 1);
-            if (n + 2 < halves) {
-                // The same half of the next tile's scores, into the columns the weights were read from.
-                // Products of different shapes are not ordered by their issue: those have to be done.
-                ok = ((n & 1) || there(tile + 2)) && wait(odone + qt, n);
+        bool ok = true;
+        int t = 0, mine = 0, pieces = 0;                             // converted tiles (keys: even), this row tile's halves, pieces
+        for (bool more = true; more && ok; more = wk.next(a)) {
+            const int halves = 2 * wk.count;
+            if (wk.it.nrow <= qt * PR_ROWS) {                        // no rows: lets the tiles go as they come
+                for (int i = 0; ok && i < halves; ++i, ++t) {
+                    ok = there(t);
+                    if (ok) done(t);
+                }
+                continue;
+            }
+            ok = wait(qready + qt, pieces++) && there(t);
+            if (ok) {
+                t5_fence_after();
+                scores(mine, t);
+                scores(mine + 1, t);
+                done(t);
+            }
+            for (int n = 0; ok && n < halves; ++n) {
+                const int tile = t + (n & ~1);                       // this half's keys; its values: the next
+                ok = ((n & 1) || there(tile + 1)) && wait(pfull + 2 * qt + (n & 1), (mine + n) >> 1);
                 if (!ok) break;
                 t5_fence_after();
-                scores(n + 2);
-                if (n & 1) done(tile + 2);
+                values(mine + n, tile + 1, n > 0);
+                if (n & 1) done(tile + 1);
+                if (n + 2 < halves) {
+                    // The same half of the next tile's scores, into the columns the weights were read from.
+                    // Products of different shapes are not ordered by their issue: those have to be done.
+                    ok = ((n & 1) || there(tile + 2)) && wait(odone + qt, mine + n);
+                    if (!ok) break;
+                    t5_fence_after();
+                    scores(mine + n + 2, tile + 2);
+                    if (n & 1) done(tile + 2);
+                }
             }
+            if (ok) pr_commit(one, t5_smem(fin + qt));
+            t += halves;
+            mine += halves;
         }
         if (!ok) {                                   // what was issued still reads shared memory
             pr_commit(one, t5_smem(last + qt));
@@ -521,36 +699,41 @@ kv8_prompt_kernel(const AtArgs a) {
     if (threadIdx.x == 0 && *abort_flag) sb_latch(a.st, SB_ERR_TIMEOUT, SBK_KV8);
 }
 
-// the chunks of a row, in their order
-__global__ void __launch_bounds__(128)
-kv8_prompt_sum_kernel(const AtArgs a) {
-    const int b = blockIdx.z, head = blockIdx.y;
-    Kv8Request rq;
-    if (!kv8_request(a.g, b, rq, a.st)) return;
-    const int rows = rq.n * a.group, D = a.g.dim, quads = D / 4;
-    const int64_t unit = (int64_t)blockIdx.x * 128 + threadIdx.x;
-    const int row = (int)(unit / quads), d = 4 * (int)(unit - (int64_t)row * quads);
-    if (row >= rows) return;
-    const int rt = row / (2 * PR_ROWS), r = row % (2 * PR_ROWS);
-    const int64_t at = (((int64_t)b * a.g.heads + head) * a.row_tiles + rt) * a.splits * (2 * PR_ROWS) + r;
+// The pieces of an item that lies in several shares, in their order. Block (c, y, z): the item that the
+// border before share c + 1 cuts, if no earlier border does; 32 of its rows, 32 of its columns.
+__global__ void __launch_bounds__(256)
+kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
+    const int c = blockIdx.x + 1;
+    const int4 s = w.start[c];
+    if (s.x < 0 || s.z <= PR_EXTRA) return;                          // the border lies before the first tile
+    const long long share = w.share[0], from = c * share - s.z;      // the item's first unit of all
+    const int c0 = (int)((from + PR_EXTRA) / share);                 // the share with its first tile
+    if (c != c0 + 1) return;
+    const PrItem it = pr_item(a, s.x, a.st);
+    const int c1 = (int)((from + it.units() - 1) / share), D = a.g.dim;
+    const int r = 32 * blockIdx.y + threadIdx.x / 8, quad = 8 * blockIdx.z + threadIdx.x % 8;
+    if (r >= it.nrow || 4 * quad >= D) return;
     float m = -INFINITY, l = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int x = 0; x < a.splits; ++x) {
-        const float2 ml = a.part_ml[at + (int64_t)x * (2 * PR_ROWS)];
-        if (ml.x == -INFINITY) continue;
-        const float4 y = *reinterpret_cast<const float4*>(a.part + (at + (int64_t)x * (2 * PR_ROWS)) * D + d);
+#pragma unroll 2
+    for (int x = c0; x <= c1; ++x) {
+        // the first piece of that share, unless the item starts inside the share
+        const int64_t slot = 2 * (int64_t)x + (from > x * share ? 1 : 0);
+        const float2 ml = a.part_ml[slot * (2 * PR_ROWS) + r];
+        const float4 y = *reinterpret_cast<const float4*>(a.part + ((slot * (D / 4) + quad) * (2 * PR_ROWS) + r) * 4);
         const float mn = fmaxf(m, ml.x);
-        const float f = m == -INFINITY ? 0.f : at_exp2(m - mn), h = at_exp2(ml.x - mn);
+        const float f = m == -INFINITY ? 0.f : at_exp2(m - mn), h = ml.x == -INFINITY ? 0.f : at_exp2(ml.x - mn);
         l = fmaf(l, f, ml.y * h);
         v.x = fmaf(v.x, f, y.x * h); v.y = fmaf(v.y, f, y.y * h); v.z = fmaf(v.z, f, y.z * h); v.w = fmaf(v.w, f, y.w * h);
         m = mn;
     }
-    const int64_t tok = rq.row0 + row / a.group;
-    const int h = head * a.group + row % a.group;
+    const int row = it.r0 + r;
+    const int64_t tok = it.rq.row0 + row / a.group;
+    const int h = s.y * a.group + row % a.group;
     const float f = at_norm(l);
-    *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) =
+    *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + 4 * quad) =
         make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
-    if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
+    if (quad == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
 }
 
 template <int TYPE, int DP>
@@ -558,33 +741,32 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     using S = PrShape<DP>;
     auto* kernel = kv8_prompt_kernel<TYPE, DP>;
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    const int64_t row_tiles = (max_new * a.group + 2 * PR_ROWS - 1) / (2 * PR_ROWS);
+    const int64_t row_tiles = (max_new * a.group + 2 * PR_ROWS - 1) / (2 * PR_ROWS), n = row_tiles * a.g.requests;
+    if (n >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
     int64_t keys = max_len;
     if (a.window > 0 && keys > a.window + max_new + PR_KEYS) keys = a.window + max_new + PR_KEYS;
-    const int64_t tiles = row_tiles * a.g.heads * a.g.requests;
-    // with fewer tiles than SMs the keys are cut too, into chunks of at least 8 tiles
-    int64_t splits = tiles < ctx->sm_count ? ctx->sm_count / tiles : 1;
-    if (splits > (keys + 8 * PR_KEYS - 1) / (8 * PR_KEYS)) splits = (keys + 8 * PR_KEYS - 1) / (8 * PR_KEYS);
-    if (splits < 1) splits = 1;
-    a.chunk = (int)(((keys + splits - 1) / splits + PR_KEYS - 1) / PR_KEYS * PR_KEYS);
-    a.splits = (int)((keys + a.chunk - 1) / a.chunk);
+    // one share per SM, fewer if there cannot be so many shares
+    const int64_t most = (n * a.g.heads * ((keys + PR_KEYS - 1) / PR_KEYS + 1 + PR_EXTRA) + PR_LEAST - 1) / PR_LEAST;
+    PrWork w{};
+    w.ctas = (int)(most < ctx->sm_count ? most : ctx->sm_count);
     a.row_tiles = (int)row_tiles;
-    if (row_tiles * a.splits > 65535) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
-    if (a.splits > 1) {
-        const size_t n = (size_t)tiles * a.splits * (2 * PR_ROWS);
-        void* arena;
-        const sb_status s = sb_scratch(ctx, Carver::need({n * a.g.dim * 4, n * 8}), &arena);
-        if (s != SB_OK) return s;
-        Carver cv(arena);
-        a.part = cv.take<float>(n * a.g.dim);
-        a.part_ml = cv.take<float2>(n);
-    }
-    const dim3 grid((unsigned)a.g.heads, (unsigned)(row_tiles * a.splits), (unsigned)a.g.requests);
-    kernel<<<grid, PR_THREADS, S::SMEM, ctx->stream>>>(a);
+    a.group_inverse = (unsigned)(((1ull << 32) + a.group - 1) / a.group);   // exact quotients of numbers below 2^32 / group
+    const size_t rows = (size_t)w.ctas * 2 * (2 * PR_ROWS);
+    void* arena;
+    const sb_status s = sb_scratch(ctx, Carver::need({((size_t)n + 1) * 8, (size_t)w.ctas * 16, 16, rows * a.g.dim * 4, rows * 8}), &arena);
+    if (s != SB_OK) return s;
+    Carver cv(arena);
+    w.prefix = cv.take<long long>((size_t)n + 1);
+    w.start = cv.take<int4>(w.ctas);
+    w.share = cv.take<long long>(2);
+    a.part = cv.take<float>(rows * a.g.dim);
+    a.part_ml = cv.take<float2>(rows);
+    kv8_prompt_plan_kernel<<<1, 1024, 0, ctx->stream>>>(a, w);
     SB_LAUNCHED(ctx);
-    if (a.splits > 1) {
-        const int64_t blocks = (max_new * a.group * (a.g.dim / 4) + 127) / 128;
-        kv8_prompt_sum_kernel<<<dim3((unsigned)blocks, (unsigned)a.g.heads, (unsigned)a.g.requests), 128, 0, ctx->stream>>>(a);
+    kernel<<<w.ctas, PR_THREADS, S::SMEM, ctx->stream>>>(a, w);
+    SB_LAUNCHED(ctx);
+    if (w.ctas > 1) {
+        kv8_prompt_sum_kernel<<<dim3((unsigned)(w.ctas - 1), 2 * PR_ROWS / 32, (unsigned)((a.g.dim + 31) / 32)), 256, 0, ctx->stream>>>(a, w);
         SB_LAUNCHED(ctx);
     }
     return SB_OK;
