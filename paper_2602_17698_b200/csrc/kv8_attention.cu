@@ -25,9 +25,10 @@
 // times its value scale, relative to a running power of two, is rounded to fp16 (2^-11): three
 // bits finer than the bf16 result.
 //
-// Long caches are cut into chunks of keys; a chunk's CTA leaves unnormalised sums, and the last
-// CTA of a row tile to finish (a counter) adds the chunks in their order: the result does not
-// depend on which one that is.
+// The work of all requests is cut into equal shares (see kv8_attention.cuh), which every CTA finds by
+// itself from the requests' lengths. Of an item that several shares hold, each leaves unnormalised sums,
+// and the last of them to finish (a counter) adds them in their order: the result does not depend on
+// which one that is.
 #include "kv8_attention.cuh"
 
 namespace {
@@ -35,9 +36,15 @@ namespace {
 constexpr int AT_PROMPT_FROM = 64;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
+constexpr int AT_EXTRA = 6;             // what an item costs besides its steps, in steps
+constexpr int AT_LEAST = 16 + AT_EXTRA; // units of a share at least: four steps of every warp
+constexpr float AT_SLACK = 8.f;         // log2 of how far a row's maximum may run ahead of its reference
 constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
 
 __device__ __forceinline__ unsigned at_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void at_copy16(unsigned dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void at_copy16(unsigned dst, const void* src, bool take) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
@@ -55,7 +62,8 @@ __device__ __forceinline__ uint32_t at_transpose(uint32_t x) {
 }
 template <int DP, int NR>
 struct AtShape {
-    static constexpr int STAGES = DP == 64 ? 4 : 3;
+    static constexpr int STAGES = DP == 64 ? 4 : NR == 1 ? 2 : 3;
+    static constexpr int CTAS = DP == 256 ? 1 : NR == 1 ? 3 : 2;     // resident per SM: registers and the rings decide
     static constexpr int SIDE = AT_STEP * DP;                      // bytes of a step's keys
     static constexpr int RING = AT_WARPS * STAGES * 2 * SIDE;
     static constexpr int ROWS = 8 * NR;
@@ -63,14 +71,15 @@ struct AtShape {
     static constexpr int Q_AT = RING;
     static constexpr int F_AT = Q_AT + ROWS * QPITCH;              // score factor of a row, fp32
     static constexpr int FLAG_AT = F_AT + ROWS * 4;
-    static constexpr int SMEM = FLAG_AT + 16;
+    static constexpr int SMEM = FLAG_AT + 64;
     static constexpr int OPITCH = DP + 4;                          // floats of a row of a warp's sums
     static_assert(AT_WARPS * ROWS * (OPITCH + 2) * 4 <= RING, "the warps' sums fit where the ring was");
+    static_assert(CTAS * 160 * ROWS * 4 + AT_WARPS * 32 * 16 <= RING && QPITCH >= 8, "so do the weights of an item's pieces");
     static constexpr bool QREGS = NR * DP <= 256;                  // query operands stay in registers
 };
 
 template <int TYPE, int DP, int NR>
-__global__ void __launch_bounds__(AT_WARPS * 32)
+__global__ void __launch_bounds__(AT_WARPS * 32, AtShape<DP, NR>::CTAS)
 kv8_rows_kernel(const AtArgs a) {
     using S = AtShape<DP, NR>;
     constexpr int KS = DP / 16;                    // contraction steps over d
@@ -79,71 +88,134 @@ kv8_rows_kernel(const AtArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
-    const int split = (int)(blockIdx.x % (unsigned)a.splits), rt = (int)(blockIdx.x / (unsigned)a.splits);
-    const int head = blockIdx.y, b = blockIdx.z;
     const int D = a.g.dim;
-    Kv8Request rq;
-    if (!kv8_request(a.g, b, rq, a.st)) return;
-    const int rows = rq.n * a.group, r0 = rt * S::ROWS;
-    if (r0 >= rows) return;
-    const int nrow = min(S::ROWS, rows - r0);
-    // keys that some row of the tile sees, from the start of a scale block
+    // ---- this CTA's share ----
+    AtWalk<S::ROWS, AT_STEP, AT_EXTRA> wk;
+    long long share;
+    {
+        // units of one head before each row tile of all requests, 128 at a time
+        long long* sums = reinterpret_cast<long long*>(smem);       // [AT_WARPS] and, behind them, where the share starts
+        const int n = a.row_tiles * a.g.requests;
+        auto units = [&](int i) -> long long {
+            if (i >= n) return 0;
+            const int steps = at_item<S::ROWS, AT_STEP>(a, i).steps;
+            return steps ? steps + AT_EXTRA : 0;
+        };
+        long long mine = units(threadIdx.x), x = mine;
+        for (int i = threadIdx.x + AT_WARPS * 32; i < n; i += AT_WARPS * 32) x += units(i);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (lane == 0) sums[warp] = x;
+        __syncthreads();
+        long long total = 0;
+#pragma unroll
+        for (int w = 0; w < AT_WARPS; ++w) total += sums[w];
+        total *= a.g.heads;
+        share = (total + gridDim.x - 1) / gridDim.x;
+        if (share < AT_LEAST) share = AT_LEAST;
+        const long long at = blockIdx.x * share;
+        if (at >= total) return;
+        long long before = 0;
+        for (int base = 0; base < n; base += AT_WARPS * 32) {
+            if (base > 0) mine = units(base + threadIdx.x);
+            x = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
+            }
+            __syncthreads();
+            if (lane == 31) sums[warp] = x;
+            __syncthreads();
+            long long all = 0, below = before;
+#pragma unroll
+            for (int w = 0; w < AT_WARPS; ++w) {
+                if (w < warp) below += sums[w];
+                all += sums[w];
+            }
+            const long long lo = (below + x - mine) * a.g.heads;     // the row tile's first unit of all
+            if (at >= lo && at < lo + mine * a.g.heads) {
+                int* found = reinterpret_cast<int*>(sums + AT_WARPS);
+                found[0] = base + threadIdx.x;
+                found[1] = (int)((at - lo) / mine);
+                found[2] = (int)((at - lo) % mine);
+            }
+            before += all;
+            if (at < before * a.g.heads) break;
+        }
+        __syncthreads();
+        const int* found = reinterpret_cast<const int*>(sums + AT_WARPS);
+        const int f0 = found[0], f1 = found[1], f2 = found[2];
+        __syncthreads();
+        if (!wk.begin(a, f0, f1, f2, at, min(share, total - at))) return;
+    }
+    for (bool more = true; more; more = wk.next(a)) {
+    const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
+    const Kv8Request rq = wk.it.rq;
     const int i0 = r0 / a.group, i1 = (r0 + nrow - 1) / a.group;
-    const int hi = rq.past + i1 + 1;
-    const int lo = a.window > 0 ? max(0, rq.past + i0 - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
-    // max_len may be too small: then the chunks grow
-    int chunk = a.chunk;
-    if ((int64_t)chunk * a.splits < hi - lo) chunk = ((hi - lo + a.splits - 1) / a.splits + AT_STEP - 1) / AT_STEP * AT_STEP;
-    const int nsplit = (hi - lo + chunk - 1) / chunk;
-    if (split >= nsplit) return;
-    const int k0 = lo + split * chunk, k1 = min(hi, k0 + chunk);
-    const int nsteps = (k1 - k0 + AT_STEP - 1) / AT_STEP;
-    const int mine = (nsteps - warp + AT_WARPS - 1) / AT_WARPS;     // steps warp, warp + 4, ...
+    const int k0 = wk.it.lo + wk.step0 * AT_STEP, k1 = min(wk.it.hi, k0 + wk.count * AT_STEP);
+    const int mine = (wk.count - warp + AT_WARPS - 1) / AT_WARPS;   // steps warp, warp + 4, ...
 
-    // ---- this warp's page numbers and scales, AT_BATCH steps at a time: lane 2 s + e holds block e of step s ----
+    // ---- where this warp's blocks lie and their scales, AT_BATCH steps at a time: lane 2 s + e holds block e
+    // of step s; the table's entries are fetched two batches ahead, scales one ----
     auto block_key = [&](int batch) { return k0 + (warp + AT_WARPS * (AT_BATCH * batch + (lane >> 1))) * AT_STEP + SB_KV8_BLOCK * (lane & 1); };
-    auto load_page = [&](int batch) -> int {
+    auto load_entry = [&](int batch) -> int {
         const int key = block_key(batch);
-        if (key >= k1) return -1;
-        int64_t page;
-        return kv8_page(a.g, b, key / a.g.page_tokens, page, a.st) ? (int)page : -1;
+        return key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : 0;
     };
-    auto load_scales = [&](int batch, int page, uint32_t& s2) {
+    // the block's first code (-1: no such block) and, fetched, its two scales
+    auto place = [&](int batch, int entry, uint32_t& s2) -> int64_t {
+        const int key = block_key(batch);
         s2 = 0;
-        if (page < 0) return;
-        const int slot = block_key(batch) % a.g.page_tokens;
-        const int64_t at = ((int64_t)page * a.g.heads + head) * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;
+        if (key >= k1) return -1;
+        if (entry < 0 || entry >= a.g.pages) {
+            sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
+            return -1;
+        }
+        const int64_t ph = (int64_t)entry * a.g.heads + head;
+        const int slot = key % a.g.page_tokens;
+        const int64_t at = ph * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;
         s2 = (uint32_t)a.k_scale[at] | (uint32_t)a.v_scale[at] << 16;
+        return (ph * a.g.page_tokens + slot) * D;
     };
-    int page_cur = load_page(0), page_next = load_page(1);
+    int entry_next = load_entry(1);
     uint32_t sc_cur, sc_next = 0;
-    load_scales(0, page_cur, sc_cur);
+    int64_t at_even = place(0, load_entry(0), sc_cur), at_odd = -1;     // of even and odd batches
 
     const unsigned ring = at_smem(smem) + (unsigned)(warp * S::STAGES * 2 * S::SIDE);
     // copies of step j of this warp into its ring
+    constexpr int TOKS = 32 / PIECES;                               // tokens a warp copies with one instruction
+    const int cp_piece = lane % PIECES, cp_tok = lane / PIECES;
+    const int cp_off = cp_tok * D + cp_piece * 16;
+    auto ring_at = [](int row, int piece) {
+        return DP == 64 ? (unsigned)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4)) : (unsigned)(row * DP + ((piece ^ (row & 7)) << 4));
+    };
     auto issue = [&](int j) {
         if (j < mine) {
             const int key = k0 + (warp + AT_WARPS * j) * AT_STEP;
             const unsigned dst = ring + (unsigned)((j % S::STAGES) * 2 * S::SIDE);
-            constexpr int TOKS = 32 / (PIECES < 32 ? PIECES : 32);  // tokens a warp copies with one instruction
-            const int piece = lane % PIECES, tok_l = lane / PIECES;
+            const int64_t held = (j / AT_BATCH) & 1 ? at_odd : at_even;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int src_lane = 2 * (j & (AT_BATCH - 1)) + e;
-                const int pg = __shfl_sync(0xffffffffu, page_cur, src_lane), pgn = __shfl_sync(0xffffffffu, page_next, src_lane);
-                const int page = (j / AT_BATCH) & 1 ? pgn : pg;     // page_cur holds even batches, page_next odd ones
-                const int slot = (key + SB_KV8_BLOCK * e) % a.g.page_tokens;
-                const int64_t base = (((int64_t)max(page, 0) * a.g.heads + head) * a.g.page_tokens + slot) * D;
+                const int64_t base = __shfl_sync(0xffffffffu, held, 2 * (j & (AT_BATCH - 1)) + e);
+                const uint8_t *kp = a.k + base + cp_off, *vp = a.v + base + cp_off;
+                if (D == DP && base >= 0 && key + SB_KV8_BLOCK * (e + 1) <= rq.len) {
 #pragma unroll
-                for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
-                    const int tok = tok_l + TOKS * i;
-                    const bool take = page >= 0 && key + SB_KV8_BLOCK * e + tok < rq.len && piece * 16 < D;
-                    const int64_t off = take ? base + tok * D + piece * 16 : 0;
-                    const int row = SB_KV8_BLOCK * e + tok;
-                    const unsigned to = DP == 64 ? (unsigned)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4))
-                                                 : (unsigned)(row * DP + ((piece ^ (row & 7)) << 4));
-                    at_copy16(dst + to, a.k + off, take);
-                    at_copy16(dst + S::SIDE + to, a.v + off, take);
+                    for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
+                        const unsigned to = ring_at(SB_KV8_BLOCK * e + cp_tok + TOKS * i, cp_piece);
+                        at_copy16(dst + to, kp + TOKS * i * DP);
+                        at_copy16(dst + S::SIDE + to, vp + TOKS * i * DP);
+                    }
+                } else {
+                    // the last block, a block that is not there, or rows shorter than the operand's: zeros fill up
+#pragma unroll
+                    for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
+                        const int tok = cp_tok + TOKS * i;
+                        const bool take = base >= 0 && key + SB_KV8_BLOCK * e + tok < rq.len && cp_piece * 16 < D;
+                        const unsigned to = ring_at(SB_KV8_BLOCK * e + tok, cp_piece);
+                        at_copy16(dst + to, take ? kp + TOKS * i * D : a.k, take);
+                        at_copy16(dst + S::SIDE + to, take ? vp + TOKS * i * D : a.v, take);
+                    }
                 }
             }
         }
@@ -208,15 +280,14 @@ kv8_rows_kernel(const AtArgs a) {
 
     for (int j = 0; j < mine; ++j) {
         if ((j & (AT_BATCH - 1)) == 0) {
-            // a new batch: its scales were fetched while the last one ran; fetch the next batch's
-            // scales and the page numbers of the one after it (into the slot of the last batch)
             const int batch = j / AT_BATCH;
-            if (batch > 0) {
-                sc_cur = sc_next;
-                if (batch & 1) page_cur = load_page(batch + 1);
-                else page_next = load_page(batch + 1);
+            if (batch > 0) sc_cur = sc_next;
+            if (AT_BATCH * (batch + 1) < mine) {
+                const int64_t at = place(batch + 1, entry_next, sc_next);
+                if (batch & 1) at_even = at;                         // the slot of the batch before this one
+                else at_odd = at;
+                entry_next = load_entry(batch + 2);
             }
-            if (AT_BATCH * (batch + 1) < mine) load_scales(batch + 1, batch & 1 ? page_cur : page_next, sc_next);
         }
         at_wait<S::STAGES - 2>();
         __syncwarp();
@@ -278,14 +349,16 @@ kv8_rows_kernel(const AtArgs a) {
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
             }
-            const bool grew = mx[0] > m[nr][0] || mx[1] > m[nr][1];
-            if (__any_sync(0xffffffffu, grew)) {
+            // the reference only moves when it is off by more than 2^8: a weight stays below 2^8
+            bool off[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + AT_SLACK || (m[nr][e] == -INFINITY && mx[e] > m[nr][e]);
+            if (__any_sync(0xffffffffu, off[0] || off[1])) {
                 float f[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float mn = fmaxf(m[nr][e], mx[e]);
-                    f[e] = mn == -INFINITY ? 1.f : at_exp2(m[nr][e] - mn);
-                    m[nr][e] = mn;
+                    f[e] = !off[e] ? 1.f : m[nr][e] == -INFINITY ? 0.f : at_exp2(m[nr][e] - mx[e]);
+                    if (off[e]) m[nr][e] = mx[e];
                     l[nr][e] *= f[e];
                 }
 #pragma unroll
@@ -383,7 +456,8 @@ kv8_rows_kernel(const AtArgs a) {
             }
         }
     __syncthreads();
-    const int64_t tile = ((int64_t)b * a.g.heads + head) * a.row_tiles + rt;
+    const bool whole = wk.count == wk.it.steps;
+    const int quads = D / 4;
     auto store = [&](int r, int d, float4 v, float mm, float sum) {
         const int row = r0 + r;
         const int64_t tok = rq.row0 + row / a.group;
@@ -393,8 +467,8 @@ kv8_rows_kernel(const AtArgs a) {
         *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) = w;
         if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(mm, sum);
     };
-    for (int idx = threadIdx.x; idx < nrow * (D / 4); idx += AT_WARPS * 32) {
-        const int r = idx / (D / 4), d = 4 * (idx - r * (D / 4));
+    for (int idx = threadIdx.x; idx < nrow * quads; idx += AT_WARPS * 32) {
+        const int r = idx / quads, d = 4 * (idx - r * quads);
         float2 ml[AT_WARPS];
         float mm = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -410,42 +484,80 @@ kv8_rows_kernel(const AtArgs a) {
             sum = fmaf(ml[w].y, f, sum);
             v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
         }
-        if (nsplit == 1) store(r, d, v, mm, sum);
+        if (whole) store(r, d, v, mm, sum);
         else {
-            const int64_t at = (tile * a.splits + split) * S::ROWS + r;
+            const int64_t at = (2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1)) * S::ROWS + r;
             *reinterpret_cast<float4*>(a.part + at * D + d) = v;
             if (d == 0) a.part_ml[at] = make_float2(mm, sum);
         }
     }
-    if (nsplit == 1) return;
-    // ---- the last chunk of the tile to finish adds them all, in order ----
-    volatile int* last = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const unsigned was = atomicAdd(a.done + tile, 1u);
-        *last = was == (unsigned)(nsplit - 1);
-        if (*last) a.done[tile] = 0;                                 // for the next call
-    }
-    __syncthreads();
-    if (!*last) return;
-    __threadfence();
-    for (int idx = threadIdx.x; idx < nrow * (D / 4); idx += AT_WARPS * 32) {
-        const int r = idx / (D / 4), d = 4 * (idx - r * (D / 4));
-        const int64_t at = tile * a.splits * S::ROWS + r;
-        float mm = -INFINITY, sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int x = 0; x < nsplit; ++x) {
-            const float2 ml = __ldcg(a.part_ml + at + (int64_t)x * S::ROWS);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (at + (int64_t)x * S::ROWS) * D + d));
-            const float mn = fmaxf(mm, ml.x);
-            const float f = mm == -INFINITY ? 0.f : at_exp2(mm - mn), h = ml.x == -INFINITY ? 0.f : at_exp2(ml.x - mn);
-            sum = fmaf(sum, f, ml.y * h);
-            v.x = fmaf(v.x, f, y.x * h); v.y = fmaf(v.y, f, y.y * h); v.z = fmaf(v.z, f, y.z * h); v.w = fmaf(v.w, f, y.w * h);
-            mm = mn;
+    if (!whole) {
+        // ---- the last of the item's pieces to finish adds them all, in order ----
+        const long long from = wk.from;
+        const int c0 = (int)((from + AT_EXTRA) / share), c1 = (int)((from + wk.units() - 1) / share), pieces = c1 - c0 + 1;
+        // a piece is the first of its share unless the item starts inside the share
+        auto slot = [&](int x) { return (2 * (int64_t)(c0 + x) + (from > (c0 + x) * share ? 1 : 0)) * S::ROWS; };
+        volatile int* last = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            unsigned* done = a.done + ((int64_t)wk.row_tile * a.g.heads + head);
+            *last = atomicAdd(done, 1u) == (unsigned)(pieces - 1);
+            if (*last) *done = 0;                                    // for the next call
         }
-        store(r, d, v, mm, sum);
+        __syncthreads();
+        if (*last) {
+            __threadfence();
+            // weights of the pieces of every row in shared memory, a row per warp
+            float* weight = reinterpret_cast<float*>(smem);          // [pieces][ROWS]
+            float2* total = reinterpret_cast<float2*>(smem + S::F_AT - S::ROWS * 8);         // (reference, sum) of a row
+            for (int r = warp; r < nrow; r += AT_WARPS) {
+                float mm = -INFINITY, sum = 0.f;
+                for (int x = lane; x < pieces; x += 32) mm = fmaxf(mm, __ldcg(a.part_ml + slot(x) + r).x);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
+                for (int x = lane; x < pieces; x += 32) {
+                    const float2 ml = __ldcg(a.part_ml + slot(x) + r);
+                    const float f = ml.x == -INFINITY ? 0.f : at_exp2(ml.x - mm);
+                    weight[x * S::ROWS + r] = f;
+                    sum = fmaf(ml.y, f, sum);
+                }
+                sum = warp_sum(sum);
+                if (lane == 0) total[r] = make_float2(mm, sum);
+            }
+            __syncthreads();
+            // with few outputs several threads share one, each a part of the pieces
+            const int outs = nrow * quads;
+            const int parts = outs >= AT_WARPS * 32 ? 1 : AT_WARPS * 32 / outs;
+            float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
+            for (int base = 0; base < outs; base += AT_WARPS * 32) {
+                const int part = (int)threadIdx.x / outs, idx = parts > 1 ? (int)threadIdx.x - part * outs : base + (int)threadIdx.x;
+                const int r = idx / quads, d = 4 * (idx - r * quads);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (idx < outs && (parts == 1 || part < parts)) {
+                    const int x0 = parts > 1 ? pieces * part / parts : 0, x1 = parts > 1 ? pieces * (part + 1) / parts : pieces;
+#pragma unroll 8
+                    for (int x = x0; x < x1; ++x) {
+                        const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x) + r) * D + d));
+                        const float f = weight[x * S::ROWS + r];
+                        v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+                    }
+                }
+                if (parts > 1) {
+                    shared_sum[threadIdx.x] = v;
+                    __syncthreads();
+                    if (threadIdx.x < outs) {
+                        for (int p = 1; p < parts; ++p) {
+                            const float4 y = shared_sum[threadIdx.x + p * outs];
+                            v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+                        }
+                        store(r, d, v, total[r].x, total[r].y);
+                    }
+                } else if (idx < outs) store(r, d, v, total[r].x, total[r].y);
+            }
+        }
+    }
+    __syncthreads();                                                 // the next piece's copies go where the sums were
     }
 }
 
@@ -455,45 +567,36 @@ sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     auto* kernel = kv8_rows_kernel<TYPE, DP, NR>;
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     const int64_t row_tiles = (max_new * a.group + S::ROWS - 1) / S::ROWS;
-    // keys a tile can see, and the chunks that make about four CTAs per SM out of all tiles; a chunk
-    // is at least eight steps of every warp
+    const int64_t tiles = row_tiles * a.g.heads * a.g.requests;
+    if (tiles >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
+    // a share per resident CTA, fewer if there cannot be so many shares
     int64_t keys = max_len;
     if (a.window > 0 && keys > a.window + S::ROWS + SB_KV8_BLOCK) keys = a.window + S::ROWS + SB_KV8_BLOCK;
-    const int64_t tiles = row_tiles * a.g.heads * a.g.requests;
-    const int64_t want = 4 * (int64_t)ctx->sm_count;
-    int64_t splits = (want + tiles - 1) / tiles;
-    const int64_t least = AT_WARPS * AT_STEP * 4;
-    if (splits > (keys + least - 1) / least) splits = (keys + least - 1) / least;
-    if (splits < 1) splits = 1;
-    a.chunk = (int)(((keys + splits - 1) / splits + AT_STEP - 1) / AT_STEP * AT_STEP);
-    a.splits = (int)((keys + a.chunk - 1) / a.chunk);
+    const int64_t most = (tiles * ((keys + AT_STEP - 1) / AT_STEP + 1 + AT_EXTRA) + AT_LEAST - 1) / AT_LEAST;
+    const int64_t ctas = most < (int64_t)S::CTAS * ctx->sm_count ? most : (int64_t)S::CTAS * ctx->sm_count;
     a.row_tiles = (int)row_tiles;
-    if (row_tiles * a.splits >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many tiles");
-    if (a.splits > 1) {
-        const size_t n = (size_t)tiles * a.splits * S::ROWS;
-        void* arena;
-        const sb_status s = sb_scratch(ctx, Carver::need({n * a.g.dim * 4, n * 8}), &arena);
-        if (s != SB_OK) return s;
-        Carver cv(arena);
-        a.part = cv.take<float>(n * a.g.dim);
-        a.part_ml = cv.take<float2>(n);
-        if (ctx->kv8_done_n < (size_t)tiles) {
-            // zeroed once; every call leaves zeros.  The old counters stay for captured launches.
-            const size_t want_n = (size_t)tiles * 2 + 4096;
-            unsigned* fresh = nullptr;
-            if (cudaMalloc(&fresh, want_n * 4) != cudaSuccess) {
-                (void)cudaGetLastError();
-                return sb_fail(ctx, SB_ERR_SCRATCH, "kv8 attention: %zu counters", want_n);
-            }
-            SB_CUDA(ctx, cudaMemsetAsync(fresh, 0, want_n * 4, ctx->stream));
-            if (ctx->kv8_done) ctx->retired.push_back(ctx->kv8_done);
-            ctx->kv8_done = fresh;
-            ctx->kv8_done_n = want_n;
+    const size_t n = (size_t)ctas * 2 * S::ROWS;
+    void* arena;
+    const sb_status s = sb_scratch(ctx, Carver::need({n * a.g.dim * 4, n * 8}), &arena);
+    if (s != SB_OK) return s;
+    Carver cv(arena);
+    a.part = cv.take<float>(n * a.g.dim);
+    a.part_ml = cv.take<float2>(n);
+    if (ctx->kv8_done_n < (size_t)tiles) {
+        // zeroed once; every call leaves zeros.  The old counters stay for captured launches.
+        const size_t want_n = (size_t)tiles * 2 + 4096;
+        unsigned* fresh = nullptr;
+        if (cudaMalloc(&fresh, want_n * 4) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return sb_fail(ctx, SB_ERR_SCRATCH, "kv8 attention: %zu counters", want_n);
         }
-        a.done = ctx->kv8_done;
+        SB_CUDA(ctx, cudaMemsetAsync(fresh, 0, want_n * 4, ctx->stream));
+        if (ctx->kv8_done) ctx->retired.push_back(ctx->kv8_done);
+        ctx->kv8_done = fresh;
+        ctx->kv8_done_n = want_n;
     }
-    const dim3 grid((unsigned)(row_tiles * a.splits), (unsigned)a.g.heads, (unsigned)a.g.requests);
-    kernel<<<grid, AT_WARPS * 32, S::SMEM, ctx->stream>>>(a);
+    a.done = ctx->kv8_done;
+    kernel<<<(unsigned)ctas, AT_WARPS * 32, S::SMEM, ctx->stream>>>(a);
     SB_LAUNCHED(ctx);
     return SB_OK;
 }

@@ -14,13 +14,12 @@ struct AtArgs {
     float* lse;
     int group;                   // query heads per cache head
     unsigned group_inverse;      // ceil(2^32 / group), for group > 1
-    int row_tiles, splits;       // of the grid
-    int chunk;                   // keys per CTA
+    int row_tiles;               // of a request with max_new new tokens
     float scale_log2;            // softmax scale * log2(e)
     int window;
-    float* part;                 // [tile][splits][rows][dim] unnormalised sums
-    float2* part_ml;             // [tile][splits][rows] (running maximum, sum)
-    unsigned* done;              // per tile: chunks finished
+    float* part;                 // two slots per CTA: unnormalised sums of an item's piece
+    float2* part_ml;             // and its rows' (reference, sum of weights)
+    unsigned* done;              // per item: pieces finished
     SbDeviceState* st;
 };
 
@@ -29,6 +28,80 @@ struct AtArgs {
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len);
 
 #ifdef __CUDACC__
+// ---- who does what -------------------------------------------------------------------------------
+// An item is a tile of query rows (new tokens x query heads of one cache head) of a request and a
+// cache head; its work, in units, is its key steps and EXTRA for its queries and results. The units of
+// all items, one after the other (requests, row tiles, heads), are cut into equal shares, one per CTA:
+// the requests' lengths are known on the device only, and a share costs the same whatever they are. An
+// item that a share's border cuts leaves a piece per share in scratch, to be added in their order.
+struct AtItem {
+    Kv8Request rq;
+    int b, r0, nrow;             // rows of the request's n * group from r0
+    int lo, hi;                  // keys that some row sees, lo at the start of a scale block
+    int steps;                   // 0: nothing to do
+};
+template <int ROWS, int KEYS>
+__device__ __forceinline__ AtItem at_item(const AtArgs& a, int row_tile) {
+    AtItem it;
+    it.b = row_tile / a.row_tiles;
+    it.r0 = (row_tile - it.b * a.row_tiles) * ROWS;
+    it.steps = 0;
+    if (!kv8_request(a.g, it.b, it.rq, a.st)) return it;
+    const int rows = it.rq.n * a.group;
+    if (it.r0 >= rows) return it;
+    it.nrow = min(ROWS, rows - it.r0);
+    const int i0 = it.r0 / a.group, i1 = (it.r0 + it.nrow - 1) / a.group;
+    it.hi = it.rq.past + i1 + 1;
+    it.lo = a.window > 0 ? max(0, it.rq.past + i0 - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
+    it.steps = (it.hi - it.lo + KEYS - 1) / KEYS;
+    return it;
+}
+// A share as its pieces of items; every warp walks through them by itself.
+template <int ROWS, int KEYS, int EXTRA>
+struct AtWalk {
+    int row_tile, head, unit;                                        // where the piece starts
+    int step0, count;                                                // its key steps: step0 .. + count of it.steps
+    long long left, from;                                            // units left; the item's first unit of all
+    bool first;                                                      // the share starts with this piece
+    AtItem it;
+    __device__ __forceinline__ int units() const { return it.steps ? it.steps + EXTRA : 0; }
+    // the piece from `unit` on; its key steps may be none (only what an item costs besides)
+    __device__ __forceinline__ void cut() {
+        const int n = (int)min((long long)(units() - unit), left);
+        step0 = max(0, unit - EXTRA);
+        count = max(0, unit + n - EXTRA) - step0;
+        left -= n;
+    }
+    __device__ __forceinline__ bool step(const AtArgs& a) {
+        while (count == 0) {
+            if (left <= 0) return false;
+            first = false;
+            unit = 0;
+            from += units();
+            if (++head >= a.g.heads || it.steps == 0) {
+                head = 0;
+                if (++row_tile >= a.row_tiles * a.g.requests) return false;
+                it = at_item<ROWS, KEYS>(a, row_tile);
+            }
+            if (it.steps) cut();
+        }
+        return true;
+    }
+    __device__ __forceinline__ bool begin(const AtArgs& a, int row_tile_, int head_, int unit_, long long at, long long units_) {
+        row_tile = row_tile_; head = head_; unit = unit_;
+        from = at - unit;
+        left = units_;
+        first = true;
+        it = at_item<ROWS, KEYS>(a, row_tile);
+        count = 0;
+        if (it.steps) cut();
+        return step(a);
+    }
+    __device__ __forceinline__ bool next(const AtArgs& a) {
+        count = 0;
+        return step(a);
+    }
+};
 __device__ __forceinline__ uint4 at_lds128(unsigned a) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));

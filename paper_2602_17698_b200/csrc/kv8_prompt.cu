@@ -147,39 +147,17 @@ __device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[PR_SUB / 
     return lo + hi;
 }
 
-// ---- who does what -------------------------------------------------------------------------------
-// An item is 256 query rows of a request and head; its work, in units, is its key tiles and PR_EXTRA
-// for its queries and results. The units of all items, one after the other (requests, row tiles,
-// heads), are cut into equal shares, one per CTA: the requests' lengths are known on the device only,
-// and a share costs the same whatever they are. An item that a share's border cuts leaves its pieces
-// in scratch, and kv8_prompt_sum_kernel adds them.
+// The plan of the shares (items: 256 query rows), written by a kernel of its own.
 struct PrWork {
-    long long* prefix;           // [items / heads + 1] units of one head before the row tile
+    long long* prefix;           // [row tiles of all requests + 1] units of one head before the row tile
     int4* start;                 // [ctas] (row tile of all requests, head, unit) a share starts with; x < 0: no share
     long long* share;            // units of a share; units in all
     int ctas;
 };
-struct PrItem {
-    Kv8Request rq;
-    int b, r0, nrow;             // rows of the request's n * group from r0
-    int lo, hi;                  // keys that some row sees
-    int tiles;
-    __device__ __forceinline__ int units() const { return tiles ? tiles + PR_EXTRA : 0; }
-};
-__device__ __forceinline__ PrItem pr_item(const AtArgs& a, int row_tile, SbDeviceState* st) {
-    PrItem it;
-    it.b = row_tile / a.row_tiles;
-    it.r0 = (row_tile - it.b * a.row_tiles) * 2 * PR_ROWS;
-    it.tiles = 0;
-    if (!kv8_request(a.g, it.b, it.rq, st)) return it;
-    const int rows = it.rq.n * a.group;
-    if (it.r0 >= rows) return it;
-    it.nrow = min(2 * PR_ROWS, rows - it.r0);
-    const int i0 = it.r0 / a.group, i1 = (it.r0 + it.nrow - 1) / a.group;
-    it.hi = it.rq.past + i1 + 1;
-    it.lo = a.window > 0 ? max(0, it.rq.past + i0 - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
-    it.tiles = (it.hi - it.lo + PR_KEYS - 1) / PR_KEYS;
-    return it;
+using PrWalk = AtWalk<2 * PR_ROWS, PR_KEYS, PR_EXTRA>;
+__device__ __forceinline__ int pr_units(const AtArgs& a, int row_tile) {
+    const int steps = at_item<2 * PR_ROWS, PR_KEYS>(a, row_tile).steps;
+    return steps ? steps + PR_EXTRA : 0;
 }
 __global__ void __launch_bounds__(1024)
 kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
@@ -188,7 +166,7 @@ kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     long long before = 0;
     for (int base = 0; base < n; base += 1024) {
         const int i = base + threadIdx.x;
-        const long long mine = i < n ? pr_item(a, i, a.st).units() : 0;
+        const long long mine = i < n ? pr_units(a, i) : 0;
         long long x = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -230,51 +208,6 @@ kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     }
 }
 
-// A share as its pieces of items; every warp walks through them by itself.
-struct PrWalk {
-    int row_tile, head, unit;                                        // where the piece starts
-    int tile0, count;                                                // its key tiles: tile0 .. + count of it.tiles
-    long long left;
-    bool first;
-    PrItem it;
-    // the piece from `unit` on; its key tiles may be none (only what an item costs besides)
-    __device__ __forceinline__ void cut() {
-        const int units = (int)min((long long)(it.units() - unit), left);
-        tile0 = max(0, unit - PR_EXTRA);
-        count = max(0, unit + units - PR_EXTRA) - tile0;
-        left -= units;
-    }
-    __device__ __forceinline__ bool step(const AtArgs& a) {
-        while (count == 0) {
-            if (left <= 0) return false;
-            first = false;
-            unit = 0;
-            if (++head >= a.g.heads || it.tiles == 0) {
-                head = 0;
-                if (++row_tile >= a.row_tiles * a.g.requests) return false;
-                it = pr_item(a, row_tile, a.st);
-            }
-            if (it.tiles) cut();
-        }
-        return true;
-    }
-    __device__ __forceinline__ bool begin(const AtArgs& a, const PrWork& w) {
-        const int4 s = w.start[blockIdx.x];
-        if (s.x < 0) return false;
-        left = min(w.share[0], w.share[1] - (long long)blockIdx.x * w.share[0]);
-        row_tile = s.x; head = s.y; unit = s.z;
-        first = true;
-        it = pr_item(a, row_tile, a.st);
-        count = 0;
-        if (it.tiles) cut();
-        return step(a);
-    }
-    __device__ __forceinline__ bool next(const AtArgs& a) {
-        count = 0;
-        return step(a);
-    }
-};
-
 template <int TYPE, int DP>
 __global__ void __launch_bounds__(PR_THREADS, 1)
 kv8_prompt_kernel(const AtArgs a, const PrWork work) {
@@ -293,7 +226,11 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int D = a.g.dim;
     PrWalk wk;
-    if (!wk.begin(a, work)) return;
+    {
+        const int4 s = work.start[blockIdx.x];
+        const long long share = work.share[0], at = blockIdx.x * share;
+        if (s.x < 0 || !wk.begin(a, s.x, s.y, s.z, at, min(share, work.share[1] - at))) return;
+    }
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::RAW_RING; ++i) {
@@ -339,7 +276,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         int tiles_all = 0, tiles_mine = 0, pieces = 0;               // key tiles and pieces so far (of this row tile)
         bool ok = true;
         for (bool more = true; more && ok; more = wk.next(a), ++tiles_all) {
-            const PrItem& it = wk.it;
+            const AtItem& it = wk.it;
             const int count = wk.count;
             tiles_all += count - 1;
             const int base_all = tiles_all - (count - 1);
@@ -389,7 +326,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             // positions of the tile's first and last row decide which key tiles need a mask
             const int pos_lo = it.rq.past + (it.r0 + qt * PR_ROWS) / a.group;
             const int pos_hi = it.rq.past + (it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1) / a.group;
-            const int k0 = it.lo + wk.tile0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
+            const int k0 = it.lo + wk.step0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
             float m = -INFINITY, l = 0.f, vref = 0.f, inv = 0.f;
             ok = wait(scfull + (base_all & 3), base_all >> 2);
             for (int n = 0; ok && n < 2 * count; ++n) {              // halves of the key tiles
@@ -456,7 +393,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             t5_fence_after();
             tiles_mine += count;
             ++pieces;
-            const bool whole = count == it.tiles;
+            const bool whole = count == it.steps;
             const int h0 = wk.head * a.group;
             const int64_t tok = it.rq.row0 + row / a.group;
             const int h = h0 + row % a.group;
@@ -551,7 +488,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         bool ok = true;
         int n = 0;                                                   // converted tiles so far
         for (bool more = true; more && ok; more = wk.next(a)) {
-            const int k0 = wk.it.lo + wk.tile0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
+            const int k0 = wk.it.lo + wk.step0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
             const int limit = min(wk.it.rq.len, (k1 + SB_KV8_BLOCK - 1) / SB_KV8_BLOCK * SB_KV8_BLOCK) - k0;
             auto entry_of = [&](int j) -> int {
                 const int key = k0 + j * PR_KEYS + sblk;
@@ -590,7 +527,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         bool ok = true;
         int issued = 0;
         for (bool more = true; more && ok; more = wk.next(a)) {
-            const int k0 = wk.it.lo + wk.tile0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
+            const int k0 = wk.it.lo + wk.step0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
             auto entry_of = [&](int j) -> int {
                 const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
                 return lane < PR_BLOCKS && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + key / a.g.page_tokens] : -1;
@@ -709,8 +646,8 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
     const long long share = w.share[0], from = c * share - s.z;      // the item's first unit of all
     const int c0 = (int)((from + PR_EXTRA) / share);                 // the share with its first tile
     if (c != c0 + 1) return;
-    const PrItem it = pr_item(a, s.x, a.st);
-    const int c1 = (int)((from + it.units() - 1) / share), D = a.g.dim;
+    const AtItem it = at_item<2 * PR_ROWS, PR_KEYS>(a, s.x);
+    const int c1 = (int)((from + it.steps + PR_EXTRA - 1) / share), D = a.g.dim;
     const int r = 32 * blockIdx.y + threadIdx.x / 8, quad = 8 * blockIdx.z + threadIdx.x % 8;
     if (r >= it.nrow || 4 * quad >= D) return;
     float m = -INFINITY, l = 0.f;
