@@ -36,7 +36,7 @@ namespace {
 constexpr int AT_PROMPT_FROM = 64;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
-constexpr int AT_EXTRA = 6;             // what an item costs besides its steps, in steps
+constexpr int AT_EXTRA = 12;            // what an item costs besides its steps, in steps
 constexpr int AT_LEAST = 16 + AT_EXTRA; // units of a share at least: four steps of every warp
 constexpr float AT_SLACK = 8.f;         // log2 of how far a row's maximum may run ahead of its reference
 constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
@@ -150,414 +150,435 @@ kv8_rows_kernel(const AtArgs a) {
         if (!wk.begin(a, f0, f1, f2, at, min(share, total - at))) return;
     }
     for (bool more = true; more; more = wk.next(a)) {
-    const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
-    const Kv8Request rq = wk.it.rq;
-    const int i0 = r0 / a.group, i1 = (r0 + nrow - 1) / a.group;
-    const int k0 = wk.it.lo + wk.step0 * AT_STEP, k1 = min(wk.it.hi, k0 + wk.count * AT_STEP);
-    const int mine = (wk.count - warp + AT_WARPS - 1) / AT_WARPS;   // steps warp, warp + 4, ...
+        const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
+        const Kv8Request rq = wk.it.rq;
+        const int i0 = r0 / a.group, i1 = (r0 + nrow - 1) / a.group;
+        const int k0 = wk.it.lo + wk.step0 * AT_STEP, k1 = min(wk.it.hi, k0 + wk.count * AT_STEP);
+        const int mine = (wk.count - warp + AT_WARPS - 1) / AT_WARPS;   // steps warp, warp + 4, ...
 
-    // ---- where this warp's blocks lie and their scales, AT_BATCH steps at a time: lane 2 s + e holds block e
-    // of step s; the table's entries are fetched two batches ahead, scales one ----
-    auto block_key = [&](int batch) { return k0 + (warp + AT_WARPS * (AT_BATCH * batch + (lane >> 1))) * AT_STEP + SB_KV8_BLOCK * (lane & 1); };
-    auto load_entry = [&](int batch) -> int {
-        const int key = block_key(batch);
-        return key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : 0;
-    };
-    // the block's first code (-1: no such block) and, fetched, its two scales
-    auto place = [&](int batch, int entry, uint32_t& s2) -> int64_t {
-        const int key = block_key(batch);
-        s2 = 0;
-        if (key >= k1) return -1;
-        if (entry < 0 || entry >= a.g.pages) {
-            sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
-            return -1;
-        }
-        const int64_t ph = (int64_t)entry * a.g.heads + head;
-        const int slot = key % a.g.page_tokens;
-        const int64_t at = ph * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;
-        s2 = (uint32_t)a.k_scale[at] | (uint32_t)a.v_scale[at] << 16;
-        return (ph * a.g.page_tokens + slot) * D;
-    };
-    int entry_next = load_entry(1);
-    uint32_t sc_cur, sc_next = 0;
-    int64_t at_even = place(0, load_entry(0), sc_cur), at_odd = -1;     // of even and odd batches
-
-    const unsigned ring = at_smem(smem) + (unsigned)(warp * S::STAGES * 2 * S::SIDE);
-    // copies of step j of this warp into its ring
-    constexpr int TOKS = 32 / PIECES;                               // tokens a warp copies with one instruction
-    const int cp_piece = lane % PIECES, cp_tok = lane / PIECES;
-    const int cp_off = cp_tok * D + cp_piece * 16;
-    auto ring_at = [](int row, int piece) {
-        return DP == 64 ? (unsigned)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4)) : (unsigned)(row * DP + ((piece ^ (row & 7)) << 4));
-    };
-    auto issue = [&](int j) {
-        if (j < mine) {
-            const int key = k0 + (warp + AT_WARPS * j) * AT_STEP;
-            const unsigned dst = ring + (unsigned)((j % S::STAGES) * 2 * S::SIDE);
-            const int64_t held = (j / AT_BATCH) & 1 ? at_odd : at_even;
+        // the queries are on their way before the chain of table, scales and codes begins
+        constexpr int QR = S::ROWS / AT_WARPS;
+        uint32_t qw[QR][DP / 64];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int64_t base = __shfl_sync(0xffffffffu, held, 2 * (j & (AT_BATCH - 1)) + e);
-                const uint8_t *kp = a.k + base + cp_off, *vp = a.v + base + cp_off;
-                if (D == DP && base >= 0 && key + SB_KV8_BLOCK * (e + 1) <= rq.len) {
-#pragma unroll
-                    for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
-                        const unsigned to = ring_at(SB_KV8_BLOCK * e + cp_tok + TOKS * i, cp_piece);
-                        at_copy16(dst + to, kp + TOKS * i * DP);
-                        at_copy16(dst + S::SIDE + to, vp + TOKS * i * DP);
-                    }
-                } else {
-                    // the last block, a block that is not there, or rows shorter than the operand's: zeros fill up
-#pragma unroll
-                    for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
-                        const int tok = cp_tok + TOKS * i;
-                        const bool take = base >= 0 && key + SB_KV8_BLOCK * e + tok < rq.len && cp_piece * 16 < D;
-                        const unsigned to = ring_at(SB_KV8_BLOCK * e + tok, cp_piece);
-                        at_copy16(dst + to, take ? kp + TOKS * i * D : a.k, take);
-                        at_copy16(dst + S::SIDE + to, take ? vp + TOKS * i * D : a.v, take);
-                    }
-                }
-            }
-        }
-        at_commit();
-    };
-#pragma unroll
-    for (int j = 0; j < S::STAGES - 1; ++j) issue(j);
-
-    // ---- queries: fp16 rows, each scaled by a power of two ----
-    for (int r = warp; r < S::ROWS; r += AT_WARPS) {
-        unsigned char* qrow = smem + S::Q_AT + r * S::QPITCH;
-        uint32_t w[DP / 64];
-        uint32_t amax = 0;
-        const int row = r0 + r;
-        const __nv_bfloat16* src = a.q + (int64_t)(rq.row0 + row / a.group) * a.q_token_stride +
-                                   (int64_t)(head * a.group + row % a.group) * a.q_head_stride;
-#pragma unroll
-        for (int i = 0; i < DP / 64; ++i) {
-            const int d = 64 * i + 2 * lane;
-            w[i] = r < nrow && d < D ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
-            amax = max(amax, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const float up = at_query_scale(amax);
-#pragma unroll
-        for (int i = 0; i < DP / 64; ++i)
-            *reinterpret_cast<uint32_t*>(qrow + 128 * i + 4 * lane) = at_half2(bf16lo(w[i]) * up, bf16hi(w[i]) * up);
-        if (lane == 0) reinterpret_cast<float*>(smem + S::F_AT)[r] = __fdiv_rn(a.scale_log2, up);
-    }
-    __syncthreads();
-    float fq[NR][2];
-    int pos[NR][2];
-#pragma unroll
-    for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = 8 * nr + 2 * t + e;
-            fq[nr][e] = reinterpret_cast<const float*>(smem + S::F_AT)[r];
-            pos[nr][e] = rq.past + (r0 + r) / a.group;          // rows past the last: queries of zeros, dropped at the end
-        }
-    // B operand of step 4 c + j: d = 64 c + 16 t + 4 j + {0, 1} and + {2, 3} of row g
-    const unsigned qlane = at_smem(smem) + S::Q_AT + (unsigned)(g * S::QPITCH + 32 * t);
-    uint2 qf[S::QREGS ? KS : 1][NR];
-    if (S::QREGS) {
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) qf[s][nr] = at_lds64(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * (s >> 2) + 8 * (s & 3)));
-    }
-
-    float o[MT][NR][4], m[NR][2], l[NR][2];
-    float vref = 0.f;
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr) o[i][nr][0] = o[i][nr][1] = o[i][nr][2] = o[i][nr][3] = 0.f;
-#pragma unroll
-    for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) { m[nr][e] = -INFINITY; l[nr][e] = 0.f; }
-
-    for (int j = 0; j < mine; ++j) {
-        if ((j & (AT_BATCH - 1)) == 0) {
-            const int batch = j / AT_BATCH;
-            if (batch > 0) sc_cur = sc_next;
-            if (AT_BATCH * (batch + 1) < mine) {
-                const int64_t at = place(batch + 1, entry_next, sc_next);
-                if (batch & 1) at_even = at;                         // the slot of the batch before this one
-                else at_odd = at;
-                entry_next = load_entry(batch + 2);
-            }
-        }
-        at_wait<S::STAGES - 2>();
-        __syncwarp();
-        issue(j + S::STAGES - 1);
-        const int key = k0 + (warp + AT_WARPS * j) * AT_STEP;
-        const unsigned kst = ring + (unsigned)((j % S::STAGES) * 2 * S::SIDE), vst = kst + S::SIDE;
-        float ksc[2], vsc[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t s2 = __shfl_sync(0xffffffffu, sc_cur, 2 * (j & (AT_BATCH - 1)) + e);
-            ksc[e] = __uint_as_float(s2 << 16);
-            vsc[e] = __uint_as_float(s2 & 0xffff0000u);
-        }
-        // scores, in units of log2
-        float s[2][NR][4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) s[e][nr][0] = s[e][nr][1] = s[e][nr][2] = s[e][nr][3] = 0.f;
+        for (int i = 0; i < QR; ++i) {
+            const int r = warp + AT_WARPS * i, row = r0 + r;
+            const __nv_bfloat16* src = a.q + (int64_t)(rq.row0 + row / a.group) * a.q_token_stride +
+                                       (int64_t)(head * a.group + row % a.group) * a.q_head_stride;
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c) {
-                const int row = SB_KV8_BLOCK * e + g;               // rows g and g + 8 have the same swizzle
-                const unsigned off = DP == 64 ? (unsigned)(row * 64 + ((t ^ ((row >> 1) & 3)) << 4))
-                                              : (unsigned)(row * DP + 128 * (c >> 1) + (((4 * (c & 1) + t) ^ (row & 7)) << 4));
-                const uint4 lo4 = at_lds128(kst + off), hi4 = at_lds128(kst + off + 8 * DP);
-                const uint32_t wl[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, wh[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+                const int d = 64 * c + 2 * lane;
+                qw[i][c] = r < nrow && d < D ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
+            }
+        }
+
+        // ---- where this warp's blocks lie and their scales, AT_BATCH steps at a time: lane 2 s + e holds block e
+        // of step s; the table's entries are fetched two batches ahead, scales one ----
+        auto block_key = [&](int batch) { return k0 + (warp + AT_WARPS * (AT_BATCH * batch + (lane >> 1))) * AT_STEP + SB_KV8_BLOCK * (lane & 1); };
+        auto load_entry = [&](int batch) -> int {
+            const int key = block_key(batch);
+            return key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : 0;
+        };
+        // the block's first code (-1: no such block) and, fetched, its two scales
+        auto place = [&](int batch, int entry, uint32_t& s2) -> int64_t {
+            const int key = block_key(batch);
+            s2 = 0;
+            if (key >= k1) return -1;
+            if (entry < 0 || entry >= a.g.pages) {
+                sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
+                return -1;
+            }
+            const int64_t ph = (int64_t)entry * a.g.heads + head;
+            const int slot = key % a.g.page_tokens;
+            const int64_t at = ph * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;
+            s2 = (uint32_t)a.k_scale[at] | (uint32_t)a.v_scale[at] << 16;
+            return (ph * a.g.page_tokens + slot) * D;
+        };
+        int entry_next = load_entry(1);
+        uint32_t sc_cur, sc_next = 0;
+        int64_t at_even = place(0, load_entry(0), sc_cur), at_odd = -1;     // of even and odd batches
+
+        const unsigned ring = at_smem(smem) + (unsigned)(warp * S::STAGES * 2 * S::SIDE);
+        // copies of step j of this warp into its ring
+        constexpr int TOKS = 32 / PIECES;                               // tokens a warp copies with one instruction
+        const int cp_piece = lane % PIECES, cp_tok = lane / PIECES;
+        const int cp_off = cp_tok * D + cp_piece * 16;
+        auto ring_at = [](int row, int piece) {
+            return DP == 64 ? (unsigned)(row * 64 + ((piece ^ ((row >> 1) & 3)) << 4)) : (unsigned)(row * DP + ((piece ^ (row & 7)) << 4));
+        };
+        auto issue = [&](int j) {
+            if (j < mine) {
+                const int key = k0 + (warp + AT_WARPS * j) * AT_STEP;
+                const unsigned dst = ring + (unsigned)((j % S::STAGES) * 2 * S::SIDE);
+                const int64_t held = (j / AT_BATCH) & 1 ? at_odd : at_even;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = at_flip<TYPE>(wl[i]), y = at_flip<TYPE>(wh[i]);
-                    const uint32_t a0 = at_pair<TYPE, 0>(x), a1 = at_pair<TYPE, 0>(y), a2 = at_pair<TYPE, 1>(x), a3 = at_pair<TYPE, 1>(y);
+                for (int e = 0; e < 2; ++e) {
+                    const int64_t base = __shfl_sync(0xffffffffu, held, 2 * (j & (AT_BATCH - 1)) + e);
+                    const uint8_t *kp = a.k + base + cp_off, *vp = a.v + base + cp_off;
+                    if (D == DP && base >= 0 && key + SB_KV8_BLOCK * (e + 1) <= rq.len) {
 #pragma unroll
-                    for (int nr = 0; nr < NR; ++nr) {
-                        uint2 qb;
-                        if constexpr (S::QREGS) qb = qf[4 * c + i][nr];
-                        else qb = at_lds64(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * c + 8 * i));
-                        at_mma(s[e][nr], a0, a1, a2, a3, qb.x, qb.y);
+                        for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
+                            const unsigned to = ring_at(SB_KV8_BLOCK * e + cp_tok + TOKS * i, cp_piece);
+                            at_copy16(dst + to, kp + TOKS * i * DP);
+                            at_copy16(dst + S::SIDE + to, vp + TOKS * i * DP);
+                        }
+                    } else {
+                        // the last block, a block that is not there, or rows shorter than the operand's: zeros fill up
+#pragma unroll
+                        for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
+                            const int tok = cp_tok + TOKS * i;
+                            const bool take = base >= 0 && key + SB_KV8_BLOCK * e + tok < rq.len && cp_piece * 16 < D;
+                            const unsigned to = ring_at(SB_KV8_BLOCK * e + tok, cp_piece);
+                            at_copy16(dst + to, take ? kp + TOKS * i * D : a.k, take);
+                            at_copy16(dst + S::SIDE + to, take ? vp + TOKS * i * D : a.v, take);
+                        }
                     }
                 }
             }
+            at_commit();
+        };
+#pragma unroll
+        for (int j = 0; j < S::STAGES - 1; ++j) issue(j);
+
+        // ---- queries: fp16 rows, each scaled by a power of two ----
+#pragma unroll
+        for (int i = 0; i < QR; ++i) {
+            const int r = warp + AT_WARPS * i;
+            unsigned char* qrow = smem + S::Q_AT + r * S::QPITCH;
+            uint32_t amax = 0;
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c) amax = max(amax, max(qw[i][c] & 0x7fffu, (qw[i][c] >> 16) & 0x7fffu));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            const float up = at_query_scale(amax);
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c)
+                *reinterpret_cast<uint32_t*>(qrow + 128 * c + 4 * lane) = at_half2(bf16lo(qw[i][c]) * up, bf16hi(qw[i][c]) * up);
+            if (lane == 0) reinterpret_cast<float*>(smem + S::F_AT)[r] = __fdiv_rn(a.scale_log2, up);
         }
-        const bool edge = key + AT_STEP > rq.past + i0 + 1 || key + AT_STEP > k1 || (a.window > 0 && key <= rq.past + i1 - a.window);
+        __syncthreads();
+        float fq[NR][2];
+        int pos[NR][2];
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) {
-            float mx[2] = {-INFINITY, -INFINITY};
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * nr + 2 * t + e;
+                fq[nr][e] = reinterpret_cast<const float*>(smem + S::F_AT)[r];
+                pos[nr][e] = rq.past + (r0 + r) / a.group;          // rows past the last: queries of zeros, dropped at the end
+            }
+        // B operand of step 4 c + j: d = 64 c + 16 t + 4 j + {0, 1} and + {2, 3} of row g
+        const unsigned qlane = at_smem(smem) + S::Q_AT + (unsigned)(g * S::QPITCH + 32 * t);
+        uint2 qf[S::QREGS ? KS : 1][NR];
+        if (S::QREGS) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = s[e][nr][i] * (ksc[e] * fq[nr][i & 1]);
-                    if (edge) {
-                        const int kk = key + SB_KV8_BLOCK * e + g + 8 * (i >> 1), p = pos[nr][i & 1];
-                        if (kk > p || kk >= k1 || (a.window > 0 && kk <= p - a.window)) x = -INFINITY;
-                    }
-                    s[e][nr][i] = x;
-                    mx[i & 1] = fmaxf(mx[i & 1], x);
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) qf[s][nr] = at_lds64(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * (s >> 2) + 8 * (s & 3)));
+        }
+
+        float o[MT][NR][4], m[NR][2], l[NR][2];
+        float vref = 0.f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) o[i][nr][0] = o[i][nr][1] = o[i][nr][2] = o[i][nr][3] = 0.f;
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) { m[nr][e] = -INFINITY; l[nr][e] = 0.f; }
+
+        for (int j = 0; j < mine; ++j) {
+            if ((j & (AT_BATCH - 1)) == 0) {
+                const int batch = j / AT_BATCH;
+                if (batch > 0) sc_cur = sc_next;
+                if (AT_BATCH * (batch + 1) < mine) {
+                    const int64_t at = place(batch + 1, entry_next, sc_next);
+                    if (batch & 1) at_even = at;                         // the slot of the batch before this one
+                    else at_odd = at;
+                    entry_next = load_entry(batch + 2);
                 }
+            }
+            at_wait<S::STAGES - 2>();
+            __syncwarp();
+            issue(j + S::STAGES - 1);
+            const int key = k0 + (warp + AT_WARPS * j) * AT_STEP;
+            const unsigned kst = ring + (unsigned)((j % S::STAGES) * 2 * S::SIDE), vst = kst + S::SIDE;
+            float ksc[2], vsc[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t s2 = __shfl_sync(0xffffffffu, sc_cur, 2 * (j & (AT_BATCH - 1)) + e);
+                ksc[e] = __uint_as_float(s2 << 16);
+                vsc[e] = __uint_as_float(s2 & 0xffff0000u);
+            }
+            // scores, in units of log2
+            float s[2][NR][4];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                for (int w = 4; w < 32; w <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
-            }
-            // the reference only moves when it is off by more than 2^8: a weight stays below 2^8
-            bool off[2];
+                for (int nr = 0; nr < NR; ++nr) s[e][nr][0] = s[e][nr][1] = s[e][nr][2] = s[e][nr][3] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + AT_SLACK || (m[nr][e] == -INFINITY && mx[e] > m[nr][e]);
-            if (__any_sync(0xffffffffu, off[0] || off[1])) {
-                float f[2];
+                for (int c = 0; c < DP / 64; ++c) {
+                    const int row = SB_KV8_BLOCK * e + g;               // rows g and g + 8 have the same swizzle
+                    const unsigned off = DP == 64 ? (unsigned)(row * 64 + ((t ^ ((row >> 1) & 3)) << 4))
+                                                  : (unsigned)(row * DP + 128 * (c >> 1) + (((4 * (c & 1) + t) ^ (row & 7)) << 4));
+                    const uint4 lo4 = at_lds128(kst + off), hi4 = at_lds128(kst + off + 8 * DP);
+                    const uint32_t wl[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, wh[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    f[e] = !off[e] ? 1.f : m[nr][e] == -INFINITY ? 0.f : at_exp2(m[nr][e] - mx[e]);
-                    if (off[e]) m[nr][e] = mx[e];
-                    l[nr][e] *= f[e];
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x = at_flip<TYPE>(wl[i]), y = at_flip<TYPE>(wh[i]);
+                        const uint32_t a0 = at_pair<TYPE, 0>(x), a1 = at_pair<TYPE, 0>(y), a2 = at_pair<TYPE, 1>(x), a3 = at_pair<TYPE, 1>(y);
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr) {
+                            uint2 qb;
+                            if constexpr (S::QREGS) qb = qf[4 * c + i][nr];
+                            else qb = at_lds64(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * c + 8 * i));
+                            at_mma(s[e][nr], a0, a1, a2, a3, qb.x, qb.y);
+                        }
+                    }
                 }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    o[i][nr][0] *= f[0]; o[i][nr][1] *= f[1]; o[i][nr][2] *= f[0]; o[i][nr][3] *= f[1];
-                }
             }
-        }
-        // value scales relative to a power of two that only grows
-        const float vmax = fmaxf(vsc[0], vsc[1]);
-        if (vmax > vref) {
-            const float fresh = at_value_ref(vmax);
-            const float f = __fdiv_rn(vref, fresh);
-            vref = fresh;
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o[i][nr][k] *= f;
-        }
-        const float inv = at_value_inv(vref);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float vw = vsc[e] * inv;
-            uint32_t pb[NR][2];
+            const bool edge = key + AT_STEP > rq.past + i0 + 1 || key + AT_STEP > k1 || (a.window > 0 && key <= rq.past + i1 - a.window);
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
-                float p[4];
+                float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float mm = m[nr][i & 1];
-                    p[i] = at_exp2(s[e][nr][i] - (mm == -INFINITY ? 0.f : mm));
-                    l[nr][i & 1] += p[i];
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x = s[e][nr][i] * (ksc[e] * fq[nr][i & 1]);
+                        if (edge) {
+                            const int kk = key + SB_KV8_BLOCK * e + g + 8 * (i >> 1), p = pos[nr][i & 1];
+                            if (kk > p || kk >= k1 || (a.window > 0 && kk <= p - a.window)) x = -INFINITY;
+                        }
+                        s[e][nr][i] = x;
+                        mx[i & 1] = fmaxf(mx[i & 1], x);
+                    }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
                 }
-                pb[nr][0] = at_transpose(at_half2(p[0] * vw, p[1] * vw));
-                pb[nr][1] = at_transpose(at_half2(p[2] * vw, p[3] * vw));
-            }
-            constexpr int VP = DP / 128 > 0 ? DP / 128 : 1;          // panels of 128 d
-            constexpr int VW = DP == 64 ? 2 : 4;                     // words a lane takes of a row and panel
+                // the reference only moves when it is off by more than 2^8: a weight stays below 2^8
+                bool off[2];
 #pragma unroll
-            for (int pn = 0; pn < VP; ++pn) {
-                uint32_t w[4][VW];
+                for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + AT_SLACK || (m[nr][e] == -INFINITY && mx[e] > m[nr][e]);
+                if (__any_sync(0xffffffffu, off[0] || off[1])) {
+                    float f[2];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = SB_KV8_BLOCK * e + 2 * t + (k & 1) + 8 * (k >> 1);
-                    if constexpr (DP == 64) {
-                        const uint2 x = at_lds64(vst + (unsigned)(row * 64 + (((g >> 1) ^ ((row >> 1) & 3)) << 4) + 8 * (g & 1)));
-                        w[k][0] = at_flip<TYPE>(x.x); w[k][1] = at_flip<TYPE>(x.y);
-                    } else {
-                        const uint4 x = at_lds128(vst + (unsigned)(row * DP + 128 * pn + ((g ^ (row & 7)) << 4)));
-                        w[k][0] = at_flip<TYPE>(x.x); w[k][1] = at_flip<TYPE>(x.y);
-                        w[k][2] = at_flip<TYPE>(x.z); w[k][3] = at_flip<TYPE>(x.w);
+                    for (int e = 0; e < 2; ++e) {
+                        f[e] = !off[e] ? 1.f : m[nr][e] == -INFINITY ? 0.f : at_exp2(m[nr][e] - mx[e]);
+                        if (off[e]) m[nr][e] = mx[e];
+                        l[nr][e] *= f[e];
+                    }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        o[i][nr][0] *= f[0]; o[i][nr][1] *= f[1]; o[i][nr][2] *= f[0]; o[i][nr][3] *= f[1];
                     }
                 }
+            }
+            // value scales relative to a power of two that only grows
+            const float vmax = fmaxf(vsc[0], vsc[1]);
+            if (vmax > vref) {
+                const float fresh = at_value_ref(vmax);
+                const float f = __fdiv_rn(vref, fresh);
+                vref = fresh;
 #pragma unroll
-                for (int c = 0; c < VW; ++c) {
-                    // bytes 0, 1 and 2, 3 of the two key pairs, interleaved
-                    const uint32_t l01 = __byte_perm(w[0][c], w[1][c], 0x5140), l23 = __byte_perm(w[0][c], w[1][c], 0x7362);
-                    const uint32_t h01 = __byte_perm(w[2][c], w[3][c], 0x5140), h23 = __byte_perm(w[2][c], w[3][c], 0x7362);
-                    const uint32_t a0 = at_pair<TYPE, 0>(l01), a1 = at_pair<TYPE, 1>(l01), a2 = at_pair<TYPE, 0>(h01), a3 = at_pair<TYPE, 1>(h01);
-                    const uint32_t c0 = at_pair<TYPE, 0>(l23), c1 = at_pair<TYPE, 1>(l23), c2 = at_pair<TYPE, 0>(h23), c3 = at_pair<TYPE, 1>(h23);
-                    const int i = 2 * (VW * pn + c);
+                for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int nr = 0; nr < NR; ++nr) {
-                        at_mma(o[i][nr], a0, a1, a2, a3, pb[nr][0], pb[nr][1]);
-                        at_mma(o[i + 1][nr], c0, c1, c2, c3, pb[nr][0], pb[nr][1]);
+                    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[i][nr][k] *= f;
+            }
+            const float inv = at_value_inv(vref);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float vw = vsc[e] * inv;
+                uint32_t pb[NR][2];
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) {
+                    float p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float mm = m[nr][i & 1];
+                        p[i] = at_exp2(s[e][nr][i] - (mm == -INFINITY ? 0.f : mm));
+                        l[nr][i & 1] += p[i];
+                    }
+                    pb[nr][0] = at_transpose(at_half2(p[0] * vw, p[1] * vw));
+                    pb[nr][1] = at_transpose(at_half2(p[2] * vw, p[3] * vw));
+                }
+                constexpr int VP = DP / 128 > 0 ? DP / 128 : 1;          // panels of 128 d
+                constexpr int VW = DP == 64 ? 2 : 4;                     // words a lane takes of a row and panel
+#pragma unroll
+                for (int pn = 0; pn < VP; ++pn) {
+                    uint32_t w[4][VW];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int row = SB_KV8_BLOCK * e + 2 * t + (k & 1) + 8 * (k >> 1);
+                        if constexpr (DP == 64) {
+                            const uint2 x = at_lds64(vst + (unsigned)(row * 64 + (((g >> 1) ^ ((row >> 1) & 3)) << 4) + 8 * (g & 1)));
+                            w[k][0] = at_flip<TYPE>(x.x); w[k][1] = at_flip<TYPE>(x.y);
+                        } else {
+                            const uint4 x = at_lds128(vst + (unsigned)(row * DP + 128 * pn + ((g ^ (row & 7)) << 4)));
+                            w[k][0] = at_flip<TYPE>(x.x); w[k][1] = at_flip<TYPE>(x.y);
+                            w[k][2] = at_flip<TYPE>(x.z); w[k][3] = at_flip<TYPE>(x.w);
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < VW; ++c) {
+                        // bytes 0, 1 and 2, 3 of the two key pairs, interleaved
+                        const uint32_t l01 = __byte_perm(w[0][c], w[1][c], 0x5140), l23 = __byte_perm(w[0][c], w[1][c], 0x7362);
+                        const uint32_t h01 = __byte_perm(w[2][c], w[3][c], 0x5140), h23 = __byte_perm(w[2][c], w[3][c], 0x7362);
+                        const uint32_t a0 = at_pair<TYPE, 0>(l01), a1 = at_pair<TYPE, 1>(l01), a2 = at_pair<TYPE, 0>(h01), a3 = at_pair<TYPE, 1>(h01);
+                        const uint32_t c0 = at_pair<TYPE, 0>(l23), c1 = at_pair<TYPE, 1>(l23), c2 = at_pair<TYPE, 0>(h23), c3 = at_pair<TYPE, 1>(h23);
+                        const int i = 2 * (VW * pn + c);
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr) {
+                            at_mma(o[i][nr], a0, a1, a2, a3, pb[nr][0], pb[nr][1]);
+                            at_mma(o[i + 1][nr], c0, c1, c2, c3, pb[nr][0], pb[nr][1]);
+                        }
                     }
                 }
             }
         }
-    }
-    at_wait<0>();
-    __syncthreads();
+        at_wait<0>();
+        __syncthreads();
 
-    // ---- the warps' sums side by side where the ring was ----
-    float* osm = reinterpret_cast<float*>(smem);                     // [warp][row][OPITCH]
-    float2* mlsm = reinterpret_cast<float2*>(smem + (size_t)AT_WARPS * S::ROWS * S::OPITCH * 4);      // [warp][row]
+        // ---- the warps' sums side by side where the ring was ----
+        float* osm = reinterpret_cast<float*>(smem);                     // [warp][row][OPITCH]
+        float2* mlsm = reinterpret_cast<float2*>(smem + (size_t)AT_WARPS * S::ROWS * S::OPITCH * 4);      // [warp][row]
 #pragma unroll
-    for (int nr = 0; nr < NR; ++nr)
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float sum = l[nr][e];
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[nr][e];
 #pragma unroll
-            for (int w = 4; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-            const int r = 8 * nr + 2 * t + e;
-            if (g == 0) mlsm[warp * S::ROWS + r] = make_float2(m[nr][e], sum);
-            float* row = osm + (warp * S::ROWS + r) * S::OPITCH;
+                for (int w = 4; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                const int r = 8 * nr + 2 * t + e;
+                if (g == 0) mlsm[warp * S::ROWS + r] = make_float2(m[nr][e], sum);
+                float* row = osm + (warp * S::ROWS + r) * S::OPITCH;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                // o[i][.][e] and [2 + e]: two neighbouring d of row r
-                constexpr int LW = DP == 64 ? 8 : 16;                // d a lane holds per panel
-                const int d = LW * g + 128 * (i / (LW / 2)) + 2 * (i % (LW / 2));
-                *reinterpret_cast<float2*>(row + d) = make_float2(o[i][nr][e] * vref, o[i][nr][2 + e] * vref);
+                for (int i = 0; i < MT; ++i) {
+                    // o[i][.][e] and [2 + e]: two neighbouring d of row r
+                    constexpr int LW = DP == 64 ? 8 : 16;                // d a lane holds per panel
+                    const int d = LW * g + 128 * (i / (LW / 2)) + 2 * (i % (LW / 2));
+                    *reinterpret_cast<float2*>(row + d) = make_float2(o[i][nr][e] * vref, o[i][nr][2 + e] * vref);
+                }
+            }
+        __syncthreads();
+        const bool whole = wk.count == wk.it.steps;
+        const int quads = D / 4;
+        auto store = [&](int r, int d, float4 v, float mm, float sum) {
+            const int row = r0 + r;
+            const int64_t tok = rq.row0 + row / a.group;
+            const int h = head * a.group + row % a.group;
+            const float f = at_norm(sum);
+            const uint2 w = make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
+            *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) = w;
+            if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(mm, sum);
+        };
+        for (int idx = threadIdx.x; idx < nrow * quads; idx += AT_WARPS * 32) {
+            const int r = idx / quads, d = 4 * (idx - r * quads);
+            float2 ml[AT_WARPS];
+            float mm = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < AT_WARPS; ++w) {
+                ml[w] = mlsm[w * S::ROWS + r];
+                mm = fmaxf(mm, ml[w].x);
+            }
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < AT_WARPS; ++w) {
+                const float f = ml[w].x == -INFINITY ? 0.f : at_exp2(ml[w].x - mm);
+                const float4 x = *reinterpret_cast<const float4*>(osm + (w * S::ROWS + r) * S::OPITCH + d);
+                sum = fmaf(ml[w].y, f, sum);
+                v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+            }
+            if (whole) store(r, d, v, mm, sum);
+            else {
+                const int64_t at = (2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1)) * S::ROWS + r;
+                *reinterpret_cast<float4*>(a.part + at * D + d) = v;
+                if (d == 0) a.part_ml[at] = make_float2(mm, sum);
             }
         }
-    __syncthreads();
-    const bool whole = wk.count == wk.it.steps;
-    const int quads = D / 4;
-    auto store = [&](int r, int d, float4 v, float mm, float sum) {
-        const int row = r0 + r;
-        const int64_t tok = rq.row0 + row / a.group;
-        const int h = head * a.group + row % a.group;
-        const float f = at_norm(sum);
-        const uint2 w = make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
-        *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) = w;
-        if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(mm, sum);
-    };
-    for (int idx = threadIdx.x; idx < nrow * quads; idx += AT_WARPS * 32) {
-        const int r = idx / quads, d = 4 * (idx - r * quads);
-        float2 ml[AT_WARPS];
-        float mm = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < AT_WARPS; ++w) {
-            ml[w] = mlsm[w * S::ROWS + r];
-            mm = fmaxf(mm, ml[w].x);
-        }
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < AT_WARPS; ++w) {
-            const float f = ml[w].x == -INFINITY ? 0.f : at_exp2(ml[w].x - mm);
-            const float4 x = *reinterpret_cast<const float4*>(osm + (w * S::ROWS + r) * S::OPITCH + d);
-            sum = fmaf(ml[w].y, f, sum);
-            v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-        }
-        if (whole) store(r, d, v, mm, sum);
-        else {
-            const int64_t at = (2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1)) * S::ROWS + r;
-            *reinterpret_cast<float4*>(a.part + at * D + d) = v;
-            if (d == 0) a.part_ml[at] = make_float2(mm, sum);
-        }
-    }
-    if (!whole) {
-        // ---- the last of the item's pieces to finish adds them all, in order ----
-        const long long from = wk.from;
-        const int c0 = (int)((from + AT_EXTRA) / share), c1 = (int)((from + wk.units() - 1) / share), pieces = c1 - c0 + 1;
-        // a piece is the first of its share unless the item starts inside the share
-        auto slot = [&](int x) { return (2 * (int64_t)(c0 + x) + (from > (c0 + x) * share ? 1 : 0)) * S::ROWS; };
-        volatile int* last = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            unsigned* done = a.done + ((int64_t)wk.row_tile * a.g.heads + head);
-            *last = atomicAdd(done, 1u) == (unsigned)(pieces - 1);
-            if (*last) *done = 0;                                    // for the next call
-        }
-        __syncthreads();
-        if (*last) {
+        if (!whole) {
+            // ---- the last of the item's pieces to finish adds them all, in order ----
+            const long long from = wk.from;
+            const int c0 = (int)((from + AT_EXTRA) / share), c1 = (int)((from + wk.units() - 1) / share), pieces = c1 - c0 + 1;
+            // a piece is the first of its share unless the item starts inside the share
+            auto slot = [&](int x) { return (2 * (int64_t)(c0 + x) + (from > (c0 + x) * share ? 1 : 0)) * S::ROWS; };
+            volatile int* last = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
             __threadfence();
-            // weights of the pieces of every row in shared memory, a row per warp
-            float* weight = reinterpret_cast<float*>(smem);          // [pieces][ROWS]
-            float2* total = reinterpret_cast<float2*>(smem + S::F_AT - S::ROWS * 8);         // (reference, sum) of a row
-            for (int r = warp; r < nrow; r += AT_WARPS) {
-                float mm = -INFINITY, sum = 0.f;
-                for (int x = lane; x < pieces; x += 32) mm = fmaxf(mm, __ldcg(a.part_ml + slot(x) + r).x);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
-                for (int x = lane; x < pieces; x += 32) {
-                    const float2 ml = __ldcg(a.part_ml + slot(x) + r);
-                    const float f = ml.x == -INFINITY ? 0.f : at_exp2(ml.x - mm);
-                    weight[x * S::ROWS + r] = f;
-                    sum = fmaf(ml.y, f, sum);
-                }
-                sum = warp_sum(sum);
-                if (lane == 0) total[r] = make_float2(mm, sum);
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                unsigned* done = a.done + ((int64_t)wk.row_tile * a.g.heads + head);
+                *last = atomicAdd(done, 1u) == (unsigned)(pieces - 1);
+                if (*last) *done = 0;                                    // for the next call
             }
             __syncthreads();
-            // with few outputs several threads share one, each a part of the pieces
-            const int outs = nrow * quads;
-            const int parts = outs >= AT_WARPS * 32 ? 1 : AT_WARPS * 32 / outs;
-            float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
-            for (int base = 0; base < outs; base += AT_WARPS * 32) {
-                const int part = (int)threadIdx.x / outs, idx = parts > 1 ? (int)threadIdx.x - part * outs : base + (int)threadIdx.x;
-                const int r = idx / quads, d = 4 * (idx - r * quads);
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (idx < outs && (parts == 1 || part < parts)) {
-                    const int x0 = parts > 1 ? pieces * part / parts : 0, x1 = parts > 1 ? pieces * (part + 1) / parts : pieces;
-#pragma unroll 8
-                    for (int x = x0; x < x1; ++x) {
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x) + r) * D + d));
-                        const float f = weight[x * S::ROWS + r];
-                        v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+            if (*last) {
+                __threadfence();
+                // weights of the pieces of every row in shared memory, a row per warp
+                float* weight = reinterpret_cast<float*>(smem);          // [pieces][ROWS]
+                float2* total = reinterpret_cast<float2*>(smem + S::F_AT - S::ROWS * 8);         // (reference, sum) of a row
+                for (int r = warp; r < nrow; r += AT_WARPS) {
+                    constexpr int HELD = 4;                              // of a lane's pieces in registers: 128 in all
+                    float2 ml[HELD];
+                    float mm = -INFINITY, sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < HELD; ++i) {
+                        const int x = lane + 32 * i;
+                        ml[i] = x < pieces ? __ldcg(a.part_ml + slot(x) + r) : make_float2(-INFINITY, 0.f);
                     }
+#pragma unroll
+                    for (int i = 0; i < HELD; ++i) mm = fmaxf(mm, ml[i].x);
+                    for (int x = lane + 32 * HELD; x < pieces; x += 32) mm = fmaxf(mm, __ldcg(a.part_ml + slot(x) + r).x);
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
+                    auto put = [&](int x, float2 p) {
+                        const float f = p.x == -INFINITY ? 0.f : at_exp2(p.x - mm);
+                        weight[x * S::ROWS + r] = f;
+                        sum = fmaf(p.y, f, sum);
+                    };
+#pragma unroll
+                    for (int i = 0; i < HELD; ++i)
+                        if (lane + 32 * i < pieces) put(lane + 32 * i, ml[i]);
+                    for (int x = lane + 32 * HELD; x < pieces; x += 32) put(x, __ldcg(a.part_ml + slot(x) + r));
+                    sum = warp_sum(sum);
+                    if (lane == 0) total[r] = make_float2(mm, sum);
                 }
-                if (parts > 1) {
-                    shared_sum[threadIdx.x] = v;
-                    __syncthreads();
-                    if (threadIdx.x < outs) {
-                        for (int p = 1; p < parts; ++p) {
-                            const float4 y = shared_sum[threadIdx.x + p * outs];
-                            v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+                __syncthreads();
+                // with few outputs several threads share one, each a part of the pieces
+                const int outs = nrow * quads;
+                const int parts = outs >= AT_WARPS * 32 ? 1 : AT_WARPS * 32 / outs;
+                float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
+                for (int base = 0; base < outs; base += AT_WARPS * 32) {
+                    const int part = (int)threadIdx.x / outs, idx = parts > 1 ? (int)threadIdx.x - part * outs : base + (int)threadIdx.x;
+                    const int r = idx / quads, d = 4 * (idx - r * quads);
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (idx < outs && (parts == 1 || part < parts)) {
+                        const int x0 = parts > 1 ? pieces * part / parts : 0, x1 = parts > 1 ? pieces * (part + 1) / parts : pieces;
+#pragma unroll 8
+                        for (int x = x0; x < x1; ++x) {
+                            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x) + r) * D + d));
+                            const float f = weight[x * S::ROWS + r];
+                            v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
                         }
-                        store(r, d, v, total[r].x, total[r].y);
                     }
-                } else if (idx < outs) store(r, d, v, total[r].x, total[r].y);
+                    if (parts > 1) {
+                        shared_sum[threadIdx.x] = v;
+                        __syncthreads();
+                        if (threadIdx.x < outs) {
+                            for (int p = 1; p < parts; ++p) {
+                                const float4 y = shared_sum[threadIdx.x + p * outs];
+                                v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+                            }
+                            store(r, d, v, total[r].x, total[r].y);
+                        }
+                    } else if (idx < outs) store(r, d, v, total[r].x, total[r].y);
+                }
             }
         }
-    }
-    __syncthreads();                                                 // the next piece's copies go where the sums were
+        __syncthreads();                                                 // the next piece's copies go where the sums were
     }
 }
 
@@ -604,9 +625,10 @@ sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
 template <int TYPE, int DP>
 sb_status rows_by_count(sb_ctx* ctx, const AtArgs& a, int64_t max_new, int64_t max_len) {
     const int64_t rows = max_new * a.group;
-    return rows <= 8 ? rows_launch<TYPE, DP, 1>(ctx, a, max_new, max_len)
-         : rows <= 16 || DP == 256 ? rows_launch<TYPE, DP, 2>(ctx, a, max_new, max_len)
-                                   : rows_launch<TYPE, DP, DP == 256 ? 2 : 4>(ctx, a, max_new, max_len);
+    if (rows <= 8) return rows_launch<TYPE, DP, 1>(ctx, a, max_new, max_len);
+    if (rows <= 16 || DP == 256) return rows_launch<TYPE, DP, 2>(ctx, a, max_new, max_len);
+    if (rows <= 24) return rows_launch<TYPE, DP, DP == 256 ? 2 : 3>(ctx, a, max_new, max_len);
+    return rows_launch<TYPE, DP, DP == 256 ? 2 : 4>(ctx, a, max_new, max_len);
 }
 template <int TYPE>
 sb_status rows_by_dim(sb_ctx* ctx, const AtArgs& a, int64_t max_new, int64_t max_len) {
