@@ -137,6 +137,16 @@ __device__ __forceinline__ uint2 ld_stream8(const void* p) {
     return v;
 }
 
+// 32 bytes of one lane (32-byte aligned): the whole sector in one request
+__device__ __forceinline__ void ld_stream32(const void* p, uint32_t (&v)[8]) {
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
+}
+__device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                 ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p) : "memory");
+}
+
 __device__ __forceinline__ unsigned ld_acquire_u32(const unsigned* p) {
     unsigned v;
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
@@ -202,6 +212,16 @@ __device__ __forceinline__ void group_minmax(const uint32_t (&w)[NW], int team, 
     }
     lo = bf16lo(p);
     hi = -bf16hi(p);
+}
+
+// x / d rounded to nearest for r = RN(1 / d), at three instructions instead of a division: with
+// q = RN(x r), RN(q + r (x - q d)) is the correctly rounded quotient (Markstein, "Computation of
+// elementary functions on the IBM RISC System/6000 processor", 1990). d and r have to be normal
+// numbers with room below and above (div_in_range); a quotient that underflows comes out tiny.
+__device__ __forceinline__ bool div_in_range(float d) { return d > 0x1p-100f && d < 0x1p100f; }
+__device__ __forceinline__ float div_rn(float x, float d, float r) {
+    const float q = x * r;
+    return fmaf(-fmaf(q, d, -x), r, q);                      // in this form -0 stays -0
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

@@ -1,6 +1,7 @@
 // Quantisation to the microscaled 4-bit formats and back.
 //
-// One thread takes 16 consecutive columns of a row: two 16-byte loads, eight bytes of codes. That
+// One thread takes 16 consecutive columns of a row: one 32-byte load (two of 16 bytes where rows are
+// aligned no better), eight bytes of codes. That
 // is one block of SB_FP4_NV; two neighbouring lanes share a block of SB_FP4_MX and exchange their
 // maxima. The scales of four consecutive blocks are four consecutive bytes of a scale tile: the
 // lanes that hold them pass them to the first, which stores one word. Nothing is read twice; the
@@ -10,133 +11,172 @@
 namespace {
 
 constexpr int FQ_THREADS = 256;
+// Pieces of 16 columns a thread takes. With four the loads of a thread overlap and a block lives long
+// enough to hide its start; a call with too few pieces for that takes one.
+constexpr int FQ_MANY = 4;
 
-// x / d for every element of a block at the price of three instructions instead of a division:
-// with r = RN(1 / d) and q = RN(x r), RN(q + r (x - q d)) is the correctly rounded quotient
-// (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).
-// It needs r, q and the residual in the range of normal numbers: d between 2^-100 and 2^100 (a
-// quotient that underflows then is far below the smallest code and rounds to 0 either way).
-__device__ __forceinline__ float quotient(float x, float d, float r, bool plain) {
-    if (plain) return __fdiv_rn(x, d);
-    const float q = x * r;
-    return copysignf(fmaf(fmaf(-q, d, x), r, q), x);         // -0 would come out as 0
-}
+// A row's pieces are counted through the whole matrix; index / pieces by a multiplication: with
+// M = floor(2^64 / pieces) + 1, exact for index < 2^37 (checked) and pieces < 2^27.
+struct FqDiv {
+    uint64_t m;
+    unsigned n;
+    explicit FqDiv(int pieces) : m(pieces > 1 ? ~0ull / (unsigned)pieces + 1 : 0), n((unsigned)pieces) {}
+#ifdef __CUDACC__
+    __device__ __forceinline__ int64_t row(int64_t i, int& rest) const {
+        const int64_t r = n > 1 ? (int64_t)__umul64hi((unsigned long long)i, m) : i;
+        rest = (int)(i - r * n);
+        return r;
+    }
+#endif
+};
 
-template <int FORMAT>
-__global__ void __launch_bounds__(FQ_THREADS)
-fp4_quantize_kernel(const __nv_bfloat16* __restrict__ X, int64_t R, int64_t C, int64_t ldx, int64_t rows_padded,
-                    int units, const float* __restrict__ tensor_scale, uint8_t* __restrict__ codes,
-                    uint8_t* __restrict__ scales) {
-    // units: groups of 16 columns of a row, a whole number of scale tiles
-    const int64_t first = (int64_t)blockIdx.x * FQ_THREADS;
-    const int64_t row0 = first / units;
-    const unsigned off = (unsigned)(first - row0 * units) + threadIdx.x;
-    const int64_t r = row0 + off / (unsigned)units;
-    const int u = (int)(off % (unsigned)units);
-    const int64_t c0 = (int64_t)u * 16;
-    const int64_t Cp = fp4_padded_cols(C);
-    uint32_t w[8];
+// 16 columns of a row as bf16 pairs; columns from `left` on read as zero
+__device__ __forceinline__ void fq_load(const __nv_bfloat16* p, int64_t left, int wide, uint32_t (&w)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = 0;
-    if (r < R && c0 < C) {
-        const __nv_bfloat16* p = X + r * ldx + c0;
-        if (c0 + 16 <= C) {
+    if (left >= 16) {
+        if (wide) ld_stream32(p, w);
+        else {
             const uint4 a = ld_stream16(p), b = ld_stream16(p + 8);
             w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
             w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-        } else {
-            const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (c0 + i < C) w[i >> 1] |= (uint32_t)q[i] << (16 * (i & 1));
         }
-    }
-    // the largest magnitude as bf16 bits: their order is the order of the numbers, NaN above infinity
-    uint32_t m = w[0] & 0x7fff7fffu;
+    } else if (left > 0) {
+        const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+        for (int i = 0; i < 16; ++i)
+            if (i < left) w[i >> 1] |= (uint32_t)q[i] << (16 * (i & 1));
+    }
+}
+// codes of 16 columns and the scale byte of their block; g, rg: tensor scale and RN(1 / g)
+template <int FORMAT>
+__device__ __forceinline__ uint2 fq_codes(uint32_t (&w)[8], float g, float rg, uint32_t& scale) {
+    // the largest magnitude as bf16 bits, whose order is the order of the numbers; a NaN stays one, above infinity
+    __nv_bfloat162 m2 = __habs2(b162(w[0]));
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m2 = __hmax2_nan(m2, __habs2(b162(w[i])));
+    const uint32_t m = u32(m2);
     uint32_t amax = max(m & 0xffffu, m >> 16);
-    if (FORMAT == SB_FP4_MX) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-
-    float v[16];
-    uint32_t scale;
+    float v[2][8];
     if (FORMAT == SB_FP4_MX) {
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         // floor(log2 amax) is the exponent of amax; below the smallest normal number the clamp decides
         const int e = (int)(amax >> 7) - 2;
         scale = amax >= 0x7f80u ? 255u : (uint32_t)max(e, 0);
         const float inv = __uint_as_float((254u - min(scale, 253u)) << 23);     // 2^-e, exact
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            v[2 * i] = bf16lo(w[i]) * inv;
-            v[2 * i + 1] = bf16hi(w[i]) * inv;
+            v[i >> 2][2 * (i & 3)] = bf16lo(w[i]) * inv;
+            v[i >> 2][2 * (i & 3) + 1] = bf16hi(w[i]) * inv;
         }
     } else {
-        const float g = tensor_scale ? __ldg(tensor_scale) : 1.f;
-        const float t = __fdiv_rn(__fdiv_rn(__uint_as_float(amax << 16), 6.f), g);
+        const float am = __uint_as_float(amax << 16);
+        // the two quotients the short way where everything stays in range
+        const bool near = g > 0x1p-50f && g < 0x1p30f && am > 0x1p-60f && am < 0x1p60f;
+        const float t = near ? div_rn(div_rn(am, 6.f, 0.16666667f), g, rg) : __fdiv_rn(__fdiv_rn(am, 6.f), g);
         scale = !(g > 0.f) || !(t >= 0.f && t < __uint_as_float(0x7f800000u)) ? 0x7fu : e4m3_of(t);
         const float d = scale == 0x7fu ? 0.f : e4m3_value(scale) * g;
-        const bool plain = !(d > 0x1p-100f && d < 0x1p100f);
-        const float r1 = __frcp_rn(d);
+        if (div_in_range(d) || d == 0.f) {
+            // d = 0: every code is 0
+            const float dd = d > 0.f ? d : 1.f, r1 = __frcp_rn(dd);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[2 * i] = d > 0.f ? quotient(bf16lo(w[i]), d, r1, plain) : 0.f;
-            v[2 * i + 1] = d > 0.f ? quotient(bf16hi(w[i]), d, r1, plain) : 0.f;
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t x = d > 0.f ? w[i] : 0u;
+                v[i >> 2][2 * (i & 3)] = div_rn(bf16lo(x), dd, r1);
+                v[i >> 2][2 * (i & 3) + 1] = div_rn(bf16hi(x), dd, r1);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = __fdiv_rn((i & 1) ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]), d);
         }
     }
-    if (r < R && c0 < Cp) {
-        const float (&lo)[8] = *reinterpret_cast<float (*)[8]>(&v[0]);
-        const float (&hi)[8] = *reinterpret_cast<float (*)[8]>(&v[8]);
-        *reinterpret_cast<uint2*>(codes + r * (Cp >> 1) + (c0 >> 1)) = make_uint2(fp4_pack8(lo), fp4_pack8(hi));
-    }
-    // padding rows and blocks: 0
-    if (r >= R || c0 >= Cp) scale = 0;
-    constexpr int STEP = FORMAT == SB_FP4_MX ? 2 : 1;          // lanes per block
-    uint32_t word = scale;
-    word |= __shfl_down_sync(0xffffffffu, scale, STEP) << 8;
-    word |= __shfl_down_sync(0xffffffffu, word, 2 * STEP) << 16;
-    if (r < rows_padded && (u & (4 * STEP - 1)) == 0)
-        *reinterpret_cast<uint32_t*>(scales + fp4_scale_at(r, u / STEP, units / (4 * STEP))) = word;
+    return make_uint2(fp4_pack8(v[0]), fp4_pack8(v[1]));
 }
 
-template <int FORMAT>
+template <int FORMAT, int U>
+__global__ void __launch_bounds__(FQ_THREADS)
+fp4_quantize_kernel(const __nv_bfloat16* __restrict__ X, int64_t R, int64_t C, int64_t ldx, int64_t rows_padded,
+                    const FqDiv div, int wide, const float* __restrict__ tensor_scale, uint8_t* __restrict__ codes,
+                    uint8_t* __restrict__ scales) {
+    const int64_t Cp = fp4_padded_cols(C);
+    const float g = FORMAT == SB_FP4_NV && tensor_scale ? __ldg(tensor_scale) : 1.f, rg = __frcp_rn(g);
+    const int64_t first = (int64_t)blockIdx.x * (FQ_THREADS * U) + threadIdx.x;
+    uint32_t w[U][8];
+    int64_t row[U];
+    int piece[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        row[u] = div.row(first + u * FQ_THREADS, piece[u]);
+        fq_load(X + row[u] * ldx + piece[u] * 16, row[u] < R ? C - (int64_t)piece[u] * 16 : 0, wide, w[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        uint32_t scale;
+        const uint2 q = fq_codes<FORMAT>(w[u], g, rg, scale);
+        const int64_t r = row[u];
+        const int64_t c0 = (int64_t)piece[u] * 16;
+        const bool there = r < R && c0 < Cp;
+        if (there) *reinterpret_cast<uint2*>(codes + r * (Cp >> 1) + (c0 >> 1)) = q;
+        else scale = 0;                                        // padding rows and blocks
+        constexpr int STEP = FORMAT == SB_FP4_MX ? 2 : 1;      // lanes per block
+        uint32_t word = scale;
+        word |= __shfl_down_sync(0xffffffffu, scale, STEP) << 8;
+        word |= __shfl_down_sync(0xffffffffu, word, 2 * STEP) << 16;
+        if (r < rows_padded && (piece[u] & (4 * STEP - 1)) == 0)
+            *reinterpret_cast<uint32_t*>(scales + fp4_scale_at(r, piece[u] / STEP, div.n / (4 * STEP))) = word;
+    }
+}
+
+template <int FORMAT, int U>
 __global__ void __launch_bounds__(FQ_THREADS)
 fp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t R, int64_t C,
-                      int units, int64_t tiles, const float* __restrict__ tensor_scale, __nv_bfloat16* __restrict__ Y,
+                      const FqDiv div, int64_t tiles, const float* __restrict__ tensor_scale, __nv_bfloat16* __restrict__ Y,
                       int64_t ldy, int wide) {
-    const int64_t first = (int64_t)blockIdx.x * FQ_THREADS;
-    const int64_t row0 = first / units;
-    const unsigned off = (unsigned)(first - row0 * units) + threadIdx.x;
-    const int64_t r = row0 + off / (unsigned)units;
-    const int u = (int)(off % (unsigned)units);
-    if (r >= R) return;
-    const int64_t c0 = (int64_t)u * 16;
-    const uint2 q = *reinterpret_cast<const uint2*>(codes + r * (fp4_padded_cols(C) >> 1) + (c0 >> 1));
-    const uint32_t s = scales[fp4_scale_at(r, FORMAT == SB_FP4_MX ? u >> 1 : u, tiles)];
-    float d;
-    if (FORMAT == SB_FP4_MX) d = e8m0_value(s);
-    else d = e4m3_value(s) * (tensor_scale ? __ldg(tensor_scale) : 1.f);
-    uint32_t h[8];
-    fp4_unpack8(q.x, *reinterpret_cast<uint32_t (*)[4]>(&h[0]));
-    fp4_unpack8(q.y, *reinterpret_cast<uint32_t (*)[4]>(&h[4]));
-    uint32_t o[8];
+    const float g = FORMAT == SB_FP4_NV && tensor_scale ? __ldg(tensor_scale) : 1.f;
+    const int64_t first = (int64_t)blockIdx.x * (FQ_THREADS * U) + threadIdx.x;
+    uint2 q[U];
+    uint32_t s[U];
+    int64_t row[U];
+    int piece[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        o[i] = u32(__floats2bfloat162_rn(f.x * d, f.y * d));
+    for (int u = 0; u < U; ++u) {
+        row[u] = div.row(first + u * FQ_THREADS, piece[u]);
+        if (row[u] < R) {
+            q[u] = ld_stream8(codes + row[u] * (fp4_padded_cols(C) >> 1) + piece[u] * 8);
+            s[u] = scales[fp4_scale_at(row[u], FORMAT == SB_FP4_MX ? piece[u] >> 1 : piece[u], tiles)];
+        }
     }
-    __nv_bfloat16* y = Y + r * ldy + c0;
-    if (wide && c0 + 16 <= C) {
-        reinterpret_cast<uint4*>(y)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-        reinterpret_cast<uint4*>(y)[1] = make_uint4(o[4], o[5], o[6], o[7]);
-    } else {
-        uint16_t* p = reinterpret_cast<uint16_t*>(y);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (c0 + i < C) p[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+    for (int u = 0; u < U; ++u) {
+        if (row[u] >= R) break;
+        const float d = FORMAT == SB_FP4_MX ? e8m0_value(s[u]) : e4m3_value(s[u]) * g;
+        uint32_t h[2][4], o[8];
+        fp4_unpack8(q[u].x, h[0]);
+        fp4_unpack8(q[u].y, h[1]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i >> 2][i & 3]));
+            o[i] = u32(__floats2bfloat162_rn(f.x * d, f.y * d));
+        }
+        const int64_t c0 = (int64_t)piece[u] * 16;
+        __nv_bfloat16* y = Y + row[u] * ldy + c0;
+        if (wide && c0 + 16 <= C) st_global32(y, o);
+        else {
+            uint16_t* p = reinterpret_cast<uint16_t*>(y);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (c0 + i < C) p[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+        }
     }
 }
 
 bool format_ok(int format) { return format == SB_FP4_MX || format == SB_FP4_NV; }
+// four pieces a thread when that still makes four blocks per SM
+bool fq_many(const sb_ctx* ctx, int64_t total) { return total >= (int64_t)FQ_THREADS * FQ_MANY * 4 * ctx->sm_count; }
+unsigned fq_blocks(int64_t total, bool many) {
+    const int64_t per = FQ_THREADS * (many ? FQ_MANY : 1);
+    return (unsigned)((total + per - 1) / per);
+}
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace
@@ -161,15 +201,17 @@ extern "C" sb_status sb_fp4_quantize(sb_ctx* ctx, const void* X, int64_t R, int6
         return sb_fail(ctx, SB_ERR_SHAPE, "fp4 quantize: ldx %% 8 == 0, ldx >= C and 16-byte aligned pointers");
     if (R >= (1ll << 31) - 128 || C >= (1ll << 30)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 quantize: R and C must fit 31 bits");
     const int64_t rows = (R + 127) / 128 * 128;
-    const int units = (int)(fp4_scale_tiles(C, format) * 4 * fp4_block(format) / 16);
-    const int64_t blocks = (rows * units + FQ_THREADS - 1) / FQ_THREADS;
-    if (blocks >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 quantize: too many elements");
+    const FqDiv div((int)(fp4_scale_tiles(C, format) * 4 * fp4_block(format) / 16));
+    const int64_t total = rows * div.n;
+    if (total >= (1ll << 37)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 quantize: too many elements");
     SB_CUDA(ctx, cudaSetDevice(ctx->device));
     auto* x = static_cast<const __nv_bfloat16*>(X);
-    if (format == SB_FP4_MX)
-        fp4_quantize_kernel<SB_FP4_MX><<<(unsigned)blocks, FQ_THREADS, 0, ctx->stream>>>(x, R, C, ldx, rows, units, nullptr, codes, scales);
-    else
-        fp4_quantize_kernel<SB_FP4_NV><<<(unsigned)blocks, FQ_THREADS, 0, ctx->stream>>>(x, R, C, ldx, rows, units, tensor_scale, codes, scales);
+    const int wide = ldx % 16 == 0 && (reinterpret_cast<uintptr_t>(X) & 31) == 0;
+    const bool many = fq_many(ctx, total);
+    const unsigned blocks = fq_blocks(total, many);
+    auto launch = [&](auto kernel) { kernel<<<blocks, FQ_THREADS, 0, ctx->stream>>>(x, R, C, ldx, rows, div, wide, tensor_scale, codes, scales); };
+    if (format == SB_FP4_MX) many ? launch(fp4_quantize_kernel<SB_FP4_MX, FQ_MANY>) : launch(fp4_quantize_kernel<SB_FP4_MX, 1>);
+    else many ? launch(fp4_quantize_kernel<SB_FP4_NV, FQ_MANY>) : launch(fp4_quantize_kernel<SB_FP4_NV, 1>);
     SB_LAUNCHED(ctx);
     return SB_OK;
 }
@@ -184,17 +226,17 @@ extern "C" sb_status sb_fp4_dequantize(sb_ctx* ctx, const uint8_t* codes, const 
     if (ldy < C || !aligned16(codes) || !aligned16(scales) || (reinterpret_cast<uintptr_t>(Y) & 1))
         return sb_fail(ctx, SB_ERR_SHAPE, "fp4 dequantize: ldy >= C and 16-byte aligned codes and scales");
     if (R >= (1ll << 31) - 128 || C >= (1ll << 30)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 dequantize: R and C must fit 31 bits");
-    const int units = (int)((C + 15) / 16);
-    const int64_t blocks = (R * units + FQ_THREADS - 1) / FQ_THREADS;
-    if (blocks >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 dequantize: too many elements");
+    const FqDiv div((int)((C + 15) / 16));
+    const int64_t total = R * div.n, tiles = fp4_scale_tiles(C, format);
+    if (total >= (1ll << 37)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 dequantize: too many elements");
     SB_CUDA(ctx, cudaSetDevice(ctx->device));
     auto* y = static_cast<__nv_bfloat16*>(Y);
-    const int wide = ldy % 8 == 0 && aligned16(Y);
-    const int64_t tiles = fp4_scale_tiles(C, format);
-    if (format == SB_FP4_MX)
-        fp4_dequantize_kernel<SB_FP4_MX><<<(unsigned)blocks, FQ_THREADS, 0, ctx->stream>>>(codes, scales, R, C, units, tiles, nullptr, y, ldy, wide);
-    else
-        fp4_dequantize_kernel<SB_FP4_NV><<<(unsigned)blocks, FQ_THREADS, 0, ctx->stream>>>(codes, scales, R, C, units, tiles, tensor_scale, y, ldy, wide);
+    const int wide = ldy % 16 == 0 && (reinterpret_cast<uintptr_t>(Y) & 31) == 0;
+    const bool many = fq_many(ctx, total);
+    const unsigned blocks = fq_blocks(total, many);
+    auto launch = [&](auto kernel) { kernel<<<blocks, FQ_THREADS, 0, ctx->stream>>>(codes, scales, R, C, div, tiles, tensor_scale, y, ldy, wide); };
+    if (format == SB_FP4_MX) many ? launch(fp4_dequantize_kernel<SB_FP4_MX, FQ_MANY>) : launch(fp4_dequantize_kernel<SB_FP4_MX, 1>);
+    else many ? launch(fp4_dequantize_kernel<SB_FP4_NV, FQ_MANY>) : launch(fp4_dequantize_kernel<SB_FP4_NV, 1>);
     SB_LAUNCHED(ctx);
     return SB_OK;
 }

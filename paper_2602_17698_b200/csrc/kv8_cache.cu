@@ -24,30 +24,28 @@ __device__ __forceinline__ uint32_t bf16_up(float x) {
     return (u + 0xffffu) >> 16;
 }
 
-// eight fp32 values to eight codes
+// eight fp32 values within the type's range to eight codes
 template <int TYPE>
 __device__ __forceinline__ uint2 to_codes(const float (&v)[8]) {
-    uint2 r;
+    uint32_t w[2];
     if (TYPE == SB_KV_INT8) {
-        uint32_t w[2];
+        // 1.5 * 2^23 rounds to a whole number (nearest, ties to even) and leaves it in the low byte
+        uint32_t b[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            w[h] = 0;
+        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(v[i] + 12582912.f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int q = max(-127, min(127, __float2int_rn(v[4 * h + i])));
-                w[h] |= (uint32_t)(q & 0xff) << (8 * i);
-            }
-        }
-        r = make_uint2(w[0], w[1]);
+        for (int h = 0; h < 2; ++h)
+            w[h] = __byte_perm(__byte_perm(b[4 * h], b[4 * h + 1], 0x0040), __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040), 0x5410);
     } else {
-        uint16_t p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(p[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-        r = make_uint2(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16);
+        for (int h = 0; h < 2; ++h)
+            asm("{\n\t.reg .b16 a, b;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
+                "mov.b32 %0, {a, b};\n\t}"
+                : "=r"(w[h]) : "f"(v[4 * h]), "f"(v[4 * h + 1]), "f"(v[4 * h + 2]), "f"(v[4 * h + 3]));
     }
-    return r;
+    return make_uint2(w[0], w[1]);
 }
 template <int TYPE>
 __device__ __forceinline__ void from_codes(uint2 c, float (&v)[8]) {
@@ -92,8 +90,7 @@ kv8_append_kernel(const Kv8Geom g, const KvSide ks, const KvSide vs, SbDeviceSta
     const int per_tok = g.dim >> 3;                                      // pieces of 8 elements per token
     const int old_toks = max(0, min(SB_KV8_BLOCK, rq.past - tok0)), toks = min(SB_KV8_BLOCK, rq.len - tok0);
     uint4 x[NC];
-    uint32_t amax = 0;
-    bool bad = false;
+    uint32_t m2 = 0;                                                     // largest magnitudes, as bf16 bits
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         const int piece = lane + 32 * i, tok = piece / per_tok;
@@ -103,25 +100,34 @@ kv8_append_kernel(const Kv8Geom g, const KvSide ks, const KvSide vs, SbDeviceSta
             x[i] = ld_stream16(sd.x + row * sd.token_stride + head * sd.head_stride + 8 * (piece - tok * per_tok));
         }
     }
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t a = (w[k >> 1] >> (16 * (k & 1))) & 0x7fffu;
-            if (a >= 0x7f80u) bad = true;
-            else amax = max(amax, a);
-        }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    constexpr float QMAX = TYPE == SB_KV_INT8 ? 127.f : 448.f;
-    uint32_t sbits = bf16_up(__fdiv_rn(__uint_as_float(amax << 16), QMAX));
     const uint32_t before = old_toks ? *scale_at : 0u;                   // non-negative: the bits are ordered as the numbers
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+        m2 = __vmaxu2(m2, __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu)));
+    uint32_t amax = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
+    constexpr float QMAX = TYPE == SB_KV_INT8 ? 127.f : 448.f;
+    const bool bad = amax >= 0x7f80u;
+    if (bad) {
+        // a NaN or an infinity: the scale is the finite elements'
+        amax = 0;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t e = (w[k >> 1] >> (16 * (k & 1))) & 0x7fffu;
+                if (e < 0x7f80u) amax = max(amax, e);
+            }
+        }
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        if (lane == 0) sb_latch(st, SB_ERR_NONFINITE, SBK_KV8);
+    }
+    uint32_t sbits = bf16_up(__fdiv_rn(__uint_as_float(amax << 16), QMAX));
     const bool grew = sbits > before;
     if (!grew) sbits = before;
     const float s = __uint_as_float(sbits << 16), s_old = __uint_as_float(before << 16);
-    if (bad) sb_latch(st, SB_ERR_NONFINITE, SBK_KV8);
+    const bool quick = div_in_range(s) && !bad;
+    const float rs = quick ? __frcp_rn(s) : 0.f;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         const int piece = lane + 32 * i, tok = piece / per_tok;
@@ -134,10 +140,15 @@ kv8_append_kernel(const Kv8Geom g, const KvSide ks, const KvSide vs, SbDeviceSta
             for (int k = 0; k < 8; ++k) v[k] = __fdiv_rn(v[k] * s_old, s);
         } else {
             const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            if (quick) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float e = (k & 1) ? bf16hi(w[k >> 1]) : bf16lo(w[k >> 1]);
-                v[k] = e != e ? 0.f : fabsf(e) > 3.4e38f ? copysignf(QMAX, e) : s > 0.f ? __fdiv_rn(e, s) : 0.f;
+                for (int k = 0; k < 8; ++k) v[k] = div_rn((k & 1) ? bf16hi(w[k >> 1]) : bf16lo(w[k >> 1]), s, rs);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float e = (k & 1) ? bf16hi(w[k >> 1]) : bf16lo(w[k >> 1]);
+                    v[k] = e != e ? 0.f : fabsf(e) > 3.4e38f ? copysignf(QMAX, e) : s > 0.f ? __fdiv_rn(e, s) : 0.f;
+                }
             }
         }
         *at = to_codes<TYPE>(v);
