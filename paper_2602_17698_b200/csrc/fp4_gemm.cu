@@ -44,12 +44,12 @@ struct FgShape {
     static constexpr int ATOMS = FORMAT == SB_FP4_MX ? 2 : 4;        // scale tiles of a slab
     static constexpr int W_BYTES = FG_ROWS * 128, X_BYTES = NT * 128, S_BYTES = ATOMS * 512;
     static constexpr int STAGE = W_BYTES + X_BYTES + 2 * S_BYTES;
-    static constexpr int STAGES = 4;
+    static constexpr int STAGES = NT <= 32 ? 4 : 3;                  // two CTAs per SM
     static constexpr int SMEM = STAGES * STAGE + 1024 + 256;
     static constexpr int SF_COLS = 2 * 4 * ATOMS;                    // scale columns of a stage
     static constexpr int D_COLS = NT < 32 ? 32 : NT;
     static constexpr int TMEM = D_COLS + STAGES * SF_COLS <= 128 ? 128 : 256;
-    static_assert(D_COLS + STAGES * SF_COLS <= 256, "tensor memory of two CTAs of an SM");
+    static_assert(D_COLS + STAGES * SF_COLS <= 256 && SMEM + 1024 <= 227 * 512, "two CTAs of an SM");
     static_assert(FG_ROWS * NT * 4 <= STAGES * STAGE, "partial sums fit where the ring was");
 };
 
@@ -83,13 +83,13 @@ __device__ __forceinline__ void fg_copy_scales(bool one, unsigned taddr, unsigne
         asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
                      ::"r"(taddr), "l"(t5_desc_rows16(smem)), "r"((unsigned)one) : "memory");
 }
-// the barrier (PAIR: of both CTAs) is arrived on when everything issued so far is done
+// the barrier (PAIR: of the CTAs in the mask) is arrived on when everything issued so far is done
 template <bool PAIR>
-__device__ __forceinline__ void fg_commit(bool one, unsigned bar) {
+__device__ __forceinline__ void fg_commit(bool one, unsigned bar, unsigned ctas = 0) {
     if (PAIR)
         asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
                      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
-                     ::"r"(bar), "h"((unsigned short)3), "r"((unsigned)one) : "memory");
+                     ::"r"(bar), "h"((unsigned short)ctas), "r"((unsigned)one) : "memory");
     else
         asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
                      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
@@ -99,21 +99,22 @@ template <typename OUT>
 __device__ __forceinline__ void fg_put(OUT* p, float v);
 template <> __device__ __forceinline__ void fg_put(float* p, float v) { *p = v; }
 template <> __device__ __forceinline__ void fg_put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-// 32 columns (tokens) of one weight row: p, then every ldy; n of them exist
-template <typename OUT>
-__device__ __forceinline__ void fg_store32(OUT* p, int64_t ldy, const unsigned (&r)[32], float alpha, int n) {
-    if (n >= 32) {
+// COLS columns (tokens) of one weight row: p, then every ldy; n of them exist
+template <typename OUT, int COLS>
+__device__ __forceinline__ void fg_store_row(OUT* p, int64_t ldy, const unsigned (&r)[COLS], float alpha, int n) {
+    if (n >= COLS) {
 #pragma unroll
-        for (int k = 0; k < 32; ++k, p += ldy) fg_put(p, alpha * __uint_as_float(r[k]));
+        for (int k = 0; k < COLS; ++k, p += ldy) fg_put(p, alpha * __uint_as_float(r[k]));
     } else {
 #pragma unroll
-        for (int k = 0; k < 32; ++k, p += ldy)
+        for (int k = 0; k < COLS; ++k, p += ldy)
             if (k < n) fg_put(p, alpha * __uint_as_float(r[k]));
     }
 }
-__device__ __forceinline__ void fg_store_columns(const FgArgs& a, int64_t m, int64_t n, const unsigned (&r)[32], float alpha, int count) {
-    if (a.out_f32) fg_store32(static_cast<float*>(a.Y) + m * a.ldy + n, a.ldy, r, alpha, count);
-    else fg_store32(static_cast<__nv_bfloat16*>(a.Y) + m * a.ldy + n, a.ldy, r, alpha, count);
+template <int COLS>
+__device__ __forceinline__ void fg_store_columns(const FgArgs& a, int64_t m, int64_t n, const unsigned (&r)[COLS], float alpha, int count) {
+    if (a.out_f32) fg_store_row(static_cast<float*>(a.Y) + m * a.ldy + n, a.ldy, r, alpha, count);
+    else fg_store_row(static_cast<__nv_bfloat16*>(a.Y) + m * a.ldy + n, a.ldy, r, alpha, count);
 }
 __device__ __forceinline__ float fg_alpha(const FgArgs& a) {
     return (a.w_tensor ? __ldg(a.w_tensor) : 1.f) * (a.x_tensor ? __ldg(a.x_tensor) : 1.f);
@@ -271,8 +272,9 @@ struct FpShape {
     static constexpr int STAGES = 5;
     static constexpr int SMEM = STAGES * STAGE + 1024 + 256;
     static constexpr int TMEM = 512;
-    static constexpr int ACC = 192;                                  // second accumulator's first column
-    static constexpr int SF = 448;                                   // two areas of scales, 24 columns each
+    static constexpr int ACC = 160;                                  // second accumulator's first column
+    static constexpr int BOTH = TOKENS - ACC;                        // columns that both accumulators use
+    static constexpr int SF = ACC + TOKENS;                          // scales: of two slabs, 24 columns each half of a slab
     static constexpr int EPI_WARPS = 8;
     static constexpr int THREADS = (2 + EPI_WARPS) * 32;
 };
@@ -284,7 +286,9 @@ __device__ __forceinline__ void fp_load(unsigned dst, const CUtensorMap* map, in
         ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
 
-template <int FORMAT>
+// SPLIT: a tile per cluster, its columns cut into segments, one per pair of the cluster's CTAs, added in
+// segment order through distributed shared memory.
+template <int FORMAT, bool SPLIT>
 __global__ void __launch_bounds__(FpShape<FORMAT>::THREADS, 1)
 fp4_pair_kernel(const __grid_constant__ FgMaps maps, const FgArgs a) {
     using S = FpShape<FORMAT>;
@@ -297,8 +301,11 @@ fp4_pair_kernel(const __grid_constant__ FgMaps maps, const FgArgs a) {
     unsigned* tmem_slot = reinterpret_cast<unsigned*>(acc_free + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const unsigned rank = t5_cta_rank();                             // 0: leader
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const unsigned crank = t5_cta_rank(), rank = crank & 1, leader = crank & ~1u;       // rank 0 of a pair leads it
+    const unsigned both = 3u << leader;
+    const int segs = SPLIT ? (int)t5_cluster_size() / 2 : 1, seg = SPLIT ? (int)(crank >> 1) : 0;
+    const int pair = (int)(blockIdx.x >> 1) / segs, pairs = (int)(gridDim.x >> 1) / segs;
+    const int s0 = SPLIT ? (int)((int64_t)a.slabs * seg / segs) : 0, s1 = SPLIT ? (int)((int64_t)a.slabs * (seg + 1) / segs) : a.slabs;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) {
@@ -327,11 +334,11 @@ fp4_pair_kernel(const __grid_constant__ FgMaps maps, const FgArgs a) {
         for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
             const int rt = tile % a.row_tiles, tt = tile / a.row_tiles;
             const int n0 = rt * 256 + (int)rank * 128, m0 = tt * S::TOKENS + (int)rank * 128;
-            for (int slab = 0; slab < a.slabs; ++slab, ++i) {
+            for (int slab = s0; slab < s1; ++slab, ++i) {
                 const int s = i % S::STAGES;
                 ok = __all_sync(0xffffffffu, t5_bar_wait(t5_smem(empty + s), ((unsigned)(i / S::STAGES) & 1u) ^ 1u, abort_flag));
                 if (!ok) break;
-                const unsigned at = t5_smem(smem + s * S::STAGE), bar = t5_cluster_addr(t5_smem(full + s), 0);
+                const unsigned at = t5_smem(smem + s * S::STAGE), bar = t5_cluster_addr(t5_smem(full + s), leader);
                 if (one) {
                     if (rank == 0) t5_bar_expect(t5_smem(full + s), 2u * S::STAGE);
                     fp_load(at, &maps.w, slab * 128, n0, bar);
@@ -358,18 +365,21 @@ fp4_pair_kernel(const __grid_constant__ FgMaps maps, const FgArgs a) {
                 if (!ok) break;
                 t5_fence_after();
                 const unsigned acc = tmem + (unsigned)((n & 1) * S::ACC);
-                for (int slab = 0; slab < a.slabs; ++slab, ++i) {
+                for (int slab = s0; slab < s1; ++slab, ++i) {
                     const int s = i % S::STAGES;
-                    ok = __all_sync(0xffffffffu, t5_bar_wait(t5_smem(full + s), (unsigned)(i / S::STAGES) & 1u, abort_flag));
+                    // the scales of two slabs ago are done with (products are not ordered before later copies);
+                    // then this slab's copies, which the products are waiting for
+                    ok = i < 2 || t5_bar_wait(t5_smem(empty + (i - 2) % S::STAGES), (unsigned)((i - 2) / S::STAGES) & 1u, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok && t5_bar_wait(t5_smem(full + s), (unsigned)(i / S::STAGES) & 1u, abort_flag));
                     if (!ok) break;
                     t5_fence_after();
                     const unsigned at = t5_smem(smem + s * S::STAGE);
                     const unsigned sw = at + 2 * S::HALF, sx = sw + S::S_BYTES;
                     const int steps = min(4, a.k64 - 4 * slab);
-                    // half a slab's scales at a time (MX: the whole slab's), into the two areas in turn
+                    // two scale tiles at a time (MX: the whole slab's)
 #pragma unroll
                     for (int h = 0; h < S::ATOMS / 2; ++h) {
-                        const unsigned area = tmem + S::SF + 24u * (unsigned)(FORMAT == SB_FP4_MX ? i & 1 : h);
+                        const unsigned area = tmem + S::SF + 48u * (unsigned)(i & 1) + 24u * (unsigned)h;
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             fg_copy_scales<true>(one, area + 4 * c, sw + 512 * (2 * h + c));
@@ -382,19 +392,19 @@ fp4_pair_kernel(const __grid_constant__ FgMaps maps, const FgArgs a) {
                             const int c = FORMAT == SB_FP4_MX ? k >> 1 : k & 1;
                             fg_mma<FORMAT, true>(one && k < steps, acc, t5_desc_sw128(at + 32 * k), t5_desc_sw128(at + S::HALF + 32 * k),
                                                  fg_idesc<FORMAT>(256, S::TOKENS, FORMAT == SB_FP4_MX ? k & 1 : 0), area + 4 * c,
-                                                 area + 8 + 8 * c, slab > 0 || k > 0);
+                                                 area + 8 + 8 * c, slab > s0 || k > 0);
                         }
                     }
-                    fg_commit<true>(one, t5_smem(empty + s));
+                    fg_commit<true>(one, t5_smem(empty + s), both);
                 }
-                fg_commit<true>(one, t5_smem(acc_full + (n & 1)));
+                fg_commit<true>(one, t5_smem(acc_full + (n & 1)), both);
             }
         }
     } else {
-        // warp: a quarter of the lanes, half of the columns; first a part of the columns that the
+        // warp: a quarter of the lanes, half of the columns; first its part of the columns that the
         // next tile's accumulator needs, then the rest
         const int q = warp & 3, half = (warp - 2) >> 2;
-        const unsigned free_leader = t5_cluster_addr(t5_smem(acc_free), 0);
+        const unsigned free_leader = t5_cluster_addr(t5_smem(acc_free), leader);
         const float alpha = fg_alpha(a);
         int n = 0;
         for (int tile = pair; tile < a.tiles; tile += pairs, ++n) {
@@ -405,21 +415,57 @@ fp4_pair_kernel(const __grid_constant__ FgMaps maps, const FgArgs a) {
             const int64_t m0 = (int64_t)tt * S::TOKENS, row = (int64_t)rt * 256 + rank * 128 + q * 32 + lane;
             const int ntok = (int)min((int64_t)S::TOKENS, a.M - m0);
             const unsigned src = tmem + ((unsigned)(q * 32) << 16) + (unsigned)(b * S::ACC);
+            // columns in pieces of 16: BOTH / 32 of the shared ones (the end of the first accumulator, the
+            // start of the second), then ACC / 32 of the others
 #pragma unroll 1
-            for (int u = 0; u < 4; ++u) {
-                // shared columns: 192 .. 255 of the first accumulator, 0 .. 63 of the second
-                const int c = (b ? (u == 0 ? 0 : 2 * u) : (u == 0 ? 6 : 2 * (u - 1))) * 32 + half * 32;
-                unsigned r[32];
-                t5_ld32(src + (unsigned)c, r);
+            for (int u = 0; u < S::TOKENS / 32; ++u) {
+                const bool shared_part = u < S::BOTH / 32;
+                const int c = shared_part ? (b ? 0 : S::ACC) + (half * (S::BOTH / 32) + u) * 16
+                                          : (b ? S::BOTH : 0) + (half * (S::ACC / 32) + u - S::BOTH / 32) * 16;
+                unsigned r[16];
+                t5_ld16(src + (unsigned)c, r);
                 t5_wait_ld();
-                if (u == 0) {
+                if (u == S::BOTH / 32 - 1) {
                     t5_fence_before();
                     __syncwarp();
                     if (lane == 0)
                         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(free_leader) : "memory");
                 }
-                if (row < a.N) fg_store_columns(a, m0 + c, row, r, alpha, ntok - c);
+                if (SPLIT) {
+                    float* part = reinterpret_cast<float*>(smem) + c * 128 + q * 32 + lane;    // [token][128], the ring is done with
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) part[k * 128] = __uint_as_float(r[k]);
+                } else if (row < a.N) fg_store_columns(a, m0 + c, row, r, alpha, ntok - c);
                 __syncwarp();
+            }
+        }
+    }
+    if (SPLIT) {
+        // every CTA adds the segments of its rows over its share of the tokens
+        __syncwarp();
+        t5_fence_before();
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        const int rt = pair % a.row_tiles, tt = pair / a.row_tiles;
+        const float* part = reinterpret_cast<const float*>(smem);
+        const float* from[FG_MAX_SPLIT / 2];
+#pragma unroll
+        for (int g = 0; g < FG_MAX_SPLIT / 2; ++g) from[g] = cluster.map_shared_rank(part, 2 * (g < segs ? g : 0) + (int)rank);
+        const float alpha = fg_alpha(a);
+        const int64_t m0 = (int64_t)tt * S::TOKENS, n0 = (int64_t)rt * 256 + rank * 128;
+        const int ntok = (int)min((int64_t)S::TOKENS, a.M - m0);
+        const int t0 = ntok * seg / segs, t1 = ntok * (seg + 1) / segs;
+        const bool fine = *abort_flag == 0;
+#pragma unroll 4
+        for (int idx = t0 * 128 + (int)threadIdx.x; idx < t1 * 128; idx += S::THREADS) {
+            float sum = from[0][idx];
+#pragma unroll
+            for (int g = 1; g < FG_MAX_SPLIT / 2; ++g)
+                if (g < segs) sum += from[g][idx];
+            const int64_t n = n0 + (idx & 127), m = m0 + idx / 128;
+            if (fine && n < a.N) {
+                if (a.out_f32) fg_put(static_cast<float*>(a.Y) + m * a.ldy + n, alpha * sum);
+                else fg_put(static_cast<__nv_bfloat16*>(a.Y) + m * a.ldy + n, alpha * sum);
             }
         }
     }
@@ -480,27 +526,19 @@ sb_status fg_tile_launch(sb_ctx* ctx, const FgArgs& a, const FgOperand& w, const
     return SB_OK;
 }
 
-template <int FORMAT>
-sb_status fg_pair_launch(sb_ctx* ctx, FgArgs a, const FgOperand& w, const FgOperand& x, int64_t K) {
+template <int FORMAT, bool SPLIT>
+sb_status fg_pair_launch(sb_ctx* ctx, const FgMaps& maps, const FgArgs& a, int64_t pairs, int segs) {
     using S = FpShape<FORMAT>;
-    FgMaps maps;
-    const sb_status st = fg_maps(ctx, &maps, a, w, x, K, FORMAT, 128, 2);
-    if (st != SB_OK) return st;
-    auto* kernel = fp4_pair_kernel<FORMAT>;
+    auto* kernel = fp4_pair_kernel<FORMAT, SPLIT>;
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    const int64_t row_tiles = (a.N + 255) / 256, tiles = row_tiles * ((a.M + S::TOKENS - 1) / S::TOKENS);
-    if (tiles >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 gemm: too many tiles");
-    a.row_tiles = (int)row_tiles;
-    a.tiles = (int)tiles;
-    const int64_t pairs = tiles < ctx->sm_count / 2 ? tiles : ctx->sm_count / 2;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(2 * pairs));
+    cfg.gridDim = dim3((unsigned)(2 * pairs * segs));
     cfg.blockDim = dim3(S::THREADS);
     cfg.dynamicSmemBytes = S::SMEM;
     cfg.stream = ctx->stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.x = (unsigned)(2 * segs);
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
@@ -509,13 +547,30 @@ sb_status fg_pair_launch(sb_ctx* ctx, FgArgs a, const FgOperand& w, const FgOper
     SB_LAUNCHED(ctx);
     return SB_OK;
 }
+template <int FORMAT>
+sb_status fg_pairs(sb_ctx* ctx, FgArgs a, const FgOperand& w, const FgOperand& x, int64_t K) {
+    using S = FpShape<FORMAT>;
+    FgMaps maps;
+    const sb_status st = fg_maps(ctx, &maps, a, w, x, K, FORMAT, 128, 2);
+    if (st != SB_OK) return st;
+    const int64_t row_tiles = (a.N + 255) / 256, tiles = row_tiles * ((a.M + S::TOKENS - 1) / S::TOKENS);
+    if (tiles >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 gemm: too many tiles");
+    a.row_tiles = (int)row_tiles;
+    a.tiles = (int)tiles;
+    // with fewer tiles than half the pairs of SMs the columns are cut too, at least eight slabs a segment
+    const int64_t slots = ctx->sm_count / 2;
+    int segs = 1;
+    while (segs < FG_MAX_SPLIT / 2 && tiles * segs * 2 <= slots && a.slabs >= 16 * segs) segs *= 2;
+    if (segs > 1) return fg_pair_launch<FORMAT, true>(ctx, maps, a, tiles, segs);
+    return fg_pair_launch<FORMAT, false>(ctx, maps, a, tiles < slots ? tiles : slots, 1);
+}
 
 template <int FORMAT>
 sb_status fg_launch(sb_ctx* ctx, const FgArgs& a, const FgOperand& w, const FgOperand& x, int64_t K) {
     return a.M <= 16 ? fg_tile_launch<FORMAT, 16>(ctx, a, w, x, K)
          : a.M <= 32 ? fg_tile_launch<FORMAT, 32>(ctx, a, w, x, K)
          : a.M <= 64 ? fg_tile_launch<FORMAT, 64>(ctx, a, w, x, K)
-         : a.M <= FG_PAIR_FROM ? fg_tile_launch<FORMAT, 128>(ctx, a, w, x, K) : fg_pair_launch<FORMAT>(ctx, a, w, x, K);
+         : a.M <= FG_PAIR_FROM ? fg_tile_launch<FORMAT, 128>(ctx, a, w, x, K) : fg_pairs<FORMAT>(ctx, a, w, x, K);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
