@@ -152,6 +152,15 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, cuda=True):
     return C.c_void_p(t.data_ptr())
 
 
+def _dev(t: Optional[torch.Tensor]):
+    """Address of a CUDA tensor (None: NULL); the calls of a decode step are as long as this binding."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor (the library has no CPU path)")
+    return t.data_ptr()
+
+
 def _bits(bits: Sequence[int]):
     return (C.c_int * len(bits))(*[int(b) for b in bits]), len(bits)
 
@@ -183,11 +192,11 @@ class Fp4Matrix:
             raise ValueError(f"unknown 4-bit format {fmt!r}")
         pitch = (cols + 31) // 32 * 16
         tiles = (rows + 127) // 128 * ((pitch * 2 // (32 if fmt == "mx" else 16) + 3) // 4)
-        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_contiguous() or not scales.is_contiguous():
+        if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or not codes.is_contiguous() or not scales.is_contiguous():
             raise TypeError("codes and scales are contiguous uint8 tensors")
         if codes.numel() != rows * pitch or scales.numel() != tiles * 512:
             raise ValueError("codes or scales have another size than the format's")
-        if tensor_scale is not None and (tensor_scale.dtype != torch.float32 or tensor_scale.numel() != 1):
+        if tensor_scale is not None and (tensor_scale.dtype is not torch.float32 or tensor_scale.numel() != 1):
             raise TypeError("tensor_scale is one fp32 element")
         self.codes, self.scales, self.rows, self.cols, self.fmt, self.tensor_scale = codes, scales, rows, cols, fmt, tensor_scale
 
@@ -197,27 +206,32 @@ class Fp4Matrix:
                    torch.empty(fp4_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device=device), rows, cols, fmt, tensor_scale)
 
 
+_KV8_TYPES = {torch.int8: SB_KV_INT8, torch.float8_e4m3fn: SB_KV_E4M3}
+
+
 class Kv8Cache:
     """A paged key/value cache in 8 bits: k, v int8 or float8_e4m3fn [pages][heads][page tokens][dim],
     k_scale, v_scale bf16 [pages][heads][page tokens / 16], table int32 [requests][pages of a request]."""
     __slots__ = ("k", "v", "k_scale", "v_scale", "table", "struct")
 
     def __init__(self, k, v, k_scale, v_scale, table):
-        pages, heads, page_tokens, dim = k.shape
-        if k.dtype not in (torch.int8, torch.float8_e4m3fn) or v.dtype != k.dtype:
+        shape = k.shape
+        pages, heads, page_tokens, dim = shape
+        kind = _KV8_TYPES.get(k.dtype)
+        if kind is None or v.dtype is not k.dtype:
             raise TypeError("keys and values are int8 or float8_e4m3fn")
-        if k_scale.dtype != torch.bfloat16 or v_scale.dtype != torch.bfloat16 or table.dtype != torch.int32:
+        if k_scale.dtype is not torch.bfloat16 or v_scale.dtype is not torch.bfloat16 or table.dtype is not torch.int32:
             raise TypeError("scales are bf16 and page numbers int32")
-        if v.shape != k.shape or k_scale.numel() * SB_KV8_BLOCK != pages * heads * page_tokens or v_scale.numel() != k_scale.numel() or table.dim() != 2:
-            raise ValueError("keys, values, scales and table do not fit one another")
-        if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()) or table.stride(1) != 1:
+        n = k_scale.numel()
+        if v.shape != shape or n * SB_KV8_BLOCK != pages * heads * page_tokens or v_scale.numel() != n:
+            raise ValueError("keys, values and scales do not fit one another")
+        requests, per = table.shape
+        stride, one = table.stride()
+        if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()) or one != 1:
             raise ValueError("the cache's tensors are contiguous")
-        if not k.is_cuda:
-            raise ValueError("expected a CUDA tensor (the library has no CPU path)")
         self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
-        self.struct = Kv8CacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(),
-                                     table.stride(0) if table.shape[0] > 1 else table.shape[1], pages, table.shape[0], heads,
-                                     page_tokens, dim, SB_KV_INT8 if k.dtype == torch.int8 else SB_KV_E4M3, 0)
+        self.struct = Kv8CacheStruct(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), _dev(table), stride if requests > 1 else per,
+                                     pages, requests, heads, page_tokens, dim, kind, 0)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_tokens: int, dim: int, table, dtype=torch.int8):
@@ -228,10 +242,12 @@ class Kv8Cache:
 
 def _heads(x: torch.Tensor, what: str):
     """(address, token stride, head stride) of a bf16 [tokens][heads][dim] tensor."""
-    if x.dim() != 3 or x.dtype != torch.bfloat16 or x.stride(2) != 1 or not x.is_cuda:
+    token, head, one = x.stride()
+    if x.dtype is not torch.bfloat16 or one != 1 or not x.is_cuda:
         raise ValueError(f"{what}: expected a bf16 [tokens][heads][dim] CUDA tensor with contiguous rows")
+    tokens, heads, _ = x.shape
     # the stride of an axis of one element is never used
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0
+    return x.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0
 
 
 class Context:
@@ -517,10 +533,10 @@ class Context:
     def fp4_quantize(self, X: torch.Tensor, out: Fp4Matrix) -> Fp4Matrix:
         """X (bf16 [rows][cols]) into `out`, whose format and tensor scale it takes."""
         R, Cc, ldx = _mat(X)
-        if (R, Cc) != (out.rows, out.cols):
+        if R != out.rows or Cc != out.cols:
             raise ValueError("X and the 4-bit matrix have different sizes")
-        self._check(lib().sb_fp4_quantize(self._h, _ptr(X), R, Cc, ldx if R > 1 else (Cc + 7) // 8 * 8, FP4_FORMATS[out.fmt],
-                                          _ptr(out.tensor_scale), _ptr(out.codes), _ptr(out.scales)))
+        self._check(lib().sb_fp4_quantize(self._h, _dev(X), R, Cc, ldx if R > 1 else (Cc + 7) // 8 * 8, FP4_FORMATS[out.fmt],
+                                          _dev(out.tensor_scale), _dev(out.codes), _dev(out.scales)))
         return out
 
     def fp4_dequantize(self, m: Fp4Matrix, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -528,40 +544,46 @@ class Context:
         if out is None:
             out = torch.empty((m.rows, m.cols), dtype=torch.bfloat16, device=m.codes.device)
         R, Cc, ldy = _mat(out)
-        if (R, Cc) != (m.rows, m.cols):
+        if R != m.rows or Cc != m.cols:
             raise ValueError("out and the 4-bit matrix have different sizes")
-        self._check(lib().sb_fp4_dequantize(self._h, _ptr(m.codes), _ptr(m.scales), R, Cc, FP4_FORMATS[m.fmt], _ptr(m.tensor_scale),
-                                            _ptr(out), ldy if R > 1 else Cc))
+        self._check(lib().sb_fp4_dequantize(self._h, _dev(m.codes), _dev(m.scales), R, Cc, FP4_FORMATS[m.fmt], _dev(m.tensor_scale),
+                                            _dev(out), ldy if R > 1 else Cc))
         return out
 
     def fp4_gemm(self, a: Fp4Matrix, b: Fp4Matrix, out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
         """a [M][K] times the transpose of b [N][K] -> [M][N] in bf16 or fp32 (out's type, or out_dtype)."""
+        M, N = a.rows, b.rows
         if a.cols != b.cols or a.fmt != b.fmt:
             raise ValueError("the two matrices need the same format and number of columns")
         if out is None:
-            out = torch.empty((a.rows, b.rows), dtype=out_dtype, device=a.codes.device)
-        if out.dtype not in (torch.bfloat16, torch.float32) or out.shape != (a.rows, b.rows) or out.stride(1) != 1:
+            out = torch.empty((M, N), dtype=out_dtype, device=a.codes.device)
+        dtype, shape = out.dtype, out.shape
+        ldy, one = out.stride()
+        if dtype is not torch.bfloat16 and dtype is not torch.float32 or shape[0] != M or shape[1] != N or one != 1:
             raise ValueError("out: a row-major bf16 or fp32 [M][N] tensor")
-        self._check(lib().sb_fp4_gemm(self._h, _ptr(a.codes), _ptr(a.scales), _ptr(a.tensor_scale), a.rows, _ptr(b.codes),
-                                      _ptr(b.scales), _ptr(b.tensor_scale), b.rows, a.cols, FP4_FORMATS[a.fmt], _ptr(out),
-                                      int(out.dtype == torch.float32), out.stride(0) if a.rows > 1 else b.rows))
+        self._check(lib().sb_fp4_gemm(self._h, _dev(a.codes), _dev(a.scales), _dev(a.tensor_scale), M, _dev(b.codes), _dev(b.scales),
+                                      _dev(b.tensor_scale), N, a.cols, FP4_FORMATS[a.fmt], _dev(out), int(dtype is torch.float32),
+                                      ldy if M > 1 else N))
         return out
 
     # ---- key/value cache in 8 bits ----------------------------------------------------------
-    def _kv8_rows(self, cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor):
+    @staticmethod
+    def _kv8_rows(cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor):
         n = cache.struct.requests
-        if starts.dtype != torch.int32 or lens.dtype != torch.int32 or starts.numel() != n + 1 or lens.numel() != n:
+        if starts.dtype is not torch.int32 or lens.dtype is not torch.int32 or starts.numel() != n + 1 or lens.numel() != n:
             raise ValueError("starts: int32 [requests + 1], lens: int32 [requests]")
-        return _ptr(starts), _ptr(lens)
+        return _dev(starts), _dev(lens)
 
     def kv8_append(self, cache: Kv8Cache, K: torch.Tensor, V: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int):
         """Writes the new tokens' keys and values (bf16 [tokens][heads][dim]); request b's rows are
         starts[b] .. starts[b + 1], its length with them lens[b]."""
         s, n = self._kv8_rows(cache, starts, lens)
-        if K.shape != V.shape or K.shape[1:] != (cache.struct.heads, cache.struct.dim):
+        tokens, heads, dim = shape = K.shape
+        if V.shape != shape or heads != cache.struct.heads or dim != cache.struct.dim:
             raise ValueError("K and V: [tokens][heads][dim] of the cache")
-        (k, kt, kh), (v, vt, vh) = _heads(K, "K"), _heads(V, "V")
-        self._check(lib().sb_kv8_append(self._h, C.byref(cache.struct), k, kt, kh, v, vt, vh, K.shape[0], s, n, int(max_new)))
+        k, kt, kh = _heads(K, "K")
+        v, vt, vh = _heads(V, "V")
+        self._check(lib().sb_kv8_append(self._h, cache.struct, k, kt, kh, v, vt, vh, tokens, s, n, max_new))
 
     def kv8_read(self, cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor, max_new: int, total: Optional[int] = None, out=None):
         """The values of the last starts[b + 1] - starts[b] tokens of every request, as bf16
@@ -571,9 +593,11 @@ class Context:
             shape = (int(starts[-1]) if total is None else total, cache.struct.heads, cache.struct.dim)
             out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
         K, V = out
-        if K.shape != V.shape or K.shape[1:] != (cache.struct.heads, cache.struct.dim) or not K.is_contiguous() or not V.is_contiguous():
-            raise ValueError("out: two contiguous [tokens][heads][dim] tensors")
-        self._check(lib().sb_kv8_read(self._h, C.byref(cache.struct), K.shape[0], s, n, int(max_new), _ptr(K, torch.bfloat16), _ptr(V, torch.bfloat16)))
+        tokens, heads, dim = shape = K.shape
+        if V.shape != shape or heads != cache.struct.heads or dim != cache.struct.dim or not K.is_contiguous() or not V.is_contiguous() \
+                or K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
+            raise ValueError("out: two contiguous bf16 [tokens][heads][dim] tensors")
+        self._check(lib().sb_kv8_read(self._h, cache.struct, tokens, s, n, max_new, _dev(K), _dev(V)))
         return K, V
 
     def kv8_attention(self, cache: Kv8Cache, Q: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int, max_len: int,
@@ -582,21 +606,21 @@ class Context:
         """Causal attention of the new tokens (Q bf16 [tokens][query heads][dim]) over the cache, which
         holds them already.  Returns (out, lse); lse is None unless given or asked for."""
         s, n = self._kv8_rows(cache, starts, lens)
-        if Q.dim() != 3 or Q.shape[2] != cache.struct.dim:
+        tokens, heads, dim = shape = Q.shape
+        if dim != cache.struct.dim:
             raise ValueError("Q: [tokens][query heads][dim of the cache]")
         q, qt, qh = _heads(Q, "Q")
         if out is None:
-            out = torch.empty(Q.shape, dtype=torch.bfloat16, device=Q.device)
-        if out.shape != Q.shape:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=Q.device)
+        elif out.shape != shape:
             raise ValueError("out: the shape of Q")
         o, ot, oh = _heads(out, "out")
         if lse is None and want_lse:
-            lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
-        if lse is not None and (lse.shape != Q.shape[:2] or not lse.is_contiguous()):
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=Q.device)
+        if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or lse.dtype is not torch.float32):
             raise ValueError("lse: contiguous fp32 [tokens][query heads]")
-        self._check(lib().sb_kv8_attention(self._h, C.byref(cache.struct), q, qt, qh, Q.shape[1], Q.shape[0], s, n, int(max_new),
-                                           int(max_len), Q.shape[2] ** -0.5 if scale is None else float(scale), int(window), o, ot, oh,
-                                           _ptr(lse, torch.float32)))
+        self._check(lib().sb_kv8_attention(self._h, cache.struct, q, qt, qh, heads, tokens, s, n, max_new, max_len,
+                                           dim ** -0.5 if scale is None else scale, window, o, ot, oh, _dev(lse)))
         return out, lse
 
 
