@@ -2,6 +2,19 @@
 #pragma once
 #include "common.cuh"
 
+// Quotients of 31-bit numbers by a divisor that the host knows: with m = ceil(2^64 / d),
+// floor(x m / 2^64) is exact while x and d are below 2^31 (d = 1: m does not fit, m = 0).
+struct KvDiv {
+    uint64_t m = 0;
+    int d = 1;
+    KvDiv() = default;
+    explicit KvDiv(int d_) : m(d_ > 1 ? ~0ull / (unsigned)d_ + 1 : 0), d(d_) {}
+#ifdef __CUDACC__
+    __device__ __forceinline__ int quot(int x) const { return d > 1 ? (int)__umul64hi((unsigned long long)(unsigned)x, m) : x; }
+    __device__ __forceinline__ int rem(int x) const { return x - quot(x) * d; }
+#endif
+};
+
 struct Kv8Geom {                 // the parts of sb_kv8_cache that kernels read
     const int32_t* table;
     int64_t table_stride, pages;
@@ -10,6 +23,7 @@ struct Kv8Geom {                 // the parts of sb_kv8_cache that kernels read
     const int32_t* lens;
     int64_t total;               // rows of the call's dense arguments
     int max_new;
+    KvDiv page;                  // by page_tokens
 };
 
 inline bool kv8_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -36,6 +50,7 @@ inline Kv8Geom kv8_geom(const sb_kv8_cache* c, int64_t total, const int32_t* sta
     g.table = c->table; g.table_stride = c->table_stride; g.pages = c->pages;
     g.requests = c->requests; g.heads = c->heads; g.page_tokens = c->page_tokens; g.dim = c->dim;
     g.starts = starts; g.lens = lens; g.total = total; g.max_new = (int)max_new;
+    g.page = KvDiv(c->page_tokens);
     return g;
 }
 

@@ -37,7 +37,7 @@ constexpr int AT_PROMPT_FROM = 64;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
 constexpr int AT_EXTRA = 12;            // what an item costs besides its steps, in steps
-constexpr int AT_LEAST = 16 + AT_EXTRA; // units of a share at least: four steps of every warp
+constexpr int AT_LEAST = 4 + AT_EXTRA;  // units of a share at least: a step of every warp
 constexpr float AT_SLACK = 8.f;         // log2 of how far a row's maximum may run ahead of its reference
 constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
 
@@ -111,7 +111,7 @@ kv8_rows_kernel(const AtArgs a) {
 #pragma unroll
         for (int w = 0; w < AT_WARPS; ++w) total += sums[w];
         total *= a.g.heads;
-        share = (total + gridDim.x - 1) / gridDim.x;
+        share = at_div(total + gridDim.x - 1, gridDim.x);
         if (share < AT_LEAST) share = AT_LEAST;
         const long long at = blockIdx.x * share;
         if (at >= total) return;
@@ -137,8 +137,8 @@ kv8_rows_kernel(const AtArgs a) {
             if (at >= lo && at < lo + mine * a.g.heads) {
                 int* found = reinterpret_cast<int*>(sums + AT_WARPS);
                 found[0] = base + threadIdx.x;
-                found[1] = (int)((at - lo) / mine);
-                found[2] = (int)((at - lo) % mine);
+                found[1] = (int)at_div(at - lo, mine);
+                found[2] = (int)(at - lo - found[1] * mine);
             }
             before += all;
             if (at < before * a.g.heads) break;
@@ -152,7 +152,7 @@ kv8_rows_kernel(const AtArgs a) {
     for (bool more = true; more; more = wk.next(a)) {
         const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
         const Kv8Request rq = wk.it.rq;
-        const int i0 = r0 / a.group, i1 = (r0 + nrow - 1) / a.group;
+        const int i0 = a.by_group.quot(r0), i1 = a.by_group.quot(r0 + nrow - 1);
         const int k0 = wk.it.lo + wk.step0 * AT_STEP, k1 = min(wk.it.hi, k0 + wk.count * AT_STEP);
         const int mine = (wk.count - warp + AT_WARPS - 1) / AT_WARPS;   // steps warp, warp + 4, ...
 
@@ -162,8 +162,8 @@ kv8_rows_kernel(const AtArgs a) {
 #pragma unroll
         for (int i = 0; i < QR; ++i) {
             const int r = warp + AT_WARPS * i, row = r0 + r;
-            const __nv_bfloat16* src = a.q + (int64_t)(rq.row0 + row / a.group) * a.q_token_stride +
-                                       (int64_t)(head * a.group + row % a.group) * a.q_head_stride;
+            const __nv_bfloat16* src = a.q + (int64_t)(rq.row0 + a.by_group.quot(row)) * a.q_token_stride +
+                                       (int64_t)(head * a.group + a.by_group.rem(row)) * a.q_head_stride;
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c) {
                 const int d = 64 * c + 2 * lane;
@@ -176,7 +176,7 @@ kv8_rows_kernel(const AtArgs a) {
         auto block_key = [&](int batch) { return k0 + (warp + AT_WARPS * (AT_BATCH * batch + (lane >> 1))) * AT_STEP + SB_KV8_BLOCK * (lane & 1); };
         auto load_entry = [&](int batch) -> int {
             const int key = block_key(batch);
-            return key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + key / a.g.page_tokens] : 0;
+            return key < k1 ? a.g.table[(int64_t)b * a.g.table_stride + a.g.page.quot(key)] : 0;
         };
         // the block's first code (-1: no such block) and, fetched, its two scales
         auto place = [&](int batch, int entry, uint32_t& s2) -> int64_t {
@@ -188,7 +188,7 @@ kv8_rows_kernel(const AtArgs a) {
                 return -1;
             }
             const int64_t ph = (int64_t)entry * a.g.heads + head;
-            const int slot = key % a.g.page_tokens;
+            const int slot = a.g.page.rem(key);
             const int64_t at = ph * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;
             s2 = (uint32_t)a.k_scale[at] | (uint32_t)a.v_scale[at] << 16;
             return (ph * a.g.page_tokens + slot) * D;
@@ -264,7 +264,7 @@ kv8_rows_kernel(const AtArgs a) {
             for (int e = 0; e < 2; ++e) {
                 const int r = 8 * nr + 2 * t + e;
                 fq[nr][e] = reinterpret_cast<const float*>(smem + S::F_AT)[r];
-                pos[nr][e] = rq.past + (r0 + r) / a.group;          // rows past the last: queries of zeros, dropped at the end
+                pos[nr][e] = rq.past + a.by_group.quot(r0 + r);          // rows past the last: queries of zeros, dropped at the end
             }
         // B operand of step 4 c + j: d = 64 c + 16 t + 4 j + {0, 1} and + {2, 3} of row g
         const unsigned qlane = at_smem(smem) + S::Q_AT + (unsigned)(g * S::QPITCH + 32 * t);
@@ -313,25 +313,40 @@ kv8_rows_kernel(const AtArgs a) {
             // scores, in units of log2
             float s[2][NR][4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int nr = 0; nr < NR; ++nr) s[e][nr][0] = s[e][nr][1] = s[e][nr][2] = s[e][nr][3] = 0.f;
 #pragma unroll
-                for (int c = 0; c < DP / 64; ++c) {
-                    const int row = SB_KV8_BLOCK * e + g;               // rows g and g + 8 have the same swizzle
+            for (int c = 0; c < DP / 64; ++c) {
+                // both blocks side by side: twice the independent products, one fetch of the queries for both
+                uint32_t wl[2][4], wh[2][4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row = SB_KV8_BLOCK * e + g;           // rows g and g + 8 have the same swizzle
                     const unsigned off = DP == 64 ? (unsigned)(row * 64 + ((t ^ ((row >> 1) & 3)) << 4))
                                                   : (unsigned)(row * DP + 128 * (c >> 1) + (((4 * (c & 1) + t) ^ (row & 7)) << 4));
                     const uint4 lo4 = at_lds128(kst + off), hi4 = at_lds128(kst + off + 8 * DP);
-                    const uint32_t wl[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, wh[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+                    wl[e][0] = at_flip<TYPE>(lo4.x); wl[e][1] = at_flip<TYPE>(lo4.y); wl[e][2] = at_flip<TYPE>(lo4.z); wl[e][3] = at_flip<TYPE>(lo4.w);
+                    wh[e][0] = at_flip<TYPE>(hi4.x); wh[e][1] = at_flip<TYPE>(hi4.y); wh[e][2] = at_flip<TYPE>(hi4.z); wh[e][3] = at_flip<TYPE>(hi4.w);
+                }
+                uint4 q4[2][NR];
+                if constexpr (!S::QREGS) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t x = at_flip<TYPE>(wl[i]), y = at_flip<TYPE>(wh[i]);
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr) q4[h][nr] = at_lds128(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * c + 16 * h));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t x = wl[e][i], y = wh[e][i];
                         const uint32_t a0 = at_pair<TYPE, 0>(x), a1 = at_pair<TYPE, 0>(y), a2 = at_pair<TYPE, 1>(x), a3 = at_pair<TYPE, 1>(y);
 #pragma unroll
                         for (int nr = 0; nr < NR; ++nr) {
                             uint2 qb;
                             if constexpr (S::QREGS) qb = qf[4 * c + i][nr];
-                            else qb = at_lds64(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * c + 8 * i));
+                            else qb = i & 1 ? make_uint2(q4[i >> 1][nr].z, q4[i >> 1][nr].w) : make_uint2(q4[i >> 1][nr].x, q4[i >> 1][nr].y);
                             at_mma(s[e][nr], a0, a1, a2, a3, qb.x, qb.y);
                         }
                     }
@@ -469,8 +484,8 @@ kv8_rows_kernel(const AtArgs a) {
         const int quads = D / 4;
         auto store = [&](int r, int d, float4 v, float mm, float sum) {
             const int row = r0 + r;
-            const int64_t tok = rq.row0 + row / a.group;
-            const int h = head * a.group + row % a.group;
+            const int64_t tok = rq.row0 + a.by_group.quot(row);
+            const int h = head * a.group + a.by_group.rem(row);
             const float f = at_norm(sum);
             const uint2 w = make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
             *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) = w;
@@ -503,7 +518,7 @@ kv8_rows_kernel(const AtArgs a) {
         if (!whole) {
             // ---- the last of the item's pieces to finish adds them all, in order ----
             const long long from = wk.from;
-            const int c0 = (int)((from + AT_EXTRA) / share), c1 = (int)((from + wk.units() - 1) / share), pieces = c1 - c0 + 1;
+            const int c0 = (int)at_div(from + AT_EXTRA, share), c1 = (int)at_div(from + wk.units() - 1, share), pieces = c1 - c0 + 1;
             // a piece is the first of its share unless the item starts inside the share
             auto slot = [&](int x) { return (2 * (int64_t)(c0 + x) + (from > (c0 + x) * share ? 1 : 0)) * S::ROWS; };
             volatile int* last = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
@@ -547,34 +562,54 @@ kv8_rows_kernel(const AtArgs a) {
                     if (lane == 0) total[r] = make_float2(mm, sum);
                 }
                 __syncthreads();
-                // with few outputs several threads share one, each a part of the pieces
+                constexpr int PER = S::ROWS * DP / 4 / (AT_WARPS * 32);  // outputs of a thread, four columns each, at most
                 const int outs = nrow * quads;
-                const int parts = outs >= AT_WARPS * 32 ? 1 : AT_WARPS * 32 / outs;
-                float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
-                for (int base = 0; base < outs; base += AT_WARPS * 32) {
-                    const int part = (int)threadIdx.x / outs, idx = parts > 1 ? (int)threadIdx.x - part * outs : base + (int)threadIdx.x;
+                if (outs <= AT_WARPS * 32) {
+                    // few outputs: one a thread, or several threads for one, each a part of the pieces
+                    const int parts = AT_WARPS * 32 / outs, part = (int)threadIdx.x / outs, idx = (int)threadIdx.x - part * outs;
                     const int r = idx / quads, d = 4 * (idx - r * quads);
+                    float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (idx < outs && (parts == 1 || part < parts)) {
-                        const int x0 = parts > 1 ? pieces * part / parts : 0, x1 = parts > 1 ? pieces * (part + 1) / parts : pieces;
+                    if (part < parts) {
+                        const int x1 = pieces * (part + 1) / parts;
 #pragma unroll 8
-                        for (int x = x0; x < x1; ++x) {
+                        for (int x = pieces * part / parts; x < x1; ++x) {
                             const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x) + r) * D + d));
                             const float f = weight[x * S::ROWS + r];
                             v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
                         }
                     }
-                    if (parts > 1) {
-                        shared_sum[threadIdx.x] = v;
-                        __syncthreads();
-                        if (threadIdx.x < outs) {
-                            for (int p = 1; p < parts; ++p) {
-                                const float4 y = shared_sum[threadIdx.x + p * outs];
-                                v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
-                            }
-                            store(r, d, v, total[r].x, total[r].y);
+                    shared_sum[threadIdx.x] = v;
+                    __syncthreads();
+                    if ((int)threadIdx.x < outs) {
+                        for (int p = 1; p < parts; ++p) {
+                            const float4 y = shared_sum[threadIdx.x + p * outs];
+                            v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
                         }
-                    } else if (idx < outs) store(r, d, v, total[r].x, total[r].y);
+                        store(r, d, v, total[r].x, total[r].y);
+                    }
+                } else {
+                    // a thread's outputs side by side, so that their loads overlap
+                    float4 v[PER];
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll (PER <= 2 ? 8 : 2)
+                    for (int x = 0; x < pieces; ++x) {
+                        const float* from_part = a.part + slot(x) * D;
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) {
+                            const int idx = (int)threadIdx.x + AT_WARPS * 32 * i;
+                            if (idx >= outs) continue;
+                            const float4 y = __ldcg(reinterpret_cast<const float4*>(from_part) + idx);
+                            const float f = weight[x * S::ROWS + idx / quads];
+                            v[i].x = fmaf(y.x, f, v[i].x); v[i].y = fmaf(y.y, f, v[i].y); v[i].z = fmaf(y.z, f, v[i].z); v[i].w = fmaf(y.w, f, v[i].w);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const int idx = (int)threadIdx.x + AT_WARPS * 32 * i, r = idx / quads;
+                        if (idx < outs) store(r, 4 * (idx - r * quads), v[i], total[r].x, total[r].y);
+                    }
                 }
             }
         }
@@ -596,6 +631,7 @@ sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     const int64_t most = (tiles * ((keys + AT_STEP - 1) / AT_STEP + 1 + AT_EXTRA) + AT_LEAST - 1) / AT_LEAST;
     const int64_t ctas = most < (int64_t)S::CTAS * ctx->sm_count ? most : (int64_t)S::CTAS * ctx->sm_count;
     a.row_tiles = (int)row_tiles;
+    a.by_row_tiles = KvDiv(a.row_tiles);
     const size_t n = (size_t)ctas * 2 * S::ROWS;
     void* arena;
     const sb_status s = sb_scratch(ctx, Carver::need({n * a.g.dim * 4, n * 8}), &arena);
@@ -663,6 +699,7 @@ extern "C" sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, co
     a.o = static_cast<__nv_bfloat16*>(O); a.o_token_stride = o_token_stride; a.o_head_stride = o_head_stride;
     a.lse = lse;
     a.group = q_heads / cache->heads;
+    a.by_group = KvDiv(a.group);
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;

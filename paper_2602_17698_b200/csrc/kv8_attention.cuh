@@ -13,8 +13,9 @@ struct AtArgs {
     int64_t o_token_stride, o_head_stride;
     float* lse;
     int group;                   // query heads per cache head
-    unsigned group_inverse;      // ceil(2^32 / group), for group > 1
+    KvDiv by_group;
     int row_tiles;               // of a request with max_new new tokens
+    KvDiv by_row_tiles;
     float scale_log2;            // softmax scale * log2(e)
     int window;
     float* part;                 // two slots per CTA: unnormalised sums of an item's piece
@@ -43,18 +44,22 @@ struct AtItem {
 template <int ROWS, int KEYS>
 __device__ __forceinline__ AtItem at_item(const AtArgs& a, int row_tile) {
     AtItem it;
-    it.b = row_tile / a.row_tiles;
+    it.b = a.by_row_tiles.quot(row_tile);
     it.r0 = (row_tile - it.b * a.row_tiles) * ROWS;
     it.steps = 0;
     if (!kv8_request(a.g, it.b, it.rq, a.st)) return it;
     const int rows = it.rq.n * a.group;
     if (it.r0 >= rows) return it;
     it.nrow = min(ROWS, rows - it.r0);
-    const int i0 = it.r0 / a.group, i1 = (it.r0 + it.nrow - 1) / a.group;
+    const int i1 = a.by_group.quot(it.r0 + it.nrow - 1);
     it.hi = it.rq.past + i1 + 1;
-    it.lo = a.window > 0 ? max(0, it.rq.past + i0 - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
+    it.lo = a.window > 0 ? max(0, it.rq.past + a.by_group.quot(it.r0) - a.window + 1) & ~(SB_KV8_BLOCK - 1) : 0;
     it.steps = (it.hi - it.lo + KEYS - 1) / KEYS;
     return it;
+}
+// quotients of the plan: 64 bits only where it takes them
+__device__ __forceinline__ long long at_div(long long x, long long d) {
+    return ((x | d) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)d) : x / d;
 }
 // A share as its pieces of items; every warp walks through them by itself.
 template <int ROWS, int KEYS, int EXTRA>

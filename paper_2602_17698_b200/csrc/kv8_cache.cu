@@ -81,8 +81,8 @@ kv8_append_kernel(const Kv8Geom g, const KvSide ks, const KvSide vs, SbDeviceSta
     const KvSide sd = (unit & 1) ? vs : ks;
     const int tok0 = (blk0 + bi) * SB_KV8_BLOCK;                         // first token of the block
     int64_t page;
-    if (!kv8_page(g, b, tok0 / g.page_tokens, page, st)) return;
-    const int slot = tok0 % g.page_tokens;
+    if (!kv8_page(g, b, g.page.quot(tok0), page, st)) return;
+    const int slot = g.page.rem(tok0);
     const int64_t ph = page * g.heads + head;
     uint8_t* codes = sd.codes + (ph * g.page_tokens + slot) * g.dim;
     uint16_t* scale_at = sd.scale + ph * (g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;
@@ -171,8 +171,8 @@ kv8_read_kernel(const Kv8Geom g, const KvSide ks, const KvSide vs, __nv_bfloat16
     const int head = rest / per_tok, piece = rest - head * per_tok;
     const int tok = rq.past + i;
     int64_t page;
-    if (!kv8_page(g, b, tok / g.page_tokens, page, st)) return;
-    const int slot = tok % g.page_tokens;
+    if (!kv8_page(g, b, g.page.quot(tok), page, st)) return;
+    const int slot = g.page.rem(tok);
     const int64_t ph = page * g.heads + head;
     const int64_t src = (ph * g.page_tokens + slot) * g.dim + 8 * piece;
     const int64_t sat = ph * (g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK;

@@ -293,13 +293,13 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 const int c = lane % LANES, sub = lane / LANES;
                 float* factor = reinterpret_cast<float*>(smem + S::F_AT) + qt * PR_ROWS;
                 unsigned char* q0 = smem + S::Q_AT + qt * S::OPERAND + (c >> 3) * S::PANEL;
-                const int tok0 = it.r0 / a.group, head0 = it.r0 - tok0 * a.group;
+                const int tok0 = a.by_group.quot(it.r0), head0 = it.r0 - tok0 * a.group;
                 const __nv_bfloat16* src = a.q + (int64_t)(it.rq.row0 + tok0) * a.q_token_stride + (int64_t)wk.head * a.group * a.q_head_stride + 8 * c;
                 uint4 x[NI];
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
                     const int rr = qt * PR_ROWS + (warp & 3) * 32 + i * RPI + sub, at = head0 + rr;
-                    const int tok = a.group > 1 ? (int)__umulhi((unsigned)at, a.group_inverse) : at;
+                    const int tok = a.by_group.quot(at);
                     x[i] = make_uint4(0, 0, 0, 0);
                     if (rr < it.nrow && 8 * c < D)
                         x[i] = *reinterpret_cast<const uint4*>(src + tok * a.q_token_stride + (at - tok * a.group) * a.q_head_stride);
@@ -322,10 +322,10 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             }
             const float fq = __fdiv_rn(a.scale_log2, reinterpret_cast<const float*>(smem + S::F_AT)[r]);
             // (a thread without a row has queries of zeros, and its results go nowhere)
-            const int pos = it.rq.past + row / a.group;
+            const int pos = it.rq.past + a.by_group.quot(row);
             // positions of the tile's first and last row decide which key tiles need a mask
-            const int pos_lo = it.rq.past + (it.r0 + qt * PR_ROWS) / a.group;
-            const int pos_hi = it.rq.past + (it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1) / a.group;
+            const int pos_lo = it.rq.past + a.by_group.quot(it.r0 + qt * PR_ROWS);
+            const int pos_hi = it.rq.past + a.by_group.quot(it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1);
             const int k0 = it.lo + wk.step0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
             float m = -INFINITY, l = 0.f, vref = 0.f, inv = 0.f;
             ok = wait(scfull + (base_all & 3), base_all >> 2);
@@ -395,8 +395,8 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             ++pieces;
             const bool whole = count == it.steps;
             const int h0 = wk.head * a.group;
-            const int64_t tok = it.rq.row0 + row / a.group;
-            const int h = h0 + row % a.group;
+            const int64_t tok = it.rq.row0 + a.by_group.quot(row);
+            const int h = h0 + a.by_group.rem(row);
             const float norm = whole ? at_norm(l) * vref : vref;
             const int64_t slot = 2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1);
             // this warp's rows in bf16 where its queries were, in the same order
@@ -429,12 +429,12 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 __syncwarp();
                 constexpr int LANES = DP / 8, RPI = 32 / LANES;
                 const int c = lane % LANES, sub = lane / LANES;
-                const int tok0 = it.r0 / a.group, head0 = it.r0 - tok0 * a.group;
+                const int tok0 = a.by_group.quot(it.r0), head0 = it.r0 - tok0 * a.group;
                 __nv_bfloat16* dst = a.o + (int64_t)(it.rq.row0 + tok0) * a.o_token_stride + (int64_t)h0 * a.o_head_stride + 8 * c;
 #pragma unroll 4
                 for (int i = 0; i < 32; i += RPI) {
                     const int rl = i + sub, rr = qt * PR_ROWS + (warp & 3) * 32 + rl, at = head0 + rr;
-                    const int tk = a.group > 1 ? (int)__umulhi((unsigned)at, a.group_inverse) : at;
+                    const int tk = a.by_group.quot(at);
                     const uint4 v = *reinterpret_cast<const uint4*>(o0 + (c >> 3) * S::PANEL + rl * 128 + (((c & 7) ^ (rl & 7)) << 4));
                     if (rr < it.nrow && 8 * c < D)
                         *reinterpret_cast<uint4*>(dst + tk * a.o_token_stride + (at - tk * a.group) * a.o_head_stride) = v;
@@ -492,11 +492,11 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int limit = min(wk.it.rq.len, (k1 + SB_KV8_BLOCK - 1) / SB_KV8_BLOCK * SB_KV8_BLOCK) - k0;
             auto entry_of = [&](int j) -> int {
                 const int key = k0 + j * PR_KEYS + sblk;
-                return brings && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + key / a.g.page_tokens] : -1;
+                return brings && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + a.g.page.quot(key)] : -1;
             };
             auto scale_of = [&](int j, int entry) -> uint16_t {
                 if (entry < 0 || entry >= a.g.pages) return 0;
-                const int slot = (k0 + j * PR_KEYS + sblk) % a.g.page_tokens;
+                const int slot = a.g.page.rem(k0 + j * PR_KEYS + sblk);
                 return scales[((int64_t)entry * a.g.heads + wk.head) * (a.g.page_tokens / SB_KV8_BLOCK) + slot / SB_KV8_BLOCK];
             };
             uint16_t scale = scale_of(0, entry_of(0));
@@ -530,12 +530,12 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int k0 = wk.it.lo + wk.step0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
             auto entry_of = [&](int j) -> int {
                 const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
-                return lane < PR_BLOCKS && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + key / a.g.page_tokens] : -1;
+                return lane < PR_BLOCKS && key < k1 ? a.g.table[(int64_t)wk.it.b * a.g.table_stride + a.g.page.quot(key)] : -1;
             };
             int entry = entry_of(0);
             for (int j = 0; ok && j < wk.count; ++j) {
                 const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
-                const int slot = key % a.g.page_tokens;
+                const int slot = a.g.page.rem(key);
                 const bool inside = lane < PR_BLOCKS && key < k1, fine = inside && entry >= 0 && entry < a.g.pages;
                 if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
                 const int64_t at = (((int64_t)entry * a.g.heads + wk.head) * a.g.page_tokens + slot) * D;
@@ -665,8 +665,8 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
         m = mn;
     }
     const int row = it.r0 + r;
-    const int64_t tok = it.rq.row0 + row / a.group;
-    const int h = s.y * a.group + row % a.group;
+    const int64_t tok = it.rq.row0 + a.by_group.quot(row);
+    const int h = s.y * a.group + a.by_group.rem(row);
     const float f = at_norm(l);
     *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + 4 * quad) =
         make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
@@ -687,7 +687,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     PrWork w{};
     w.ctas = (int)(most < ctx->sm_count ? most : ctx->sm_count);
     a.row_tiles = (int)row_tiles;
-    a.group_inverse = (unsigned)(((1ull << 32) + a.group - 1) / a.group);   // exact quotients of numbers below 2^32 / group
+    a.by_row_tiles = KvDiv(a.row_tiles);
     const size_t rows = (size_t)w.ctas * 2 * (2 * PR_ROWS);
     void* arena;
     const sb_status s = sb_scratch(ctx, Carver::need({((size_t)n + 1) * 8, (size_t)w.ctas * 16, 16, rows * a.g.dim * 4, rows * 8}), &arena);
