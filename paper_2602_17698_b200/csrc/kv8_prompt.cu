@@ -29,12 +29,13 @@ constexpr int PR_BLOCKS = PR_KEYS / SB_KV8_BLOCK;
 constexpr int PR_SUB = 64;               // keys of a softmax step: half a tile
 constexpr int PR_SUBBLOCKS = PR_SUB / SB_KV8_BLOCK;
 constexpr int PR_THREADS = 16 * 32;       // warp 15 only lends its registers
-// registers of a softmax, conversion and other warp's thread: 8 x 160 + 4 x 96 + 4 x 96 warps' shares <= 16 x 128
-constexpr int PR_REGS_SOFTMAX = 160, PR_REGS_CONVERT = 96, PR_REGS_REST = 96;
+// registers of a softmax, conversion and other warp's thread: 8 x 136 + 4 x 120 + 4 x 120 warps' shares <= 16 x 128
+constexpr int PR_REGS_SOFTMAX = 136, PR_REGS_CONVERT = 120, PR_REGS_REST = 120;
 static_assert(8 * PR_REGS_SOFTMAX + 4 * PR_REGS_CONVERT + 4 * PR_REGS_REST <= 16 * 128, "what the block was launched with");
-constexpr int PR_EXTRA = 4;              // what an item costs besides its key tiles, in key tiles
-constexpr int PR_LEAST = 8;              // units of a share at least
+constexpr int PR_EXTRA = 6;              // what an item costs besides its key tiles, in key tiles
+constexpr int PR_LEAST = 1 + PR_EXTRA;              // units of a share at least
 constexpr float PR_SLACK = 8.f;          // log2 of how far a row's maximum may run ahead of its reference
+constexpr float PR_LIMIT = 256.f;        // largest sum of a half tile's weights before the row's reference moves
 
 template <int DP>
 struct PrShape {
@@ -88,7 +89,6 @@ __device__ __forceinline__ constexpr unsigned pr_idesc(int n, bool b_mn) {
 
 // Column c of a row's 64 scores is seen if from < c <= upto; EDGE: some are not.
 // Largest score of a row, in units of log2 (kf: factor of each 16 columns, not negative).
-template <bool EDGE>
 __device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const float (&kf)[PR_SUBBLOCKS], int upto, int from) {
     float mx = -INFINITY;
 #pragma unroll
@@ -101,14 +101,14 @@ __device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const fl
             for (int u = 0; u < 4; ++u) {
                 const int c = 16 * h + i + u;
                 x[u] = __uint_as_float(s[c >> 5][c & 31]);
-                if (EDGE && (c > upto || c <= from)) x[u] = -INFINITY;
+                if (c > upto || c <= from) x[u] = -INFINITY;
             }
             bm[0] = fmaxf(fmaxf(bm[0], x[0]), x[1]);
             bm[1] = fmaxf(fmaxf(bm[1], x[2]), x[3]);
         }
         const float top = fmaxf(bm[0], bm[1]);
         // a factor of 0 makes 0 of any score, but no NaN of a block that is masked whole
-        mx = fmaxf(mx, EDGE && top == -INFINITY ? -INFINITY : top * kf[h]);
+        mx = fmaxf(mx, top == -INFINITY ? -INFINITY : top * kf[h]);
     }
     return mx;
 }
@@ -163,6 +163,7 @@ __global__ void __launch_bounds__(1024)
 kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     __shared__ long long warp_sum_at[32], total_at;
     const int n = a.row_tiles * a.g.requests, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    at_let_next();
     long long before = 0;
     for (int base = 0; base < n; base += 1024) {
         const int i = base + threadIdx.x;
@@ -226,6 +227,8 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int D = a.g.dim;
     PrWalk wk;
+    at_after_previous();
+    at_let_next();                           // its blocks find room when these end, and wait for that
     {
         const int4 s = work.start[blockIdx.x];
         const long long share = work.share[0], at = blockIdx.x * share;
@@ -344,13 +347,23 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 const float kf[PR_SUBBLOCKS] = {k4.x * fq, k4.y * fq, k4.z * fq, k4.w * fq};
                 const float vmax = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
                 const int upto = min(pos, k1 - 1) - key, from = a.window > 0 ? pos - a.window - key : -1;
+                // Where nothing is masked, the weights by the reference there is; their sum says whether it
+                // still does: no weight is above their sum. One above PR_LIMIT (or none: NaN), a mask, a
+                // first key or a larger value scale takes the other way, by the row's maximum.
+                float sum = 0.f;
+                bool again = edge || vmax > vref || __any_sync(0xffffffffu, m == -INFINITY);
                 t5_wait_ld();
-                const float mx = edge ? pr_max<true>(s, kf, upto, from) : pr_max<false>(s, kf, upto, from);
-                // the reference (and the power of two of the value scales) moves when it is too far off
-                const bool off = mx > m + PR_SLACK || (m == -INFINITY && mx > m) || vmax > vref;
-                if (__any_sync(0xffffffffu, off)) {
+                if (!again) {
+                    const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
+                    sum = pr_weights<false>(ts + PR_SUB * u, s, kf, vw, m, upto, from);
+                    again = __any_sync(0xffffffffu, !(sum <= PR_LIMIT));
+                }
+                if (again) {
+                    const float mx = pr_max(s, kf, upto, from);
+                    const bool far = mx > m + PR_SLACK || (m == -INFINITY && mx > m);
+                    const bool move = __any_sync(0xffffffffu, far) || vmax > vref;
                     float f = 1.f;
-                    if (mx > m + PR_SLACK || (m == -INFINITY && mx > m)) {
+                    if (far) {
                         f = m == -INFINITY ? 0.f : at_exp2(m - mx);
                         m = mx;
                         l *= f;
@@ -361,7 +374,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                         vref = fresh;
                         inv = at_value_inv(vref);
                     }
-                    if (n > 0) {
+                    if (move && n > 0) {
                         // the sums so far: the products of the half before this one have to be done
                         ok = wait(odone + qt, 2 * tiles_mine + n - 1);
                         if (!ok) break;
@@ -376,11 +389,12 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                             pr_st16(to + c, o);
                         }
                     }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
+                    pr_wait_st();
+                    sum = pr_weights<true>(ts + PR_SUB * u, s, kf, vw, ref, upto, from);
                 }
-                const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
-                const float ref = m == -INFINITY ? 0.f : m;
-                l += edge ? pr_weights<true>(ts + PR_SUB * u, s, kf, vw, ref, upto, from)
-                          : pr_weights<false>(ts + PR_SUB * u, s, kf, vw, ref, upto, from);
+                l += sum;
                 pr_wait_st();
                 t5_fence_before();
                 __syncwarp();
@@ -463,15 +477,16 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int kk = krow + PASS * i;
-                const uint32_t w[4] = {at_flip<TYPE>(x[i].x), at_flip<TYPE>(x[i].y), at_flip<TYPE>(x[i].z), at_flip<TYPE>(x[i].w)};
-                const uint4 lo4 = make_uint4(at_pair<TYPE, 0>(w[0]), at_pair<TYPE, 1>(w[0]), at_pair<TYPE, 0>(w[1]), at_pair<TYPE, 1>(w[1]));
-                const uint4 hi4 = make_uint4(at_pair<TYPE, 0>(w[2]), at_pair<TYPE, 1>(w[2]), at_pair<TYPE, 0>(w[3]), at_pair<TYPE, 1>(w[3]));
-                const int c = 2 * (piece & 3);
-                // the second panel's lanes store their halves the other way round: no two lanes of a row
-                // on the same banks
+                // the second panel's lanes convert and store their halves the other way round: no two lanes
+                // of a row on the same banks
                 const bool swap = (piece >> 2) != 0;
-                *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap ? c + 1 : c) ^ (kk & 7)) << 4)) = swap ? hi4 : lo4;
-                *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap ? c : c + 1) ^ (kk & 7)) << 4)) = swap ? lo4 : hi4;
+                const int c = 2 * (piece & 3);
+                const uint32_t w[4] = {at_flip<TYPE>(swap ? x[i].z : x[i].x), at_flip<TYPE>(swap ? x[i].w : x[i].y),
+                                       at_flip<TYPE>(swap ? x[i].x : x[i].z), at_flip<TYPE>(swap ? x[i].y : x[i].w)};
+                *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap ? c + 1 : c) ^ (kk & 7)) << 4)) =
+                    make_uint4(at_pair<TYPE, 0>(w[0]), at_pair<TYPE, 1>(w[0]), at_pair<TYPE, 0>(w[1]), at_pair<TYPE, 1>(w[1]));
+                *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap ? c : c + 1) ^ (kk & 7)) << 4)) =
+                    make_uint4(at_pair<TYPE, 0>(w[2]), at_pair<TYPE, 1>(w[2]), at_pair<TYPE, 0>(w[3]), at_pair<TYPE, 1>(w[3]));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -636,41 +651,63 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     if (threadIdx.x == 0 && *abort_flag) sb_latch(a.st, SB_ERR_TIMEOUT, SBK_KV8);
 }
 
-// The pieces of an item that lies in several shares, in their order. Block (c, y, z): the item that the
-// border before share c + 1 cuts, if no earlier border does; 32 of its rows, 32 of its columns.
+// The pieces of an item that lies in several shares, in their order. Block (c, y): the item that the
+// border before share c + 1 cuts, if no earlier border does; 32 of its rows, eight threads a row, a
+// thread every eighth four columns. The chain of dependent reads (share, item, sums) is what a block
+// takes, so all columns go through it together (a block per 32 columns took 20 us for 4
+// requests of up to 1024 tokens). What the plan says is read before the products have ended.
+template <int DP>
 __global__ void __launch_bounds__(256)
 kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
-    const int c = blockIdx.x + 1;
+    constexpr int NQ = DP / 32;
+    const int c = blockIdx.x + 1, D = a.g.dim;
     const int4 s = w.start[c];
-    if (s.x < 0 || s.z <= PR_EXTRA) return;                          // the border lies before the first tile
     const long long share = w.share[0], from = c * share - s.z;      // the item's first unit of all
-    const int c0 = (int)((from + PR_EXTRA) / share);                 // the share with its first tile
-    if (c != c0 + 1) return;
-    const AtItem it = at_item<2 * PR_ROWS, PR_KEYS>(a, s.x);
-    const int c1 = (int)((from + it.steps + PR_EXTRA - 1) / share), D = a.g.dim;
-    const int r = 32 * blockIdx.y + threadIdx.x / 8, quad = 8 * blockIdx.z + threadIdx.x % 8;
-    if (r >= it.nrow || 4 * quad >= D) return;
+    // a border that lies before the first tile, or behind one that cuts the same item, has nothing to add
+    bool mine = s.x >= 0 && s.z > PR_EXTRA;
+    const int c0 = mine ? (int)((from + PR_EXTRA) / share) : 0;      // the share with its first tile
+    mine = mine && c == c0 + 1;
+    AtItem it{};
+    if (mine) it = at_item<2 * PR_ROWS, PR_KEYS>(a, s.x);
+    const int r = 32 * blockIdx.y + threadIdx.x / 8, quad0 = threadIdx.x % 8;
+    at_after_previous();
+    if (!mine || r >= it.nrow) return;
+    const int c1 = (int)((from + it.steps + PR_EXTRA - 1) / share);
     float m = -INFINITY, l = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+    float4 v[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int x = c0; x <= c1; ++x) {
         // the first piece of that share, unless the item starts inside the share
         const int64_t slot = 2 * (int64_t)x + (from > x * share ? 1 : 0);
         const float2 ml = a.part_ml[slot * (2 * PR_ROWS) + r];
-        const float4 y = *reinterpret_cast<const float4*>(a.part + ((slot * (D / 4) + quad) * (2 * PR_ROWS) + r) * 4);
+        float4 y[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (4 * (quad0 + 8 * q) < D)
+                y[q] = *reinterpret_cast<const float4*>(a.part + ((slot * (D / 4) + quad0 + 8 * q) * (2 * PR_ROWS) + r) * 4);
+        }
         const float mn = fmaxf(m, ml.x);
         const float f = m == -INFINITY ? 0.f : at_exp2(m - mn), h = ml.x == -INFINITY ? 0.f : at_exp2(ml.x - mn);
         l = fmaf(l, f, ml.y * h);
-        v.x = fmaf(v.x, f, y.x * h); v.y = fmaf(v.y, f, y.y * h); v.z = fmaf(v.z, f, y.z * h); v.w = fmaf(v.w, f, y.w * h);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            v[q].x = fmaf(v[q].x, f, y[q].x * h); v[q].y = fmaf(v[q].y, f, y[q].y * h);
+            v[q].z = fmaf(v[q].z, f, y[q].z * h); v[q].w = fmaf(v[q].w, f, y[q].w * h);
+        }
         m = mn;
     }
     const int row = it.r0 + r;
     const int64_t tok = it.rq.row0 + a.by_group.quot(row);
     const int h = s.y * a.group + a.by_group.rem(row);
     const float f = at_norm(l);
-    *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + 4 * quad) =
-        make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
-    if (quad == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+        if (4 * (quad0 + 8 * q) < D)
+            *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + 4 * (quad0 + 8 * q)) =
+                make_uint2(u32(__floats2bfloat162_rn(v[q].x * f, v[q].y * f)), u32(__floats2bfloat162_rn(v[q].z * f, v[q].w * f)));
+    if (quad0 == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
 }
 
 template <int TYPE, int DP>
@@ -700,10 +737,25 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     a.part_ml = cv.take<float2>(rows);
     kv8_prompt_plan_kernel<<<1, 1024, 0, ctx->stream>>>(a, w);
     SB_LAUNCHED(ctx);
-    kernel<<<w.ctas, PR_THREADS, S::SMEM, ctx->stream>>>(a, w);
+    // The other two are sent off while the kernel before them still runs and wait on the device for its
+    // end (at_after_previous), which hides their launches.
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.stream = ctx->stream;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)w.ctas);
+    cfg.blockDim = dim3(PR_THREADS);
+    cfg.dynamicSmemBytes = S::SMEM;
+    SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, a, w));
     SB_LAUNCHED(ctx);
     if (w.ctas > 1) {
-        kv8_prompt_sum_kernel<<<dim3((unsigned)(w.ctas - 1), 2 * PR_ROWS / 32, (unsigned)((a.g.dim + 31) / 32)), 256, 0, ctx->stream>>>(a, w);
+        cfg.gridDim = dim3((unsigned)(w.ctas - 1), 2 * PR_ROWS / 32);
+        cfg.blockDim = dim3(256);
+        cfg.dynamicSmemBytes = 0;
+        SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kv8_prompt_sum_kernel<DP>, a, w));
         SB_LAUNCHED(ctx);
     }
     return SB_OK;
