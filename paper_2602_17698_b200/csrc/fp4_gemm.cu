@@ -504,9 +504,14 @@ sb_status fg_tile_launch(sb_ctx* ctx, const FgArgs& a, const FgOperand& w, const
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     const int64_t row_tiles = (a.N + FG_ROWS - 1) / FG_ROWS, tok_tiles = (a.M + NT - 1) / NT;
     if (row_tiles > 65535 || tok_tiles > 65535) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 gemm: too many tiles");
-    // segments of the columns: about two CTAs per SM, of at least two slabs each
-    int64_t split = 2 * (int64_t)ctx->sm_count / (row_tiles * tok_tiles);
-    if (split > a.slabs / 2) split = a.slabs / 2;
+    // Segments of the columns where the tiles leave half of the SMs idle: about two CTAs per SM, of at
+    // least four slabs each. The sums of a cluster cost more than half a row of slabs: 4096 -> 14336 (112
+    // tiles) takes 23.9 us in two segments and 16.7 in one for 128 tokens, 14.6 and 13.6 for 32; 14336 ->
+    // 4096 (32 tiles) 16.5 in eight and 18.5 in four for 64; 4096 -> 4096 12.3 in eight (of two slabs), 10.3 in
+    // four for 32.
+    const int64_t tiles = row_tiles * tok_tiles;
+    int64_t split = 2 * tiles <= ctx->sm_count ? 2 * (int64_t)ctx->sm_count / tiles : 1;
+    if (split > a.slabs / 4) split = a.slabs / 4;
     if (split > FG_MAX_SPLIT) split = FG_MAX_SPLIT;
     if (split < 1) split = 1;
     cudaLaunchConfig_t cfg{};

@@ -33,11 +33,13 @@
 
 namespace {
 
-constexpr int AT_PROMPT_FROM = 64;
+// More query rows than this per cache head go to the tcgen05 kernel, which takes 256 at the price of one. Heads of 128,
+// four query rows per token: 4 requests in 200 tokens 19 us there, 26, 39 and 47 here with 12, 24 and 32 rows; one in 8192
+// 37 and 51 with 24 rows, 39 and 68 with 32; but 16 in 2000 58 and 44 with 24 rows, 63 and 62 with 32.
+constexpr int AT_PROMPT_FROM = 24;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
 constexpr int AT_EXTRA = 12;            // what an item costs besides its steps, in steps
-constexpr int AT_LEAST = 4 + AT_EXTRA;  // units of a share at least: a step of every warp
 constexpr float AT_SLACK = 8.f;         // log2 of how far a row's maximum may run ahead of its reference
 constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
 
@@ -112,7 +114,7 @@ kv8_rows_kernel(const AtArgs a) {
         for (int w = 0; w < AT_WARPS; ++w) total += sums[w];
         total *= a.g.heads;
         share = at_div(total + gridDim.x - 1, gridDim.x);
-        if (share < AT_LEAST) share = AT_LEAST;
+        if (share < a.least) share = a.least;
         const long long at = blockIdx.x * share;
         if (at >= total) return;
         long long before = 0;
@@ -628,7 +630,13 @@ sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     // a share per resident CTA, fewer if there cannot be so many shares
     int64_t keys = max_len;
     if (a.window > 0 && keys > a.window + S::ROWS + SB_KV8_BLOCK) keys = a.window + S::ROWS + SB_KV8_BLOCK;
-    const int64_t most = (tiles * ((keys + AT_STEP - 1) / AT_STEP + 1 + AT_EXTRA) + AT_LEAST - 1) / AT_LEAST;
+    const int64_t steps = (keys + AT_STEP - 1) / AT_STEP + 1;
+    // Units of a share at least. A step takes a share about 0.22 us, and every piece of an item 0.22 us per
+    // eight rows when they are added: u units a share cost u + steps NR / u. Fixed shares of 6, 16 and
+    // 28 took 12, 16 and 18 us for one request in 2000 (8 rows), 43, 35 and 31 for one in 8192 (16 rows).
+    a.least = 6;
+    while ((int64_t)a.least * a.least < steps * NR) ++a.least;
+    const int64_t most = (tiles * (steps + AT_EXTRA) + a.least - 1) / a.least;
     const int64_t ctas = most < (int64_t)S::CTAS * ctx->sm_count ? most : (int64_t)S::CTAS * ctx->sm_count;
     a.row_tiles = (int)row_tiles;
     a.by_row_tiles = KvDiv(a.row_tiles);
@@ -663,8 +671,7 @@ sb_status rows_by_count(sb_ctx* ctx, const AtArgs& a, int64_t max_new, int64_t m
     const int64_t rows = max_new * a.group;
     if (rows <= 8) return rows_launch<TYPE, DP, 1>(ctx, a, max_new, max_len);
     if (rows <= 16 || DP == 256) return rows_launch<TYPE, DP, 2>(ctx, a, max_new, max_len);
-    if (rows <= 24) return rows_launch<TYPE, DP, DP == 256 ? 2 : 3>(ctx, a, max_new, max_len);
-    return rows_launch<TYPE, DP, DP == 256 ? 2 : 4>(ctx, a, max_new, max_len);
+    return rows_launch<TYPE, DP, DP == 256 ? 2 : 3>(ctx, a, max_new, max_len);
 }
 template <int TYPE>
 sb_status rows_by_dim(sb_ctx* ctx, const AtArgs& a, int64_t max_new, int64_t max_len) {
@@ -704,7 +711,7 @@ extern "C" sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, co
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;
     // Many query rows per cache head: a key is converted once for 256 rows and the products run at the
-    // rate of tcgen05; few: the cache's bytes bound the call and 8 to 32 rows per warp are enough.
+    // rate of tcgen05; few: the cache's bytes bound the call and 8 to 24 rows per warp are enough.
     if (max_new * a.group > AT_PROMPT_FROM && cache->dim <= 128) return kv8_prompt(ctx, a, cache->type, max_new, max_len);
     return cache->type == SB_KV_INT8 ? rows_by_dim<SB_KV_INT8>(ctx, a, max_new, max_len) : rows_by_dim<SB_KV_E4M3>(ctx, a, max_new, max_len);
 }

@@ -21,6 +21,7 @@ struct AtArgs {
     float* part;                 // two slots per CTA: unnormalised sums of an item's piece
     float2* part_ml;             // and its rows' (reference, sum of weights)
     unsigned* done;              // per item: pieces finished
+    int least;                   // units of a share at least
     SbDeviceState* st;
 };
 

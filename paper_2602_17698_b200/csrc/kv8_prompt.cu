@@ -33,7 +33,7 @@ constexpr int PR_THREADS = 16 * 32;       // warp 15 only lends its registers
 constexpr int PR_REGS_SOFTMAX = 136, PR_REGS_CONVERT = 120, PR_REGS_REST = 120;
 static_assert(8 * PR_REGS_SOFTMAX + 4 * PR_REGS_CONVERT + 4 * PR_REGS_REST <= 16 * 128, "what the block was launched with");
 constexpr int PR_EXTRA = 6;              // what an item costs besides its key tiles, in key tiles
-constexpr int PR_LEAST = 1 + PR_EXTRA;              // units of a share at least
+constexpr int PR_LEAST = 4;              // units of a share at least
 constexpr float PR_SLACK = 8.f;          // log2 of how far a row's maximum may run ahead of its reference
 constexpr float PR_LIMIT = 256.f;        // largest sum of a half tile's weights before the row's reference moves
 
