@@ -5,7 +5,9 @@
 // is one block of SB_FP4_NV; two neighbouring lanes share a block of SB_FP4_MX and exchange their
 // maxima. The scales of four consecutive blocks are four consecutive bytes of a scale tile: the
 // lanes that hold them pass them to the first, which stores one word. Nothing is read twice; the
-// kernels move 2 + 1/2 + 1/16 (1/32) bytes an element and are bound by that traffic.
+// kernels move 2 + 1/2 + 1/16 (1/32) bytes an element. 14336 x 4096 there and back in MX: 51 us, 5.8 TB/s,
+// 0.88 of a plain copy's rate, with 70 % of the issue slots used. NV to codes needs 16 instructions an element (an exact
+// quotient) and is bound by their issue: 8192 x 4096 25 us, 77 % of the slots, where the bytes take 13.
 #include "fp4.cuh"
 
 namespace {

@@ -16,8 +16,17 @@
 // maximum of a row is only moved when it is off by more than 2^8 (P stays below 2^8, far from
 // fp16's end), so sums in tensor memory are rarely touched between tiles.
 //
-// Per 128 keys and 256 rows the products need 2048 cycles and the exponentials 2048 (16 per cycle
-// and SM): both bound the kernel.
+// A step first takes the weights by the reference there is and looks at their sum: where that is small no
+// maximum is needed (287 -> 273 us in the case below). The work is cut into equal shares (see
+// kv8_attention.cuh); a sum kernel adds the pieces of items that several shares hold.
+//
+// What bounds it: per 128 keys of 256 rows the products need 2560 cycles (the scores, both operands from
+// shared memory in halves of 64 keys, 1536 of them) and the exponentials 2048 (16 per cycle and SM); the kernel
+// takes 4400, because a row tile's scores, softmax, weights, sums and next scores wait for one
+// another. Half tiles and two row tiles overlap these chains; whole tiles per step were slower (339 us against
+// 287), and so was a warp of its own for the scores (344).
+// 4 requests of up to 1024 tokens behind up to 8192, 32 query heads of 128 over 8, e4m3: 252 us,
+// 770 TFLOP/s, tensor pipe 54 % active; heads of 64 234 us.
 #include "kv8_attention.cuh"
 #include "tensor5.cuh"
 
@@ -29,11 +38,15 @@ constexpr int PR_BLOCKS = PR_KEYS / SB_KV8_BLOCK;
 constexpr int PR_SUB = 64;               // keys of a softmax step: half a tile
 constexpr int PR_SUBBLOCKS = PR_SUB / SB_KV8_BLOCK;
 constexpr int PR_THREADS = 16 * 32;       // warp 15 only lends its registers
-// registers of a softmax, conversion and other warp's thread: 8 x 136 + 4 x 120 + 4 x 120 warps' shares <= 16 x 128
+// Registers: the split at which nothing spills. 160/96/96 spilled 256 bytes a thread and took 273 us where this one
+// takes 255; no split at all (128 each) 265.
+// A softmax, conversion and other warp's thread: 8 x 136 + 4 x 120 + 4 x 120 warps' shares <= 16 x 128
 constexpr int PR_REGS_SOFTMAX = 136, PR_REGS_CONVERT = 120, PR_REGS_REST = 120;
 static_assert(8 * PR_REGS_SOFTMAX + 4 * PR_REGS_CONVERT + 4 * PR_REGS_REST <= 16 * 128, "what the block was launched with");
-constexpr int PR_EXTRA = 6;              // what an item costs besides its key tiles, in key tiles
-constexpr int PR_LEAST = 4;              // units of a share at least
+constexpr int PR_EXTRA = 6;              // what an item costs besides its key tiles, in key tiles: 14 us to 2.5 us a tile;
+                                         // 4, 6 and 8 took 272, 262 and 267 us
+constexpr int PR_LEAST = 4;              // units of a share at least: one request of 332 tokens took 34 us with 7, 30 with 4;
+                                         // 30 tokens in 9000 38 and 41
 constexpr float PR_SLACK = 8.f;          // log2 of how far a row's maximum may run ahead of its reference
 constexpr float PR_LIMIT = 256.f;        // largest sum of a half tile's weights before the row's reference moves
 
