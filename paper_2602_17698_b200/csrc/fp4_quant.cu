@@ -5,8 +5,8 @@
 // is one block of SB_FP4_NV; two neighbouring lanes share a block of SB_FP4_MX and exchange their
 // maxima. The scales of four consecutive blocks are four consecutive bytes of a scale tile: the
 // lanes that hold them pass them to the first, which stores one word. Nothing is read twice; the
-// kernels move 2 + 1/2 + 1/16 (1/32) bytes an element. 14336 x 4096 there and back in MX: 51 us, 5.8 TB/s,
-// 0.88 of a plain copy's rate, with 70 % of the issue slots used. NV to codes needs 16 instructions an element (an exact
+// kernels move 2 + 1/2 + 1/16 (1/32) bytes an element. 14336 x 4096 there and back in MX: 51 to 53 us, 5.7 TB/s,
+// 0.87 of a plain copy's rate, with 70 % of the issue slots used. NV to codes needs 16 instructions an element (an exact
 // quotient) and is bound by their issue: 8192 x 4096 25 us, 77 % of the slots, where the bytes take 13.
 #include "fp4.cuh"
 
@@ -129,11 +129,12 @@ fp4_quantize_kernel(const __nv_bfloat16* __restrict__ X, int64_t R, int64_t C, i
     }
 }
 
-template <int FORMAT, int U>
+// LOOSE: rows of Y are aligned to 2 or 4 bytes only.
+template <int FORMAT, int U, bool LOOSE>
 __global__ void __launch_bounds__(FQ_THREADS)
 fp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t R, int64_t C,
                       const FqDiv div, int64_t tiles, const float* __restrict__ tensor_scale, __nv_bfloat16* __restrict__ Y,
-                      int64_t ldy, int wide) {
+                      int64_t ldy, int align) {
     const float g = FORMAT == SB_FP4_NV && tensor_scale ? __ldg(tensor_scale) : 1.f;
     const int64_t first = (int64_t)blockIdx.x * (FQ_THREADS * U) + threadIdx.x;
     uint2 q[U];
@@ -148,27 +149,61 @@ fp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
             s[u] = scales[fp4_scale_at(row[u], FORMAT == SB_FP4_MX ? piece[u] >> 1 : piece[u], tiles)];
         }
     }
+    __shared__ uint4 words[LOOSE ? FQ_THREADS / 32 : 1][2 * 32];
+    const int lane = threadIdx.x & 31;
+    uint4* const mine = words[LOOSE ? threadIdx.x >> 5 : 0];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (row[u] >= R) break;
-        const float d = FORMAT == SB_FP4_MX ? e8m0_value(s[u]) : e4m3_value(s[u]) * g;
-        uint32_t h[2][4], o[8];
-        fp4_unpack8(q[u].x, h[0]);
-        fp4_unpack8(q[u].y, h[1]);
+        const bool in = row[u] < R;
+        uint32_t o[8] = {};
+        if (in) {
+            const float d = FORMAT == SB_FP4_MX ? e8m0_value(s[u]) : e4m3_value(s[u]) * g;
+            uint32_t h[2][4];
+            fp4_unpack8(q[u].x, h[0]);
+            fp4_unpack8(q[u].y, h[1]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i >> 2][i & 3]));
+                o[i] = u32(__floats2bfloat162_rn(f.x * d, f.y * d));
+            }
+        }
+        const int64_t c0 = (int64_t)piece[u] * 16, at = row[u] * ldy + c0;
+        const int left = in ? (int)(C - c0 < 16 ? (C > c0 ? C - c0 : 0) : 16) : 0;
+        if (!LOOSE) {
+            if (left == 16) {
+                if (align >= 32) st_global32(Y + at, o);
+                else {
+                    *reinterpret_cast<uint4*>(Y + at) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4*>(Y + at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+            } else {
+                uint16_t* p = reinterpret_cast<uint16_t*>(Y + at);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i < left) p[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+            }
+            continue;
+        }
+        // Rows that are aligned no better than their elements: the warp's 512 values change lanes, so that
+        // a store of 32 lanes covers 128 consecutive bytes: 14336 x 4090 there and back (MX) 75 us, 365 with every lane
+        // storing its own 16 values one by one.
+        mine[2 * lane] = make_uint4(o[0], o[1], o[2], o[3]);
+        mine[2 * lane + 1] = make_uint4(o[4], o[5], o[6], o[7]);
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i >> 2][i & 3]));
-            o[i] = u32(__floats2bfloat162_rn(f.x * d, f.y * d));
+            const int from = 4 * i + (lane >> 3), k = 2 * (lane & 7);
+            const int64_t to = __shfl_sync(0xffffffffu, (long long)at, from) + k;
+            const int there = __shfl_sync(0xffffffffu, left, from) - k;
+            const uint32_t w = reinterpret_cast<const uint32_t*>(mine)[32 * i + lane];
+            uint16_t* p = reinterpret_cast<uint16_t*>(Y + to);
+            if (align >= 4 && there >= 2) *reinterpret_cast<uint32_t*>(p) = w;
+            else {
+                if (there >= 1) p[0] = (uint16_t)w;
+                if (there >= 2) p[1] = (uint16_t)(w >> 16);
+            }
         }
-        const int64_t c0 = (int64_t)piece[u] * 16;
-        __nv_bfloat16* y = Y + row[u] * ldy + c0;
-        if (wide && c0 + 16 <= C) st_global32(y, o);
-        else {
-            uint16_t* p = reinterpret_cast<uint16_t*>(y);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (c0 + i < C) p[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
-        }
+        __syncwarp();
     }
 }
 
@@ -234,12 +269,19 @@ extern "C" sb_status sb_fp4_dequantize(sb_ctx* ctx, const uint8_t* codes, const 
     if (total >= (1ll << 37)) return sb_fail(ctx, SB_ERR_SHAPE, "fp4 dequantize: too many elements");
     SB_CUDA(ctx, cudaSetDevice(ctx->device));
     auto* y = static_cast<__nv_bfloat16*>(Y);
-    const int wide = ldy % 16 == 0 && (reinterpret_cast<uintptr_t>(Y) & 31) == 0;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(Y) | (uintptr_t)(2 * ldy);       // what every row is aligned to
+    const int align = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
     const bool many = fq_many(ctx, total);
     const unsigned blocks = fq_blocks(total, many);
-    auto launch = [&](auto kernel) { kernel<<<blocks, FQ_THREADS, 0, ctx->stream>>>(codes, scales, R, C, div, tiles, tensor_scale, y, ldy, wide); };
-    if (format == SB_FP4_MX) many ? launch(fp4_dequantize_kernel<SB_FP4_MX, FQ_MANY>) : launch(fp4_dequantize_kernel<SB_FP4_MX, 1>);
-    else many ? launch(fp4_dequantize_kernel<SB_FP4_NV, FQ_MANY>) : launch(fp4_dequantize_kernel<SB_FP4_NV, 1>);
+    auto launch = [&](auto kernel) { kernel<<<blocks, FQ_THREADS, 0, ctx->stream>>>(codes, scales, R, C, div, tiles, tensor_scale, y, ldy, align); };
+    auto by_size = [&](auto one, auto four) { many ? launch(four) : launch(one); };
+    if (format == SB_FP4_MX) {
+        if (align >= 16) by_size(fp4_dequantize_kernel<SB_FP4_MX, 1, false>, fp4_dequantize_kernel<SB_FP4_MX, FQ_MANY, false>);
+        else by_size(fp4_dequantize_kernel<SB_FP4_MX, 1, true>, fp4_dequantize_kernel<SB_FP4_MX, FQ_MANY, true>);
+    } else {
+        if (align >= 16) by_size(fp4_dequantize_kernel<SB_FP4_NV, 1, false>, fp4_dequantize_kernel<SB_FP4_NV, FQ_MANY, false>);
+        else by_size(fp4_dequantize_kernel<SB_FP4_NV, 1, true>, fp4_dequantize_kernel<SB_FP4_NV, FQ_MANY, true>);
+    }
     SB_LAUNCHED(ctx);
     return SB_OK;
 }
