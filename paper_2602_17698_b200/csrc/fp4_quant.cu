@@ -154,7 +154,8 @@ fp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
     uint4* const mine = words[LOOSE ? threadIdx.x >> 5 : 0];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const bool in = row[u] < R;
+        if (!LOOSE && row[u] >= R) break;
+        const bool in = !LOOSE || row[u] < R;
         uint32_t o[8] = {};
         if (in) {
             const float d = FORMAT == SB_FP4_MX ? e8m0_value(s[u]) : e4m3_value(s[u]) * g;
