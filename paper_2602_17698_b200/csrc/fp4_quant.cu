@@ -169,14 +169,15 @@ fp4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
             }
         }
         const int64_t c0 = (int64_t)piece[u] * 16, at = row[u] * ldy + c0;
+        if (!LOOSE && align == 32 && c0 + 16 <= C) {
+            st_global32(Y + at, o);
+            continue;
+        }
         const int left = in ? (int)(C - c0 < 16 ? (C > c0 ? C - c0 : 0) : 16) : 0;
         if (!LOOSE) {
             if (left == 16) {
-                if (align >= 32) st_global32(Y + at, o);
-                else {
-                    *reinterpret_cast<uint4*>(Y + at) = make_uint4(o[0], o[1], o[2], o[3]);
-                    *reinterpret_cast<uint4*>(Y + at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-                }
+                *reinterpret_cast<uint4*>(Y + at) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(Y + at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
             } else {
                 uint16_t* p = reinterpret_cast<uint16_t*>(Y + at);
 #pragma unroll
