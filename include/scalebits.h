@@ -447,6 +447,7 @@ sb_status sb_kv8_read(sb_ctx* ctx, const sb_kv8_cache* cache, int64_t total, con
  * lse[i][h] (or NULL): the natural log of the sum of exp(scale q k); a query that sees no key
  * gets O = 0 and lse = -inf.  One new token per request (decode), a few (drafts) or whole
  * prompts; max_len: at least every lens[b] (it decides how the keys are split, nothing else).
+ * scale: any sign.
  * Queries are multiplied in fp16 after an exact power-of-two scaling per row, weights of a key
  * are rounded to fp16, sums and softmax statistics are fp32.
  * Q, O: bf16, element (token, head, d) at token * token_stride + head * head_stride + d; strides

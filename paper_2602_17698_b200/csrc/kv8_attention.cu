@@ -256,11 +256,11 @@ kv8_rows_kernel(const AtArgs a) {
             for (int c = 0; c < DP / 64; ++c) amax = max(amax, max(qw[i][c] & 0x7fffu, (qw[i][c] >> 16) & 0x7fffu));
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            const float up = at_query_scale(amax);
+            const float up = at_query_scale(amax), by = at_signed(up, a.scale_log2);
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c)
-                *reinterpret_cast<uint32_t*>(qrow + 128 * c + 4 * lane) = at_half2(bf16lo(qw[i][c]) * up, bf16hi(qw[i][c]) * up);
-            if (lane == 0) reinterpret_cast<float*>(smem + S::F_AT)[r] = __fdiv_rn(a.scale_log2, up);
+                *reinterpret_cast<uint32_t*>(qrow + 128 * c + 4 * lane) = at_half2(bf16lo(qw[i][c]) * by, bf16hi(qw[i][c]) * by);
+            if (lane == 0) reinterpret_cast<float*>(smem + S::F_AT)[r] = __fdiv_rn(fabsf(a.scale_log2), up);
         }
         __syncthreads();
         float fq[NR][2];

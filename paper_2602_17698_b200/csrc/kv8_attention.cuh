@@ -16,7 +16,7 @@ struct AtArgs {
     KvDiv by_group;
     int row_tiles;               // of a request with max_new new tokens
     KvDiv by_row_tiles;
-    float scale_log2;            // softmax scale * log2(e)
+    float scale_log2;            // softmax scale * log2(e); kernels take its sign into the queries (at_query_scale)
     int window;
     float* part;                 // two slots per CTA: unnormalised sums of an item's piece
     float2* part_ml;             // and its rows' (reference, sum of weights)
@@ -144,11 +144,14 @@ __device__ __forceinline__ uint32_t at_pair(uint32_t w) {
     }
     return e4m3x2_to_f16x2(HALF ? w >> 16 : w);
 }
-// power of two by which a bf16 query row with largest element (as bits) amax is scaled into fp16
+// power of two by which a bf16 query row with largest element (as bits) amax is scaled into fp16. Queries are
+// multiplied with at_signed of it, scores with |scale| over it: the factor of a block's scores is never negative, so
+// the largest score of a block is the largest product's.
 __device__ __forceinline__ float at_query_scale(uint32_t amax) {
     const int ex = max(14, min(254, (int)(amax >> 7)));              // largest element in 2^(ex - 127) [1, 2)
     return __uint_as_float((uint32_t)min(254, 267 - ex) << 23);
 }
+__device__ __forceinline__ float at_signed(float up, float scale_log2) { return copysignf(up, scale_log2); }
 // running power of two that is not below a value scale; 2^-e of such a 2^e
 __device__ __forceinline__ float at_value_ref(float vmax) {
     return __uint_as_float(max((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u, 0x00800000u));

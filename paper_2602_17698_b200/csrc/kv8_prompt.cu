@@ -325,18 +325,18 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                     uint32_t m = __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
 #pragma unroll
                     for (int o = 1; o < LANES; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    const float up = at_query_scale(max(m & 0xffffu, m >> 16));
+                    const float up = at_query_scale(max(m & 0xffffu, m >> 16)), by = at_signed(up, a.scale_log2);
                     const int rr = (warp & 3) * 32 + i * RPI + sub;
                     if (c == 0) factor[rr] = up;
                     *reinterpret_cast<uint4*>(q0 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
-                        make_uint4(at_half2(bf16lo(x[i].x) * up, bf16hi(x[i].x) * up), at_half2(bf16lo(x[i].y) * up, bf16hi(x[i].y) * up),
-                                   at_half2(bf16lo(x[i].z) * up, bf16hi(x[i].z) * up), at_half2(bf16lo(x[i].w) * up, bf16hi(x[i].w) * up));
+                        make_uint4(at_half2(bf16lo(x[i].x) * by, bf16hi(x[i].x) * by), at_half2(bf16lo(x[i].y) * by, bf16hi(x[i].y) * by),
+                                   at_half2(bf16lo(x[i].z) * by, bf16hi(x[i].z) * by), at_half2(bf16lo(x[i].w) * by, bf16hi(x[i].w) * by));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) t5_bar_arrive(t5_smem(qready + qt));
             }
-            const float fq = __fdiv_rn(a.scale_log2, reinterpret_cast<const float*>(smem + S::F_AT)[r]);
+            const float fq = __fdiv_rn(fabsf(a.scale_log2), reinterpret_cast<const float*>(smem + S::F_AT)[r]);
             // (a thread without a row has queries of zeros, and its results go nowhere)
             const int pos = it.rq.past + a.by_group.quot(row);
             // positions of the tile's first and last row decide which key tiles need a mask
