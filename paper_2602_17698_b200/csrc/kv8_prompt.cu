@@ -232,7 +232,8 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + S::BAR_AT);
     // raw tiles: landed, converted; converted tiles: there, multiplied; per row tile (and half of a key
     // tile): scores, weights, sums; all sums of a piece.  A wait tells a phase from its neighbours only
-    // (one bit), so every barrier is waited for by someone who cannot be two phases away.
+    // (one bit), so every barrier is waited for by someone who cannot be two phases away: the next phases wait for
+    // something he does later, and what he has waited for before holds the phase before to have ended.
     unsigned long long *raw_full = bars, *raw_empty = bars + 4, *full = bars + 8, *empty = bars + 12, *sfull = bars + 16,
                        *pfull = bars + 20, *odone = bars + 24, *scfull = bars + 26, *qready = bars + 30, *last = bars + 32, *fin = bars + 34;
     unsigned* tmem_slot = reinterpret_cast<unsigned*>(bars + 36);
@@ -290,14 +291,16 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         const unsigned lanes = (unsigned)((warp & 3) * 32) << 16;
         const unsigned ts = tmem + lanes + S::S_COL + qt * 128, to = tmem + lanes + S::O_COL + qt * DP;
         int tiles_all = 0, tiles_mine = 0, pieces = 0;               // key tiles and pieces so far (of this row tile)
-        bool ok = true;
+        bool ok = true, skipped = false;
         for (bool more = true; more && ok; more = wk.next(a), ++tiles_all) {
             const AtItem& it = wk.it;
             const int count = wk.count;
             tiles_all += count - 1;
             const int base_all = tiles_all - (count - 1);
-            if (it.nrow <= qt * PR_ROWS) {                           // no rows, but no phase of a barrier is left out
-                for (int j = 0; ok && j < count; ++j) ok = wait(scfull + ((base_all + j) & 3), (base_all + j) >> 2);
+            // No rows: nothing of these tiles waits for these warps, so they must not wait for a phase of them either (two
+            // phases late they would wait for one that may never come).
+            if (it.nrow <= qt * PR_ROWS) {
+                skipped = true;
                 continue;
             }
             const int r = threadIdx.x, row = it.r0 + r;              // row of the item, of the request
@@ -344,7 +347,11 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int pos_hi = it.rq.past + a.by_group.quot(it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1);
             const int k0 = it.lo + wk.step0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
             float m = -INFINITY, l = 0.f, vref = 0.f, inv = 0.f;
-            ok = wait(scfull + (base_all & 3), base_all >> 2);
+            // After tiles without rows the scales' phase before this one need not have ended. It has once there are scores: a
+            // tile's scales come before its keys are converted.
+            if (skipped) ok = wait(sfull + 2 * qt, tiles_mine);
+            skipped = false;
+            ok = ok && wait(scfull + (base_all & 3), base_all >> 2);
             for (int n = 0; ok && n < 2 * count; ++n) {              // halves of the key tiles
                 const int j = n >> 1, u = n & 1;
                 ok = wait(sfull + 2 * qt + u, tiles_mine + j);
