@@ -414,14 +414,14 @@ enum { SB_KV_INT8 = 0, SB_KV_E4M3 = 1, SB_KV8_BLOCK = 16 };
 typedef struct {                /* host struct, read during the call                             */
     void *k, *v;                /* device codes [pages][heads][page_tokens][dim], 16-byte aligned */
     void *k_scale, *v_scale;    /* device bf16 [pages][heads][page_tokens / 16]                  */
-    const int32_t* table;       /* device page numbers [requests][table_stride]                  */
-    int64_t table_stride;       /* pages a request may have                                      */
+    const int32_t* table;       /* device page numbers: request b's at table + b * table_stride  */
+    int64_t table_stride;       /* 0: all requests share one row (for reading)                   */
     int64_t pages;
     int32_t requests, heads;
     int32_t page_tokens;        /* a multiple of 16                                              */
     int32_t dim;                /* a multiple of 16, 16 .. 256                                   */
     int32_t type;               /* SB_KV_INT8 or SB_KV_E4M3                                      */
-    int32_t reserved;
+    int32_t table_pages;        /* pages a request may have (0: table_stride)                    */
 } sb_kv8_cache;
 
 /* Writes the new tokens.  Per 16 tokens and head: amax over the new tokens' elements,

@@ -73,7 +73,7 @@ class Kv8CacheStruct(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("table", C.c_void_p), ("table_stride", C.c_int64), ("pages", C.c_int64),
                 ("requests", C.c_int32), ("heads", C.c_int32), ("page_tokens", C.c_int32), ("dim", C.c_int32),
-                ("type", C.c_int32), ("reserved", C.c_int32)]
+                ("type", C.c_int32), ("table_pages", C.c_int32)]
 
 
 _lib = None
@@ -211,7 +211,8 @@ _KV8_TYPES = {torch.int8: SB_KV_INT8, torch.float8_e4m3fn: SB_KV_E4M3}
 
 class Kv8Cache:
     """A paged key/value cache in 8 bits: k, v int8 or float8_e4m3fn [pages][heads][page tokens][dim],
-    k_scale, v_scale bf16 [pages][heads][page tokens / 16], table int32 [requests][pages of a request]."""
+    k_scale, v_scale bf16 [pages][heads][page tokens / 16], table int32 [requests][pages of a request]: rows may
+    be part of longer ones (table[:, :n]), or for reading the same one (expand)."""
     __slots__ = ("k", "v", "k_scale", "v_scale", "table", "struct")
 
     def __init__(self, k, v, k_scale, v_scale, table):
@@ -227,11 +228,13 @@ class Kv8Cache:
             raise ValueError("keys, values and scales do not fit one another")
         requests, per = table.shape
         stride, one = table.stride()
+        if per < 1:
+            raise ValueError("a request needs room for a page in the table")
         if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()) or one != 1:
             raise ValueError("the cache's tensors are contiguous")
         self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
         self.struct = Kv8CacheStruct(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), _dev(table), stride if requests > 1 else per,
-                                     pages, requests, heads, page_tokens, dim, kind, 0)
+                                     pages, requests, heads, page_tokens, dim, kind, per)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_tokens: int, dim: int, table, dtype=torch.int8):

@@ -19,6 +19,7 @@ struct Kv8Geom {                 // the parts of sb_kv8_cache that kernels read
     const int32_t* table;
     int64_t table_stride, pages;
     int requests, heads, page_tokens, dim;
+    int most;                    // tokens a request may have: what its pages hold
     const int32_t* starts;
     const int32_t* lens;
     int64_t total;               // rows of the call's dense arguments
@@ -28,18 +29,19 @@ struct Kv8Geom {                 // the parts of sb_kv8_cache that kernels read
 
 inline bool kv8_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+inline int64_t kv8_table_pages(const sb_kv8_cache* c) { return c->table_pages ? c->table_pages : c->table_stride; }
 // host checks shared by the calls on a cache
 inline sb_status kv8_check(sb_ctx* ctx, const char* what, const sb_kv8_cache* c, int64_t total, const int32_t* starts,
                            const int32_t* lens, int64_t max_new) {
     if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->table || !starts || !lens)
         return sb_fail(ctx, SB_ERR_INVALID, "%s: null", what);
-    if (c->requests <= 0 || c->heads <= 0 || c->pages <= 0 || c->table_stride <= 0 || total < 0 || max_new < 0)
+    if (c->requests <= 0 || c->heads <= 0 || c->pages <= 0 || c->table_stride < 0 || kv8_table_pages(c) <= 0 || total < 0 || max_new < 0)
         return sb_fail(ctx, SB_ERR_INVALID, "%s: empty cache or negative sizes", what);
     if (c->type != SB_KV_INT8 && c->type != SB_KV_E4M3) return sb_fail(ctx, SB_ERR_INVALID, "%s: unknown type %d", what, c->type);
     if (c->page_tokens <= 0 || c->page_tokens % SB_KV8_BLOCK || c->dim <= 0 || c->dim % 16 || c->dim > 256)
         return sb_fail(ctx, SB_ERR_SHAPE, "%s: page_tokens a multiple of 16 and dim a multiple of 16 up to 256", what);
     if (c->requests > 65535 || c->heads > 65535 || c->pages >= (1ll << 31) || total >= (1ll << 31) || max_new >= (1ll << 31) ||
-        c->table_stride * c->page_tokens >= (1ll << 31))
+        kv8_table_pages(c) > ((1ll << 31) - 1) / c->page_tokens)
         return sb_fail(ctx, SB_ERR_SHAPE, "%s: at most 65535 requests and heads, and 2^31 pages, rows and tokens of a request", what);
     if (!kv8_aligned16(c->k) || !kv8_aligned16(c->v) || (reinterpret_cast<uintptr_t>(c->k_scale) & 1) || (reinterpret_cast<uintptr_t>(c->v_scale) & 1))
         return sb_fail(ctx, SB_ERR_SHAPE, "%s: 16-byte aligned codes and 2-byte aligned scales", what);
@@ -51,6 +53,7 @@ inline Kv8Geom kv8_geom(const sb_kv8_cache* c, int64_t total, const int32_t* sta
     g.requests = c->requests; g.heads = c->heads; g.page_tokens = c->page_tokens; g.dim = c->dim;
     g.starts = starts; g.lens = lens; g.total = total; g.max_new = (int)max_new;
     g.page = KvDiv(c->page_tokens);
+    g.most = (int)(kv8_table_pages(c) * c->page_tokens);
     return g;
 }
 
@@ -64,7 +67,7 @@ __device__ __forceinline__ bool kv8_request(const Kv8Geom& g, int b, Kv8Request&
     r.n = (int)n;
     r.past = r.len - r.n;
     const bool ok = r.row0 >= 0 && n >= 0 && n <= g.max_new && r.row0 + n <= g.total && r.len >= n &&
-                    r.len <= g.table_stride * g.page_tokens;
+                    r.len <= g.most;
     if (!ok) sb_latch(st, SB_ERR_INVALID, SBK_KV8);
     return ok;
 }

@@ -698,7 +698,8 @@ extern "C" sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, co
     if (q_heads <= 0 || q_heads % cache->heads) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: q_heads must be a multiple of the cache's heads");
     if (max_len < 1 || window < 0 || !(scale == scale))
         return sb_fail(ctx, SB_ERR_INVALID, "kv8 attention: max_len below 1, negative window or scale not a number");
-    if (max_len > cache->table_stride * cache->page_tokens) max_len = cache->table_stride * cache->page_tokens;
+    const int64_t most = kv8_table_pages(cache) * cache->page_tokens;
+    if (max_len > most) max_len = most;
     if (!kv8_aligned16(Q) || !kv8_aligned16(O) || q_token_stride % 8 || q_head_stride % 8 || o_token_stride % 8 || o_head_stride % 8)
         return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: strides that are multiples of 8 and 16-byte aligned bases");
     if (max_new * (q_heads / cache->heads) >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: max_new x query heads too large");
