@@ -573,8 +573,9 @@ class Context:
     @staticmethod
     def _kv8_rows(cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor):
         n = cache.struct.requests
-        if starts.dtype is not torch.int32 or lens.dtype is not torch.int32 or starts.numel() != n + 1 or lens.numel() != n:
-            raise ValueError("starts: int32 [requests + 1], lens: int32 [requests]")
+        if starts.dtype is not torch.int32 or lens.dtype is not torch.int32 or starts.numel() != n + 1 or lens.numel() != n \
+                or not starts.is_contiguous() or not lens.is_contiguous():
+            raise ValueError("starts: contiguous int32 [requests + 1], lens: contiguous int32 [requests]")
         return _dev(starts), _dev(lens)
 
     def kv8_append(self, cache: Kv8Cache, K: torch.Tensor, V: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int):
