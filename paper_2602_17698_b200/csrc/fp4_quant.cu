@@ -76,10 +76,11 @@ __device__ __forceinline__ uint2 fq_codes(uint32_t (&w)[8], float g, float rg, u
         // the two quotients the short way where everything stays in range
         const bool near = g > 0x1p-50f && g < 0x1p30f && am > 0x1p-60f && am < 0x1p60f;
         const float t = near ? div_rn(div_rn(am, 6.f, 0.16666667f), g, rg) : __fdiv_rn(__fdiv_rn(am, 6.f), g);
-        scale = !(g > 0.f) || !(t >= 0.f && t < __uint_as_float(0x7f800000u)) ? 0x7fu : e4m3_of(t);
+        // a quotient beyond the end of fp32 is one beyond the end of e4m3
+        scale = amax >= 0x7f80u || !(g > 0.f) || !(t >= 0.f) ? 0x7fu : e4m3_of(fminf(t, 448.f));
         const float d = scale == 0x7fu ? 0.f : e4m3_value(scale) * g;
-        if (div_in_range(d) || d == 0.f) {
-            // d = 0: every code is 0
+        if ((div_in_range(d) && t < 0x1p100f) || d == 0.f) {
+            // x / d is at most 7 t / 448 where t passes 448, so it stays in range too; d = 0: every code is 0
             const float dd = d > 0.f ? d : 1.f, r1 = __frcp_rn(dd);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
