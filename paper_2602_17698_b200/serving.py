@@ -14,7 +14,7 @@ from typing import Callable, Optional
 
 import torch
 
-from .binding import SB_KV8_BLOCK, Context, Fp4Matrix, Kv8Cache
+from .binding import SB_KV8_BLOCK, Context, Fp4Matrix, Kv8Cache, fp4_scale_bytes
 
 
 def tensor_scale(x: torch.Tensor) -> torch.Tensor:
@@ -61,13 +61,16 @@ class QuantizedAttention:
         self.qkv = torch.empty((max_tokens, w_qkv.shape[0]), dtype=torch.bfloat16, device=dev)
         self.att = torch.empty((max_tokens, heads, dim), dtype=torch.bfloat16, device=dev)
         self.y = torch.empty((max_tokens, hidden), dtype=torch.bfloat16, device=dev)
-        self._low = {}                                 # 4-bit workspaces by number of rows
+        # 4-bit workspaces of max_tokens rows by width; a call's matrix is the first part of both tensors
+        self._low = {c: Fp4Matrix.empty(max_tokens, c, fmt, None, dev) for c in (hidden, heads * dim)}
+        self._part = {}                                # the last call's matrix by width
 
     def _in_4_bits(self, x: torch.Tensor, scale) -> Fp4Matrix:
-        key = tuple(x.shape)
-        if key not in self._low:
-            self._low[key] = Fp4Matrix.empty(*key, self.fmt, None, x.device)
-        m = self._low[key]
+        rows, cols = x.shape
+        m = self._part.get(cols)
+        if m is None or m.rows != rows:
+            whole = self._low[cols]
+            m = self._part[cols] = Fp4Matrix(whole.codes[:rows], whole.scales[:fp4_scale_bytes(rows, cols, self.fmt)], rows, cols, self.fmt)
         m.tensor_scale = scale
         return self.ctx.fp4_quantize(x, m)
 
@@ -77,6 +80,8 @@ class QuantizedAttention:
         length with them.  rotate(q, k): called on the projected queries and keys, in place.  Returns
         the block's output (a workspace: valid until the next call)."""
         t, ctx = x.shape[0], self.ctx
+        if not 0 < t <= len(self.y) or x.shape[1] != self.y.shape[1]:
+            raise ValueError("x: [tokens][hidden], one token at least and max_tokens at most")
         nq, nk = self.heads * self.dim, self.kv_heads * self.dim
         qkv = ctx.fp4_gemm(self._in_4_bits(x, self.x_scale), self.w_qkv, out=self.qkv[:t])
         q = qkv[:, :nq].view(t, self.heads, self.dim)
