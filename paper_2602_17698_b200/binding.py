@@ -282,6 +282,17 @@ class Context:
         if st != SB_OK:
             raise SbError(st, lib().sb_last_error(self._h).decode())
 
+    def _result(self, shape, dtype, device) -> torch.Tensor:
+        """Memory for a result of the 4-bit and cache calls: the context's stream writes it, so it comes from what that
+        stream has let go, and it is not given away before the stream that is torch's current one now is done with it."""
+        here = torch.cuda.current_stream(self.device)
+        if here == self.stream:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(self.stream):
+            out = torch.empty(shape, dtype=dtype, device=device)
+        out.record_stream(here)
+        return out
+
     # ---- the C-ABI calls, one method each -------------------------------------------------
     def sync(self):
         self._check(lib().sb_sync(self._h))
@@ -545,7 +556,7 @@ class Context:
     def fp4_dequantize(self, m: Fp4Matrix, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The bf16 values a 4-bit matrix stands for."""
         if out is None:
-            out = torch.empty((m.rows, m.cols), dtype=torch.bfloat16, device=m.codes.device)
+            out = self._result((m.rows, m.cols), torch.bfloat16, m.codes.device)
         R, Cc, ldy = _mat(out)
         if R != m.rows or Cc != m.cols:
             raise ValueError("out and the 4-bit matrix have different sizes")
@@ -559,7 +570,7 @@ class Context:
         if a.cols != b.cols or a.fmt != b.fmt:
             raise ValueError("the two matrices need the same format and number of columns")
         if out is None:
-            out = torch.empty((M, N), dtype=out_dtype, device=a.codes.device)
+            out = self._result((M, N), out_dtype, a.codes.device)
         dtype, shape = out.dtype, out.shape
         ldy, one = out.stride()
         if dtype is not torch.bfloat16 and dtype is not torch.float32 or shape[0] != M or shape[1] != N or one != 1:
@@ -595,7 +606,7 @@ class Context:
         s, n = self._kv8_rows(cache, starts, lens)
         if out is None:
             shape = (int(starts[-1]) if total is None else total, cache.struct.heads, cache.struct.dim)
-            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
+            out = tuple(self._result(shape, torch.bfloat16, cache.k.device) for _ in range(2))
         K, V = out
         tokens, heads, dim = shape = K.shape
         if V.shape != shape or heads != cache.struct.heads or dim != cache.struct.dim or not K.is_contiguous() or not V.is_contiguous() \
@@ -615,12 +626,12 @@ class Context:
             raise ValueError("Q: [tokens][query heads][dim of the cache]")
         q, qt, qh = _heads(Q, "Q")
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=Q.device)
+            out = self._result(shape, torch.bfloat16, Q.device)
         elif out.shape != shape:
             raise ValueError("out: the shape of Q")
         o, ot, oh = _heads(out, "out")
         if lse is None and want_lse:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=Q.device)
+            lse = self._result(shape[:2], torch.float32, Q.device)
         if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or lse.dtype is not torch.float32):
             raise ValueError("lse: contiguous fp32 [tokens][query heads]")
         self._check(lib().sb_kv8_attention(self._h, cache.struct, q, qt, qh, heads, tokens, s, n, max_new, max_len,
