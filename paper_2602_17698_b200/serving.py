@@ -10,11 +10,27 @@ device, so one captured CUDA graph serves a decode batch while its requests grow
 """
 from __future__ import annotations
 
+from contextlib import contextmanager
 from typing import Callable, Optional
 
 import torch
 
 from .binding import SB_KV8_BLOCK, Context, Fp4Matrix, Kv8Cache, fp4_scale_bytes
+
+
+@contextmanager
+def _stream_of(ctx: Context, *inputs: torch.Tensor):
+    """Makes the context's stream torch's current one, behind what the current one has enqueued and ahead of what it will."""
+    here = torch.cuda.current_stream(ctx.device)
+    if here == ctx.stream:
+        yield
+        return
+    ctx.stream.wait_stream(here)
+    for t in inputs:
+        t.record_stream(ctx.stream)
+    with torch.cuda.stream(ctx.stream):
+        yield
+    here.wait_stream(ctx.stream)
 
 
 def tensor_scale(x: torch.Tensor) -> torch.Tensor:
@@ -25,8 +41,9 @@ def tensor_scale(x: torch.Tensor) -> torch.Tensor:
 
 def quantize_weight(ctx: Context, W: torch.Tensor, fmt: str = "nv") -> Fp4Matrix:
     """A bf16 weight [out][in] in 4 bits, with a tensor scale of its own where the format has one."""
-    m = Fp4Matrix.empty(W.shape[0], W.shape[1], fmt, tensor_scale(W) if fmt == "nv" else None, W.device)
-    return ctx.fp4_quantize(W, m)
+    with _stream_of(ctx, W):
+        m = Fp4Matrix.empty(W.shape[0], W.shape[1], fmt, tensor_scale(W) if fmt == "nv" else None, W.device)
+        return ctx.fp4_quantize(W, m)
 
 
 def page_table(lens, page_tokens: int, pages: int, device="cuda") -> torch.Tensor:
@@ -47,7 +64,8 @@ class QuantizedAttention:
 
     w_qkv: bf16 [(heads + 2 kv_heads) dim][hidden], w_o: bf16 [hidden][heads dim].  x_scale, o_scale:
     tensor scales of the block's input and of the attention's output ("nv" only; None: 1, which suits
-    activations of the order of 1).  max_tokens: rows of a call at most."""
+    activations of the order of 1).  max_tokens: rows of a call at most.  Everything runs on the context's stream; where
+    torch's current stream is another, that waits for this one and this one for that."""
 
     def __init__(self, ctx: Context, w_qkv: torch.Tensor, w_o: torch.Tensor, heads: int, kv_heads: int, dim: int, cache: Kv8Cache,
                  max_tokens: int, fmt: str = "nv", x_scale: Optional[torch.Tensor] = None, o_scale: Optional[torch.Tensor] = None):
@@ -58,11 +76,12 @@ class QuantizedAttention:
         self.w_qkv, self.w_o = quantize_weight(ctx, w_qkv, fmt), quantize_weight(ctx, w_o, fmt)
         self.x_scale, self.o_scale = x_scale, o_scale
         dev = w_o.device
-        self.qkv = torch.empty((max_tokens, w_qkv.shape[0]), dtype=torch.bfloat16, device=dev)
-        self.att = torch.empty((max_tokens, heads, dim), dtype=torch.bfloat16, device=dev)
-        self.y = torch.empty((max_tokens, hidden), dtype=torch.bfloat16, device=dev)
-        # 4-bit workspaces of max_tokens rows by width; a call's matrix is the first part of both tensors
-        self._low = {c: Fp4Matrix.empty(max_tokens, c, fmt, None, dev) for c in (hidden, heads * dim)}
+        with _stream_of(ctx):
+            self.qkv = torch.empty((max_tokens, w_qkv.shape[0]), dtype=torch.bfloat16, device=dev)
+            self.att = torch.empty((max_tokens, heads, dim), dtype=torch.bfloat16, device=dev)
+            self.y = torch.empty((max_tokens, hidden), dtype=torch.bfloat16, device=dev)
+            # 4-bit workspaces of max_tokens rows by width; a call's matrix is the first part of both tensors
+            self._low = {c: Fp4Matrix.empty(max_tokens, c, fmt, None, dev) for c in (hidden, heads * dim)}
         self._part = {}                                # the last call's matrix by width
 
     def _in_4_bits(self, x: torch.Tensor, scale) -> Fp4Matrix:
@@ -77,21 +96,23 @@ class QuantizedAttention:
     def __call__(self, x: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int, max_len: int, window: int = 0,
                  rotate: Optional[Callable] = None) -> torch.Tensor:
         """x: bf16 [tokens][hidden], request b's new tokens in rows starts[b] .. starts[b + 1]; lens: its
-        length with them.  rotate(q, k): called on the projected queries and keys, in place.  Returns
-        the block's output (a workspace: valid until the next call)."""
+        length with them.  rotate(q, k): called on the projected queries and keys, in place, with the
+        context's stream as torch's current one.  Returns the block's output (a workspace: valid until
+        the next call)."""
         t, ctx = x.shape[0], self.ctx
         if not 0 < t <= len(self.y) or x.shape[1] != self.y.shape[1]:
             raise ValueError("x: [tokens][hidden], one token at least and max_tokens at most")
         nq, nk = self.heads * self.dim, self.kv_heads * self.dim
-        qkv = ctx.fp4_gemm(self._in_4_bits(x, self.x_scale), self.w_qkv, out=self.qkv[:t])
-        q = qkv[:, :nq].view(t, self.heads, self.dim)
-        k = qkv[:, nq:nq + nk].view(t, self.kv_heads, self.dim)
-        v = qkv[:, nq + nk:].view(t, self.kv_heads, self.dim)
-        if rotate is not None:
-            rotate(q, k)
-        ctx.kv8_append(self.cache, k, v, starts, lens, max_new)
-        att, _ = ctx.kv8_attention(self.cache, q, starts, lens, max_new, max_len, window=window, out=self.att[:t])
-        return ctx.fp4_gemm(self._in_4_bits(att.view(t, nq), self.o_scale), self.w_o, out=self.y[:t])
+        with _stream_of(ctx, x, starts, lens):
+            qkv = ctx.fp4_gemm(self._in_4_bits(x, self.x_scale), self.w_qkv, out=self.qkv[:t])
+            q = qkv[:, :nq].view(t, self.heads, self.dim)
+            k = qkv[:, nq:nq + nk].view(t, self.kv_heads, self.dim)
+            v = qkv[:, nq + nk:].view(t, self.kv_heads, self.dim)
+            if rotate is not None:
+                rotate(q, k)
+            ctx.kv8_append(self.cache, k, v, starts, lens, max_new)
+            att, _ = ctx.kv8_attention(self.cache, q, starts, lens, max_new, max_len, window=window, out=self.att[:t])
+            return ctx.fp4_gemm(self._in_4_bits(att.view(t, nq), self.o_scale), self.w_o, out=self.y[:t])
 
 
 def main() -> None:
