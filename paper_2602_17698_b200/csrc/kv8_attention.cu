@@ -653,14 +653,24 @@ sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     a.part = cv.take<float>(n * a.g.dim);
     a.part_ml = cv.take<float2>(n);
     if (ctx->kv8_done_n < (size_t)tiles) {
-        // zeroed once; every call leaves zeros.  The old counters stay for captured launches.
+        // Zeroed once; every call leaves zeros.  The old counters stay for captured launches.  They are zeroed here and
+        // now, on a stream of their own: in a capture the context's stream would only do it when the graph is replayed.
         const size_t want_n = (size_t)tiles * 2 + 4096;
         unsigned* fresh = nullptr;
         if (cudaMalloc(&fresh, want_n * 4) != cudaSuccess) {
             (void)cudaGetLastError();
             return sb_fail(ctx, SB_ERR_SCRATCH, "kv8 attention: %zu counters", want_n);
         }
-        SB_CUDA(ctx, cudaMemsetAsync(fresh, 0, want_n * 4, ctx->stream));
+        cudaStream_t once = nullptr;
+        cudaError_t e = cudaStreamCreateWithFlags(&once, cudaStreamNonBlocking);
+        if (e == cudaSuccess) e = cudaMemsetAsync(fresh, 0, want_n * 4, once);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(once);
+        if (once) cudaStreamDestroy(once);
+        if (e != cudaSuccess) {
+            (void)cudaGetLastError();
+            cudaFree(fresh);
+            return sb_fail(ctx, SB_ERR_CUDA, "kv8 attention: zeroing %zu counters: %s", want_n, cudaGetErrorString(e));
+        }
         if (ctx->kv8_done) ctx->retired.push_back(ctx->kv8_done);
         ctx->kv8_done = fresh;
         ctx->kv8_done_n = want_n;
