@@ -7,7 +7,7 @@
 // lanes that hold them pass them to the first, which stores one word. Nothing is read twice; the
 // kernels move 2 + 1/2 + 1/16 (1/32) bytes an element. 14336 x 4096 there and back in MX: 51 to 53 us, 5.7 TB/s,
 // 0.87 of a plain copy's rate, with 70 % of the issue slots used. NV to codes needs 16 instructions an element (an exact
-// quotient) and is bound by their issue: 8192 x 4096 25 us, 77 % of the slots, where the bytes take 13.
+// quotient, one number at a time) and is bound by their issue: 8192 x 4096 25 us, 77 % of the slots, where the bytes take 13.
 #include "fp4.cuh"
 
 namespace {

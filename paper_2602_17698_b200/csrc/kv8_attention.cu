@@ -23,7 +23,8 @@
 // Precision: a query row is scaled by a power of two to at most 2^14 and held in fp16 (exact for
 // every element above 2^-28 of the row's largest), scores and sums are fp32, the weight of a key
 // times its value scale, relative to a running power of two, is rounded to fp16 (2^-11): three
-// bits finer than the bf16 result.
+// bits finer than the bf16 result. That rounding is nearly all by which results differ from a form in
+// fp32 (0.0008 of their norm for 64 requests in 8192; both are 0.0017 from 64 bits, bf16's rounding).
 //
 // The work of all requests is cut into equal shares (see kv8_attention.cuh), which every CTA finds by
 // itself from the requests' lengths. Of an item that several shares hold, each leaves unnormalised sums,
@@ -40,7 +41,9 @@ namespace {
 
 // More query rows than this per cache head go to the tcgen05 kernel, which takes 256 at the price of one. Heads of 128,
 // four query rows per token: 4 requests in 200 tokens 19 us there, 26, 39 and 47 here with 12, 24 and 32 rows; one in 8192
-// 37 and 51 with 24 rows, 39 and 68 with 32; but 16 in 2000 58 and 44 with 24 rows, 63 and 62 with 32.
+// 37 and 51 with 24 rows, 39 and 68 with 32; but 16 in 2000 58 and 44 with 24 rows, 63 and 62 with 32. So rows alone do
+// not decide it: few requests would gain from the other kernel below 24 rows already, many lose until 32; the limit
+// is near where many requests change sides. Heads of more than 128 have no kernel there: all their rows run here.
 constexpr int AT_PROMPT_FROM = 24;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
@@ -727,7 +730,9 @@ extern "C" sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, co
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;
     // Many query rows per cache head: a key is converted once for 256 rows and the products run at the
-    // rate of tcgen05; few: the cache's bytes bound the call and 8 to 24 rows per warp are enough.
+    // rate of tcgen05; few: the cache's bytes bound the call and 8 to 24 rows per warp are enough. That kernel's
+    // shared memory holds heads of up to 128; wider ones stay here, where every 16 rows read and convert the cache
+    // again: 4 requests of up to 1024 tokens behind up to 8192 take 3.25 ms with heads of 256, 255 us with heads of 128.
     if (max_new * a.group > AT_PROMPT_FROM && cache->dim <= 128) return kv8_prompt(ctx, a, cache->type, max_new, max_len);
     return cache->type == SB_KV_INT8 ? rows_by_dim<SB_KV_INT8>(ctx, a, max_new, max_len) : rows_by_dim<SB_KV_E4M3>(ctx, a, max_new, max_len);
 }

@@ -26,7 +26,7 @@ struct AtArgs {
 };
 
 
-// kv8_prompt.cu: rows of one cache head on the tensor cores of the fifth generation, dim <= 128
+// kv8_prompt.cu: many rows of one cache head on the tensor cores of the fifth generation, dim <= 128
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len);
 
 #ifdef __CUDACC__
