@@ -449,9 +449,9 @@ sb_status sb_kv8_read(sb_ctx* ctx, const sb_kv8_cache* cache, int64_t total, con
  * prompts; max_len: at least every lens[b] (it decides how the keys are split, nothing else).
  * scale: any sign.
  * Queries are multiplied in fp16 after an exact power-of-two scaling per row; the weight of a key times
- * its value scale, relative to the largest value scale of the request's keys up to there, is rounded to
- * fp16 (to 2^-11 of it, and below 2^-14 to 2^-25: where value scales differ by more than that, what the
- * small ones add is lost under the largest); sums and softmax statistics are fp32.
+ * its value scale is rounded to fp16, relative to the largest such product of the query's keys up to
+ * there (to 2^-11 of it, and below 2^-18 of the largest to 2^-28 of that); sums and softmax statistics
+ * are fp32.
  * Q, O: bf16, element (token, head, d) at token * token_stride + head * head_stride + d; strides
  * multiples of 8, 16-byte aligned bases; lse fp32 [total][q_heads].                             */
 sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, const void* Q_bf16, int64_t q_token_stride,

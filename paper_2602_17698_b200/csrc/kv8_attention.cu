@@ -22,7 +22,7 @@
 //
 // Precision: a query row is scaled by a power of two to at most 2^14 and held in fp16 (exact for
 // every element above 2^-28 of the row's largest), scores and sums are fp32, the weight of a key
-// times its value scale, relative to a running power of two, is rounded to fp16 (2^-11): three
+// times its value scale, relative to a power of two of its row, is rounded to fp16 (2^-11): three
 // bits finer than the bf16 result. That rounding is nearly all by which results differ from a form in
 // fp32 (0.0008 of their norm for 64 requests in 8192; both are 0.0017 from 64 bits, bf16's rounding).
 //
@@ -48,7 +48,6 @@ constexpr int AT_PROMPT_FROM = 24;
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
 constexpr int AT_EXTRA = 12;            // what an item costs besides its steps, in steps
-constexpr float AT_SLACK = 8.f;         // log2 of how far a row's maximum may run ahead of its reference
 constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
 
 __device__ __forceinline__ unsigned at_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -286,8 +285,7 @@ kv8_rows_kernel(const AtArgs a) {
                 for (int nr = 0; nr < NR; ++nr) qf[s][nr] = at_lds64(qlane + (unsigned)(8 * nr * S::QPITCH + 128 * (s >> 2) + 8 * (s & 3)));
         }
 
-        float o[MT][NR][4], m[NR][2], l[NR][2];
-        float vref = 0.f;
+        float o[MT][NR][4], m[NR][2], l[NR][2], inv[NR][2];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -295,7 +293,7 @@ kv8_rows_kernel(const AtArgs a) {
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { m[nr][e] = -INFINITY; l[nr][e] = 0.f; }
+            for (int e = 0; e < 2; ++e) { m[nr][e] = -INFINITY; l[nr][e] = inv[nr][e] = 0.f; }
 
         for (int j = 0; j < mine; ++j) {
             if ((j & (AT_BATCH - 1)) == 0) {
@@ -362,6 +360,7 @@ kv8_rows_kernel(const AtArgs a) {
                     }
                 }
             }
+            const float vmax = fmaxf(vsc[0], vsc[1]);
             const bool edge = key + AT_STEP > rq.past + i0 + 1 || key + AT_STEP > k1 || (a.window > 0 && key <= rq.past + i1 - a.window);
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
@@ -386,14 +385,30 @@ kv8_rows_kernel(const AtArgs a) {
                 // the reference only moves when it is off by more than 2^8: a weight stays below 2^8
                 bool off[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + AT_SLACK || (m[nr][e] == -INFINITY && mx[e] > m[nr][e]);
+                for (int e = 0; e < 2; ++e)
+                    off[e] = mx[e] > m[nr][e] + AT_SLACK || (m[nr][e] == -INFINITY && mx[e] > m[nr][e]) || vmax * inv[nr][e] > AT_TOP;
                 if (__any_sync(0xffffffffu, off[0] || off[1])) {
                     float f[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        f[e] = !off[e] ? 1.f : m[nr][e] == -INFINITY ? 0.f : at_exp2(m[nr][e] - mx[e]);
-                        if (off[e]) m[nr][e] = mx[e];
-                        l[nr][e] *= f[e];
+                        const float ref = fmaxf(m[nr][e], mx[e]);
+                        // the row's largest weight times value scale, block by block
+                        float most = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            float top = fmaxf(s[k][nr][e], s[k][nr][2 + e]);
+#pragma unroll
+                            for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                            most = fmaxf(most, at_exp2(top - ref) * vsc[k]);
+                        }
+                        f[e] = 1.f;
+                        if (off[e]) {
+                            const float down = m[nr][e] == -INFINITY ? 0.f : at_exp2(m[nr][e] - ref), held = at_power_inv(inv[nr][e]) * down;
+                            inv[nr][e] = at_value_inv(most, held, vmax);
+                            m[nr][e] = ref;
+                            l[nr][e] *= down;
+                            f[e] = held * inv[nr][e];
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
@@ -401,26 +416,12 @@ kv8_rows_kernel(const AtArgs a) {
                     }
                 }
             }
-            // value scales relative to a power of two that only grows
-            const float vmax = fmaxf(vsc[0], vsc[1]);
-            if (vmax > vref) {
-                const float fresh = at_value_ref(vmax);
-                const float f = __fdiv_rn(vref, fresh);
-                vref = fresh;
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) o[i][nr][k] *= f;
-            }
-            const float inv = at_value_inv(vref);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float vw = vsc[e] * inv;
                 uint32_t pb[NR][2];
 #pragma unroll
                 for (int nr = 0; nr < NR; ++nr) {
+                    const float vw[2] = {vsc[e] * inv[nr][0], vsc[e] * inv[nr][1]};
                     float p[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -428,8 +429,8 @@ kv8_rows_kernel(const AtArgs a) {
                         p[i] = at_exp2(s[e][nr][i] - (mm == -INFINITY ? 0.f : mm));
                         l[nr][i & 1] += p[i];
                     }
-                    pb[nr][0] = at_transpose(at_half2(p[0] * vw, p[1] * vw));
-                    pb[nr][1] = at_transpose(at_half2(p[2] * vw, p[3] * vw));
+                    pb[nr][0] = at_transpose(at_half2(p[0] * vw[0], p[1] * vw[1]));
+                    pb[nr][1] = at_transpose(at_half2(p[2] * vw[0], p[3] * vw[1]));
                 }
                 constexpr int VP = DP / 128 > 0 ? DP / 128 : 1;          // panels of 128 d
                 constexpr int VW = DP == 64 ? 2 : 4;                     // words a lane takes of a row and panel
@@ -481,12 +482,13 @@ kv8_rows_kernel(const AtArgs a) {
                 const int r = 8 * nr + 2 * t + e;
                 if (g == 0) mlsm[warp * S::ROWS + r] = make_float2(m[nr][e], sum);
                 float* row = osm + (warp * S::ROWS + r) * S::OPITCH;
+                const float back = at_power_inv(inv[nr][e]);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     // o[i][.][e] and [2 + e]: two neighbouring d of row r
                     constexpr int LW = DP == 64 ? 8 : 16;                // d a lane holds per panel
                     const int d = LW * g + 128 * (i / (LW / 2)) + 2 * (i % (LW / 2));
-                    *reinterpret_cast<float2*>(row + d) = make_float2(o[i][nr][e] * vref, o[i][nr][2 + e] * vref);
+                    *reinterpret_cast<float2*>(row + d) = make_float2(o[i][nr][e] * back, o[i][nr][2 + e] * back);
                 }
             }
         __syncthreads();

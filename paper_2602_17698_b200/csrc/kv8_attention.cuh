@@ -152,12 +152,20 @@ __device__ __forceinline__ float at_query_scale(uint32_t amax) {
     return __uint_as_float((uint32_t)min(254, 267 - ex) << 23);
 }
 __device__ __forceinline__ float at_signed(float up, float scale_log2) { return copysignf(up, scale_log2); }
-// running power of two that is not below a value scale; 2^-e of such a 2^e
-__device__ __forceinline__ float at_value_ref(float vmax) {
-    return __uint_as_float(max((__float_as_uint(vmax) + 0x7fffffu) & 0x7f800000u, 0x00800000u));
-}
-__device__ __forceinline__ float at_value_inv(float vref) {
-    return vref > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(vref)) : 0.f;
+// ---- the weights of the second product ----
+// A weight 2^(score - m) times its value scale times `inv`, a power of two per row, is what fp16 holds. A weight is at most
+// 2^8 (AT_SLACK), so a row whose value scales stay below AT_TOP / inv needs no look at them. Where the reference
+// m moves or that is passed, inv is chosen anew: by what the row's keys add, weight and scale together, so that a large
+// scale under a small weight does not push the others out of fp16's range.
+constexpr float AT_SLACK = 8.f;         // log2 of how far a row's maximum may run ahead of its reference
+constexpr float AT_TOP = 128.f;
+// 2^-e of a 2^e (0: none yet)
+__device__ __forceinline__ float at_power_inv(float p) { return p > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(p)) : 0.f; }
+// The new inv: `most` is the largest weight times value scale of the keys now, `held` 1 / inv of the keys so far (by the new
+// reference). The largest becomes 8 to 16; vmax inv stays finite, and inv and its inverse normal numbers.
+__device__ __forceinline__ float at_value_inv(float most, float held, float vmax) {
+    const float top = fmaxf(fmaxf(most, held * 16.f), fmaxf(vmax * 0x1p-96f, 0x1p-115f));
+    return __uint_as_float(0x7f000000u + (4u << 23) - ((__float_as_uint(top) + 0x7fffffu) & 0x7f800000u));
 }
 // the natural log of a row's sum; what its sums are multiplied with
 __device__ __forceinline__ float at_lse(float m, float sum) {

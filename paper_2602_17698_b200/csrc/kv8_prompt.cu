@@ -13,8 +13,8 @@
 // Warps 0-3 and 4-7: softmax of the two tiles; 8-11: conversion; 12 and 14: their products; 13: copies. A softmax
 // step takes half a key tile (64 keys): while it works on one half, the tensor cores multiply the
 // other half's weights and put the next tile's scores in their place. The running
-// maximum of a row is only moved when it is off by more than 2^8 (P stays below 2^8, far from
-// fp16's end), so sums in tensor memory are rarely touched between tiles.
+// maximum of a row is only moved when it is off by more than 2^8 (with value scales P stays below 2^15, inside
+// fp16), so sums in tensor memory are rarely touched between tiles.
 //
 // A step first takes the weights by the reference there is and looks at their sum: where that is small no
 // maximum is needed (287 -> 273 us in the case below). The work is cut into equal shares (see
@@ -47,8 +47,7 @@ constexpr int PR_EXTRA = 6;              // what an item costs besides its key t
                                          // 4, 6 and 8 took 272, 262 and 267 us
 constexpr int PR_LEAST = 4;              // units of a share at least: one request of 332 tokens took 34 us with 7, 30 with 4;
                                          // 30 tokens in 9000 38 and 41
-constexpr float PR_SLACK = 8.f;          // log2 of how far a row's maximum may run ahead of its reference
-constexpr float PR_LIMIT = 256.f;        // largest sum of a half tile's weights before the row's reference moves
+constexpr float PR_LIMIT = 256.f;        // 2^AT_SLACK: largest sum of a half tile's weights before the row's reference moves
 
 template <int DP>
 struct PrShape {
@@ -101,8 +100,9 @@ __device__ __forceinline__ constexpr unsigned pr_idesc(int n, bool b_mn) {
 }
 
 // Column c of a row's 64 scores is seen if from < c <= upto; EDGE: some are not.
-// Largest score of a row, in units of log2 (kf: factor of each 16 columns, not negative).
-__device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const float (&kf)[PR_SUBBLOCKS], int upto, int from) {
+// Largest score of a row and of each 16 columns, in units of log2 (kf: their factors, not negative).
+__device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const float (&kf)[PR_SUBBLOCKS], int upto, int from,
+                                        float (&tops)[PR_SUBBLOCKS]) {
     float mx = -INFINITY;
 #pragma unroll
     for (int h = 0; h < PR_SUBBLOCKS; ++h) {
@@ -121,7 +121,8 @@ __device__ __forceinline__ float pr_max(unsigned (&s)[PR_SUB / 32][32], const fl
         }
         const float top = fmaxf(bm[0], bm[1]);
         // a factor of 0 makes 0 of any score, but no NaN of a block that is masked whole
-        mx = fmaxf(mx, top == -INFINITY ? -INFINITY : top * kf[h]);
+        tops[h] = top == -INFINITY ? -INFINITY : top * kf[h];
+        mx = fmaxf(mx, tops[h]);
     }
     return mx;
 }
@@ -346,7 +347,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int pos_lo = it.rq.past + a.by_group.quot(it.r0 + qt * PR_ROWS);
             const int pos_hi = it.rq.past + a.by_group.quot(it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1);
             const int k0 = it.lo + wk.step0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
-            float m = -INFINITY, l = 0.f, vref = 0.f, inv = 0.f;
+            float m = -INFINITY, l = 0.f, inv = 0.f;
             // After tiles without rows the scales' phase before this one need not have ended. It has once there are scores: a
             // tile's scales come before its keys are converted.
             if (skipped) ok = wait(sfull + 2 * qt, tiles_mine);
@@ -369,9 +370,9 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 const int upto = min(pos, k1 - 1) - key, from = a.window > 0 ? pos - a.window - key : -1;
                 // Where nothing is masked, the weights by the reference there is; their sum says whether it
                 // still does: no weight is above their sum. One above PR_LIMIT (or none: NaN), a mask, a
-                // first key or a larger value scale takes the other way, by the row's maximum.
+                // first key or a value scale too large takes the other way, by the row's maximum.
                 float sum = 0.f;
-                bool again = edge || vmax > vref || __any_sync(0xffffffffu, m == -INFINITY);
+                bool again = edge || __any_sync(0xffffffffu, m == -INFINITY || vmax * inv > AT_TOP);
                 t5_wait_ld();
                 if (!again) {
                     const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
@@ -379,22 +380,20 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                     again = __any_sync(0xffffffffu, !(sum <= PR_LIMIT));
                 }
                 if (again) {
-                    const float mx = pr_max(s, kf, upto, from);
-                    const bool far = mx > m + PR_SLACK || (m == -INFINITY && mx > m);
-                    const bool move = __any_sync(0xffffffffu, far) || vmax > vref;
+                    float tops[PR_SUBBLOCKS];
+                    const float mx = pr_max(s, kf, upto, from, tops);
+                    const bool far = mx > m + AT_SLACK || (m == -INFINITY && mx > m) || vmax * inv > AT_TOP;
                     float f = 1.f;
                     if (far) {
-                        f = m == -INFINITY ? 0.f : at_exp2(m - mx);
-                        m = mx;
-                        l *= f;
+                        const float ref = fmaxf(m, mx), down = m == -INFINITY ? 0.f : at_exp2(m - ref), held = at_power_inv(inv) * down;
+                        const float most = fmaxf(fmaxf(at_exp2(tops[0] - ref) * v4.x, at_exp2(tops[1] - ref) * v4.y),
+                                                 fmaxf(at_exp2(tops[2] - ref) * v4.z, at_exp2(tops[3] - ref) * v4.w));
+                        inv = at_value_inv(most, held, vmax);
+                        m = ref;
+                        l *= down;
+                        f = held * inv;
                     }
-                    if (vmax > vref) {
-                        const float fresh = at_value_ref(vmax);
-                        f *= __fdiv_rn(vref, fresh);
-                        vref = fresh;
-                        inv = at_value_inv(vref);
-                    }
-                    if (move && n > 0) {
+                    if (__any_sync(0xffffffffu, far) && n > 0) {
                         // the sums so far: the products of the half before this one have to be done
                         ok = wait(odone + qt, 2 * tiles_mine + n - 1);
                         if (!ok) break;
@@ -431,7 +430,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int h0 = wk.head * a.group;
             const int64_t tok = it.rq.row0 + a.by_group.quot(row);
             const int h = h0 + a.by_group.rem(row);
-            const float norm = whole ? at_norm(l) * vref : vref;
+            const float back = at_power_inv(inv), norm = whole ? at_norm(l) * back : back;
             const int64_t slot = 2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1);
             // this warp's rows in bf16 where its queries were, in the same order
             unsigned char* o0 = smem + S::Q_AT + qt * S::OPERAND + (warp & 3) * 32 * 128;
