@@ -24,6 +24,8 @@ SB_FP4_MX, SB_FP4_NV = 0, 1
 SB_KV_INT8, SB_KV_E4M3 = 0, 1
 SB_KV8_BLOCK = 16
 FP4_FORMATS = {"mx": SB_FP4_MX, "nv": SB_FP4_NV}
+# a module's attribute is looked up at every use, which the calls of a decode step notice
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 EXPORTS = ["sb_create", "sb_destroy", "sb_sync", "sb_last_error", "sb_kernel_launches", "sb_debug_lookback",
            "sb_checked_build",
@@ -166,7 +168,7 @@ def _bits(bits: Sequence[int]):
 
 
 def _mat(W: torch.Tensor):
-    if W.dim() != 2 or W.dtype != torch.bfloat16 or W.stride(1) != 1:
+    if W.dim() != 2 or W.dtype != _BF16 or W.stride(1) != 1:
         raise ValueError("expected a row-major 2-D bf16 tensor")
     return W.shape[0], W.shape[1], W.stride(0)
 
@@ -221,7 +223,7 @@ class Kv8Cache:
         kind = _KV8_TYPES.get(k.dtype)
         if kind is None or v.dtype is not k.dtype:
             raise TypeError("keys and values are int8 or float8_e4m3fn")
-        if k_scale.dtype is not torch.bfloat16 or v_scale.dtype is not torch.bfloat16 or table.dtype is not torch.int32:
+        if k_scale.dtype is not _BF16 or v_scale.dtype is not _BF16 or table.dtype is not _I32:
             raise TypeError("scales are bf16 and page numbers int32")
         n = k_scale.numel()
         if v.shape != shape or n * SB_KV8_BLOCK != pages * heads * page_tokens or v_scale.numel() != n:
@@ -246,7 +248,7 @@ class Kv8Cache:
 def _heads(x: torch.Tensor, what: str):
     """(address, token stride, head stride) of a bf16 [tokens][heads][dim] tensor."""
     token, head, one = x.stride()
-    if x.dtype is not torch.bfloat16 or one != 1 or not x.is_cuda:
+    if x.dtype is not _BF16 or one != 1 or not x.is_cuda:
         raise ValueError(f"{what}: expected a bf16 [tokens][heads][dim] CUDA tensor with contiguous rows")
     tokens, heads, _ = x.shape
     # the stride of an axis of one element is never used
@@ -573,10 +575,10 @@ class Context:
             out = self._result((M, N), out_dtype, a.codes.device)
         dtype, shape = out.dtype, out.shape
         ldy, one = out.stride()
-        if dtype is not torch.bfloat16 and dtype is not torch.float32 or shape[0] != M or shape[1] != N or one != 1:
+        if dtype is not _BF16 and dtype is not _F32 or shape[0] != M or shape[1] != N or one != 1:
             raise ValueError("out: a row-major bf16 or fp32 [M][N] tensor")
         self._check(lib().sb_fp4_gemm(self._h, _dev(a.codes), _dev(a.scales), _dev(a.tensor_scale), M, _dev(b.codes), _dev(b.scales),
-                                      _dev(b.tensor_scale), N, a.cols, FP4_FORMATS[a.fmt], _dev(out), int(dtype is torch.float32),
+                                      _dev(b.tensor_scale), N, a.cols, FP4_FORMATS[a.fmt], _dev(out), int(dtype is _F32),
                                       ldy if M > 1 else N))
         return out
 
@@ -584,7 +586,7 @@ class Context:
     @staticmethod
     def _kv8_rows(cache: Kv8Cache, starts: torch.Tensor, lens: torch.Tensor):
         n = cache.struct.requests
-        if starts.dtype is not torch.int32 or lens.dtype is not torch.int32 or starts.numel() != n + 1 or lens.numel() != n \
+        if starts.dtype is not _I32 or lens.dtype is not _I32 or starts.numel() != n + 1 or lens.numel() != n \
                 or not starts.is_contiguous() or not lens.is_contiguous():
             raise ValueError("starts: contiguous int32 [requests + 1], lens: contiguous int32 [requests]")
         return _dev(starts), _dev(lens)
@@ -606,11 +608,11 @@ class Context:
         s, n = self._kv8_rows(cache, starts, lens)
         if out is None:
             shape = (int(starts[-1]) if total is None else total, cache.struct.heads, cache.struct.dim)
-            out = tuple(self._result(shape, torch.bfloat16, cache.k.device) for _ in range(2))
+            out = tuple(self._result(shape, _BF16, cache.k.device) for _ in range(2))
         K, V = out
         tokens, heads, dim = shape = K.shape
         if V.shape != shape or heads != cache.struct.heads or dim != cache.struct.dim or not K.is_contiguous() or not V.is_contiguous() \
-                or K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
+                or K.dtype is not _BF16 or V.dtype is not _BF16:
             raise ValueError("out: two contiguous bf16 [tokens][heads][dim] tensors")
         self._check(lib().sb_kv8_read(self._h, cache.struct, tokens, s, n, max_new, _dev(K), _dev(V)))
         return K, V
@@ -626,13 +628,13 @@ class Context:
             raise ValueError("Q: [tokens][query heads][dim of the cache]")
         q, qt, qh = _heads(Q, "Q")
         if out is None:
-            out = self._result(shape, torch.bfloat16, Q.device)
+            out = self._result(shape, _BF16, Q.device)
         elif out.shape != shape:
             raise ValueError("out: the shape of Q")
         o, ot, oh = _heads(out, "out")
         if lse is None and want_lse:
-            lse = self._result(shape[:2], torch.float32, Q.device)
-        if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or lse.dtype is not torch.float32):
+            lse = self._result(shape[:2], _F32, Q.device)
+        if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or lse.dtype is not _F32):
             raise ValueError("lse: contiguous fp32 [tokens][query heads]")
         self._check(lib().sb_kv8_attention(self._h, cache.struct, q, qt, qh, heads, tokens, s, n, max_new, max_len,
                                            dim ** -0.5 if scale is None else scale, window, o, ot, oh, _dev(lse)))
