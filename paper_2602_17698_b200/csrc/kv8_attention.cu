@@ -31,9 +31,9 @@
 // and the last of them to finish (a counter) adds them in their order: the result does not depend on
 // which one that is.
 //
-// Measured (heads of 128, four query heads per cache head, 8 cache heads): 64 requests in 8192 89 us, 5.7 TB/s, 0.87
+// Measured (heads of 128, four query heads per cache head, 8 cache heads): 64 requests in 8192 88 us, 5.7 TB/s, 0.88
 // of a plain copy's rate; one in 100000 47 us, of which 35 stream at 5.9 TB/s and the rest is the start and the
-// sum of the pieces; 16 x 5 tokens in a window of 4096 (20 rows) 59 us: 253 registers leave two warps a scheduler,
+// sum of the pieces; 16 x 5 tokens in a window of 4096 (20 rows) 58 us: 251 registers leave two warps a scheduler,
 // and their latencies bound it.
 #include "kv8_attention.cuh"
 
@@ -734,7 +734,7 @@ extern "C" sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, co
     // Many query rows per cache head: a key is converted once for 256 rows and the products run at the
     // rate of tcgen05; few: the cache's bytes bound the call and 8 to 24 rows per warp are enough. That kernel's
     // shared memory holds heads of up to 128; wider ones stay here, where every 16 rows read and convert the cache
-    // again: 4 requests of up to 1024 tokens behind up to 8192 take 3.25 ms with heads of 256, 255 us with heads of 128.
+    // again: 4 requests of up to 1024 tokens behind up to 8192 take 3.3 ms with heads of 256, 255 us with heads of 128.
     if (max_new * a.group > AT_PROMPT_FROM && cache->dim <= 128) return kv8_prompt(ctx, a, cache->type, max_new, max_len);
     return cache->type == SB_KV_INT8 ? rows_by_dim<SB_KV_INT8>(ctx, a, max_new, max_len) : rows_by_dim<SB_KV_E4M3>(ctx, a, max_new, max_len);
 }

@@ -26,7 +26,7 @@
 // another. Half tiles and two row tiles overlap these chains; whole tiles per step were slower (339 us against
 // 287), and so was a warp of its own for the scores (344).
 // 4 requests of up to 1024 tokens behind up to 8192, 32 query heads of 128 over 8, e4m3: 255 us,
-// 761 TFLOP/s, tensor pipe 54 % active; heads of 64 231 us, of 80 and 96 250.
+// 761 TFLOP/s, tensor pipe 54 % active; heads of 64 231 us, of 80 and 96 252.
 #include "kv8_attention.cuh"
 #include "tensor5.cuh"
 
