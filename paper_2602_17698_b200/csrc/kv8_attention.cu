@@ -35,7 +35,7 @@
 // of a plain copy's rate; one in 100000 47 us, of which 35 stream at 5.9 TB/s and the rest is the start and the
 // sum of the pieces; 16 x 5 tokens in a window of 4096 (20 rows) 58 us: 251 registers leave two warps a scheduler,
 // and their latencies bound it.
-#include "kv8_attention.cuh"
+#include "kv_rows.cuh"
 
 namespace {
 
@@ -45,30 +45,6 @@ namespace {
 // not decide it: few requests would gain from the other kernel below 24 rows already, many lose until 32; the limit
 // is near where many requests change sides. Heads of more than 128 have no kernel there: all their rows run here.
 constexpr int AT_PROMPT_FROM = 24;
-constexpr int AT_WARPS = 4;
-constexpr int AT_STEP = 32;             // keys a warp takes at a time: two scale blocks
-constexpr int AT_EXTRA = 12;            // what an item costs besides its steps, in steps
-constexpr int AT_BATCH = 16;            // steps whose page numbers and scales a warp holds, two lanes a step
-
-__device__ __forceinline__ unsigned at_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void at_copy16(unsigned dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void at_copy16(unsigned dst, const void* src, bool take) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void at_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void at_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void at_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t at_transpose(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
 template <int DP, int NR>
 struct AtShape {
     static constexpr int STAGES = DP == 64 ? 4 : NR == 1 ? 2 : 3;
@@ -98,66 +74,9 @@ kv8_rows_kernel(const AtArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const int D = a.g.dim;
-    // ---- this CTA's share ----
     AtWalk<S::ROWS, AT_STEP, AT_EXTRA> wk;
     long long share;
-    {
-        // units of one head before each row tile of all requests, 128 at a time
-        long long* sums = reinterpret_cast<long long*>(smem);       // [AT_WARPS] and, behind them, where the share starts
-        const int n = a.row_tiles * a.g.requests;
-        auto units = [&](int i) -> long long {
-            if (i >= n) return 0;
-            const int steps = at_item<S::ROWS, AT_STEP>(a, i).steps;
-            return steps ? steps + AT_EXTRA : 0;
-        };
-        long long mine = units(threadIdx.x), x = mine;
-        for (int i = threadIdx.x + AT_WARPS * 32; i < n; i += AT_WARPS * 32) x += units(i);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        if (lane == 0) sums[warp] = x;
-        __syncthreads();
-        long long total = 0;
-#pragma unroll
-        for (int w = 0; w < AT_WARPS; ++w) total += sums[w];
-        total *= a.g.heads;
-        share = at_div(total + gridDim.x - 1, gridDim.x);
-        if (share < a.least) share = a.least;
-        const long long at = blockIdx.x * share;
-        if (at >= total) return;
-        long long before = 0;
-        for (int base = 0; base < n; base += AT_WARPS * 32) {
-            if (base > 0) mine = units(base + threadIdx.x);
-            x = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            __syncthreads();
-            if (lane == 31) sums[warp] = x;
-            __syncthreads();
-            long long all = 0, below = before;
-#pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) {
-                if (w < warp) below += sums[w];
-                all += sums[w];
-            }
-            const long long lo = (below + x - mine) * a.g.heads;     // the row tile's first unit of all
-            if (at >= lo && at < lo + mine * a.g.heads) {
-                int* found = reinterpret_cast<int*>(sums + AT_WARPS);
-                found[0] = base + threadIdx.x;
-                found[1] = (int)at_div(at - lo, mine);
-                found[2] = (int)(at - lo - found[1] * mine);
-            }
-            before += all;
-            if (at < before * a.g.heads) break;
-        }
-        __syncthreads();
-        const int* found = reinterpret_cast<const int*>(sums + AT_WARPS);
-        const int f0 = found[0], f1 = found[1], f2 = found[2];
-        __syncthreads();
-        if (!wk.begin(a, f0, f1, f2, at, min(share, total - at))) return;
-    }
+    if (!at_share<S>(a, smem, wk, share)) return;
     for (bool more = true; more; more = wk.next(a)) {
         const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
         const Kv8Request rq = wk.it.rq;
@@ -492,139 +411,7 @@ kv8_rows_kernel(const AtArgs a) {
                 }
             }
         __syncthreads();
-        const bool whole = wk.count == wk.it.steps;
-        const int quads = D / 4;
-        auto store = [&](int r, int d, float4 v, float mm, float sum) {
-            const int row = r0 + r;
-            const int64_t tok = rq.row0 + a.by_group.quot(row);
-            const int h = head * a.group + a.by_group.rem(row);
-            const float f = at_norm(sum);
-            const uint2 w = make_uint2(u32(__floats2bfloat162_rn(v.x * f, v.y * f)), u32(__floats2bfloat162_rn(v.z * f, v.w * f)));
-            *reinterpret_cast<uint2*>(a.o + tok * a.o_token_stride + h * a.o_head_stride + d) = w;
-            if (d == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(mm, sum);
-        };
-        for (int idx = threadIdx.x; idx < nrow * quads; idx += AT_WARPS * 32) {
-            const int r = idx / quads, d = 4 * (idx - r * quads);
-            float2 ml[AT_WARPS];
-            float mm = -INFINITY, sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) {
-                ml[w] = mlsm[w * S::ROWS + r];
-                mm = fmaxf(mm, ml[w].x);
-            }
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) {
-                const float f = ml[w].x == -INFINITY ? 0.f : at_exp2(ml[w].x - mm);
-                const float4 x = *reinterpret_cast<const float4*>(osm + (w * S::ROWS + r) * S::OPITCH + d);
-                sum = fmaf(ml[w].y, f, sum);
-                v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-            }
-            if (whole) store(r, d, v, mm, sum);
-            else {
-                const int64_t at = (2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1)) * S::ROWS + r;
-                *reinterpret_cast<float4*>(a.part + at * D + d) = v;
-                if (d == 0) a.part_ml[at] = make_float2(mm, sum);
-            }
-        }
-        if (!whole) {
-            // ---- the last of the item's pieces to finish adds them all, in order ----
-            const long long from = wk.from;
-            const int c0 = (int)at_div(from + AT_EXTRA, share), c1 = (int)at_div(from + wk.units() - 1, share), pieces = c1 - c0 + 1;
-            // a piece is the first of its share unless the item starts inside the share
-            auto slot = [&](int x) { return (2 * (int64_t)(c0 + x) + (from > (c0 + x) * share ? 1 : 0)) * S::ROWS; };
-            volatile int* last = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                unsigned* done = a.done + ((int64_t)wk.row_tile * a.g.heads + head);
-                *last = atomicAdd(done, 1u) == (unsigned)(pieces - 1);
-                if (*last) *done = 0;                                    // for the next call
-            }
-            __syncthreads();
-            if (*last) {
-                __threadfence();
-                // weights of the pieces of every row in shared memory, a row per warp
-                float* weight = reinterpret_cast<float*>(smem);          // [pieces][ROWS]
-                float2* total = reinterpret_cast<float2*>(smem + S::F_AT - S::ROWS * 8);         // (reference, sum) of a row
-                for (int r = warp; r < nrow; r += AT_WARPS) {
-                    constexpr int HELD = 4;                              // of a lane's pieces in registers: 128 in all
-                    float2 ml[HELD];
-                    float mm = -INFINITY, sum = 0.f;
-#pragma unroll
-                    for (int i = 0; i < HELD; ++i) {
-                        const int x = lane + 32 * i;
-                        ml[i] = x < pieces ? __ldcg(a.part_ml + slot(x) + r) : make_float2(-INFINITY, 0.f);
-                    }
-#pragma unroll
-                    for (int i = 0; i < HELD; ++i) mm = fmaxf(mm, ml[i].x);
-                    for (int x = lane + 32 * HELD; x < pieces; x += 32) mm = fmaxf(mm, __ldcg(a.part_ml + slot(x) + r).x);
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
-                    auto put = [&](int x, float2 p) {
-                        const float f = p.x == -INFINITY ? 0.f : at_exp2(p.x - mm);
-                        weight[x * S::ROWS + r] = f;
-                        sum = fmaf(p.y, f, sum);
-                    };
-#pragma unroll
-                    for (int i = 0; i < HELD; ++i)
-                        if (lane + 32 * i < pieces) put(lane + 32 * i, ml[i]);
-                    for (int x = lane + 32 * HELD; x < pieces; x += 32) put(x, __ldcg(a.part_ml + slot(x) + r));
-                    sum = warp_sum(sum);
-                    if (lane == 0) total[r] = make_float2(mm, sum);
-                }
-                __syncthreads();
-                constexpr int PER = S::ROWS * DP / 4 / (AT_WARPS * 32);  // outputs of a thread, four columns each, at most
-                const int outs = nrow * quads;
-                if (outs <= AT_WARPS * 32) {
-                    // few outputs: one a thread, or several threads for one, each a part of the pieces
-                    const int parts = AT_WARPS * 32 / outs, part = (int)threadIdx.x / outs, idx = (int)threadIdx.x - part * outs;
-                    const int r = idx / quads, d = 4 * (idx - r * quads);
-                    float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (part < parts) {
-                        const int x1 = pieces * (part + 1) / parts;
-#pragma unroll 8
-                        for (int x = pieces * part / parts; x < x1; ++x) {
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x) + r) * D + d));
-                            const float f = weight[x * S::ROWS + r];
-                            v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-                        }
-                    }
-                    shared_sum[threadIdx.x] = v;
-                    __syncthreads();
-                    if ((int)threadIdx.x < outs) {
-                        for (int p = 1; p < parts; ++p) {
-                            const float4 y = shared_sum[threadIdx.x + p * outs];
-                            v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
-                        }
-                        store(r, d, v, total[r].x, total[r].y);
-                    }
-                } else {
-                    // a thread's outputs side by side, so that their loads overlap
-                    float4 v[PER];
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll (PER <= 2 ? 8 : 2)
-                    for (int x = 0; x < pieces; ++x) {
-                        const float* from_part = a.part + slot(x) * D;
-#pragma unroll
-                        for (int i = 0; i < PER; ++i) {
-                            const int idx = (int)threadIdx.x + AT_WARPS * 32 * i;
-                            if (idx >= outs) continue;
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(from_part) + idx);
-                            const float f = weight[x * S::ROWS + idx / quads];
-                            v[i].x = fmaf(y.x, f, v[i].x); v[i].y = fmaf(y.y, f, v[i].y); v[i].z = fmaf(y.z, f, v[i].z); v[i].w = fmaf(y.w, f, v[i].w);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        const int idx = (int)threadIdx.x + AT_WARPS * 32 * i, r = idx / quads;
-                        if (idx < outs) store(r, 4 * (idx - r * quads), v[i], total[r].x, total[r].y);
-                    }
-                }
-            }
-        }
+        at_finish<S, DP>(a, smem, wk, share);
         __syncthreads();                                                 // the next piece's copies go where the sums were
     }
 }
@@ -634,53 +421,9 @@ sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = AtShape<DP, NR>;
     auto* kernel = kv8_rows_kernel<TYPE, DP, NR>;
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    const int64_t row_tiles = (max_new * a.group + S::ROWS - 1) / S::ROWS;
-    const int64_t tiles = row_tiles * a.g.heads * a.g.requests;
-    if (tiles >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
-    // a share per resident CTA, fewer if there cannot be so many shares
-    int64_t keys = max_len;
-    if (a.window > 0 && keys > a.window + S::ROWS + SB_KV8_BLOCK) keys = a.window + S::ROWS + SB_KV8_BLOCK;
-    const int64_t steps = (keys + AT_STEP - 1) / AT_STEP + 1;
-    // Units of a share at least. A step takes a share about 0.22 us, and every piece of an item 0.22 us per
-    // eight rows when they are added: u units a share cost u + steps NR / u. Fixed shares of 6, 16 and
-    // 28 took 12, 16 and 18 us for one request in 2000 (8 rows), 43, 35 and 31 for one in 8192 (16 rows).
-    a.least = 6;
-    while ((int64_t)a.least * a.least < steps * NR) ++a.least;
-    const int64_t most = (tiles * (steps + AT_EXTRA) + a.least - 1) / a.least;
-    const int64_t ctas = most < (int64_t)S::CTAS * ctx->sm_count ? most : (int64_t)S::CTAS * ctx->sm_count;
-    a.row_tiles = (int)row_tiles;
-    a.by_row_tiles = KvDiv(a.row_tiles);
-    const size_t n = (size_t)ctas * 2 * S::ROWS;
-    void* arena;
-    const sb_status s = sb_scratch(ctx, Carver::need({n * a.g.dim * 4, n * 8}), &arena);
+    int64_t ctas;
+    const sb_status s = at_rows_plan<S>(ctx, "kv8 attention", a, max_new, max_len, ctas);
     if (s != SB_OK) return s;
-    Carver cv(arena);
-    a.part = cv.take<float>(n * a.g.dim);
-    a.part_ml = cv.take<float2>(n);
-    if (ctx->kv8_done_n < (size_t)tiles) {
-        // Zeroed once; every call leaves zeros.  The old counters stay for captured launches.  They are zeroed here and
-        // now, on a stream of their own: in a capture the context's stream would only do it when the graph is replayed.
-        const size_t want_n = (size_t)tiles * 2 + 4096;
-        unsigned* fresh = nullptr;
-        if (cudaMalloc(&fresh, want_n * 4) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return sb_fail(ctx, SB_ERR_SCRATCH, "kv8 attention: %zu counters", want_n);
-        }
-        cudaStream_t once = nullptr;
-        cudaError_t e = cudaStreamCreateWithFlags(&once, cudaStreamNonBlocking);
-        if (e == cudaSuccess) e = cudaMemsetAsync(fresh, 0, want_n * 4, once);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(once);
-        if (once) cudaStreamDestroy(once);
-        if (e != cudaSuccess) {
-            (void)cudaGetLastError();
-            cudaFree(fresh);
-            return sb_fail(ctx, SB_ERR_CUDA, "kv8 attention: zeroing %zu counters: %s", want_n, cudaGetErrorString(e));
-        }
-        if (ctx->kv8_done) ctx->retired.push_back(ctx->kv8_done);
-        ctx->kv8_done = fresh;
-        ctx->kv8_done_n = want_n;
-    }
-    a.done = ctx->kv8_done;
     kernel<<<(unsigned)ctas, AT_WARPS * 32, S::SMEM, ctx->stream>>>(a);
     SB_LAUNCHED(ctx);
     return SB_OK;
