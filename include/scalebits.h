@@ -459,6 +459,101 @@ sb_status sb_kv8_attention(sb_ctx* ctx, const sb_kv8_cache* cache, const void* Q
                            const int32_t* lens, int64_t max_new, int64_t max_len, float scale, int64_t window,
                            void* O_bf16, int64_t o_token_stride, int64_t o_head_stride, float* lse);
 
+/* ---- Key/value cache in 4 bits ----------------------------------------------------------------
+ * The same paged cache with e2m1 codes (as SB_FP4_NV has them): a token's row of a head in blocks of 16
+ * elements with one e4m3 scale each, and one fp32 scale per head.  An element stands for
+ * code * scale * head scale.  Rows are independent of one another: nothing is requantised.  starts, lens, max_new,
+ * what a request may have and what does not fit: as for the 8-bit cache.
+ *   C' = dim rounded up to a multiple of 32: a row of codes has C' / 2 bytes, element 2 i in the low and 2 i + 1 in
+ *   the high half of byte i; a row of scales has dim / 16 bytes rounded up to a multiple of 4.  Padding of
+ *   either holds zeros.                                                                          */
+typedef struct {                /* host struct, read during the call                             */
+    void *k, *v;                /* device codes [pages][heads][page_tokens][C' / 2], 16-byte aligned */
+    void *k_scale, *v_scale;    /* device e4m3 [pages][heads][page_tokens][scale bytes], 16-byte aligned */
+    const float *k_head, *v_head;   /* device fp32 [heads], positive and finite, or NULL (1)     */
+    const int32_t* table;       /* device page numbers: request b's at table + b * table_stride  */
+    int64_t table_stride;       /* 0: all requests share one row (for reading)                   */
+    int64_t pages;
+    int32_t requests, heads;
+    int32_t page_tokens;        /* a multiple of 16                                              */
+    int32_t dim;                /* a multiple of 16, 16 .. 256                                   */
+    int32_t table_pages;        /* pages a request may have (0: table_stride)                    */
+    int32_t reserved;           /* 0                                                             */
+} sb_kv4_cache;
+
+/* Writes the new tokens, every block of 16 as sb_fp4_quantize (SB_FP4_NV) does with the head's scale g:
+ *   s = e4m3((amax / 6) / g), d = s g, code = e2m1(x / d), nearest even, at most 6; 0 where d = 0.
+ * NaN is stored as 0, an infinity as the largest code (amax is the finite elements'), and SB_ERR_NONFINITE is
+ * latched; so it is where g is not positive and finite, and zeros are stored: the cache never holds a NaN.
+ * K, V, total: as for sb_kv8_append.                                                            */
+sb_status sb_kv4_append(sb_ctx* ctx, const sb_kv4_cache* cache, const void* K_bf16, int64_t k_token_stride,
+                        int64_t k_head_stride, const void* V_bf16, int64_t v_token_stride, int64_t v_head_stride,
+                        int64_t total, const int32_t* starts, const int32_t* lens, int64_t max_new);
+/* The values of the last n tokens of every request, rounded to bf16: K, V [total][heads][dim].
+ * Rows of no request are left as they were.                                                     */
+sb_status sb_kv4_read(sb_ctx* ctx, const sb_kv4_cache* cache, int64_t total, const int32_t* starts,
+                      const int32_t* lens, int64_t max_new, void* K_bf16, void* V_bf16);
+/* Attention of the new tokens over the cache: the formula, arguments and limits of sb_kv8_attention.
+ * Codes times block scales are exact in fp16; queries are multiplied in fp16 after an exact power-of-two
+ * scaling per row; the weight of a key is rounded to fp16 (to 2^-11 of it, below 2^-20 of the largest to
+ * 2^-31 of that); sums and softmax statistics are fp32.                                         */
+sb_status sb_kv4_attention(sb_ctx* ctx, const sb_kv4_cache* cache, const void* Q_bf16, int64_t q_token_stride,
+                           int64_t q_head_stride, int q_heads, int64_t total, const int32_t* starts,
+                           const int32_t* lens, int64_t max_new, int64_t max_len, float scale, int64_t window,
+                           void* O_bf16, int64_t o_token_stride, int64_t o_head_stride, float* lse);
+
+/* ---- Rotary positions -------------------------------------------------------------------------
+ * For a row at position p, every head, and i < rotated / 2, with a = p * freq[i] and the pair
+ * (u, w) = (x[i], x[i + rotated / 2]), or with `interleaved` (x[2 i], x[2 i + 1]):
+ *   u' = factor (u cos a - w sin a),   w' = factor (w cos a + u sin a)
+ * and with `inverse` by -a: the gradient's way back (factor is not inverted).  Elements from `rotated` on
+ * are copied.  Angles (below 2^40) are reduced in 64 bits, so far positions lose nothing; cos, sin and the
+ * products are fp32, and the result is rounded once.                                             */
+typedef struct {                /* host struct, read during the call                             */
+    const float* freq;          /* device fp32 [rotated / 2], radians per position, finite       */
+    int32_t rotated;            /* even, 2 .. dim                                                */
+    int32_t interleaved;        /* 0 or 1                                                        */
+    int32_t inverse;            /* 0 or 1                                                        */
+    float factor;               /* finite; 1 unless the scaling for long contexts has one        */
+} sb_rotary_table;
+typedef struct {                /* one tensor of rows: element (row, head, d) at row * token_stride + head * head_stride + d */
+    const void* x;
+    int64_t x_token_stride, x_head_stride;
+    void* y;                    /* may be x with x's strides; must not overlap it otherwise      */
+    int64_t y_token_stride, y_head_stride;
+    int32_t heads, reserved;
+} sb_rotary_part;
+/* parts: HOST array of 1 or 2 (queries and keys), of bf16 (f32 = 0) or fp32 (1) elements, any alignment of
+ * their type; 16-byte aligned rows are fastest.  dim: even, 2 .. 1024.
+ * Positions: `positions` device int32 [total], any sign, one per row; or NULL and starts, lens as for the
+ * caches: row starts[b] + i is at lens[b] - n + i (lens[b] is any number from n on).  Rows of no request are left as
+ * they were; a request whose numbers do not fit is skipped and SB_ERR_INVALID is latched.       */
+sb_status sb_rotary(sb_ctx* ctx, const sb_rotary_table* table, const sb_rotary_part* parts, int n_parts, int dim, int f32,
+                    int64_t total, const int32_t* positions, const int32_t* starts, const int32_t* lens, int requests,
+                    int64_t max_new);
+
+/* ---- Low-rank adapters ------------------------------------------------------------------------
+ * What the adapters of many requests add to a projection that they share, for the rows t of request b
+ * (starts[b] .. starts[b + 1], at most max_new) and its adapter a = ids[b]:
+ *   Y[t] = base[t] + scale[a] B_a (A_a x[t])         (a = -1: Y[t] = base[t])
+ * An id outside -1 .. adapters - 1 counts as -1 and latches SB_ERR_INVALID, as a request does whose rows do not fit
+ * (it is skipped).  Rows of no request are left as they were.
+ * Products of bf16 numbers are summed in fp32; A_a x is held for the second product as the sum of two bf16
+ * numbers (2^-17 of it); the result is rounded once.  The sums of a call are always taken in the same order.  */
+typedef struct {                /* host struct, read during the call                             */
+    const void* a;              /* device bf16 [adapters][rank][in], 16-byte aligned             */
+    const void* b;              /* device bf16 [adapters][out][rank], 16-byte aligned            */
+    const float* scale;         /* device fp32 [adapters] or NULL (1)                            */
+    int64_t in, out;            /* in: a multiple of 8                                           */
+    int32_t adapters, rank;     /* rank: a multiple of 8, 8 .. 128 (smaller ones padded with zeros) */
+} sb_lora_adapters;
+/* X: bf16 [total][in], leading dimension ldx (a multiple of 8, 16-byte aligned base); base, Y: bf16 (f32 = 0) or fp32 (1)
+ * [total][out], any alignment of their type; Y may be base (then with the same leading dimension), and must not overlap
+ * it, or X, otherwise.  starts: device int32 [requests + 1], ids: device int32 [requests].      */
+sb_status sb_lora_add(sb_ctx* ctx, const sb_lora_adapters* adapters, const void* X_bf16, int64_t ldx, const void* base, int64_t ld_base,
+                      void* Y, int64_t ldy, int f32, int64_t total, const int32_t* starts, const int32_t* ids, int requests,
+                      int64_t max_new);
+
 #ifdef __cplusplus
 }
 #endif

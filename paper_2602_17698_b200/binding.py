@@ -7,6 +7,7 @@ fails loudly when `libscalebits.so` has not been built.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional, Sequence
 
@@ -25,7 +26,7 @@ SB_KV_INT8, SB_KV_E4M3 = 0, 1
 SB_KV8_BLOCK = 16
 FP4_FORMATS = {"mx": SB_FP4_MX, "nv": SB_FP4_NV}
 # a module's attribute is looked up at every use, which the calls of a decode step notice
-_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 
 EXPORTS = ["sb_create", "sb_destroy", "sb_sync", "sb_last_error", "sb_kernel_launches", "sb_debug_lookback",
            "sb_checked_build",
@@ -36,7 +37,8 @@ EXPORTS = ["sb_create", "sb_destroy", "sb_sync", "sb_last_error", "sb_kernel_lau
            "sb_reorder_channels_first_order", "sb_calib_gram",
            "sb_block_scores_full", "sb_dequant_gemm",
            "sb_fp4_code_bytes", "sb_fp4_scale_bytes", "sb_fp4_quantize", "sb_fp4_dequantize", "sb_fp4_gemm",
-           "sb_kv8_append", "sb_kv8_read", "sb_kv8_attention"]
+           "sb_kv8_append", "sb_kv8_read", "sb_kv8_attention",
+           "sb_kv4_append", "sb_kv4_read", "sb_kv4_attention", "sb_rotary", "sb_lora_add"]
 
 
 class SbError(RuntimeError):
@@ -76,6 +78,27 @@ class Kv8CacheStruct(C.Structure):
                 ("table", C.c_void_p), ("table_stride", C.c_int64), ("pages", C.c_int64),
                 ("requests", C.c_int32), ("heads", C.c_int32), ("page_tokens", C.c_int32), ("dim", C.c_int32),
                 ("type", C.c_int32), ("table_pages", C.c_int32)]
+
+
+class Kv4CacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_head", C.c_void_p), ("v_head", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64), ("pages", C.c_int64),
+                ("requests", C.c_int32), ("heads", C.c_int32), ("page_tokens", C.c_int32), ("dim", C.c_int32),
+                ("table_pages", C.c_int32), ("reserved", C.c_int32)]
+
+
+class RotaryTableStruct(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rotated", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32), ("factor", C.c_float)]
+
+
+class RotaryPartStruct(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_token_stride", C.c_int64), ("x_head_stride", C.c_int64),
+                ("y", C.c_void_p), ("y_token_stride", C.c_int64), ("y_head_stride", C.c_int64), ("heads", C.c_int32), ("reserved", C.c_int32)]
+
+
+class LoraAdaptersStruct(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p), ("in_", C.c_int64), ("out", C.c_int64),
+                ("adapters", C.c_int32), ("rank", C.c_int32)]
 
 
 _lib = None
@@ -136,6 +159,12 @@ def lib() -> C.CDLL:
         L.sb_kv8_append.argtypes = [vp, cp, vp, i64, i64, vp, i64, i64, i64, vp, vp, i64]
         L.sb_kv8_read.argtypes = [vp, cp, i64, vp, vp, i64, vp, vp]
         L.sb_kv8_attention.argtypes = [vp, cp, vp, i64, i64, i32, i64, vp, vp, i64, i64, f32, i64, vp, i64, i64, vp]
+        c4 = C.POINTER(Kv4CacheStruct)
+        L.sb_kv4_append.argtypes = [vp, c4, vp, i64, i64, vp, i64, i64, i64, vp, vp, i64]
+        L.sb_kv4_read.argtypes = [vp, c4, i64, vp, vp, i64, vp, vp]
+        L.sb_kv4_attention.argtypes = [vp, c4, vp, i64, i64, i32, i64, vp, vp, i64, i64, f32, i64, vp, i64, i64, vp]
+        L.sb_rotary.argtypes = [vp, C.POINTER(RotaryTableStruct), C.POINTER(RotaryPartStruct), i32, i32, i32, i64, vp, vp, vp, i32, i64]
+        L.sb_lora_add.argtypes = [vp, C.POINTER(LoraAdaptersStruct), vp, i64, vp, i64, vp, i64, i32, i64, vp, vp, i32, i64]
         L.sb_fp4_code_bytes.restype = L.sb_fp4_scale_bytes.restype = i64
         for name in EXPORTS:
             if name not in ("sb_last_error", "sb_kernel_launches", "sb_fp4_code_bytes", "sb_fp4_scale_bytes"):
@@ -208,6 +237,7 @@ class Fp4Matrix:
                    torch.empty(fp4_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device=device), rows, cols, fmt, tensor_scale)
 
 
+_E4M3_BYTES = (torch.uint8, torch.float8_e4m3fn)
 _KV8_TYPES = {torch.int8: SB_KV_INT8, torch.float8_e4m3fn: SB_KV_E4M3}
 
 
@@ -243,6 +273,93 @@ class Kv8Cache:
         kv = torch.zeros((2, pages, heads, page_tokens, dim), dtype=torch.uint8, device=table.device).view(dtype)
         sc = torch.zeros((2, pages, heads, page_tokens // SB_KV8_BLOCK), dtype=torch.bfloat16, device=table.device)
         return cls(kv[0], kv[1], sc[0], sc[1], table)
+
+
+class Kv4Cache:
+    """A paged key/value cache in 4 bits: k, v uint8 [pages][heads][page tokens][padded dim / 2] (e2m1, two to a byte, rows padded with zeros to 32
+    elements), k_scale, v_scale uint8 or float8_e4m3fn [pages][heads][page tokens][scales of a row, padded to 4], k_head, v_head fp32 [heads] (None: 1),
+    table int32 [requests][pages of a request] as in Kv8Cache."""
+    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "dim", "k_head", "v_head", "struct")
+
+    def __init__(self, k, v, k_scale, v_scale, table, dim: int, k_head=None, v_head=None):
+        pages, heads, page_tokens, row = shape = k.shape
+        if k.dtype is not _U8 or v.dtype is not _U8 or k_scale.dtype not in _E4M3_BYTES or v_scale.dtype not in _E4M3_BYTES or table.dtype is not _I32:
+            raise TypeError("codes are uint8, scales uint8 or float8_e4m3fn, page numbers int32")
+        scales = (pages, heads, page_tokens, (dim + 63) // 64 * 4)
+        if v.shape != shape or row != (dim + 31) // 32 * 16 or k_scale.shape != scales or v_scale.shape != scales:
+            raise ValueError("codes and scales do not fit one another and dim")
+        requests, per = table.shape
+        stride, one = table.stride()
+        if per < 1:
+            raise ValueError("a request needs room for a page in the table")
+        if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()) or one != 1:
+            raise ValueError("the cache's tensors are contiguous")
+        for t in (k_head, v_head):
+            if t is not None and (t.dtype is not _F32 or t.shape != (heads,) or not t.is_contiguous()):
+                raise ValueError("k_head, v_head: contiguous fp32 [heads]")
+        self.k, self.v, self.k_scale, self.v_scale, self.table, self.dim, self.k_head, self.v_head = k, v, k_scale, v_scale, table, dim, k_head, v_head
+        self.struct = Kv4CacheStruct(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), _dev(k_head), _dev(v_head), _dev(table),
+                                     stride if requests > 1 else per, pages, requests, heads, page_tokens, dim, per, 0)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_tokens: int, dim: int, table, k_head=None, v_head=None):
+        kv = torch.zeros((2, pages, heads, page_tokens, (dim + 31) // 32 * 16), dtype=torch.uint8, device=table.device)
+        sc = torch.zeros((2, pages, heads, page_tokens, (dim + 63) // 64 * 4), dtype=torch.uint8, device=table.device)
+        return cls(kv[0], kv[1], sc[0], sc[1], table, dim, k_head, v_head)
+
+
+class RotaryTable:
+    """Frequencies of rotary positions: fp32 [rotated / 2] on the device, radians per position (`rotary_frequencies` makes them), how a head's
+    elements pair up, and the factor on cos and sin."""
+    __slots__ = ("freq", "rotated", "interleaved", "factor", "structs")
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, factor: float = 1.0):
+        if freq.dtype is not _F32 or freq.dim() != 1 or not freq.is_contiguous() or freq.numel() < 1:
+            raise ValueError("freq: contiguous fp32 [rotated / 2]")
+        self.freq, self.rotated, self.interleaved, self.factor = freq, 2 * freq.numel(), bool(interleaved), float(factor)
+        self.structs = tuple(RotaryTableStruct(_dev(freq), self.rotated, int(self.interleaved), inverse, self.factor) for inverse in (0, 1))
+
+
+class LoraAdapters:
+    """Low-rank adapters of one projection: a bf16 [adapters][rank][in], b bf16 [adapters][out][rank], scale fp32 [adapters] (None: 1).  The rank is a
+    multiple of 8, up to 128; smaller ones are padded with zeros."""
+    __slots__ = ("a", "b", "scale", "adapters", "rank", "inner", "outer", "struct")
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None):
+        if a.dtype is not _BF16 or b.dtype is not _BF16 or not a.is_contiguous() or not b.is_contiguous():
+            raise TypeError("a and b are contiguous bf16 tensors")
+        n, rank, inner = a.shape
+        outer = b.shape[1]
+        if b.shape != (n, outer, rank):
+            raise ValueError("a: [adapters][rank][in], b: [adapters][out][rank]")
+        if scale is not None and (scale.dtype is not _F32 or scale.shape != (n,) or not scale.is_contiguous()):
+            raise ValueError("scale: contiguous fp32 [adapters]")
+        self.a, self.b, self.scale, self.adapters, self.rank, self.inner, self.outer = a, b, scale, n, rank, inner, outer
+        self.struct = LoraAdaptersStruct(_dev(a), _dev(b), _dev(scale), inner, outer, n, rank)
+
+
+def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: Optional[str] = None, stretch: float = 1.0, trained: int = 8192,
+                       low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """Frequencies base^(-2 i / rotated), fp32 on the host (computed in 64 bits), scaled for contexts `stretch` times as long as the
+    `trained` one: None: not; "linear": all divided by stretch; "base": with a base of base stretch^(rotated / (rotated - 2)), under which the slowest pair turns
+    stretch times as slowly and the fastest as before; "parts": divided by stretch where a pair turns less than `low` times in the trained
+    length, left where it turns more than `high` times, and in between by both in proportion."""
+    if rotated < 2 or rotated % 2 or stretch <= 0:
+        raise ValueError("rotated is even and at least 2, stretch positive")
+    i = torch.arange(rotated // 2, dtype=torch.float64)
+    if scaling == "base" and rotated > 2:
+        base = base * stretch ** (rotated / (rotated - 2))
+    f = base ** (-2 * i / rotated)
+    if scaling == "linear":
+        f = f / stretch
+    elif scaling == "parts":
+        if not 0 <= low < high:
+            raise ValueError("0 <= low < high")
+        keep = ((f * trained / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / stretch)
+    elif scaling not in (None, "base"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f.float()
 
 
 def _heads(x: torch.Tensor, what: str):
@@ -639,6 +756,123 @@ class Context:
         self._check(lib().sb_kv8_attention(self._h, cache.struct, q, qt, qh, heads, tokens, s, n, max_new, max_len,
                                            dim ** -0.5 if scale is None else scale, window, o, ot, oh, _dev(lse)))
         return out, lse
+
+    # ---- key/value cache in 4 bits ----------------------------------------------------------
+    def kv4_append(self, cache: Kv4Cache, K: torch.Tensor, V: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int):
+        """Writes the new tokens' keys and values (bf16 [tokens][heads][dim]); requests as in kv8_append."""
+        s, n = self._kv8_rows(cache, starts, lens)
+        tokens, heads, dim = shape = K.shape
+        if V.shape != shape or heads != cache.struct.heads or dim != cache.dim:
+            raise ValueError("K and V: [tokens][heads][dim] of the cache")
+        k, kt, kh = _heads(K, "K")
+        v, vt, vh = _heads(V, "V")
+        self._check(lib().sb_kv4_append(self._h, cache.struct, k, kt, kh, v, vt, vh, tokens, s, n, max_new))
+
+    def kv4_read(self, cache: Kv4Cache, starts: torch.Tensor, lens: torch.Tensor, max_new: int, total: Optional[int] = None, out=None):
+        """The values of the last starts[b + 1] - starts[b] tokens of every request, as bf16
+        [tokens][heads][dim] keys and values; `out`, or `total` = starts[-1] to allocate them."""
+        s, n = self._kv8_rows(cache, starts, lens)
+        if out is None:
+            shape = (int(starts[-1]) if total is None else total, cache.struct.heads, cache.dim)
+            out = tuple(self._result(shape, _BF16, cache.k.device) for _ in range(2))
+        K, V = out
+        tokens, heads, dim = shape = K.shape
+        if V.shape != shape or heads != cache.struct.heads or dim != cache.dim or not K.is_contiguous() or not V.is_contiguous() \
+                or K.dtype is not _BF16 or V.dtype is not _BF16:
+            raise ValueError("out: two contiguous bf16 [tokens][heads][dim] tensors")
+        self._check(lib().sb_kv4_read(self._h, cache.struct, tokens, s, n, max_new, _dev(K), _dev(V)))
+        return K, V
+
+    def kv4_attention(self, cache: Kv4Cache, Q: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, max_new: int, max_len: int,
+                      scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, want_lse: bool = False):
+        """Causal attention of the new tokens (Q bf16 [tokens][query heads][dim]) over the cache, which
+        holds them already.  Returns (out, lse); lse is None unless given or asked for."""
+        s, n = self._kv8_rows(cache, starts, lens)
+        tokens, heads, dim = shape = Q.shape
+        if dim != cache.dim:
+            raise ValueError("Q: [tokens][query heads][dim of the cache]")
+        q, qt, qh = _heads(Q, "Q")
+        if out is None:
+            out = self._result(shape, _BF16, Q.device)
+        elif out.shape != shape:
+            raise ValueError("out: the shape of Q")
+        o, ot, oh = _heads(out, "out")
+        if lse is None and want_lse:
+            lse = self._result(shape[:2], _F32, Q.device)
+        if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or lse.dtype is not _F32):
+            raise ValueError("lse: contiguous fp32 [tokens][query heads]")
+        self._check(lib().sb_kv4_attention(self._h, cache.struct, q, qt, qh, heads, tokens, s, n, max_new, max_len,
+                                           dim ** -0.5 if scale is None else scale, window, o, ot, oh, _dev(lse)))
+        return out, lse
+
+    # ---- rotary positions -------------------------------------------------------------------
+    def rotary(self, table: RotaryTable, q: torch.Tensor, k: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
+               lens: Optional[torch.Tensor] = None, max_new: int = 0, positions: Optional[torch.Tensor] = None, inverse: bool = False, out=None):
+        """Turns q and, if given, k ([tokens][heads][dim], bf16 or fp32) by their positions: those of the requests' new tokens (starts, lens, max_new
+        as in the cache calls), or `positions`, int32 [tokens].  In place, or into `out` (a tensor for each); inverse: the way
+        back of gradients.  Returns (q, k) as written."""
+        xs = (q,) if k is None else (q, k)
+        ys = xs if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)[:len(xs)]
+        tokens, _, dim = q.shape
+        dtype = q.dtype
+        if dtype is not _BF16 and dtype is not _F32:
+            raise TypeError("rotary: bf16 or fp32 tensors")
+        if len(ys) != len(xs):
+            raise ValueError("out: a tensor for q and, where it is given, one for k")
+        parts = (RotaryPartStruct * len(xs))()
+        for p, x, y in zip(parts, xs, ys):
+            n, heads, d = shape = x.shape
+            if n != tokens or d != dim or y.shape != shape or x.dtype is not dtype or y.dtype is not dtype:
+                raise ValueError("rotary: tensors of one type, [tokens][heads][dim] with the same tokens and dim, and out like them")
+            xt, xh, one = x.stride()
+            yt, yh, two = y.stride()
+            if one != 1 or two != 1:
+                raise ValueError("rotary: elements of a head are contiguous")
+            p.x, p.x_token_stride, p.x_head_stride = _dev(x), xt, xh
+            p.y, p.y_token_stride, p.y_head_stride = _dev(y), yt, yh
+            p.heads = heads
+        requests, at, s, n = 0, None, None, None
+        if positions is not None:
+            if starts is not None or lens is not None:
+                raise ValueError("rotary: positions, or starts and lens")
+            if positions.dtype is not _I32 or positions.shape != (tokens,) or not positions.is_contiguous():
+                raise ValueError("positions: contiguous int32 [tokens]")
+            at = _dev(positions)
+        else:
+            if starts is None or lens is None:
+                raise ValueError("rotary: positions, or starts and lens")
+            requests = lens.numel()
+            if starts.dtype is not _I32 or lens.dtype is not _I32 or starts.numel() != requests + 1 or not starts.is_contiguous() or not lens.is_contiguous():
+                raise ValueError("starts: contiguous int32 [requests + 1], lens: contiguous int32 [requests]")
+            s, n = _dev(starts), _dev(lens)
+        self._check(lib().sb_rotary(self._h, table.structs[1 if inverse else 0], parts, len(xs), dim, int(dtype is _F32), tokens, at, s, n,
+                                    requests, max_new))
+        return (ys[0], ys[1] if len(ys) > 1 else None)
+
+    # ---- low-rank adapters ------------------------------------------------------------------
+    def lora_add(self, adapters: LoraAdapters, X: torch.Tensor, base: torch.Tensor, ids: torch.Tensor, starts: torch.Tensor, max_new: int,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """base (bf16 or fp32 [tokens][out]) plus what the requests' adapters make of X (bf16 [tokens][in]): request b has the rows starts[b] ..
+        starts[b + 1] and the adapter ids[b] (-1: none).  In place, or into `out`."""
+        tokens, inner, ldx = _mat(X)
+        if out is None:
+            out = base
+        shape, dtype = (tokens, adapters.outer), base.dtype
+        if inner != adapters.inner or base.shape != shape or out.shape != shape:
+            raise ValueError("X: [tokens][in of the adapters], base and out: [tokens][out]")
+        if dtype is not _BF16 and dtype is not _F32 or out.dtype is not dtype:
+            raise TypeError("base and out: both bf16 or both fp32")
+        ldb, one = base.stride()
+        ldy, two = out.stride()
+        if one != 1 and shape[1] > 1 or two != 1 and shape[1] > 1:
+            raise ValueError("base and out: row-major")
+        requests = ids.numel()
+        if starts.dtype is not _I32 or ids.dtype is not _I32 or starts.numel() != requests + 1 or not starts.is_contiguous() or not ids.is_contiguous():
+            raise ValueError("starts: contiguous int32 [requests + 1], ids: contiguous int32 [requests]")
+        self._check(lib().sb_lora_add(self._h, adapters.struct, _dev(X), ldx, _dev(base), ldb, _dev(out), ldy, int(dtype is _F32), tokens,
+                                      _dev(starts), _dev(ids), requests, max_new))
+        return out
 
 
 def checked_build() -> bool:

@@ -1,4 +1,4 @@
-// Pieces shared by the attention kernels over the 8-bit cache (kv8_attention.cu: few query rows,
+// Pieces shared by the attention kernels over the caches (kv8_attention.cu and kv4_attention.cu: few query rows,
 // kv8_prompt.cu: many).
 #pragma once
 #include "kv8.cuh"
@@ -6,7 +6,9 @@
 struct AtArgs {
     Kv8Geom g;
     const uint8_t *k, *v;
-    const uint16_t *k_scale, *v_scale;
+    const uint16_t *k_scale, *v_scale;           // 8-bit cache: bf16 scales of 16 tokens
+    const uint8_t *k_scale4, *v_scale4;          // 4-bit cache: e4m3 scales of 16 elements
+    const float *k_head, *v_head;                // and its heads' scales (NULL: 1)
     const __nv_bfloat16* q;
     int64_t q_token_stride, q_head_stride;
     __nv_bfloat16* o;
