@@ -38,6 +38,11 @@ __device__ __forceinline__ void fp4_unpack8(uint32_t codes, uint32_t (&h)[4]) {
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
         : "r"(codes));
 }
+__device__ __forceinline__ uint32_t f16x2_mul(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 // e4m3 of a non-negative number, at most 448; and back
 __device__ __forceinline__ uint32_t e4m3_of(float x) {
     uint16_t r;

@@ -20,14 +20,8 @@
 
 namespace {
 
-// log2 of a weight when the row's reference is set to it, and how far it may grow before the reference moves: below 2^15
-constexpr float K4_UP = 6.f, K4_FAR = 14.f;
+constexpr int K4_PROMPT_FROM = 24;       // more query rows than this per cache head go to the tcgen05 kernel
 
-__device__ __forceinline__ uint32_t k4_mul2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 template <int BYTES>
 __device__ __forceinline__ void k4_copy(unsigned dst, const void* src, bool take) {
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
@@ -288,7 +282,7 @@ kv4_rows_kernel(const AtArgs a) {
                         for (int h = 0; h < 2; ++h) {
                             fp4_unpack8(w[e][h][i], p[e][h]);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) p[e][h][k] = k4_mul2(p[e][h][k], sc[e][h][i >> 1]);
+                            for (int k = 0; k < 4; ++k) p[e][h][k] = f16x2_mul(p[e][h][k], sc[e][h][i >> 1]);
                         }
                     uint4 q4[NR];
                     if constexpr (!S::QREGS) {
@@ -329,17 +323,17 @@ kv4_rows_kernel(const AtArgs a) {
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
                 }
-                // the reference only moves when a weight would pass 2^K4_FAR
+                // the reference only moves when a weight would pass 2^AT4_FAR
                 bool off[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + K4_FAR;
+                for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + AT4_FAR;
                 if (__any_sync(0xffffffffu, off[0] || off[1])) {
                     float f[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         f[e] = 1.f;
                         if (off[e]) {
-                            const float ref = mx[e] - K4_UP;
+                            const float ref = mx[e] - AT4_UP;
                             f[e] = at_exp2(m[nr][e] - ref);
                             m[nr][e] = ref;
                             l[nr][e] *= f[e];
@@ -394,7 +388,7 @@ kv4_rows_kernel(const AtArgs a) {
                         fp4_unpack8((w[2][i] >> 4 & LO) | (w[3][i] & ~LO), oh);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const uint32_t a0 = k4_mul2(el[k], slo), a1 = k4_mul2(ol[k], slo), a2 = k4_mul2(eh[k], shi), a3 = k4_mul2(oh[k], shi);
+                            const uint32_t a0 = f16x2_mul(el[k], slo), a1 = f16x2_mul(ol[k], slo), a2 = f16x2_mul(eh[k], shi), a3 = f16x2_mul(oh[k], shi);
 #pragma unroll
                             for (int nr = 0; nr < NR; ++nr) at_mma(o[4 * (VW * c + i) + k][nr], a0, a1, a2, a3, pb[nr][0], pb[nr][1]);
                         }
@@ -486,6 +480,7 @@ extern "C" sb_status sb_kv4_attention(sb_ctx* ctx, const sb_kv4_cache* cache, co
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;
+    if (max_new * a.group > K4_PROMPT_FROM && cache->dim <= 128) return kv8_prompt(ctx, a, AT_E2M1, max_new, max_len);
     return cache->dim <= 64 ? rows_by_count<64>(ctx, a, max_new, max_len)
          : cache->dim <= 128 ? rows_by_count<128>(ctx, a, max_new, max_len) : rows_by_count<256>(ctx, a, max_new, max_len);
 }

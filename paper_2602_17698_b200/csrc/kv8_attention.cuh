@@ -28,6 +28,12 @@ struct AtArgs {
 };
 
 
+// What an element of the cache is, beside SB_KV_INT8 and SB_KV_E4M3: a code of the 4-bit cache
+constexpr int AT_E2M1 = 2;
+// There a weight is held in fp16 without a value scale: log2 of the largest when the row's reference is set to it, and how far one may
+// be above the reference before that moves (below 2^15)
+constexpr float AT4_UP = 6.f, AT4_FAR = 14.f;
+
 // kv8_prompt.cu: many rows of one cache head on the tensor cores of the fifth generation, dim <= 128
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len);
 

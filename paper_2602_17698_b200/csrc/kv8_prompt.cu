@@ -1,4 +1,4 @@
-// Attention of many query rows over the 8-bit cache (prompts and chunks of prompts) on tcgen05.
+// Attention of many query rows over the 8-bit or the 4-bit cache (prompts and chunks of prompts) on tcgen05.
 //
 // A CTA takes 256 query rows of one cache head (new tokens x query heads that share it) as two
 // tiles of 128, one row per softmax thread, and walks over the keys in tiles of 128:
@@ -7,8 +7,9 @@
 //     O += P V    (A from tensor memory, V with d contiguous, fp32 in tensor memory)
 // The tensor cores cannot multiply 8-bit by 16-bit operands, so four warps convert a tile of K and
 // of V to fp16 (exact) into the 128-byte-swizzled layout the instructions read; 256 rows share the
-// conversion. Scales never touch K and V: a scale block is 16 columns of S, its key scale goes
-// into the factor of S, its value scale into P.
+// conversion. Scales of the 8-bit cache never touch K and V: a scale block is 16 columns of S, its key scale goes
+// into the factor of S, its value scale into P. A scale of the 4-bit cache belongs to 16 elements of one token: it is multiplied in
+// when they are converted (exact in fp16), the heads' scales go into the factor of S and the results.
 //
 // Warps 0-3 and 4-7: softmax of the two tiles; 8-11: conversion; 12 and 14: their products; 13: copies. A softmax
 // step takes half a key tile (64 keys): while it works on one half, the tensor cores multiply the
@@ -28,6 +29,7 @@
 // 4 requests of up to 1024 tokens behind up to 8192, 32 query heads of 128 over 8, e4m3: 255 us,
 // 761 TFLOP/s, tensor pipe 54 % active; heads of 64 231 us, of 80 and 96 252.
 #include "kv8_attention.cuh"
+#include "kv4.cuh"
 #include "tensor5.cuh"
 
 namespace {
@@ -47,6 +49,7 @@ constexpr int PR_EXTRA = 6;              // what an item costs besides its key t
                                          // 4, 6 and 8 took 272, 262 and 267 us
 constexpr int PR_LEAST = 4;              // units of a share at least: one request of 332 tokens took 34 us with 7, 30 with 4;
                                          // 30 tokens in 9000 38 and 41
+constexpr float PR_LIMIT4 = 16384.f;     // and over the 4-bit cache: 2^AT4_FAR
 constexpr float PR_LIMIT = 256.f;        // 2^AT_SLACK: largest sum of a half tile's weights before the row's reference moves
 
 template <int DP>
@@ -161,6 +164,42 @@ __device__ __forceinline__ float pr_weights(unsigned ts, unsigned (&s)[PR_SUB / 
     return lo + hi;
 }
 
+// The same for the 4-bit cache: one factor for all scores of a row, no value scales.
+__device__ __forceinline__ float pr_max4(unsigned (&s)[PR_SUB / 32][32], float kf, int upto, int from) {
+    float bm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int c = 0; c < PR_SUB; c += 4)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) bm[u] = fmaxf(bm[u], c + u > upto || c + u <= from ? -INFINITY : __uint_as_float(s[(c + u) >> 5][(c + u) & 31]));
+    const float top = fmaxf(fmaxf(bm[0], bm[1]), fmaxf(bm[2], bm[3]));
+    return top == -INFINITY ? -INFINITY : top * kf;                  // a factor of 0 makes no NaN of a half that is masked whole
+}
+template <bool EDGE>
+__device__ __forceinline__ float pr_weights4(unsigned ts, unsigned (&s)[PR_SUB / 32][32], float kf, float ref, int upto, int from) {
+    f32x2 sum[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
+    const f32x2 off = pk2(-ref, -ref), kk = pk2(kf, kf);
+#pragma unroll
+    for (int c = 0; c < PR_SUB / 32; ++c) {
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            float e[2];
+            upk2(fma2(pk2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])), kk, off), e[0], e[1]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                e[u] = at_exp2(e[u]);
+                if (EDGE && (32 * c + i + u > upto || 32 * c + i + u <= from)) e[u] = 0.f;
+            }
+            sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pk2(e[0], e[1]));
+            p[i / 2] = at_half2(e[0], e[1]);
+        }
+        pr_st16(ts + 16 * c, p);
+    }
+    float lo, hi;
+    upk2(add2(sum[0], sum[1]), lo, hi);
+    return lo + hi;
+}
+
 // The plan of the shares (items: 256 query rows), written by a kernel of its own.
 struct PrWork {
     long long* prefix;           // [row tiles of all requests + 1] units of one head before the row tile
@@ -241,6 +280,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int D = a.g.dim;
+    const int pitch = TYPE == AT_E2M1 ? kv4_code_pitch(D) : D, spitch = kv4_scale_pitch(D);        // bytes of a token's codes and scales
     PrWalk wk;
     at_after_previous();
     at_let_next();                           // its blocks find room when these end, and wait for that
@@ -340,19 +380,37 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 __syncwarp();
                 if (lane == 0) t5_bar_arrive(t5_smem(qready + qt));
             }
-            const float fq = __fdiv_rn(fabsf(a.scale_log2), reinterpret_cast<const float*>(smem + S::F_AT)[r]);
+            const float fq = __fdiv_rn(fabsf(a.scale_log2), reinterpret_cast<const float*>(smem + S::F_AT)[r]) *
+                             (TYPE == AT_E2M1 && a.k_head ? __ldg(a.k_head + wk.head) : 1.f);
             // (a thread without a row has queries of zeros, and its results go nowhere)
             const int pos = it.rq.past + a.by_group.quot(row);
             // positions of the tile's first and last row decide which key tiles need a mask
             const int pos_lo = it.rq.past + a.by_group.quot(it.r0 + qt * PR_ROWS);
             const int pos_hi = it.rq.past + a.by_group.quot(it.r0 + min(it.nrow, (qt + 1) * PR_ROWS) - 1);
             const int k0 = it.lo + wk.step0 * PR_KEYS, k1 = min(it.hi, k0 + count * PR_KEYS);
+            // the sums so far in another scale: the products of the half before this one have to be done
+            auto rescale = [&](int n, float f) -> bool {
+                if (!wait(odone + qt, 2 * tiles_mine + n - 1)) return false;
+                t5_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < DP; c += 16) {
+                    unsigned o[16];
+                    t5_ld16(to + c, o);
+                    t5_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    pr_st16(to + c, o);
+                }
+                return true;
+            };
             float m = -INFINITY, l = 0.f, inv = 0.f;
             // After tiles without rows the scales' phase before this one need not have ended. It has once there are scores: a
             // tile's scales come before its keys are converted.
-            if (skipped) ok = wait(sfull + 2 * qt, tiles_mine);
-            skipped = false;
-            ok = ok && wait(scfull + (base_all & 3), base_all >> 2);
+            if constexpr (TYPE != AT_E2M1) {
+                if (skipped) ok = wait(sfull + 2 * qt, tiles_mine);
+                skipped = false;
+                ok = ok && wait(scfull + (base_all & 3), base_all >> 2);
+            }
             for (int n = 0; ok && n < 2 * count; ++n) {              // halves of the key tiles
                 const int j = n >> 1, u = n & 1;
                 ok = wait(sfull + 2 * qt + u, tiles_mine + j);
@@ -363,62 +421,78 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 t5_ld32(ts + PR_SUB * u + 32, s[1]);
                 const int key = k0 + n * PR_SUB;
                 const bool edge = key + PR_SUB > pos_lo + 1 || key + PR_SUB > k1 || (a.window > 0 && key <= pos_hi - a.window);
-                const float4* scj = reinterpret_cast<const float4*>(sc + 16 * ((base_all + j) & 3) + PR_SUBBLOCKS * u);
-                const float4 k4 = scj[0], v4 = scj[PR_BLOCKS / 4];
-                const float kf[PR_SUBBLOCKS] = {k4.x * fq, k4.y * fq, k4.z * fq, k4.w * fq};
-                const float vmax = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
                 const int upto = min(pos, k1 - 1) - key, from = a.window > 0 ? pos - a.window - key : -1;
-                // Where nothing is masked, the weights by the reference there is; their sum says whether it
-                // still does: no weight is above their sum. One above PR_LIMIT (or none: NaN), a mask, a
-                // first key or a value scale too large takes the other way, by the row's maximum.
                 float sum = 0.f;
-                bool again = edge || __any_sync(0xffffffffu, m == -INFINITY || vmax * inv > AT_TOP);
-                t5_wait_ld();
-                if (!again) {
-                    const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
-                    sum = pr_weights<false>(ts + PR_SUB * u, s, kf, vw, m, upto, from);
-                    again = __any_sync(0xffffffffu, !(sum <= PR_LIMIT));
-                }
-                if (again) {
-                    float tops[PR_SUBBLOCKS];
-                    const float mx = pr_max(s, kf, upto, from, tops);
-                    const bool far = mx > m + AT_SLACK || (m == -INFINITY && mx > m) || vmax * inv > AT_TOP;
-                    float f = 1.f;
-                    if (far) {
-                        const float ref = fmaxf(m, mx), down = m == -INFINITY ? 0.f : at_exp2(m - ref), held = at_power_inv(inv) * down;
-                        const float most = fmaxf(fmaxf(at_exp2(tops[0] - ref) * v4.x, at_exp2(tops[1] - ref) * v4.y),
-                                                 fmaxf(at_exp2(tops[2] - ref) * v4.z, at_exp2(tops[3] - ref) * v4.w));
-                        inv = at_value_inv(most, held, vmax);
-                        m = ref;
-                        l *= down;
-                        f = held * inv;
+                if constexpr (TYPE == AT_E2M1) {
+                    // as below, with one factor and no value scales
+                    bool again = edge || __any_sync(0xffffffffu, m == -INFINITY);
+                    t5_wait_ld();
+                    if (!again) {
+                        sum = pr_weights4<false>(ts + PR_SUB * u, s, fq, m, upto, from);
+                        again = __any_sync(0xffffffffu, !(sum <= PR_LIMIT4));
                     }
-                    if (__any_sync(0xffffffffu, far) && n > 0) {
-                        // the sums so far: the products of the half before this one have to be done
-                        ok = wait(odone + qt, 2 * tiles_mine + n - 1);
-                        if (!ok) break;
-                        t5_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < DP; c += 16) {
-                            unsigned o[16];
-                            t5_ld16(to + c, o);
-                            t5_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            pr_st16(to + c, o);
+                    if (again) {
+                        const float mx = pr_max4(s, fq, upto, from);
+                        const bool far = mx > m + AT4_FAR;
+                        float f = 1.f;
+                        if (far) {
+                            const float ref = mx - AT4_UP;
+                            f = at_exp2(m - ref);
+                            m = ref;
+                            l *= f;
                         }
+                        if (__any_sync(0xffffffffu, far) && n > 0) {
+                            ok = rescale(n, f);
+                            if (!ok) break;
+                        }
+                        pr_wait_st();
+                        sum = pr_weights4<true>(ts + PR_SUB * u, s, fq, m == -INFINITY ? 0.f : m, upto, from);
                     }
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
-                    pr_wait_st();
-                    sum = pr_weights<true>(ts + PR_SUB * u, s, kf, vw, ref, upto, from);
+                } else {
+                    const float4* scj = reinterpret_cast<const float4*>(sc + 16 * ((base_all + j) & 3) + PR_SUBBLOCKS * u);
+                    const float4 k4 = scj[0], v4 = scj[PR_BLOCKS / 4];
+                    const float kf[PR_SUBBLOCKS] = {k4.x * fq, k4.y * fq, k4.z * fq, k4.w * fq};
+                    const float vmax = fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w));
+                    // Where nothing is masked, the weights by the reference there is; their sum says whether it
+                    // still does: no weight is above their sum. One above PR_LIMIT (or none: NaN), a mask, a
+                    // first key or a value scale too large takes the other way, by the row's maximum.
+                    bool again = edge || __any_sync(0xffffffffu, m == -INFINITY || vmax * inv > AT_TOP);
+                    t5_wait_ld();
+                    if (!again) {
+                        const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
+                        sum = pr_weights<false>(ts + PR_SUB * u, s, kf, vw, m, upto, from);
+                        again = __any_sync(0xffffffffu, !(sum <= PR_LIMIT));
+                    }
+                    if (again) {
+                        float tops[PR_SUBBLOCKS];
+                        const float mx = pr_max(s, kf, upto, from, tops);
+                        const bool far = mx > m + AT_SLACK || (m == -INFINITY && mx > m) || vmax * inv > AT_TOP;
+                        float f = 1.f;
+                        if (far) {
+                            const float ref = fmaxf(m, mx), down = m == -INFINITY ? 0.f : at_exp2(m - ref), held = at_power_inv(inv) * down;
+                            const float most = fmaxf(fmaxf(at_exp2(tops[0] - ref) * v4.x, at_exp2(tops[1] - ref) * v4.y),
+                                                     fmaxf(at_exp2(tops[2] - ref) * v4.z, at_exp2(tops[3] - ref) * v4.w));
+                            inv = at_value_inv(most, held, vmax);
+                            m = ref;
+                            l *= down;
+                            f = held * inv;
+                        }
+                        if (__any_sync(0xffffffffu, far) && n > 0) {
+                            ok = rescale(n, f);
+                            if (!ok) break;
+                        }
+                        const float ref = m == -INFINITY ? 0.f : m;
+                        const float vw[PR_SUBBLOCKS] = {v4.x * inv, v4.y * inv, v4.z * inv, v4.w * inv};
+                        pr_wait_st();
+                        sum = pr_weights<true>(ts + PR_SUB * u, s, kf, vw, ref, upto, from);
+                    }
                 }
                 l += sum;
                 pr_wait_st();
                 t5_fence_before();
                 __syncwarp();
                 if (lane == 0) t5_bar_arrive(t5_smem(pfull + 2 * qt + u));
-                if (u && j + 1 < count) ok = wait(scfull + ((base_all + j + 1) & 3), (base_all + j + 1) >> 2);
+                if (TYPE != AT_E2M1 && u && j + 1 < count) ok = wait(scfull + ((base_all + j + 1) & 3), (base_all + j + 1) >> 2);
             }
             // ---- results ----
             if (ok) ok = wait(fin + qt, pieces);
@@ -430,7 +504,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int h0 = wk.head * a.group;
             const int64_t tok = it.rq.row0 + a.by_group.quot(row);
             const int h = h0 + a.by_group.rem(row);
-            const float back = at_power_inv(inv), norm = whole ? at_norm(l) * back : back;
+            const float back = TYPE != AT_E2M1 ? at_power_inv(inv) : a.v_head ? __ldg(a.v_head + wk.head) : 1.f, norm = whole ? at_norm(l) * back : back;
             const int64_t slot = 2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1);
             // this warp's rows in bf16 where its queries were, in the same order
             unsigned char* o0 = smem + S::Q_AT + qt * S::OPERAND + (warp & 3) * 32 * 128;
@@ -483,7 +557,45 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         constexpr int PIECES = DP / 16, PASS = 128 / PIECES, NP = PR_KEYS / PASS;
         const int tid = threadIdx.x - 256, piece = tid % PIECES, krow = tid / PIECES;
         // n: converted tile of all, left: rows that were copied and belong to the request (the rest: zeros)
-        auto convert = [&](int n, int left) {
+        [[maybe_unused]] auto convert4 = [&](int n, int left) {
+            const unsigned src = t5_smem(smem + S::RAW_AT + n % S::RAW_RING * S::RAW) + (unsigned)(krow * pitch + 8 * piece);
+            const unsigned ssrc = t5_smem(smem + S::RAW_AT + n % S::RAW_RING * S::RAW) + (unsigned)(PR_KEYS * DP / 2 + krow * spitch + piece);
+            unsigned char* dst = smem + S::T_AT + n % S::RING * S::OPERAND + (piece >> 2) * S::PANEL;
+            if (16 * piece >= D) left = 0;
+            uint2 x[NP];
+            uint32_t sb[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                x[i] = make_uint2(0, 0);
+                sb[i] = 0;
+                if (krow + PASS * i < left) {
+                    x[i] = at_lds64(src + (unsigned)(PASS * i * pitch));
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(sb[i]) : "r"(ssrc + (unsigned)(PASS * i * spitch)));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int kk = krow + PASS * i;
+                // as below: the second panel's lanes the other way round
+                const bool swap = (piece >> 2) != 0;
+                const int c = 2 * (piece & 3);
+                const uint32_t s2 = e4m3x2_to_f16x2(sb[i] | sb[i] << 8);
+                uint32_t h[2][4];
+                fp4_unpack8(swap ? x[i].y : x[i].x, h[0]);
+                fp4_unpack8(swap ? x[i].x : x[i].y, h[1]);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<uint4*>(dst + kk * 128 + (((swap != (u != 0) ? c + 1 : c) ^ (kk & 7)) << 4)) =
+                        make_uint4(f16x2_mul(h[u][0], s2), f16x2_mul(h[u][1], s2), f16x2_mul(h[u][2], s2), f16x2_mul(h[u][3], s2));
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                t5_bar_arrive(t5_smem(full + n % S::RING));
+                t5_bar_arrive(t5_smem(raw_empty + n % S::RAW_RING));
+            }
+        };
+        [[maybe_unused]] auto convert = [&](int n, int left) {
             const unsigned src = t5_smem(smem + S::RAW_AT + n % S::RAW_RING * S::RAW) + (unsigned)(krow * D + 16 * piece);
             unsigned char* dst = smem + S::T_AT + n % S::RING * S::OPERAND + (piece >> 2) * S::PANEL;
             if (16 * piece >= D) left = 0;
@@ -518,7 +630,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         // (u = 1), fetched a tile ahead, its page two tiles ahead.
         const int sblk = SB_KV8_BLOCK * (lane & 7);
         const uint16_t* const scales = (lane & 8) ? a.v_scale : a.k_scale;
-        const bool brings = warp == 8 && lane < 2 * PR_BLOCKS;
+        const bool brings = TYPE != AT_E2M1 && warp == 8 && lane < 2 * PR_BLOCKS;
         bool ok = true;
         int n = 0;                                                   // converted tiles so far
         for (bool more = true; more && ok; more = wk.next(a)) {
@@ -538,7 +650,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             for (int i = 0; i < 2 * wk.count; ++i, ++n) {
                 ok = wait(empty + n % S::RING, n / S::RING + 1);
                 if (!ok) break;
-                if (warp == 8 && !(i & 1)) {
+                if (TYPE != AT_E2M1 && warp == 8 && !(i & 1)) {
                     // whoever read the scales of four tiles ago is done: the slot's last tile came after them
                     const int j = n >> 1;
                     if (brings) sc[16 * (j & 3) + lane] = __uint_as_float((uint32_t)scale << 16);
@@ -549,7 +661,8 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 }
                 ok = wait(raw_full + n % S::RAW_RING, n / S::RAW_RING);
                 if (!ok) break;
-                convert(n, limit - (i >> 1) * PR_KEYS);
+                if constexpr (TYPE == AT_E2M1) convert4(n, limit - (i >> 1) * PR_KEYS);
+                else convert(n, limit - (i >> 1) * PR_KEYS);
             }
         }
     } else {
@@ -557,7 +670,8 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     }
     if (warp == 13) {
         // ---- copies: a tile is eight scale blocks, each contiguous in its page; lane i brings block i ----
-        const unsigned bytes = (unsigned)(SB_KV8_BLOCK * D);
+        // (of the 4-bit cache codes and scales)
+        const unsigned bytes = (unsigned)(SB_KV8_BLOCK * pitch), sbytes = TYPE == AT_E2M1 ? (unsigned)(SB_KV8_BLOCK * spitch) : 0u;
         bool ok = true;
         int issued = 0;
         for (bool more = true; more && ok; more = wk.next(a)) {
@@ -572,7 +686,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 const int slot = a.g.page.rem(key);
                 const bool inside = lane < PR_BLOCKS && key < k1, fine = inside && entry >= 0 && entry < a.g.pages;
                 if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
-                const int64_t at = (((int64_t)entry * a.g.heads + wk.head) * a.g.page_tokens + slot) * D;
+                const int64_t at = ((int64_t)entry * a.g.heads + wk.head) * a.g.page_tokens + slot;
                 const unsigned blocks = (unsigned)__popc(__ballot_sync(0xffffffffu, fine));
                 entry = entry_of(j + 1);
 #pragma unroll
@@ -581,9 +695,20 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                     ok = ok && wait(raw_empty + rs, issued / S::RAW_RING + 1);
                     if (!ok) break;
                     const unsigned bar = t5_smem(raw_full + rs);
-                    if (lane == 0) t5_bar_expect(bar, blocks * bytes);
+                    if (TYPE == AT_E2M1 && inside && !fine) {
+                        // no such page: zeros, where a scale that was left there could be no number
+                        unsigned char* raw = smem + S::RAW_AT + rs * S::RAW;
+                        for (unsigned i = 0; i < bytes; i += 16) *reinterpret_cast<uint4*>(raw + lane * bytes + i) = make_uint4(0, 0, 0, 0);
+                        for (unsigned i = 0; i < sbytes; i += 16) *reinterpret_cast<uint4*>(raw + PR_KEYS * DP / 2 + lane * sbytes + i) = make_uint4(0, 0, 0, 0);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
                     __syncwarp();
-                    if (fine) t5_load_bulk(t5_smem(smem + S::RAW_AT + rs * S::RAW) + (unsigned)lane * bytes, (u ? a.v : a.k) + at, bytes, bar);
+                    if (lane == 0) t5_bar_expect(bar, blocks * (bytes + sbytes));
+                    __syncwarp();
+                    const unsigned dst = t5_smem(smem + S::RAW_AT + rs * S::RAW);
+                    if (fine) t5_load_bulk(dst + (unsigned)lane * bytes, (u ? a.v : a.k) + at * pitch, bytes, bar);
+                    if (TYPE == AT_E2M1 && fine)
+                        t5_load_bulk(dst + (unsigned)(PR_KEYS * DP / 2) + (unsigned)lane * sbytes, (u ? a.v_scale4 : a.k_scale4) + at * spitch, sbytes, bar);
                     __syncwarp();
                     ++issued;
                 }
@@ -783,6 +908,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
 }  // namespace
 
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len) {
+    if (type == AT_E2M1) return a.g.dim <= 64 ? prompt_launch<AT_E2M1, 64>(ctx, a, max_new, max_len) : prompt_launch<AT_E2M1, 128>(ctx, a, max_new, max_len);
     if (type == SB_KV_INT8)
         return a.g.dim <= 64 ? prompt_launch<SB_KV_INT8, 64>(ctx, a, max_new, max_len) : prompt_launch<SB_KV_INT8, 128>(ctx, a, max_new, max_len);
     return a.g.dim <= 64 ? prompt_launch<SB_KV_E4M3, 64>(ctx, a, max_new, max_len) : prompt_launch<SB_KV_E4M3, 128>(ctx, a, max_new, max_len);

@@ -156,12 +156,13 @@ def test_requests_that_do_not_fit_are_skipped_and_reported(ctx):
     from paper_2602_17698_b200.binding import SB_ERR_INVALID, SbError
     rng = np.random.default_rng(8)
     heads, dim, page = 2, 64, 16
-    cache = _cache([20, 40, 16], heads, page, dim, rng, spare=0)
-    for rows in (4, 12):
+    for rows in (4, 12, 30):
+        held = [20, 40, 16] if rows < 16 else [60, 80, 48]
+        cache = _cache(held, heads, page, dim, rng, spare=0)
         x, q = _tokens(5 * rows, heads, dim, rng), _tokens(5 * rows, 2 * heads, dim, rng)
         for case in range(6):
             dev = cache.device(DEV)
-            lens, starts = [20, 40, 16], [0, rows, 2 * rows, 3 * rows]
+            lens, starts = list(held), [0, rows, 2 * rows, 3 * rows]
             if case == 0: lens[2] = 1000                          # more tokens than pages
             if case == 1: lens[2] = 3                             # fewer tokens than new ones
             if case == 2: starts[3] = 5 * rows + 1                # past the dense rows
@@ -178,7 +179,7 @@ def test_requests_that_do_not_fit_are_skipped_and_reported(ctx):
                     ctx.kv4_read(dev, _ints(starts), _ints(lens), rows, out=got)
                     out = torch.cat(got, 1)
                 else:
-                    ctx.kv4_attention(dev, _device(q), _ints(starts), _ints(lens), rows, 48, out=out)
+                    ctx.kv4_attention(dev, _device(q), _ints(starts), _ints(lens), rows, 96, out=out)
                 with pytest.raises(SbError) as e:
                     ctx.sync()
                 assert e.value.status == SB_ERR_INVALID
