@@ -1,14 +1,19 @@
 // What low-rank adapters add to a shared projection: Y = base + scale B (A x), the adapter by request.
 //
-// Two kernels: the first leaves H = A x (fp32, rank numbers a row) in scratch, split along `in` where rows are few, the second adds
-// the splits' sums, multiplies with B and adds the base. Both products run on mma.sync m16n8k16 with rows on the 16-row side: they
-// are a few operations a byte, so the bytes of X, of base and Y and of the adapters bound them, and tcgen05 would have nothing to
-// win. The contraction may visit its index in any order: a lane takes consecutive elements of its operand rows, so both operands go
-// from global memory straight into registers, 16 bytes at a time. In the second product a lane's columns are made consecutive
-// too (column 8 (n / 2) + 2 j + n % 2 is column n of tile j), so base and Y move in 16-byte pieces.
+// Both products run on mma.sync m16n8k16 with rows on the 16-row side: they are a few operations a byte, so the bytes of X, of base
+// and Y and of the adapters bound them, and tcgen05 would have little to win.
 //
-// H is held for the second product as the sum of two bf16 numbers, h = hi + lo with lo = bf16(h - hi): what is lost is
-// below 2^-17 of h, so the result's one rounding decides.
+// Few rows a request (decode steps, drafts): one kernel. A cluster of blocks takes a request; each block multiplies its part of `in`,
+// adds all parts through distributed shared memory and takes its part of `out`. Operands go from global memory straight into
+// registers: the contraction may visit its index in any order, so a lane takes consecutive elements of its operand rows.
+//
+// Many rows (prompts): two kernels over tiles of 64 rows. The first leaves H = A x in scratch, the blocks of a cluster with a part of
+// `in` each; the second adds B H to the base. Both are fed by cp.async through rings in shared memory. The second is launched
+// while the first runs and has its first tiles there when that ends.
+//
+// In the second product a lane's columns are made consecutive (column 8 (n / 2) + 2 j + n % 2 is column n of tile j), so base and Y
+// move in 16-byte pieces. H is held as the sum of two bf16 numbers, h = hi + lo with lo = bf16(h - hi): what is lost is below 2^-17 of
+// h, so the result's one rounding decides.
 #include "kv8.cuh"
 
 namespace {
@@ -22,9 +27,9 @@ struct LoArgs {
     const int32_t *starts, *ids;
     int requests, adapters, rank, max_new;
     int direct;                  // a row tile per request (no request has more rows), else tiles of all requests one after the other
-    int splits;                  // of `in`
-    int64_t columns;             // of a block of the second kernel, a multiple of 32
-    float* h;                    // [splits][total][padded rank]
+    int splits;                  // of `in`: blocks of a cluster
+    int64_t columns;             // of a block of the second product, a multiple of its tiles' columns
+    uint16_t* h;                 // [2: hi, lo][total][padded rank], bf16
     SbDeviceState* st;
 };
 
@@ -99,52 +104,53 @@ __device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
     return t;
 }
 
-// ---- H = A x ----
-// 8 warps: MG groups of 16 rows, 8 / MG parts of the block's range of `in`.
-template <int RP, int MG>
-__global__ void __launch_bounds__(256)
-lora_down_kernel(const LoArgs a) {
-    constexpr int KG = 8 / MG, NT = RP / 8, TM = 16 * MG;
-    extern __shared__ __align__(16) float lo_sums[];                 // [KG][TM][RP]
-    const LoTile tile = lo_tile<TM, 256>(a, blockIdx.x);
-    if (tile.rows <= 0 || tile.adapter < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int mg = warp % MG, kg = warp / MG;
-    const int64_t units = (a.in + 31) / 32, parts = (int64_t)a.splits * KG, part = (int64_t)blockIdx.y * KG + kg;
-    const int64_t u0 = units * part / parts, u1 = units * (part + 1) / parts;
-    float acc[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
-    const int r0 = 16 * mg + g, r1 = r0 + 8;
-    const __nv_bfloat16 *x0 = a.x + (tile.row0 + min(r0, tile.rows - 1)) * a.ldx + 8 * t, *x1 = a.x + (tile.row0 + min(r1, tile.rows - 1)) * a.ldx + 8 * t;
-    const __nv_bfloat16* w = a.a + ((int64_t)tile.adapter * a.rank + g) * a.in + 8 * t;
-    const bool live = 16 * mg < tile.rows;
-#pragma unroll 2
-    for (int64_t u = u0; live && u < u1; ++u) {
-        const int64_t k = 32 * u;
-        const bool in = k + 8 * t < a.in;
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        const uint4 p = in && r0 < tile.rows ? lo_ld16(x0 + k) : zero, q = in && r1 < tile.rows ? lo_ld16(x1 + k) : zero;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const uint4 v = in && 8 * n < a.rank ? lo_ld16(w + 8 * n * a.in + k) : zero;
-            lo_mma(acc[n], p.x, q.x, p.y, q.y, v.x, v.y);
-            lo_mma(acc[n], p.z, q.z, p.w, q.w, v.z, v.w);
-        }
+__device__ __forceinline__ unsigned lo_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void lo_copy16(unsigned dst, const void* src, bool take) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void lo_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void lo_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void lo_ldsm4(unsigned a, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ uint4 lo_lds16(unsigned a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lo_lds8(unsigned a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void lo_cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void lo_cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// four floats of another block's shared memory, where they are `own` in this one
+__device__ __forceinline__ float4 lo_peer(const float* own, unsigned rank) {
+    unsigned at;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(lo_smem(own)), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// the sum of all blocks' four floats, in the blocks' order, as two pairs of bf16 each: hi and lo
+__device__ __forceinline__ void lo_total(const float* own, int blocks, uint2& hi, uint2& lo) {
+    float4 v = blocks > 1 ? lo_peer(own, 0) : *reinterpret_cast<const float4*>(own);
+    for (int b = 1; b < blocks; ++b) {
+        const float4 w = lo_peer(own, b);
+        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
     }
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    uint32_t top[2], rest[2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float* s = lo_sums + ((kg * TM + r0) * RP + 8 * n + 2 * t);
-        *reinterpret_cast<float2*>(s) = make_float2(acc[n][0], acc[n][1]);
-        *reinterpret_cast<float2*>(s + 8 * RP) = make_float2(acc[n][2], acc[n][3]);
+    for (int i = 0; i < 2; ++i) {
+        top[i] = u32(__floats2bfloat162_rn(f[2 * i], f[2 * i + 1]));
+        // (of an infinity nothing is left)
+        const float x = f[2 * i] - bf16lo(top[i]), y = f[2 * i + 1] - bf16hi(top[i]);
+        rest[i] = u32(__floats2bfloat162_rn(fabsf(bf16lo(top[i])) < INFINITY ? x : 0.f, fabsf(bf16hi(top[i])) < INFINITY ? y : 0.f));
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < tile.rows * RP; i += 256) {
-        float sum = lo_sums[i];
-#pragma unroll
-        for (int k = 1; k < KG; ++k) sum += lo_sums[k * TM * RP + i];
-        a.h[((int64_t)blockIdx.y * a.total + tile.row0) * RP + i] = sum;
-    }
+    hi = make_uint2(top[0], top[1]);
+    lo = make_uint2(rest[0], rest[1]);
 }
 
 // ---- Y = base + scale B H ----
@@ -206,160 +212,486 @@ template <> struct LoOut<float> {
     }
 };
 
-// 8 warps: RG groups of 16 MW rows, 8 / RG groups of 32 columns. RP: rank rounded up to 16, 32, 64 or 128.
-template <int RP, int MW, int RG, typename T>
-__global__ void __launch_bounds__(256)
-lora_up_kernel(const LoArgs a, const int wide) {
-    constexpr int TM = 16 * MW * RG, CG = 8 / RG, KS = RP / 16, KW = RP / 8;       // KW: words of a row that a lane takes
-    const LoTile tile = lo_tile<TM, 256>(a, blockIdx.x);
-    if (tile.rows <= 0) return;
+// Rows without an adapter: base as it is, columns c0 to c1.
+template <typename T>
+__device__ __forceinline__ void lo_pass(const LoArgs& a, const LoTile& tile, int64_t c0, int64_t c1, int wide) {
     const T* base = static_cast<const T*>(a.base) + tile.row0 * a.ld_base;
-    T* const y = static_cast<T*>(a.y) + tile.row0 * a.ldy;
-    const int64_t c0 = (int64_t)blockIdx.y * a.columns, c1 = min(a.out, c0 + a.columns);
-    if (tile.adapter < 0) {
-        if (base != y) {
-            for (int r = threadIdx.x >> 5; r < tile.rows; r += 8)
-                for (int64_t c = c0 + 8 * (threadIdx.x & 31); c < c1; c += 256) {
-                    LoOut<T> v;
-                    const int left = (int)min((int64_t)8, c1 - c);
-                    v.load(base + r * a.ld_base + c, left, wide);
-                    v.store(y + r * a.ldy + c, left, wide);
-                }
+    T* y = static_cast<T*>(a.y) + tile.row0 * a.ldy;
+    if (base == y) return;
+    for (int r = threadIdx.x >> 5; r < tile.rows; r += 8)
+        for (int64_t c = c0 + 8 * (threadIdx.x & 31); c < c1; c += 256) {
+            LoOut<T> v;
+            const int left = (int)min((int64_t)8, c1 - c);
+            v.load(base + r * a.ld_base + c, left, wide);
+            v.store(y + r * a.ldy + c, left, wide);
         }
+}
+// The KW words (pairs along the rank) of a row of 32 KW / 8 .. that lane t takes
+template <int KW>
+__device__ __forceinline__ void lo_words(const __nv_bfloat16* row, int t, int rank, uint32_t (&v)[KW]) {
+    const __nv_bfloat16* p = row + 2 * KW * t;
+    if (rank == 8 * KW) {
+        if constexpr (KW >= 4) {
+#pragma unroll
+            for (int i = 0; i < KW / 4; ++i) {
+                const uint4 x = lo_ld16(p + 8 * i);
+                v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+            }
+        } else {
+            const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
+            v[0] = x.x; v[1] = x.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < KW; ++i) v[i] = 2 * (KW * t + i) < rank ? __ldg(reinterpret_cast<const uint32_t*>(p) + i) : 0u;
+    }
+}
+
+// ---- few rows ----
+// A cluster per request, 8 warps a block. RP: rank rounded up to 16, 32, 64 or 128.
+template <int RP, typename T>
+__global__ void __launch_bounds__(256)
+lora_few_kernel(const LoArgs a, const int wide) {
+    constexpr int NG = RP > 64 ? RP / 64 : 1, KG = 8 / NG, NT = RP / 8 / NG;       // warps along the rank and along `in`; tiles of a warp
+    constexpr int U = RP == 16 ? 4 : 2;                                          // units of 32 of `in` whose loads overlap
+    constexpr int KS = RP / 16, KW = RP / 8;
+    extern __shared__ __align__(16) float lo_sums[];                 // [KG][16][RP]; then the first is the block's sum
+    __shared__ __align__(16) uint16_t held[2][16][RP + 8];             // H: hi, lo
+    const LoTile tile = lo_tile<16, 256>(a, blockIdx.x / a.splits);
+    const int rank = blockIdx.x % a.splits;                          // of the block in its cluster
+    if (tile.rows <= 0) return;
+    const int64_t c0 = min(a.out, rank * a.columns), c1 = min(a.out, c0 + a.columns);
+    if (tile.adapter < 0) {
+        lo_pass<T>(a, tile, c0, c1, wide);
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int rg = warp % RG, cg = warp / RG;
-    if (16 * MW * rg >= tile.rows) return;
-    const float scale = a.scale ? __ldg(a.scale + tile.adapter) : 1.f;
-    const int kl = a.rank / 4;                                       // elements of a row of B that a lane takes, from kl t on
-    // operands of H: word i of a lane is elements kl t + 2 i, + 1
-    uint32_t hi[MW][2][KW], lo[MW][2][KW];
+    {
+        const int ng = warp % NG, kg = warp / NG;
+        const int64_t units = (a.in + 31) / 32, parts = (int64_t)a.splits * KG, part = (int64_t)rank * KG + kg;
+        const int64_t u0 = units * part / parts, u1 = units * (part + 1) / parts;
+        float acc[NT][4];
 #pragma unroll
-    for (int m = 0; m < MW; ++m)
+        for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+        const __nv_bfloat16 *x0 = a.x + (tile.row0 + min(g, tile.rows - 1)) * a.ldx + 8 * t, *x1 = a.x + (tile.row0 + min(g + 8, tile.rows - 1)) * a.ldx + 8 * t;
+        const __nv_bfloat16* w = a.a + ((int64_t)tile.adapter * a.rank + 8 * NT * ng + g) * a.in + 8 * t;
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        for (int64_t u = u0; u < u1; u += U) {
+            uint4 p[U], q[U], v[U][NT];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = 16 * (MW * rg + m) + g + 8 * e;
+            for (int i = 0; i < U; ++i) {
+                const int64_t k = 32 * (u + i);
+                const bool in = u + i < u1 && k + 8 * t < a.in;
+                p[i] = in && g < tile.rows ? lo_ld16(x0 + k) : zero;
+                q[i] = in && g + 8 < tile.rows ? lo_ld16(x1 + k) : zero;
 #pragma unroll
-            for (int i = 0; i < KW; ++i) {
-                float2 v = make_float2(0.f, 0.f);
-                if (r < tile.rows && 2 * i < kl) {
-                    const float* h = a.h + (tile.row0 + r) * RP + kl * t + 2 * i;
-                    v = *reinterpret_cast<const float2*>(h);
-                    for (int s = 1; s < a.splits; ++s) {
-                        const float2 w = *reinterpret_cast<const float2*>(h + (int64_t)s * a.total * RP);
-                        v.x += w.x;
-                        v.y += w.y;
-                    }
-                }
-                const uint32_t top = u32(__floats2bfloat162_rn(v.x, v.y));
-                hi[m][e][i] = top;
-                // (of an infinity nothing is left)
-                const float x = v.x - bf16lo(top), y = v.y - bf16hi(top);
-                lo[m][e][i] = u32(__floats2bfloat162_rn(fabsf(bf16lo(top)) < INFINITY ? x : 0.f, fabsf(bf16hi(top)) < INFINITY ? y : 0.f));
+                for (int n = 0; n < NT; ++n) v[i][n] = in && 8 * (NT * ng + n) < a.rank ? lo_ld16(w + 8 * n * a.in + k) : zero;
             }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    lo_mma(acc[n], p[i].x, q[i].x, p[i].y, q[i].y, v[i][n].x, v[i][n].y);
+                    lo_mma(acc[n], p[i].z, q[i].z, p[i].w, q[i].w, v[i][n].z, v[i][n].w);
+                }
         }
-    const __nv_bfloat16* w = a.b + (int64_t)tile.adapter * a.out * a.rank + kl * t;
-    for (int64_t c = c0 + 32 * cg; c < c1; c += 32 * CG) {
-        float acc[MW][4][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float* s = lo_sums + ((kg * 16 + g) * RP + 8 * (NT * ng + n) + 2 * t);
+            *reinterpret_cast<float2*>(s) = make_float2(acc[n][0], acc[n][1]);
+            *reinterpret_cast<float2*>(s + 8 * RP) = make_float2(acc[n][2], acc[n][3]);
+        }
+    }
+    // the first columns' operands are on their way while the parts are added
+    const int64_t first = c0 + 32 * warp;
+    const __nv_bfloat16* w = a.b + (int64_t)tile.adapter * a.out * a.rank;
+    constexpr bool AHEAD = RP <= 64;                                 // registers for the columns after these
+    uint32_t v[4][KW], next[AHEAD ? 4 : 1][KW];
+    auto fetch = [&](int64_t c, auto& v) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             // column n of tile j is c + 8 (n / 2) + 2 j + n % 2
             const int64_t col = c + 8 * (g >> 1) + 2 * j + (g & 1);
-            uint32_t v[KW];
-            const __nv_bfloat16* p = w + col * a.rank;
-            if (col >= c1) {
+            if (col < c1) lo_words<KW>(w + col * a.rank, t, a.rank, v[j]);
+            else {
 #pragma unroll
-                for (int i = 0; i < KW; ++i) v[i] = 0;
-            } else if (a.rank == RP && RP >= 32) {
+                for (int i = 0; i < KW; ++i) v[j][i] = 0;
+            }
+        }
+    };
+    fetch(first, v);
+    if constexpr (AHEAD) fetch(first + 256, next);
+    __syncthreads();
+    for (int i = 4 * threadIdx.x; i < tile.rows * RP; i += 1024) {
+        float4 sum = *reinterpret_cast<const float4*>(lo_sums + i);
 #pragma unroll
-                for (int i = 0; i < KW / 4; ++i) {
-                    const uint4 x = lo_ld16(p + 8 * i);
-                    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
-                }
-            } else if (a.rank == 16 && RP == 16) {
-                const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
-                v[0] = x.x; v[1] = x.y;
-            } else {
+        for (int k = 1; k < KG; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(lo_sums + k * 16 * RP + i);
+            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+        }
+        *reinterpret_cast<float4*>(lo_sums + i) = sum;
+    }
+    if (a.splits > 1) {
+        lo_cluster_arrive();
+        lo_cluster_wait();
+    } else __syncthreads();
+    for (int i = 4 * threadIdx.x; i < 16 * RP; i += 1024) {
+        uint2 hi = make_uint2(0, 0), lo = hi;
+        if (i < tile.rows * RP) lo_total(lo_sums + i, a.splits, hi, lo);
+        *reinterpret_cast<uint2*>(&held[0][i / RP][i % RP]) = hi;
+        *reinterpret_cast<uint2*>(&held[1][i / RP][i % RP]) = lo;
+    }
+    if (a.splits > 1) lo_cluster_arrive();                           // what others hold has been read
+    __syncthreads();
+    uint32_t h[2][2][KW];                                            // [hi, lo][row g, g + 8]
 #pragma unroll
-                for (int i = 0; i < KW; ++i) v[i] = 2 * i < kl ? __ldg(reinterpret_cast<const uint32_t*>(p) + i) : 0u;
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(&held[k][g + 8 * e][2 * KW * t]);
+#pragma unroll
+            for (int i = 0; i < KW; ++i) h[k][e][i] = p[i];
+        }
+    const float scale = a.scale ? __ldg(a.scale + tile.adapter) : 1.f;
+    const T* base = static_cast<const T*>(a.base) + tile.row0 * a.ld_base;
+    T* y = static_cast<T*>(a.y) + tile.row0 * a.ldy;
+    for (int64_t c = first; c < c1; c += 256) {
+        if (!AHEAD && c != first) fetch(c, v);
+        const int64_t col = c + 8 * t;                               // a lane's eight columns
+        const int left = (int)max((int64_t)0, min((int64_t)8, c1 - col));
+        LoOut<T> o[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (left > 0 && g + 8 * e < tile.rows) o[e].load(base + (g + 8 * e) * a.ld_base + col, left, wide);
+        float acc[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int k = 1; k >= 0; --k)
+                    lo_mma(acc[j], h[k][0][2 * s], h[k][1][2 * s], h[k][0][2 * s + 1], h[k][1][2 * s + 1], v[j][2 * s], v[j][2 * s + 1]);
+        }
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < KW; ++i) v[j][i] = next[j][i];
+            fetch(c + 512, next);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (left > 0 && g + 8 * e < tile.rows) {
+                const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
+                                    acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
+                o[e].add(x, scale);
+                o[e].store(y + (g + 8 * e) * a.ldy + col, left, wide);
+            }
+    }
+    if (a.splits > 1) lo_cluster_wait();
+}
+
+// ---- many rows: H = A x ----
+constexpr int LM_ROWS = 64;
+template <int RP>
+struct LmDown {
+    static constexpr int STAGES = 4, X = LM_ROWS * 128, STAGE = X + RP * 128;      // a step: 64 of `in`
+    static constexpr int SUMS = (RP == 16 ? 2 : 1) * LM_ROWS * RP * 4;
+    static constexpr int SMEM = STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS;
+};
+// 8 warps: 4 groups of 16 rows; 2 halves of the rank, or where that is 16 of every step.
+template <int RP>
+__global__ void __launch_bounds__(256)
+lora_down_kernel(const LoArgs a) {
+    using S = LmDown<RP>;
+    constexpr int NT = RP == 16 ? 2 : RP / 16;                        // tiles of 8 of the rank a warp has
+    extern __shared__ __align__(128) unsigned char lm_smem[];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x / a.splits);
+    const int part = blockIdx.x % a.splits;
+    if (tile.rows <= 0 || tile.adapter < 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rg = warp & 3, half = warp >> 2;
+    const int64_t steps = (a.in + 63) / 64, s0 = steps * part / a.splits;
+    const int mine = (int)(steps * (part + 1) / a.splits - s0);
+    const unsigned ring = lo_smem(lm_smem);
+    // copies: 16-byte pieces XOR-ed with the row, eight lanes a row
+    const int row = threadIdx.x >> 3, piece = threadIdx.x & 7;
+    const __nv_bfloat16* x = a.x + tile.row0 * a.ldx + 8 * piece;
+    const __nv_bfloat16* w = a.a + (int64_t)tile.adapter * a.rank * a.in + 8 * piece;
+    auto issue = [&](int s) {
+        if (s < mine) {
+            const unsigned dst = ring + (unsigned)((s % S::STAGES) * S::STAGE + (piece ^ (row & 7)) * 16);
+            const int64_t k = 64 * (s0 + s);
+            const bool in = k + 8 * piece < a.in;
+#pragma unroll
+            for (int i = 0; i < LM_ROWS; i += 32) {
+                const bool take = in && row + i < tile.rows;
+                lo_copy16(dst + (unsigned)((row + i) * 128), take ? x + (row + i) * a.ldx + k : a.x, take);
             }
 #pragma unroll
-            for (int m = 0; m < MW; ++m) {
-                acc[m][j][0] = acc[m][j][1] = acc[m][j][2] = acc[m][j][3] = 0.f;
+            for (int i = 0; i < RP; i += 32) {
+                if (RP < 32 && row >= RP) break;
+                const bool take = in && row + i < a.rank;
+                lo_copy16(dst + S::X + (unsigned)((row + i) * 128), take ? w + (row + i) * a.in + k : a.a, take);
+            }
+        }
+        lo_commit();
+    };
+    float acc[NT][4];
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    lo_mma(acc[m][j], lo[m][0][2 * s], lo[m][1][2 * s], lo[m][0][2 * s + 1], lo[m][1][2 * s + 1], v[2 * s], v[2 * s + 1]);
-                    lo_mma(acc[m][j], hi[m][0][2 * s], hi[m][1][2 * s], hi[m][0][2 * s + 1], hi[m][1][2 * s + 1], v[2 * s], v[2 * s + 1]);
+    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s) issue(s);
+    const int xr = 16 * rg + (lane & 15), wr = (RP == 16 ? 0 : RP / 2 * half) + (lane & 7) + ((lane >> 4) << 3);
+    for (int s = 0; s < mine; ++s) {
+        lo_wait<S::STAGES - 2>();
+        __syncthreads();
+        issue(s + S::STAGES - 1);
+        const unsigned at = ring + (unsigned)((s % S::STAGES) * S::STAGE);
+#pragma unroll
+        for (int k = 0; k < (RP == 16 ? 2 : 4); ++k) {
+            const int ks = RP == 16 ? 2 * half + k : k;
+            uint32_t xa[4];
+            lo_ldsm4(at + (unsigned)(xr * 128 + (((2 * ks + (lane >> 4)) ^ (xr & 7)) << 4)), xa);
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                uint32_t wb[4];
+                lo_ldsm4(at + S::X + (unsigned)((wr + 8 * n) * 128 + (((2 * ks + ((lane >> 3) & 1)) ^ (wr & 7)) << 4)), wb);
+                lo_mma(acc[n], xa[0], xa[1], xa[2], xa[3], wb[0], wb[1]);
+                lo_mma(acc[n + 1], xa[0], xa[1], xa[2], xa[3], wb[2], wb[3]);
+            }
+        }
+    }
+    lo_wait<0>();
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(lm_smem);                 // [64][RP] (twice where the halves are of the steps)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float* s = sums + ((RP == 16 ? LM_ROWS * half : 0) + 16 * rg + g) * RP + (RP == 16 ? 0 : RP / 2 * half) + 8 * n + 2 * t;
+        *reinterpret_cast<float2*>(s) = make_float2(acc[n][0], acc[n][1]);
+        *reinterpret_cast<float2*>(s + 8 * RP) = make_float2(acc[n][2], acc[n][3]);
+    }
+    __syncthreads();
+    if (RP == 16) {
+        for (int i = threadIdx.x; i < LM_ROWS * RP; i += 256) sums[i] += sums[LM_ROWS * RP + i];
+        __syncthreads();
+    }
+    if (a.splits > 1) {
+        lo_cluster_arrive();
+        lo_cluster_wait();
+    }
+    // a part of the rows for every block
+    const int r0 = tile.rows * part / a.splits, r1 = tile.rows * (part + 1) / a.splits;
+    for (int i = r0 * RP + 4 * threadIdx.x; i < r1 * RP; i += 1024) {
+        uint2 hi, lo;
+        lo_total(sums + i, a.splits, hi, lo);
+        uint16_t* h = a.h + tile.row0 * RP + i;
+        *reinterpret_cast<uint2*>(h) = hi;
+        *reinterpret_cast<uint2*>(h + a.total * RP) = lo;
+    }
+    if (a.splits > 1) {
+        lo_cluster_arrive();
+        lo_cluster_wait();
+    }
+}
+
+// ---- many rows: Y = base + scale B H ----
+constexpr int LM_COLS = 64;
+template <int RP, typename T>
+struct LmUp {
+    static constexpr int B = LM_COLS * RP * 2, BASE = LM_ROWS * LM_COLS * (int)sizeof(T), STAGE = B + BASE;
+    static constexpr int STAGES = STAGE <= 16384 ? 4 : 3;
+    static constexpr int SMEM = STAGES * STAGE;
+};
+// Place of a 16-byte piece of row `row` of B: the eight lanes that load together take every 2 RP / 64-th piece of two neighbouring rows.
+template <int RP>
+__device__ __forceinline__ unsigned lm_b_at(int row, int piece) {
+    if (RP == 128) piece ^= ((piece >> 3) << 1) ^ (row & 1);
+    if (RP == 64) piece ^= row & 1;
+    return (unsigned)(row * RP * 2 + piece * 16);
+}
+template <typename T>
+__device__ __forceinline__ unsigned lm_base_at(int row, int piece) {
+    return (unsigned)(row * LM_COLS * (int)sizeof(T) + ((piece ^ (sizeof(T) == 2 ? (row & 1) << 2 : row & 1)) << 4));
+}
+// 8 warps: 4 groups of 16 rows, 2 of 32 columns.
+template <int RP, typename T>
+__global__ void __launch_bounds__(256)
+lora_up_kernel(const LoArgs a, const int wide) {
+    using S = LmUp<RP, T>;
+    constexpr int KS = RP / 16, KW = RP / 8;
+    extern __shared__ __align__(128) unsigned char lm_smem[];
+    const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x);
+    const int64_t c0 = (int64_t)blockIdx.y * a.columns, c1 = min(a.out, c0 + a.columns);
+    if (tile.rows <= 0 || tile.adapter < 0) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (tile.rows > 0) lo_pass<T>(a, tile, c0, c1, wide);
+        return;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rg = warp & 3, cg = warp >> 2;
+    const T* base = static_cast<const T*>(a.base) + tile.row0 * a.ld_base;
+    T* y = static_cast<T*>(a.y) + tile.row0 * a.ldy;
+    const __nv_bfloat16* w = a.b + (int64_t)tile.adapter * a.out * a.rank;
+    const int tiles = (int)((c1 - c0 + LM_COLS - 1) / LM_COLS);
+    const unsigned ring = lo_smem(lm_smem);
+    auto issue = [&](int n) {
+        if (n < tiles) {
+            const unsigned dst = ring + (unsigned)((n % S::STAGES) * S::STAGE);
+            const int64_t c = c0 + LM_COLS * n;
+            constexpr int PB = RP / 8;                               // pieces of a row of B
+#pragma unroll
+            for (int i = 0; i < LM_COLS * PB; i += 256) {
+                const int row = (i + (int)threadIdx.x) / PB, piece = (i + (int)threadIdx.x) % PB;
+                if (LM_COLS * PB < 256 && row >= LM_COLS) break;
+                const bool take = c + row < c1 && 8 * piece < a.rank;
+                lo_copy16(dst + lm_b_at<RP>(row, piece), take ? w + (c + row) * a.rank + 8 * piece : a.b, take);
+            }
+            if (wide) {
+                constexpr int PT = LM_COLS * (int)sizeof(T) / 16, PE = 16 / (int)sizeof(T);
+#pragma unroll
+                for (int i = 0; i < LM_ROWS * PT; i += 256) {
+                    const int row = (i + (int)threadIdx.x) / PT, piece = (i + (int)threadIdx.x) % PT;
+                    const bool take = row < tile.rows && c + PE * (piece + 1) <= c1;
+                    lo_copy16(dst + S::B + lm_base_at<T>(row, piece), take ? static_cast<const void*>(base + row * a.ld_base + c + PE * piece) : a.b, take);
                 }
             }
         }
-        const int64_t col = c + 8 * t;                               // a lane's eight columns
-        const int left = (int)min((int64_t)8, c1 - col);
-        if (left <= 0) continue;
+        lo_commit();
+    };
 #pragma unroll
-        for (int m = 0; m < MW; ++m)
+    for (int n = 0; n < S::STAGES - 1; ++n) issue(n);
+    asm volatile("griddepcontrol.wait;" ::: "memory");                // H is there from here on
+    uint32_t h[2][2][KW];                                            // [hi, lo][row g, g + 8]
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = 16 * (MW * rg + m) + g + 8 * e;
-                if (r >= tile.rows) continue;
-                const float x[8] = {acc[m][0][2 * e], acc[m][0][2 * e + 1], acc[m][1][2 * e], acc[m][1][2 * e + 1],
-                                    acc[m][2][2 * e], acc[m][2][2 * e + 1], acc[m][3][2 * e], acc[m][3][2 * e + 1]};
-                LoOut<T> o;
-                o.load(base + r * a.ld_base + col, left, wide);
-                o.add(x, scale);
-                o.store(y + r * a.ldy + col, left, wide);
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 16 * rg + g + 8 * e;
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(a.h + (k * a.total + tile.row0 + min(r, tile.rows - 1)) * RP + 2 * KW * t);
+#pragma unroll
+            for (int i = 0; i < KW; i += 2) {
+                const uint2 x = __ldcg(reinterpret_cast<const uint2*>(p + i));
+                h[k][e][i] = r < tile.rows ? x.x : 0u;
+                h[k][e][i + 1] = r < tile.rows ? x.y : 0u;
             }
+        }
+    const float scale = a.scale ? __ldg(a.scale + tile.adapter) : 1.f;
+    for (int n = 0; n < tiles; ++n) {
+        lo_wait<S::STAGES - 2>();
+        __syncthreads();
+        issue(n + S::STAGES - 1);
+        const unsigned at = ring + (unsigned)((n % S::STAGES) * S::STAGE);
+        float acc[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = 32 * cg + 8 * (g >> 1) + 2 * j + (g & 1);                // column n of tile j: 8 (n / 2) + 2 j + n % 2
+            uint32_t v[KW];
+            if constexpr (KW >= 4) {
+#pragma unroll
+                for (int i = 0; i < KW / 4; ++i) {
+                    const uint4 x = lo_lds16(at + lm_b_at<RP>(row, KW / 4 * t + i));
+                    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+                }
+            } else {
+                const uint2 x = lo_lds8(at + (unsigned)(row * RP * 2 + 8 * t));
+                v[0] = x.x; v[1] = x.y;
+            }
+            acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int k = 1; k >= 0; --k)
+                    lo_mma(acc[j], h[k][0][2 * s], h[k][1][2 * s], h[k][0][2 * s + 1], h[k][1][2 * s + 1], v[2 * s], v[2 * s + 1]);
+        }
+        const int64_t col = c0 + LM_COLS * n + 32 * cg + 8 * t;      // a lane's eight columns
+        const int left = (int)min((int64_t)8, c1 - col);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 16 * rg + g + 8 * e;
+            if (left <= 0 || r >= tile.rows) continue;
+            LoOut<T> o;
+            if (wide && left == 8) {
+                if constexpr (sizeof(T) == 2) o.v = lo_lds16(at + S::B + lm_base_at<T>(r, 4 * cg + t));
+                else {
+                    const uint4 p = lo_lds16(at + S::B + lm_base_at<T>(r, 8 * cg + 2 * t)), q = lo_lds16(at + S::B + lm_base_at<T>(r, 8 * cg + 2 * t + 1));
+                    o.v[0] = __uint_as_float(p.x); o.v[1] = __uint_as_float(p.y); o.v[2] = __uint_as_float(p.z); o.v[3] = __uint_as_float(p.w);
+                    o.v[4] = __uint_as_float(q.x); o.v[5] = __uint_as_float(q.y); o.v[6] = __uint_as_float(q.z); o.v[7] = __uint_as_float(q.w);
+                }
+            } else o.load(base + r * a.ld_base + col, left, false);
+            const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
+                                acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
+            o.add(x, scale);
+            o.store(y + r * a.ldy + col, left, wide);
+        }
     }
+    lo_wait<0>();
 }
 
-template <int RP, int MG>
-sb_status down_launch(sb_ctx* ctx, const LoArgs& a, int64_t tiles) {
-    auto* kernel = lora_down_kernel<RP, MG>;
-    constexpr int smem = 8 * 16 * RP * 4;
-    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    kernel<<<dim3((unsigned)tiles, (unsigned)a.splits), 256, smem, ctx->stream>>>(a);
+// A launch in clusters of `cluster` blocks along x, or one that starts while the kernel before it still runs.
+template <typename... P>
+sb_status lo_launch(sb_ctx* ctx, void (*kernel)(P...), dim3 grid, int smem, int cluster, bool early, P... args) {
+    if (smem > 40 * 1024) SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (cluster > 8) SB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchAttribute at[2];
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cfg.attrs = at;
+    if (cluster > 1) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        at[cfg.numAttrs].val.clusterDim.x = cluster;
+        at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    if (early) {
+        at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
+    SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, args...));
     SB_LAUNCHED(ctx);
     return SB_OK;
 }
-template <int RP, int MW, int RG>
-sb_status up_launch(sb_ctx* ctx, const LoArgs& a, int64_t tiles, int f32, int wide) {
-    const dim3 grid((unsigned)tiles, (unsigned)((a.out + a.columns - 1) / a.columns));
-    if (f32) lora_up_kernel<RP, MW, RG, float><<<grid, 256, 0, ctx->stream>>>(a, wide);
-    else lora_up_kernel<RP, MW, RG, __nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(a, wide);
-    SB_LAUNCHED(ctx);
-    return SB_OK;
-}
 
-// Rows of a tile of either kernel: 16 where every request fits into that, else 64.
-template <int RP>
-sb_status lo_run(sb_ctx* ctx, LoArgs& a, int f32, int wide) {
+template <int RP, typename T>
+sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
     a.direct = a.max_new <= 16;
-    const int64_t tiles = a.direct ? a.requests : (a.total + 63) / 64 + a.requests;
-    if (tiles >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "lora: too many rows");
-    // parts of `in`: four blocks a multiprocessor, of 1024 at least
-    int64_t splits = 4 * ctx->sm_count / tiles, most = (a.in + 1023) / 1024;
-    splits = splits > most ? most : splits;
-    a.splits = splits < 1 ? 1 : (int)splits;
-    void* arena;
-    sb_status s = sb_scratch(ctx, Carver::need({(size_t)a.splits * (size_t)a.total * RP * 4}), &arena);
-    if (s != SB_OK) return s;
-    a.h = Carver(arena).take<float>((size_t)a.splits * (size_t)a.total * RP);
-    // columns of a block of the second kernel: eight blocks a multiprocessor
-    int64_t parts = 8 * ctx->sm_count / tiles, unit = a.direct ? 256 : 32 * (RP == 128 ? 2 : 4);
-    most = (a.out + unit - 1) / unit;
-    parts = parts > most ? most : parts;
-    if (parts < 1) parts = 1;
-    if (parts > 65535) parts = 65535;
-    a.columns = (most + parts - 1) / parts * unit;
+    auto cut = [](int64_t x, int64_t most) { return x < 1 ? 1 : x > most ? most : x; };
     if (a.direct) {
-        s = down_launch<RP, 1>(ctx, a, tiles);
-        return s != SB_OK ? s : up_launch<RP, 1, 1>(ctx, a, tiles, f32, wide);
+        // blocks of a cluster, a power of two: eight a multiprocessor, but 512 of `in` and of `out` each at least
+        int64_t want = cut(8 * ctx->sm_count / a.requests, 16), most = cut((a.in + a.out + 1023) / 1024, 16);
+        if (want > most) want = most;
+        for (a.splits = 1; 2 * a.splits <= want;) a.splits *= 2;
+        a.columns = ((a.out + a.splits - 1) / a.splits + 255) / 256 * 256;
+        return lo_launch(ctx, lora_few_kernel<RP, T>, dim3((unsigned)(a.requests * a.splits)), 8 / (RP > 64 ? RP / 64 : 1) * 16 * RP * 4, a.splits, false, a, wide);
     }
-    s = down_launch<RP, 4>(ctx, a, tiles);
+    const int64_t tiles = (a.total + LM_ROWS - 1) / LM_ROWS + a.requests, full = (a.total + LM_ROWS - 1) / LM_ROWS;
+    // parts of `in`: two blocks a multiprocessor, but 512 each at least
+    int64_t want = cut(2 * ctx->sm_count / full, 16), most = cut((a.in + 511) / 512, 16);
+    if (want > most) want = most;
+    for (a.splits = 1; 2 * a.splits <= want;) a.splits *= 2;
+    if (tiles * a.splits >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "lora: too many rows");
+    const size_t n = (size_t)a.total * RP;
+    void* arena;
+    sb_status s = sb_scratch(ctx, Carver::need({2 * n * 2}), &arena);
     if (s != SB_OK) return s;
-    if constexpr (RP == 128) return up_launch<RP, 1, 4>(ctx, a, tiles, f32, wide);
-    else return up_launch<RP, 2, 2>(ctx, a, tiles, f32, wide);
+    a.h = Carver(arena).take<uint16_t>(2 * n);
+    s = lo_launch(ctx, lora_down_kernel<RP>, dim3((unsigned)(tiles * a.splits)), LmDown<RP>::SMEM, a.splits, false, a);
+    if (s != SB_OK) return s;
+    // columns of a block of the second kernel: eight blocks a multiprocessor, four tiles each at least
+    most = (a.out + 4 * LM_COLS - 1) / (4 * LM_COLS);
+    const int64_t parts = cut(8 * ctx->sm_count / full, most < 65535 ? most : 65535), each = (a.out + LM_COLS - 1) / LM_COLS;
+    a.columns = (each + parts - 1) / parts * LM_COLS;
+    return lo_launch(ctx, lora_up_kernel<RP, T>, dim3((unsigned)tiles, (unsigned)((a.out + a.columns - 1) / a.columns)), LmUp<RP, T>::SMEM, 1, true, a, wide);
+}
+template <int RP>
+sb_status lo_by_type(sb_ctx* ctx, LoArgs& a, int f32, int wide) {
+    return f32 ? lo_run<RP, float>(ctx, a, wide) : lo_run<RP, __nv_bfloat16>(ctx, a, wide);
 }
 
 }  // namespace
@@ -390,6 +722,6 @@ extern "C" sb_status sb_lora_add(sb_ctx* ctx, const sb_lora_adapters* ad, const 
     a.starts = starts; a.ids = ids; a.requests = requests; a.adapters = ad->adapters; a.rank = ad->rank;
     a.max_new = (int)max_new; a.st = ctx->dstate;
     const int wide = (ends & 15) == 0 && (total == 1 || ((ld_base * size) % 16 == 0 && (ldy * size) % 16 == 0));
-    return ad->rank <= 16 ? lo_run<16>(ctx, a, f32, wide) : ad->rank <= 32 ? lo_run<32>(ctx, a, f32, wide)
-         : ad->rank <= 64 ? lo_run<64>(ctx, a, f32, wide) : lo_run<128>(ctx, a, f32, wide);
+    return ad->rank <= 16 ? lo_by_type<16>(ctx, a, f32, wide) : ad->rank <= 32 ? lo_by_type<32>(ctx, a, f32, wide)
+         : ad->rank <= 64 ? lo_by_type<64>(ctx, a, f32, wide) : lo_by_type<128>(ctx, a, f32, wide);
 }

@@ -62,7 +62,8 @@ class Case:
     ([1], [0], 8, 1, 8, 1), ([1], [2], 4096, 512, 16, 3), ([1] * 20, list(range(20)), 256, 96, 8, 20), ([1, 0, 3, 5], [1, 0, -1, 1], 520, 264, 24, 2),
     ([16, 15, 1], [0, 1, 0], 1000, 333, 32, 2), ([17], [0], 64, 40, 64, 1), ([100, 0, 1, 64], [1, 1, 0, -1], 776, 100, 40, 2),
     ([65, 63], [0, 0], 2048, 1032, 128, 1), ([200, 33], [1, 0], 136, 77, 104, 2), ([130], [0], 4104, 256, 16, 1), ([300, 5, 70], [2, 1, 0], 512, 640, 64, 3),
-    ([90], [-1], 64, 50, 8, 1), ([2, 16], [1, 1], 14336, 64, 48, 2)])
+    ([90], [-1], 64, 50, 8, 1), ([90, 80], [1, 0], 1032, 200, 24, 2), ([80], [0], 6000, 300, 32, 1), ([1], [0], 14336, 4100, 128, 1), ([3], [0], 9000, 9000, 64, 1),
+    ([20] * 40, [i % 7 - 1 for i in range(40)], 1024, 128, 32, 6), ([2, 16], [1, 1], 14336, 64, 48, 2)])
 def test_sizes(ctx, dtype, new, ids, inner, outer, rank, adapters):
     case = Case(new, ids, inner, outer, rank, adapters, dtype)
     x, base = _device(case.x), case.base.clone()
