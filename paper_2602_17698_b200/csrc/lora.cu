@@ -157,6 +157,8 @@ __device__ __forceinline__ void lo_total(const float* own, int blocks, uint2& hi
 template <typename T> struct LoOut;
 template <> struct LoOut<__nv_bfloat16> {
     uint4 v;
+    // from shared memory: 16 bytes (fp32: and 16 more)
+    __device__ __forceinline__ void take(unsigned at, unsigned) { v = lo_lds16(at); }
     __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool wide) {
         if (wide && left >= 8) v = *reinterpret_cast<const uint4*>(p);
         else {
@@ -187,6 +189,11 @@ template <> struct LoOut<__nv_bfloat16> {
 };
 template <> struct LoOut<float> {
     float v[8];
+    __device__ __forceinline__ void take(unsigned at, unsigned more) {
+        const uint4 p = lo_lds16(at), q = lo_lds16(more);
+        v[0] = __uint_as_float(p.x); v[1] = __uint_as_float(p.y); v[2] = __uint_as_float(p.z); v[3] = __uint_as_float(p.w);
+        v[4] = __uint_as_float(q.x); v[5] = __uint_as_float(q.y); v[6] = __uint_as_float(q.z); v[7] = __uint_as_float(q.w);
+    }
     __device__ __forceinline__ void load(const float* p, int left, bool wide) {
         if (wide && left >= 8) {
             const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
@@ -226,37 +233,58 @@ __device__ __forceinline__ void lo_pass(const LoArgs& a, const LoTile& tile, int
             v.store(y + r * a.ldy + c, left, wide);
         }
 }
-// The KW words (pairs along the rank) of a row of 32 KW / 8 .. that lane t takes
-template <int KW>
-__device__ __forceinline__ void lo_words(const __nv_bfloat16* row, int t, int rank, uint32_t (&v)[KW]) {
-    const __nv_bfloat16* p = row + 2 * KW * t;
-    if (rank == 8 * KW) {
-        if constexpr (KW >= 4) {
+// Place of a 16-byte piece of row `row` of B: the eight lanes that load together take every 2 RP / 64-th piece of two neighbouring rows.
+template <int RP>
+__device__ __forceinline__ unsigned lm_b_at(int row, int piece) {
+    if (RP == 128) piece ^= ((piece >> 3) << 1) ^ (row & 1);
+    if (RP == 64) piece ^= row & 1;
+    return (unsigned)(row * RP * 2 + piece * 16);
+}
+// The words (pairs along the rank) of row `row` of B that lane t takes
+template <int RP>
+__device__ __forceinline__ void lo_words(unsigned at, int row, int t, uint32_t (&v)[RP / 8]) {
+    constexpr int KW = RP / 8;
+    if constexpr (KW >= 4) {
 #pragma unroll
-            for (int i = 0; i < KW / 4; ++i) {
-                const uint4 x = lo_ld16(p + 8 * i);
-                v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
-            }
-        } else {
-            const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
-            v[0] = x.x; v[1] = x.y;
+        for (int i = 0; i < KW / 4; ++i) {
+            const uint4 x = lo_lds16(at + lm_b_at<RP>(row, KW / 4 * t + i));
+            v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
         }
     } else {
-#pragma unroll
-        for (int i = 0; i < KW; ++i) v[i] = 2 * (KW * t + i) < rank ? __ldg(reinterpret_cast<const uint32_t*>(p) + i) : 0u;
+        const uint2 x = lo_lds8(at + (unsigned)(row * RP * 2 + 8 * t));
+        v[0] = x.x; v[1] = x.y;
     }
+}
+template <typename T>
+__device__ __forceinline__ unsigned lf_base_at(int row, int piece) {
+    return (unsigned)(row * 32 * (int)sizeof(T) + ((sizeof(T) == 2 ? piece : piece ^ (row & 1)) << 4));
 }
 
 // ---- few rows ----
-// A cluster per request, 8 warps a block. RP: rank rounded up to 16, 32, 64 or 128.
 template <int RP, typename T>
-__global__ void __launch_bounds__(256)
+struct LfShape {
+    static constexpr int NG = RP > 64 ? RP / 64 : 1, KG = 8 / NG;     // warps along the rank and along `in`
+    static constexpr int B = 32 * RP * 2, BASE = 16 * 32 * (int)sizeof(T), STAGE = B + BASE;      // of a warp: 32 columns
+    static constexpr int CTAS = RP >= 64 ? 1 : 2;                    // resident per SM
+    static constexpr int SUMS = KG * 16 * RP * 4;
+    static constexpr int H = 2 * 16 * (RP + 8) * 2;
+    static constexpr int FIT = (224 * 1024 / CTAS - SUMS - H) / (8 * STAGE), STAGES = FIT > 4 ? 4 : FIT;
+    static_assert(STAGES >= 2, "");
+    static constexpr int RING = 8 * STAGES * STAGE;
+    static constexpr int SMEM = RING + SUMS + H;
+};
+// A cluster per request, 8 warps a block. RP: rank rounded up to 16, 32, 64 or 128. Every warp brings the operands of its columns
+// through a ring of its own, from the start on: they do not wait for the first product.
+template <int RP, typename T>
+__global__ void __launch_bounds__(256, LfShape<RP, T>::CTAS)
 lora_few_kernel(const LoArgs a, const int wide) {
-    constexpr int NG = RP > 64 ? RP / 64 : 1, KG = 8 / NG, NT = RP / 8 / NG;       // warps along the rank and along `in`; tiles of a warp
+    using S = LfShape<RP, T>;
+    constexpr int NG = S::NG, KG = S::KG, NT = RP / 8 / NG;                       // NT: tiles of 8 of the rank a warp has
     constexpr int U = RP == 16 ? 4 : 2;                                          // units of 32 of `in` whose loads overlap
     constexpr int KS = RP / 16, KW = RP / 8;
-    extern __shared__ __align__(16) float lo_sums[];                 // [KG][16][RP]; then the first is the block's sum
-    __shared__ __align__(16) uint16_t held[2][16][RP + 8];             // H: hi, lo
+    extern __shared__ __align__(128) unsigned char lm_smem[];
+    float* lo_sums = reinterpret_cast<float*>(lm_smem + S::RING);    // [KG][16][RP]; then the first is the block's sum
+    uint16_t* held = reinterpret_cast<uint16_t*>(lm_smem + S::RING + S::SUMS);     // H: [hi, lo][16][RP + 8]
     const LoTile tile = lo_tile<16, 256>(a, blockIdx.x / a.splits);
     const int rank = blockIdx.x % a.splits;                          // of the block in its cluster
     if (tile.rows <= 0) return;
@@ -266,6 +294,36 @@ lora_few_kernel(const LoArgs a, const int wide) {
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const T* base = static_cast<const T*>(a.base) + tile.row0 * a.ld_base;
+    T* y = static_cast<T*>(a.y) + tile.row0 * a.ldy;
+    const __nv_bfloat16* b = a.b + (int64_t)tile.adapter * a.out * a.rank;
+    const int64_t first = c0 + 32 * warp;
+    const unsigned ring = lo_smem(lm_smem) + (unsigned)(warp * S::STAGES * S::STAGE);
+    auto issue = [&](int n) {
+        const int64_t c = first + 256 * (int64_t)n;
+        const unsigned dst = ring + (unsigned)((n % S::STAGES) * S::STAGE);
+        if (c < c1) {
+            constexpr int PB = RP / 8;                               // pieces of a row of B
+#pragma unroll
+            for (int i = 0; i < PB; ++i) {
+                const int row = (32 * i + lane) / PB, piece = (32 * i + lane) % PB;
+                const bool take = c + row < c1 && 8 * piece < a.rank;
+                lo_copy16(dst + lm_b_at<RP>(row, piece), take ? b + (c + row) * a.rank + 8 * piece : a.b, take);
+            }
+            if (wide) {
+                constexpr int PT = 2 * (int)sizeof(T), PE = 16 / (int)sizeof(T);      // pieces of a row of base, elements of one
+#pragma unroll
+                for (int i = 0; i < PT / 2; ++i) {
+                    const int row = (32 * i + lane) / PT, piece = (32 * i + lane) % PT;
+                    const bool take = row < tile.rows && c + PE * (piece + 1) <= c1;
+                    lo_copy16(dst + S::B + lf_base_at<T>(row, piece), take ? static_cast<const void*>(base + row * a.ld_base + c + PE * piece) : a.b, take);
+                }
+            }
+        }
+        lo_commit();
+    };
+#pragma unroll
+    for (int n = 0; n < S::STAGES - 1; ++n) issue(n);
     {
         const int ng = warp % NG, kg = warp / NG;
         const int64_t units = (a.in + 31) / 32, parts = (int64_t)a.splits * KG, part = (int64_t)rank * KG + kg;
@@ -302,25 +360,6 @@ lora_few_kernel(const LoArgs a, const int wide) {
             *reinterpret_cast<float2*>(s + 8 * RP) = make_float2(acc[n][2], acc[n][3]);
         }
     }
-    // the first columns' operands are on their way while the parts are added
-    const int64_t first = c0 + 32 * warp;
-    const __nv_bfloat16* w = a.b + (int64_t)tile.adapter * a.out * a.rank;
-    constexpr bool AHEAD = RP <= 64;                                 // registers for the columns after these
-    uint32_t v[4][KW], next[AHEAD ? 4 : 1][KW];
-    auto fetch = [&](int64_t c, auto& v) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            // column n of tile j is c + 8 (n / 2) + 2 j + n % 2
-            const int64_t col = c + 8 * (g >> 1) + 2 * j + (g & 1);
-            if (col < c1) lo_words<KW>(w + col * a.rank, t, a.rank, v[j]);
-            else {
-#pragma unroll
-                for (int i = 0; i < KW; ++i) v[j][i] = 0;
-            }
-        }
-    };
-    fetch(first, v);
-    if constexpr (AHEAD) fetch(first + 256, next);
     __syncthreads();
     for (int i = 4 * threadIdx.x; i < tile.rows * RP; i += 1024) {
         float4 sum = *reinterpret_cast<const float4*>(lo_sums + i);
@@ -338,8 +377,8 @@ lora_few_kernel(const LoArgs a, const int wide) {
     for (int i = 4 * threadIdx.x; i < 16 * RP; i += 1024) {
         uint2 hi = make_uint2(0, 0), lo = hi;
         if (i < tile.rows * RP) lo_total(lo_sums + i, a.splits, hi, lo);
-        *reinterpret_cast<uint2*>(&held[0][i / RP][i % RP]) = hi;
-        *reinterpret_cast<uint2*>(&held[1][i / RP][i % RP]) = lo;
+        *reinterpret_cast<uint2*>(held + i / RP * (RP + 8) + i % RP) = hi;
+        *reinterpret_cast<uint2*>(held + (16 + i / RP) * (RP + 8) + i % RP) = lo;
     }
     if (a.splits > 1) lo_cluster_arrive();                           // what others hold has been read
     __syncthreads();
@@ -348,47 +387,46 @@ lora_few_kernel(const LoArgs a, const int wide) {
     for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(&held[k][g + 8 * e][2 * KW * t]);
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(held + (16 * k + g + 8 * e) * (RP + 8) + 2 * KW * t);
 #pragma unroll
             for (int i = 0; i < KW; ++i) h[k][e][i] = p[i];
         }
     const float scale = a.scale ? __ldg(a.scale + tile.adapter) : 1.f;
-    const T* base = static_cast<const T*>(a.base) + tile.row0 * a.ld_base;
-    T* y = static_cast<T*>(a.y) + tile.row0 * a.ldy;
-    for (int64_t c = first; c < c1; c += 256) {
-        if (!AHEAD && c != first) fetch(c, v);
-        const int64_t col = c + 8 * t;                               // a lane's eight columns
-        const int left = (int)max((int64_t)0, min((int64_t)8, c1 - col));
-        LoOut<T> o[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (left > 0 && g + 8 * e < tile.rows) o[e].load(base + (g + 8 * e) * a.ld_base + col, left, wide);
+    int n = 0;
+    for (int64_t c = first; c < c1; c += 256, ++n) {
+        lo_wait<S::STAGES - 2>();
+        __syncwarp();
+        issue(n + S::STAGES - 1);
+        const unsigned at = ring + (unsigned)((n % S::STAGES) * S::STAGE);
         float acc[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            uint32_t v[KW];
+            lo_words<RP>(at, 8 * (g >> 1) + 2 * j + (g & 1), t, v);         // column n of tile j is c + 8 (n / 2) + 2 j + n % 2
             acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
                 for (int k = 1; k >= 0; --k)
-                    lo_mma(acc[j], h[k][0][2 * s], h[k][1][2 * s], h[k][0][2 * s + 1], h[k][1][2 * s + 1], v[j][2 * s], v[j][2 * s + 1]);
+                    lo_mma(acc[j], h[k][0][2 * s], h[k][1][2 * s], h[k][0][2 * s + 1], h[k][1][2 * s + 1], v[2 * s], v[2 * s + 1]);
         }
-        if constexpr (AHEAD) {
+        const int64_t col = c + 8 * t;                               // a lane's eight columns
+        const int left = (int)min((int64_t)8, c1 - col);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < KW; ++i) v[j][i] = next[j][i];
-            fetch(c + 512, next);
+        for (int e = 0; e < 2; ++e) {
+            const int r = g + 8 * e;
+            if (left <= 0 || r >= tile.rows) continue;
+            LoOut<T> o;
+            if (wide && left == 8) o.take(at + S::B + lf_base_at<T>(r, (int)sizeof(T) / 2 * t), at + S::B + lf_base_at<T>(r, 2 * t + 1));
+            else o.load(base + r * a.ld_base + col, left, false);
+            const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
+                                acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
+            o.add(x, scale);
+            o.store(y + r * a.ldy + col, left, wide);
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (left > 0 && g + 8 * e < tile.rows) {
-                const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
-                                    acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
-                o[e].add(x, scale);
-                o[e].store(y + (g + 8 * e) * a.ldy + col, left, wide);
-            }
+        __syncwarp();
     }
+    lo_wait<0>();
     if (a.splits > 1) lo_cluster_wait();
 }
 
@@ -505,13 +543,6 @@ struct LmUp {
     static constexpr int STAGES = STAGE <= 16384 ? 4 : 3;
     static constexpr int SMEM = STAGES * STAGE;
 };
-// Place of a 16-byte piece of row `row` of B: the eight lanes that load together take every 2 RP / 64-th piece of two neighbouring rows.
-template <int RP>
-__device__ __forceinline__ unsigned lm_b_at(int row, int piece) {
-    if (RP == 128) piece ^= ((piece >> 3) << 1) ^ (row & 1);
-    if (RP == 64) piece ^= row & 1;
-    return (unsigned)(row * RP * 2 + piece * 16);
-}
 template <typename T>
 __device__ __forceinline__ unsigned lm_base_at(int row, int piece) {
     return (unsigned)(row * LM_COLS * (int)sizeof(T) + ((piece ^ (sizeof(T) == 2 ? (row & 1) << 2 : row & 1)) << 4));
@@ -589,16 +620,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
         for (int j = 0; j < 4; ++j) {
             const int row = 32 * cg + 8 * (g >> 1) + 2 * j + (g & 1);                // column n of tile j: 8 (n / 2) + 2 j + n % 2
             uint32_t v[KW];
-            if constexpr (KW >= 4) {
-#pragma unroll
-                for (int i = 0; i < KW / 4; ++i) {
-                    const uint4 x = lo_lds16(at + lm_b_at<RP>(row, KW / 4 * t + i));
-                    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
-                }
-            } else {
-                const uint2 x = lo_lds8(at + (unsigned)(row * RP * 2 + 8 * t));
-                v[0] = x.x; v[1] = x.y;
-            }
+            lo_words<RP>(at, row, t, v);
             acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 #pragma unroll
             for (int s = 0; s < KS; ++s)
@@ -613,14 +635,9 @@ lora_up_kernel(const LoArgs a, const int wide) {
             const int r = 16 * rg + g + 8 * e;
             if (left <= 0 || r >= tile.rows) continue;
             LoOut<T> o;
-            if (wide && left == 8) {
-                if constexpr (sizeof(T) == 2) o.v = lo_lds16(at + S::B + lm_base_at<T>(r, 4 * cg + t));
-                else {
-                    const uint4 p = lo_lds16(at + S::B + lm_base_at<T>(r, 8 * cg + 2 * t)), q = lo_lds16(at + S::B + lm_base_at<T>(r, 8 * cg + 2 * t + 1));
-                    o.v[0] = __uint_as_float(p.x); o.v[1] = __uint_as_float(p.y); o.v[2] = __uint_as_float(p.z); o.v[3] = __uint_as_float(p.w);
-                    o.v[4] = __uint_as_float(q.x); o.v[5] = __uint_as_float(q.y); o.v[6] = __uint_as_float(q.z); o.v[7] = __uint_as_float(q.w);
-                }
-            } else o.load(base + r * a.ld_base + col, left, false);
+            if (wide && left == 8)
+                o.take(at + S::B + lm_base_at<T>(r, (int)sizeof(T) / 2 * (4 * cg + t)), at + S::B + lm_base_at<T>(r, (int)sizeof(T) / 2 * (4 * cg + t) + 1));
+            else o.load(base + r * a.ld_base + col, left, false);
             const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
                                 acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
             o.add(x, scale);
@@ -663,12 +680,12 @@ sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
     a.direct = a.max_new <= 16;
     auto cut = [](int64_t x, int64_t most) { return x < 1 ? 1 : x > most ? most : x; };
     if (a.direct) {
-        // blocks of a cluster, a power of two: eight a multiprocessor, but 512 of `in` and of `out` each at least
-        int64_t want = cut(8 * ctx->sm_count / a.requests, 16), most = cut((a.in + a.out + 1023) / 1024, 16);
+        // blocks of a cluster, a power of two: as many as are resident at once, but 512 of `in` and of `out` each at least
+        int64_t want = cut(LfShape<RP, T>::CTAS * ctx->sm_count / a.requests, 16), most = cut((a.in + a.out + 1023) / 1024, 16);
         if (want > most) want = most;
         for (a.splits = 1; 2 * a.splits <= want;) a.splits *= 2;
         a.columns = ((a.out + a.splits - 1) / a.splits + 255) / 256 * 256;
-        return lo_launch(ctx, lora_few_kernel<RP, T>, dim3((unsigned)(a.requests * a.splits)), 8 / (RP > 64 ? RP / 64 : 1) * 16 * RP * 4, a.splits, false, a, wide);
+        return lo_launch(ctx, lora_few_kernel<RP, T>, dim3((unsigned)(a.requests * a.splits)), LfShape<RP, T>::SMEM, a.splits, false, a, wide);
     }
     const int64_t tiles = (a.total + LM_ROWS - 1) / LM_ROWS + a.requests, full = (a.total + LM_ROWS - 1) / LM_ROWS;
     // parts of `in`: two blocks a multiprocessor, but 512 each at least
