@@ -23,9 +23,12 @@ namespace {
 constexpr int K4_PROMPT_FROM = 24;       // more query rows than this per cache head go to the tcgen05 kernel
 
 template <int BYTES>
-__device__ __forceinline__ void k4_copy(unsigned dst, const void* src, bool take) {
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(take ? BYTES : 0) : "memory");
+__device__ __forceinline__ void k4_copy(unsigned dst, const void* src) {
+    if (BYTES == 16) at_copy16(dst, src);
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void k4_copy4(unsigned dst, const void* src, bool take) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(take ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ uint32_t k4_lds32(unsigned a) {
     uint32_t v;
@@ -74,7 +77,8 @@ __device__ __forceinline__ unsigned k4_at(int row, int piece) {
     return (unsigned)(row * 128 + ((piece ^ ((row & 3) << 1) ^ (row & 4)) << 4));
 }
 
-template <int DP, int NR>
+// FULL: a head has DP elements, so a token's bytes are known here.
+template <int DP, int NR, bool FULL>
 __global__ void __launch_bounds__(AT_WARPS * 32, K4Shape<DP, NR>::CTAS)
 kv4_rows_kernel(const AtArgs a) {
     using S = K4Shape<DP, NR>;
@@ -87,7 +91,7 @@ kv4_rows_kernel(const AtArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const int D = a.g.dim;
-    const int pitch = kv4_code_pitch(D), spitch = kv4_scale_pitch(D);
+    const int pitch = FULL ? S::ROW : kv4_code_pitch(D), spitch = FULL ? S::SROW : kv4_scale_pitch(D);
     AtWalk<S::ROWS, AT_STEP, AT_EXTRA> wk;
     long long share;
     if (!at_share<S>(a, smem, wk, share)) return;
@@ -137,40 +141,53 @@ kv4_rows_kernel(const AtArgs a) {
         // copies of step j of this warp into its ring
         constexpr int PIECES = DP / 32, TOKS = 32 / PIECES;          // 16-byte pieces of a token; tokens of one instruction
         const int cp_piece = lane % PIECES, cp_tok = lane / PIECES;
+        const int cp_off = cp_tok * pitch + cp_piece * 16, sc_off = (lane & (SB_KV8_BLOCK - 1)) * spitch;
+        unsigned cp_to[SB_KV8_BLOCK / TOKS];                         // where this lane's pieces of a block go
+#pragma unroll
+        for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) cp_to[i] = ring + k4_at<DP>(cp_tok + TOKS * i, cp_piece);
+        const unsigned sc_to = ring + (unsigned)(2 * S::CODES + lane * S::SROW);
         auto issue = [&](int j) {
             if (j < mine) {
                 const int key = k0 + (warp + AT_WARPS * j) * AT_STEP;
-                const unsigned dst = ring + (unsigned)((j % S::STAGES) * S::STAGE);
+                const unsigned dst = (unsigned)((j % S::STAGES) * S::STAGE);
                 const int64_t held = (j / AT_BATCH) & 1 ? at_odd : at_even;
                 int64_t base[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    base[e] = __shfl_sync(0xffffffffu, held, 2 * (j & (AT_BATCH - 1)) + e);
-                    const uint8_t *kp = a.k + base[e] * pitch + cp_piece * 16, *vp = a.v + base[e] * pitch + cp_piece * 16;
+                for (int e = 0; e < 2; ++e) base[e] = __shfl_sync(0xffffffffu, held, 2 * (j & (AT_BATCH - 1)) + e);
+                const int64_t sat = (lane < SB_KV8_BLOCK ? base[0] : base[1]) * spitch + sc_off;        // a token's scales per lane
+                if (FULL && base[0] >= 0 && base[1] >= 0 && key + AT_STEP <= rq.len) {
 #pragma unroll
-                    for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
-                        // zeros where there is no block, behind the request's end and behind the row's
-                        const int tok = cp_tok + TOKS * i;
-                        const bool take = base[e] >= 0 && key + SB_KV8_BLOCK * e + tok < rq.len && cp_piece * 16 < pitch;
-                        const unsigned to = k4_at<DP>(SB_KV8_BLOCK * e + tok, cp_piece);
-                        k4_copy<16>(dst + to, take ? kp + tok * pitch : a.k, take);
-                        k4_copy<16>(dst + S::CODES + to, take ? vp + tok * pitch : a.v, take);
+                    for (int e = 0; e < 2; ++e) {
+                        const uint8_t *kp = a.k + (base[e] * pitch + cp_off), *vp = a.v + (base[e] * pitch + cp_off);
+#pragma unroll
+                        for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
+                            // (a block further on the swizzle is the same)
+                            const unsigned to = cp_to[i] + dst + (unsigned)(SB_KV8_BLOCK * e * S::ROW);
+                            at_copy16(to, kp + TOKS * i * S::ROW);
+                            at_copy16(to + S::CODES, vp + TOKS * i * S::ROW);
+                        }
                     }
-                }
-                // a token's scales per lane
-                const int64_t sbase = lane < SB_KV8_BLOCK ? base[0] : base[1];
-                const bool take = sbase >= 0 && key + lane < rq.len;
-                const int64_t at = (sbase + (lane & (SB_KV8_BLOCK - 1))) * spitch;
-                const unsigned to = dst + 2 * S::CODES + (unsigned)(lane * S::SROW);
-                if (spitch == S::SROW) {
-                    k4_copy<S::SROW>(to, take ? a.k_scale4 + at : a.k_scale4, take);
-                    k4_copy<S::SROW>(to + S::SCALES, take ? a.v_scale4 + at : a.v_scale4, take);
+                    k4_copy<S::SROW>(sc_to + dst, a.k_scale4 + sat);
+                    k4_copy<S::SROW>(sc_to + dst + S::SCALES, a.v_scale4 + sat);
                 } else {
+                    // zeros where there is no block, behind the request's end and behind the row's
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int i = 0; i < SB_KV8_BLOCK / TOKS; ++i) {
+                            const int tok = cp_tok + TOKS * i;
+                            const bool take = base[e] >= 0 && key + SB_KV8_BLOCK * e + tok < rq.len && cp_piece * 16 < pitch;
+                            const int64_t at = base[e] * pitch + cp_off + TOKS * i * pitch;
+                            const unsigned to = cp_to[i] + dst + (unsigned)(SB_KV8_BLOCK * e * S::ROW);
+                            at_copy16(to, take ? a.k + at : a.k, take);
+                            at_copy16(to + S::CODES, take ? a.v + at : a.v, take);
+                        }
+                    const bool take = (lane < SB_KV8_BLOCK ? base[0] : base[1]) >= 0 && key + lane < rq.len;
 #pragma unroll
                     for (int i = 0; i < S::SROW; i += 4) {
                         const bool in = take && i < spitch;
-                        k4_copy<4>(to + i, in ? a.k_scale4 + at + i : a.k_scale4, in);
-                        k4_copy<4>(to + S::SCALES + i, in ? a.v_scale4 + at + i : a.v_scale4, in);
+                        k4_copy4(sc_to + dst + i, in ? a.k_scale4 + sat + i : a.k_scale4, in);
+                        k4_copy4(sc_to + dst + S::SCALES + i, in ? a.v_scale4 + sat + i : a.v_scale4, in);
                     }
                 }
             }
@@ -194,7 +211,8 @@ kv4_rows_kernel(const AtArgs a) {
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c)
                 *reinterpret_cast<uint32_t*>(qrow + 128 * c + 4 * lane) = at_half2(bf16lo(qw[i][c]) * by, bf16hi(qw[i][c]) * by);
-            if (lane == 0) reinterpret_cast<float*>(smem + S::F_AT)[r] = __fdiv_rn(fabsf(a.scale_log2), up) * by_head;
+            // (never 0, so that what is masked stays -inf)
+            if (lane == 0) reinterpret_cast<float*>(smem + S::F_AT)[r] = fmaxf(__fdiv_rn(fabsf(a.scale_log2), up) * by_head, 1e-37f);
         }
         __syncthreads();
         float fq[NR][2];
@@ -310,18 +328,17 @@ kv4_rows_kernel(const AtArgs a) {
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float x = s[e][nr][i] * fq[nr][i & 1];
                         if (edge) {
                             const int kk = key + SB_KV8_BLOCK * e + tg + 8 * (i >> 1), p = pos[nr][i & 1];
-                            if (kk > p || kk >= k1 || (a.window > 0 && kk <= p - a.window)) x = -INFINITY;
+                            if (kk > p || kk >= k1 || (a.window > 0 && kk <= p - a.window)) s[e][nr][i] = -INFINITY;
                         }
-                        s[e][nr][i] = x;
-                        mx[i & 1] = fmaxf(mx[i & 1], x);
+                        mx[i & 1] = fmaxf(mx[i & 1], s[e][nr][i]);
                     }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
+                    mx[e] *= fq[nr][e];                                  // factors are positive
                 }
                 // the reference only moves when a weight would pass 2^AT4_FAR
                 bool off[2];
@@ -354,7 +371,7 @@ kv4_rows_kernel(const AtArgs a) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float mm = m[nr][i & 1];
-                        p[i] = at_exp2(s[e][nr][i] - (mm == -INFINITY ? 0.f : mm));
+                        p[i] = at_exp2(fmaf(s[e][nr][i], fq[nr][i & 1], mm == -INFINITY ? 0.f : -mm));
                         l[nr][i & 1] += p[i];
                     }
                     pb[nr][0] = at_transpose(at_half2(p[0], p[1]));
@@ -430,7 +447,7 @@ kv4_rows_kernel(const AtArgs a) {
 template <int DP, int NR>
 sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = K4Shape<DP, NR>;
-    auto* kernel = kv4_rows_kernel<DP, NR>;
+    auto* kernel = a.g.dim == DP ? kv4_rows_kernel<DP, NR, true> : kv4_rows_kernel<DP, NR, false>;
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     int64_t ctas;
     const sb_status s = at_rows_plan<S>(ctx, "kv4 attention", a, max_new, max_len, ctas);
