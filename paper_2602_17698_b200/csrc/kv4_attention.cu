@@ -20,6 +20,7 @@
 
 namespace {
 
+constexpr float K4_LIMIT = 16384.f;      // 2^AT4_FAR
 constexpr int K4_PROMPT_FROM = 24;       // more query rows than this per cache head go to the tcgen05 kernel
 
 template <int BYTES>
@@ -321,36 +322,51 @@ kv4_rows_kernel(const AtArgs a) {
                 }
             }
             const bool edge = key + AT_STEP > rq.past + i0 + 1 || key + AT_STEP > k1 || (a.window > 0 && key <= rq.past + i1 - a.window);
+            if (edge) {
 #pragma unroll
-            for (int nr = 0; nr < NR; ++nr) {
-                float mx[2] = {-INFINITY, -INFINITY};
+                for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                    for (int e = 0; e < 2; ++e)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (edge) {
+                        for (int i = 0; i < 4; ++i) {
                             const int kk = key + SB_KV8_BLOCK * e + tg + 8 * (i >> 1), p = pos[nr][i & 1];
                             if (kk > p || kk >= k1 || (a.window > 0 && kk <= p - a.window)) s[e][nr][i] = -INFINITY;
                         }
-                        mx[i & 1] = fmaxf(mx[i & 1], s[e][nr][i]);
+            }
+            // The weights by the reference there is. A lane's sum says whether that still does: no weight is above it. One above 2^AT4_FAR
+            // (or none: NaN), or a row's first key, takes the way by the rows' maxima, and the weights anew.
+            uint32_t pb[2][NR][2];
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+                float sum[2];
+                auto weights = [&]() {
+                    sum[0] = sum[1] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float p[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float mm = m[nr][i & 1];
+                            p[i] = at_exp2(fmaf(s[e][nr][i], fq[nr][i & 1], mm == -INFINITY ? 0.f : -mm));
+                            sum[i & 1] += p[i];
+                        }
+                        pb[e][nr][0] = at_half2(p[0], p[1]);
+                        pb[e][nr][1] = at_half2(p[2], p[3]);
                     }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int w = 4; w < 32; w <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
-                    mx[e] *= fq[nr][e];                                  // factors are positive
-                }
-                // the reference only moves when a weight would pass 2^AT4_FAR
-                bool off[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) off[e] = mx[e] > m[nr][e] + AT4_FAR;
-                if (__any_sync(0xffffffffu, off[0] || off[1])) {
+                };
+                weights();
+                const bool far = !(sum[0] <= K4_LIMIT && sum[1] <= K4_LIMIT) || m[nr][0] == -INFINITY || m[nr][1] == -INFINITY;
+                if (__any_sync(0xffffffffu, far)) {
                     float f[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(fmaxf(s[0][nr][e], s[0][nr][2 + e]), fmaxf(s[1][nr][e], s[1][nr][2 + e]));
+#pragma unroll
+                        for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                        mx *= fq[nr][e];                                 // factors are positive
                         f[e] = 1.f;
-                        if (off[e]) {
-                            const float ref = mx[e] - AT4_UP;
+                        if (mx > m[nr][e] + AT4_FAR) {
+                            const float ref = mx - AT4_UP;
                             f[e] = at_exp2(m[nr][e] - ref);
                             m[nr][e] = ref;
                             l[nr][e] *= f[e];
@@ -360,22 +376,17 @@ kv4_rows_kernel(const AtArgs a) {
                     for (int i = 0; i < MT; ++i) {
                         o[i][nr][0] *= f[0]; o[i][nr][1] *= f[1]; o[i][nr][2] *= f[0]; o[i][nr][3] *= f[1];
                     }
+                    weights();
                 }
+                l[nr][0] += sum[0];
+                l[nr][1] += sum[1];
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                uint32_t pb[NR][2];
 #pragma unroll
                 for (int nr = 0; nr < NR; ++nr) {
-                    float p[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float mm = m[nr][i & 1];
-                        p[i] = at_exp2(fmaf(s[e][nr][i], fq[nr][i & 1], mm == -INFINITY ? 0.f : -mm));
-                        l[nr][i & 1] += p[i];
-                    }
-                    pb[nr][0] = at_transpose(at_half2(p[0], p[1]));
-                    pb[nr][1] = at_transpose(at_half2(p[2], p[3]));
+                    pb[e][nr][0] = at_transpose(pb[e][nr][0]);
+                    pb[e][nr][1] = at_transpose(pb[e][nr][1]);
                 }
 #pragma unroll
                 for (int c = 0; c < PANELS; ++c) {
@@ -407,7 +418,7 @@ kv4_rows_kernel(const AtArgs a) {
                         for (int k = 0; k < 4; ++k) {
                             const uint32_t a0 = f16x2_mul(el[k], slo), a1 = f16x2_mul(ol[k], slo), a2 = f16x2_mul(eh[k], shi), a3 = f16x2_mul(oh[k], shi);
 #pragma unroll
-                            for (int nr = 0; nr < NR; ++nr) at_mma(o[4 * (VW * c + i) + k][nr], a0, a1, a2, a3, pb[nr][0], pb[nr][1]);
+                            for (int nr = 0; nr < NR; ++nr) at_mma(o[4 * (VW * c + i) + k][nr], a0, a1, a2, a3, pb[e][nr][0], pb[e][nr][1]);
                         }
                     }
                 }

@@ -192,11 +192,20 @@ __device__ __forceinline__ void at_finish(const AtArgs& a, unsigned char* smem, 
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (part < parts) {
                     const int x1 = pieces * (part + 1) / parts;
-#pragma unroll 8
-                    for (int x = pieces * part / parts; x < x1; ++x) {
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x) + r) * D + d));
-                        const float f = weight[x * S::ROWS + r];
-                        v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+                    constexpr int SIDE = 16;                             // loads side by side: their latency is what this takes
+                    for (int x0 = pieces * part / parts; x0 < x1; x0 += SIDE) {
+                        float4 y[SIDE];
+#pragma unroll
+                        for (int i = 0; i < SIDE; ++i) {
+                            y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (x0 + i < x1) y[i] = __ldcg(reinterpret_cast<const float4*>(a.part + (slot(x0 + i) + r) * D + d));
+                        }
+#pragma unroll
+                        for (int i = 0; i < SIDE; ++i) {
+                            if (x0 + i >= x1) continue;
+                            const float f = weight[(x0 + i) * S::ROWS + r];
+                            v.x = fmaf(y[i].x, f, v.x); v.y = fmaf(y[i].y, f, v.y); v.z = fmaf(y[i].z, f, v.z); v.w = fmaf(y[i].w, f, v.w);
+                        }
                     }
                 }
                 shared_sum[threadIdx.x] = v;
