@@ -49,7 +49,7 @@ __device__ __forceinline__ uint32_t k4_lds8(unsigned a) {
 
 template <int DP, int NR>
 struct K4Shape {
-    static constexpr int STAGES = DP == 256 ? 2 : 3;
+    static constexpr int STAGES = DP == 256 || NR == 1 ? 2 : 3;
     static constexpr int CTAS = DP == 256 ? 1 : NR == 1 ? 3 : 2;       // resident per SM: registers and the rings decide
     static constexpr int ROW = DP / 2, SROW = DP / 16;               // bytes of a token's codes and scales
     static constexpr int CODES = AT_STEP * ROW, SCALES = AT_STEP * SROW;

@@ -102,11 +102,14 @@ struct AtWalk {
         return true;
     }
     __device__ __forceinline__ bool begin(const AtArgs& a, int row_tile_, int head_, int unit_, long long at, long long units_) {
+        return begin(a, at_item<ROWS, KEYS>(a, row_tile_), row_tile_, head_, unit_, at, units_);
+    }
+    __device__ __forceinline__ bool begin(const AtArgs& a, const AtItem& it_, int row_tile_, int head_, int unit_, long long at, long long units_) {
         row_tile = row_tile_; head = head_; unit = unit_;
         from = at - unit;
         left = units_;
         first = true;
-        it = at_item<ROWS, KEYS>(a, row_tile);
+        it = it_;
         count = 0;
         if (it.steps) cut();
         return step(a);

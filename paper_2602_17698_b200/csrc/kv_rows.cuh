@@ -35,37 +35,41 @@ template <class S>
 __device__ __forceinline__ bool at_share(const AtArgs& a, unsigned char* smem, AtWalk<S::ROWS, AT_STEP, AT_EXTRA>& wk, long long& share) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // units of one head before each row tile of all requests, 128 at a time
-    long long* sums = reinterpret_cast<long long*>(smem);       // [AT_WARPS] and, behind them, where the share starts
-    const int n = a.row_tiles * a.g.requests;
-    auto units = [&](int i) -> long long {
-        if (i >= n) return 0;
-        const int steps = at_item<S::ROWS, AT_STEP>(a, i).steps;
-        return steps ? steps + AT_EXTRA : 0;
+    struct Found {
+        AtItem it;
+        int row_tile, head, unit;
     };
-    long long mine = units(threadIdx.x), x = mine;
-    for (int i = threadIdx.x + AT_WARPS * 32; i < n; i += AT_WARPS * 32) x += units(i);
+    long long* sums = reinterpret_cast<long long*>(smem);       // [AT_WARPS] and, behind them, where the share starts
+    Found* found = reinterpret_cast<Found*>(sums + AT_WARPS);
+    const int n = a.row_tiles * a.g.requests;
+    AtItem it;
+    auto units = [&](int i) -> long long {
+        it.steps = 0;
+        if (i < n) it = at_item<S::ROWS, AT_STEP>(a, i);
+        return it.steps ? it.steps + AT_EXTRA : 0;
+    };
+    long long mine = units(threadIdx.x), x = mine, total = 0;
+    if (n > AT_WARPS * 32) {
+        for (int i = threadIdx.x + AT_WARPS * 32; i < n; i += AT_WARPS * 32) x += units(i);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    if (lane == 0) sums[warp] = x;
-    __syncthreads();
-    long long total = 0;
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (lane == 0) sums[warp] = x;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < AT_WARPS; ++w) total += sums[w];
-    total *= a.g.heads;
-    share = at_div(total + gridDim.x - 1, gridDim.x);
-    if (share < a.least) share = a.least;
-    const long long at = blockIdx.x * share;
-    if (at >= total) return false;
-    long long before = 0;
+        for (int w = 0; w < AT_WARPS; ++w) total += sums[w];
+    }
+    long long before = 0, at = 0;
     for (int base = 0; base < n; base += AT_WARPS * 32) {
-        if (base > 0) mine = units(base + threadIdx.x);
+        if (n > AT_WARPS * 32) {
+            mine = units(base + threadIdx.x);
+            __syncthreads();
+        }
         x = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        __syncthreads();
         if (lane == 31) sums[warp] = x;
         __syncthreads();
         long long all = 0, below = before;
@@ -74,21 +78,27 @@ __device__ __forceinline__ bool at_share(const AtArgs& a, unsigned char* smem, A
             if (w < warp) below += sums[w];
             all += sums[w];
         }
+        if (base == 0) {
+            total = (n > AT_WARPS * 32 ? total : all) * a.g.heads;
+            share = at_div(total + gridDim.x - 1, gridDim.x);
+            if (share < a.least) share = a.least;
+            at = blockIdx.x * share;
+            if (at >= total) return false;
+        }
         const long long lo = (below + x - mine) * a.g.heads;     // the row tile's first unit of all
         if (at >= lo && at < lo + mine * a.g.heads) {
-            int* found = reinterpret_cast<int*>(sums + AT_WARPS);
-            found[0] = base + threadIdx.x;
-            found[1] = (int)at_div(at - lo, mine);
-            found[2] = (int)(at - lo - found[1] * mine);
+            found->it = it;
+            found->row_tile = base + threadIdx.x;
+            found->head = (int)at_div(at - lo, mine);
+            found->unit = (int)(at - lo - found->head * mine);
         }
         before += all;
         if (at < before * a.g.heads) break;
     }
     __syncthreads();
-    const int* found = reinterpret_cast<const int*>(sums + AT_WARPS);
-    const int f0 = found[0], f1 = found[1], f2 = found[2];
+    const Found f = *found;
     __syncthreads();
-    return wk.begin(a, f0, f1, f2, at, min(share, total - at));
+    return wk.begin(a, f.it, f.row_tile, f.head, f.unit, at, min(share, total - at));
 }
 
 // The warps' sums of a piece (osm [warp][row][OPITCH] and, behind it, their references and sums of weights) become results, or where
