@@ -162,23 +162,25 @@ __device__ __forceinline__ void at_finish(const AtArgs& a, unsigned char* smem, 
         __syncthreads();
         if (*last) {
             __threadfence();
-            // weights of the pieces of every row in shared memory, a row per warp
+            // weights of the pieces of every row in shared memory; a row for as many lanes as there are pieces, up to a warp
             float* weight = reinterpret_cast<float*>(smem);          // [pieces][ROWS]
             float2* total = reinterpret_cast<float2*>(smem + S::F_AT - S::ROWS * 8);         // (reference, sum) of a row
-            for (int r = warp; r < nrow; r += AT_WARPS) {
-                constexpr int HELD = 4;                              // of a lane's pieces in registers: 128 in all
+            const int lanes = pieces <= 4 ? 4 : pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32, part = lane & (lanes - 1);
+            for (int r0 = 0; r0 < nrow; r0 += AT_WARPS * 32 / lanes) {
+                const int r = r0 + (int)threadIdx.x / lanes;
+                const bool row = r < nrow;
+                constexpr int HELD = 4;                              // of a lane's pieces in registers
                 float2 ml[HELD];
                 float mm = -INFINITY, sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < HELD; ++i) {
-                    const int x = lane + 32 * i;
-                    ml[i] = x < pieces ? __ldcg(a.part_ml + slot(x) + r) : make_float2(-INFINITY, 0.f);
+                    const int x = part + lanes * i;
+                    ml[i] = row && x < pieces ? __ldcg(a.part_ml + slot(x) + r) : make_float2(-INFINITY, 0.f);
                 }
 #pragma unroll
                 for (int i = 0; i < HELD; ++i) mm = fmaxf(mm, ml[i].x);
-                for (int x = lane + 32 * HELD; x < pieces; x += 32) mm = fmaxf(mm, __ldcg(a.part_ml + slot(x) + r).x);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
+                for (int x = part + lanes * HELD; row && x < pieces; x += lanes) mm = fmaxf(mm, __ldcg(a.part_ml + slot(x) + r).x);
+                for (int o = lanes / 2; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
                 auto put = [&](int x, float2 p) {
                     const float f = p.x == -INFINITY ? 0.f : at_exp2(p.x - mm);
                     weight[x * S::ROWS + r] = f;
@@ -186,24 +188,24 @@ __device__ __forceinline__ void at_finish(const AtArgs& a, unsigned char* smem, 
                 };
 #pragma unroll
                 for (int i = 0; i < HELD; ++i)
-                    if (lane + 32 * i < pieces) put(lane + 32 * i, ml[i]);
-                for (int x = lane + 32 * HELD; x < pieces; x += 32) put(x, __ldcg(a.part_ml + slot(x) + r));
-                sum = warp_sum(sum);
-                if (lane == 0) total[r] = make_float2(mm, sum);
+                    if (row && part + lanes * i < pieces) put(part + lanes * i, ml[i]);
+                for (int x = part + lanes * HELD; row && x < pieces; x += lanes) put(x, __ldcg(a.part_ml + slot(x) + r));
+                for (int o = lanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (row && part == 0) total[r] = make_float2(mm, sum);
             }
             __syncthreads();
             constexpr int PER = S::ROWS * DP / 4 / (AT_WARPS * 32);  // outputs of a thread, four columns each, at most
             const int outs = nrow * quads;
             if (outs <= AT_WARPS * 32) {
                 // few outputs: one a thread, or several threads for one, each a part of the pieces
-                const int parts = AT_WARPS * 32 / outs, part = (int)threadIdx.x / outs, idx = (int)threadIdx.x - part * outs;
+                const int parts = AT_WARPS * 32 / outs, mine = (int)threadIdx.x / outs, idx = (int)threadIdx.x - mine * outs;
                 const int r = idx / quads, d = 4 * (idx - r * quads);
                 float4* shared_sum = reinterpret_cast<float4*>(smem + (S::RING - AT_WARPS * 32 * 16));
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (part < parts) {
-                    const int x1 = pieces * (part + 1) / parts;
+                if (mine < parts) {
+                    const int x1 = pieces * (mine + 1) / parts;
                     constexpr int SIDE = 16;                             // loads side by side: their latency is what this takes
-                    for (int x0 = pieces * part / parts; x0 < x1; x0 += SIDE) {
+                    for (int x0 = pieces * mine / parts; x0 < x1; x0 += SIDE) {
                         float4 y[SIDE];
 #pragma unroll
                         for (int i = 0; i < SIDE; ++i) {
