@@ -17,6 +17,7 @@
 // Precision: as kv8_attention.cu, but a weight is held in fp16 relative to 2^-6 of the row's largest so far.
 #include "kv_rows.cuh"
 #include "kv4.cuh"
+#include "launch.cuh"
 
 namespace {
 
@@ -93,6 +94,8 @@ kv4_rows_kernel(const AtArgs a) {
     const int g = lane >> 2, t = lane & 3;
     const int D = a.g.dim;
     const int pitch = FULL ? S::ROW : kv4_code_pitch(D), spitch = FULL ? S::SROW : kv4_scale_pitch(D);
+    sb_let_next();
+    sb_after_previous();
     AtWalk<S::ROWS, AT_STEP, AT_EXTRA> wk;
     long long share;
     if (!at_share<S>(a, smem, wk, share)) return;
@@ -459,13 +462,10 @@ template <int DP, int NR>
 sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = K4Shape<DP, NR>;
     auto* kernel = a.g.dim == DP ? kv4_rows_kernel<DP, NR, true> : kv4_rows_kernel<DP, NR, false>;
-    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     int64_t ctas;
     const sb_status s = at_rows_plan<S>(ctx, "kv4 attention", a, max_new, max_len, ctas);
     if (s != SB_OK) return s;
-    kernel<<<(unsigned)ctas, AT_WARPS * 32, S::SMEM, ctx->stream>>>(a);
-    SB_LAUNCHED(ctx);
-    return SB_OK;
+    return sb_launch(ctx, kernel, dim3((unsigned)ctas), AT_WARPS * 32, S::SMEM, 1, true, a);
 }
 template <int DP>
 sb_status rows_by_count(sb_ctx* ctx, const AtArgs& a, int64_t max_new, int64_t max_len) {

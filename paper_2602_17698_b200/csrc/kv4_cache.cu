@@ -4,6 +4,7 @@
 // scale byte out. The scales of four blocks are four consecutive bytes: the lanes that hold them pass them to the
 // first, which stores one word. Blocks are independent of one another, so writing needs no look at what the cache holds.
 #include "kv4.cuh"
+#include "launch.cuh"
 
 namespace {
 
@@ -64,6 +65,8 @@ __device__ __forceinline__ bool kv4_codes(const uint32_t (&w)[8], float g, uint2
 __global__ void __launch_bounds__(K4_THREADS)
 kv4_append_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvDiv per_row, const KvDiv blocks, SbDeviceState* st) {
     const int b = blockIdx.y;
+    sb_let_next();
+    sb_after_previous();
     Kv8Request rq;
     if (!kv8_request(g, b, rq, st)) return;
     const Kv4Side& sd = blockIdx.z ? vs : ks;
@@ -101,6 +104,8 @@ __global__ void __launch_bounds__(K4_THREADS)
 kv4_read_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvDiv per_row, const KvDiv blocks,
                 __nv_bfloat16* __restrict__ K, __nv_bfloat16* __restrict__ V, SbDeviceState* st) {
     const int b = blockIdx.y;
+    sb_let_next();
+    sb_after_previous();
     Kv8Request rq;
     if (!kv8_request(g, b, rq, st)) return;
     const Kv4Side& sd = blockIdx.z ? vs : ks;
@@ -155,10 +160,8 @@ extern "C" sb_status sb_kv4_append(sb_ctx* ctx, const sb_kv4_cache* cache, const
                      static_cast<const __nv_bfloat16*>(K), k_token_stride, k_head_stride};
     const Kv4Side vs{static_cast<uint8_t*>(cache->v), static_cast<uint8_t*>(cache->v_scale), cache->v_head,
                      static_cast<const __nv_bfloat16*>(V), v_token_stride, v_head_stride};
-    kv4_append_kernel<<<grid, K4_THREADS, 0, ctx->stream>>>(kv4_geom(cache, total, starts, lens, max_new), ks, vs,
-                                                            KvDiv(cache->heads * blocks), KvDiv(blocks), ctx->dstate);
-    SB_LAUNCHED(ctx);
-    return SB_OK;
+    return sb_launch(ctx, kv4_append_kernel, grid, K4_THREADS, 0, 1, true, kv4_geom(cache, total, starts, lens, max_new), ks, vs,
+                     KvDiv(cache->heads * blocks), KvDiv(blocks), ctx->dstate);
 }
 
 extern "C" sb_status sb_kv4_read(sb_ctx* ctx, const sb_kv4_cache* cache, int64_t total, const int32_t* starts,
@@ -175,9 +178,6 @@ extern "C" sb_status sb_kv4_read(sb_ctx* ctx, const sb_kv4_cache* cache, int64_t
     SB_CUDA(ctx, cudaSetDevice(ctx->device));
     const Kv4Side ks{static_cast<uint8_t*>(cache->k), static_cast<uint8_t*>(cache->k_scale), cache->k_head, nullptr, 0, 0};
     const Kv4Side vs{static_cast<uint8_t*>(cache->v), static_cast<uint8_t*>(cache->v_scale), cache->v_head, nullptr, 0, 0};
-    kv4_read_kernel<<<grid, K4_THREADS, 0, ctx->stream>>>(kv4_geom(cache, total, starts, lens, max_new), ks, vs,
-                                                          KvDiv(cache->heads * blocks), KvDiv(blocks), static_cast<__nv_bfloat16*>(K),
-                                                          static_cast<__nv_bfloat16*>(V), ctx->dstate);
-    SB_LAUNCHED(ctx);
-    return SB_OK;
+    return sb_launch(ctx, kv4_read_kernel, grid, K4_THREADS, 0, 1, true, kv4_geom(cache, total, starts, lens, max_new), ks, vs,
+                     KvDiv(cache->heads * blocks), KvDiv(blocks), static_cast<__nv_bfloat16*>(K), static_cast<__nv_bfloat16*>(V), ctx->dstate);
 }

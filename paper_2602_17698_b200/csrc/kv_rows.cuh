@@ -105,7 +105,7 @@ __device__ __forceinline__ bool at_share(const AtArgs& a, unsigned char* smem, A
 // the item has other pieces an entry in scratch; the last piece to finish adds those.
 template <class S, int DP>
 __device__ __forceinline__ void at_finish(const AtArgs& a, unsigned char* smem, const AtWalk<S::ROWS, AT_STEP, AT_EXTRA>& wk, long long share) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31;
     const int D = a.g.dim, head = wk.head, r0 = wk.it.r0, nrow = wk.it.nrow;
     const Kv8Request rq = wk.it.rq;
     const float* osm = reinterpret_cast<const float*>(smem);

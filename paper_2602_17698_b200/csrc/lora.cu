@@ -15,6 +15,7 @@
 // move in 16-byte pieces. H is held as the sum of two bf16 numbers, h = hi + lo with lo = bf16(h - hi): what is lost is below 2^-17 of
 // h, so the result's one rounding decides.
 #include "kv8.cuh"
+#include "launch.cuh"
 
 namespace {
 
@@ -285,6 +286,8 @@ lora_few_kernel(const LoArgs a, const int wide) {
     extern __shared__ __align__(128) unsigned char lm_smem[];
     float* lo_sums = reinterpret_cast<float*>(lm_smem + S::RING);    // [KG][16][RP]; then the first is the block's sum
     uint16_t* held = reinterpret_cast<uint16_t*>(lm_smem + S::RING + S::SUMS);     // H: [hi, lo][16][RP + 8]
+    sb_let_next();
+    sb_after_previous();
     const LoTile tile = lo_tile<16, 256>(a, blockIdx.x / a.splits);
     const int rank = blockIdx.x % a.splits;                          // of the block in its cluster
     if (tile.rows <= 0) return;
@@ -445,7 +448,9 @@ lora_down_kernel(const LoArgs a) {
     using S = LmDown<RP>;
     constexpr int NT = RP == 16 ? 2 : RP / 16;                        // tiles of 8 of the rank a warp has
     extern __shared__ __align__(128) unsigned char lm_smem[];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // in this order: what the next kernel reads before this one's end (all but H) is there
+    sb_after_previous();
+    sb_let_next();
     const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x / a.splits);
     const int part = blockIdx.x % a.splits;
     if (tile.rows <= 0 || tile.adapter < 0) return;
@@ -557,7 +562,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
     const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x);
     const int64_t c0 = (int64_t)blockIdx.y * a.columns, c1 = min(a.out, c0 + a.columns);
     if (tile.rows <= 0 || tile.adapter < 0) {
-        asm volatile("griddepcontrol.wait;" ::: "memory");
+        sb_after_previous();
         if (tile.rows > 0) lo_pass<T>(a, tile, c0, c1, wide);
         return;
     }
@@ -594,7 +599,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
     };
 #pragma unroll
     for (int n = 0; n < S::STAGES - 1; ++n) issue(n);
-    asm volatile("griddepcontrol.wait;" ::: "memory");                // H is there from here on
+    sb_after_previous();                                             // H is there from here on
     uint32_t h[2][2][KW];                                            // [hi, lo][row g, g + 8]
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -647,34 +652,6 @@ lora_up_kernel(const LoArgs a, const int wide) {
     lo_wait<0>();
 }
 
-// A launch in clusters of `cluster` blocks along x, or one that starts while the kernel before it still runs.
-template <typename... P>
-sb_status lo_launch(sb_ctx* ctx, void (*kernel)(P...), dim3 grid, int smem, int cluster, bool early, P... args) {
-    if (smem > 40 * 1024) SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (cluster > 8) SB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    cudaLaunchAttribute at[2];
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(256);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = ctx->stream;
-    cfg.attrs = at;
-    if (cluster > 1) {
-        at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-        at[cfg.numAttrs].val.clusterDim.x = cluster;
-        at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
-        ++cfg.numAttrs;
-    }
-    if (early) {
-        at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-        ++cfg.numAttrs;
-    }
-    SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, args...));
-    SB_LAUNCHED(ctx);
-    return SB_OK;
-}
-
 template <int RP, typename T>
 sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
     a.direct = a.max_new <= 16;
@@ -685,7 +662,7 @@ sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
         if (want > most) want = most;
         for (a.splits = 1; 2 * a.splits <= want;) a.splits *= 2;
         a.columns = ((a.out + a.splits - 1) / a.splits + 255) / 256 * 256;
-        return lo_launch(ctx, lora_few_kernel<RP, T>, dim3((unsigned)(a.requests * a.splits)), LfShape<RP, T>::SMEM, a.splits, false, a, wide);
+        return sb_launch(ctx, lora_few_kernel<RP, T>, dim3((unsigned)(a.requests * a.splits)), 256, LfShape<RP, T>::SMEM, a.splits, true, a, wide);
     }
     const int64_t tiles = (a.total + LM_ROWS - 1) / LM_ROWS + a.requests, full = (a.total + LM_ROWS - 1) / LM_ROWS;
     // parts of `in`: two blocks a multiprocessor, but 512 each at least
@@ -698,13 +675,13 @@ sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
     sb_status s = sb_scratch(ctx, Carver::need({2 * n * 2}), &arena);
     if (s != SB_OK) return s;
     a.h = Carver(arena).take<uint16_t>(2 * n);
-    s = lo_launch(ctx, lora_down_kernel<RP>, dim3((unsigned)(tiles * a.splits)), LmDown<RP>::SMEM, a.splits, false, a);
+    s = sb_launch(ctx, lora_down_kernel<RP>, dim3((unsigned)(tiles * a.splits)), 256, LmDown<RP>::SMEM, a.splits, true, a);
     if (s != SB_OK) return s;
     // columns of a block of the second kernel: eight blocks a multiprocessor, four tiles each at least
     most = (a.out + 4 * LM_COLS - 1) / (4 * LM_COLS);
     const int64_t parts = cut(8 * ctx->sm_count / full, most < 65535 ? most : 65535), each = (a.out + LM_COLS - 1) / LM_COLS;
     a.columns = (each + parts - 1) / parts * LM_COLS;
-    return lo_launch(ctx, lora_up_kernel<RP, T>, dim3((unsigned)tiles, (unsigned)((a.out + a.columns - 1) / a.columns)), LmUp<RP, T>::SMEM, 1, true, a, wide);
+    return sb_launch(ctx, lora_up_kernel<RP, T>, dim3((unsigned)tiles, (unsigned)((a.out + a.columns - 1) / a.columns)), 256, LmUp<RP, T>::SMEM, 1, true, a, wide);
 }
 template <int RP>
 sb_status lo_by_type(sb_ctx* ctx, LoArgs& a, int f32, int wide) {

@@ -6,6 +6,7 @@
 // bits, with the product's rounding error by fma, less a multiple of pi / 2 in two parts (Cody and Waite): exact to fp32 for every
 // 32-bit position. The bytes bound large calls, the chain of dependent reads small ones.
 #include "kv8.cuh"
+#include "launch.cuh"
 
 namespace {
 
@@ -66,6 +67,8 @@ template <typename T, int N, bool INTER>
 __global__ void __launch_bounds__(RO_THREADS)
 rotary_kernel(const RoArgs a) {
     extern __shared__ __align__(16) unsigned char ro_smem[];
+    sb_let_next();
+    sb_after_previous();
     const int half = a.rotated / 2;
     float2* table = reinterpret_cast<float2*>(ro_smem);              // [rows][half]
     int* pos = reinterpret_cast<int*>(ro_smem + (size_t)a.rows * half * 8);      // [rows], and whether there is one
@@ -175,9 +178,9 @@ rotary_kernel(const RoArgs a) {
 }
 
 template <typename T, int N, bool INTER>
-void ro_launch(sb_ctx* ctx, const RoArgs& a) {
+sb_status ro_launch(sb_ctx* ctx, const RoArgs& a) {
     const size_t smem = (size_t)a.rows * (a.rotated / 2) * 8 + (size_t)a.rows * 8;
-    rotary_kernel<T, N, INTER><<<(unsigned)((a.total + a.rows - 1) / a.rows), RO_THREADS, smem, ctx->stream>>>(a);
+    return sb_launch(ctx, rotary_kernel<T, N, INTER>, dim3((unsigned)((a.total + a.rows - 1) / a.rows)), RO_THREADS, (int)smem, 1, true, a);
 }
 
 }  // namespace
@@ -233,16 +236,10 @@ extern "C" sb_status sb_rotary(sb_ctx* ctx, const sb_rotary_table* table, const 
     a.rows = (int)rows;
     if (rows * a.heads * a.slots >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "rotary: too many heads");
     SB_CUDA(ctx, cudaSetDevice(ctx->device));
-    if (f32) {
-        if (table->interleaved) n == 4 ? ro_launch<float, 4, true>(ctx, a) : n == 2 ? ro_launch<float, 2, true>(ctx, a) : ro_launch<float, 1, true>(ctx, a);
-        else n == 4 ? ro_launch<float, 4, false>(ctx, a) : n == 2 ? ro_launch<float, 2, false>(ctx, a) : ro_launch<float, 1, false>(ctx, a);
-    } else {
-        using B = __nv_bfloat16;
-        if (table->interleaved)
-            n == 8 ? ro_launch<B, 8, true>(ctx, a) : n == 4 ? ro_launch<B, 4, true>(ctx, a) : n == 2 ? ro_launch<B, 2, true>(ctx, a) : ro_launch<B, 1, true>(ctx, a);
-        else
-            n == 8 ? ro_launch<B, 8, false>(ctx, a) : n == 4 ? ro_launch<B, 4, false>(ctx, a) : n == 2 ? ro_launch<B, 2, false>(ctx, a) : ro_launch<B, 1, false>(ctx, a);
-    }
-    SB_LAUNCHED(ctx);
-    return SB_OK;
+    using B = __nv_bfloat16;
+    if (f32 && table->interleaved) return n == 4 ? ro_launch<float, 4, true>(ctx, a) : n == 2 ? ro_launch<float, 2, true>(ctx, a) : ro_launch<float, 1, true>(ctx, a);
+    if (f32) return n == 4 ? ro_launch<float, 4, false>(ctx, a) : n == 2 ? ro_launch<float, 2, false>(ctx, a) : ro_launch<float, 1, false>(ctx, a);
+    if (table->interleaved)
+        return n == 8 ? ro_launch<B, 8, true>(ctx, a) : n == 4 ? ro_launch<B, 4, true>(ctx, a) : n == 2 ? ro_launch<B, 2, true>(ctx, a) : ro_launch<B, 1, true>(ctx, a);
+    return n == 8 ? ro_launch<B, 8, false>(ctx, a) : n == 4 ? ro_launch<B, 4, false>(ctx, a) : n == 2 ? ro_launch<B, 2, false>(ctx, a) : ro_launch<B, 1, false>(ctx, a);
 }
