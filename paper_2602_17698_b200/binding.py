@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -163,7 +164,7 @@ def lib() -> C.CDLL:
         L.sb_kv4_append.argtypes = [vp, c4, vp, i64, i64, vp, i64, i64, i64, vp, vp, i64]
         L.sb_kv4_read.argtypes = [vp, c4, i64, vp, vp, i64, vp, vp]
         L.sb_kv4_attention.argtypes = [vp, c4, vp, i64, i64, i32, i64, vp, vp, i64, i64, f32, i64, vp, i64, i64, vp]
-        L.sb_rotary.argtypes = [vp, C.POINTER(RotaryTableStruct), C.POINTER(RotaryPartStruct), i32, i32, i32, i64, vp, vp, vp, i32, i64]
+        L.sb_rotary.argtypes = [vp, C.POINTER(RotaryTableStruct), vp, i32, i32, i32, i64, vp, vp, vp, i32, i64]
         L.sb_lora_add.argtypes = [vp, C.POINTER(LoraAdaptersStruct), vp, i64, vp, i64, vp, i64, i32, i64, vp, vp, i32, i64]
         L.sb_fp4_code_bytes.restype = L.sb_fp4_scale_bytes.restype = i64
         for name in EXPORTS:
@@ -285,8 +286,8 @@ class Kv4Cache:
         pages, heads, page_tokens, row = shape = k.shape
         if k.dtype is not _U8 or v.dtype is not _U8 or k_scale.dtype not in _E4M3_BYTES or v_scale.dtype not in _E4M3_BYTES or table.dtype is not _I32:
             raise TypeError("codes are uint8, scales uint8 or float8_e4m3fn, page numbers int32")
-        scales = (pages, heads, page_tokens, (dim + 63) // 64 * 4)
-        if v.shape != shape or row != (dim + 31) // 32 * 16 or k_scale.shape != scales or v_scale.shape != scales:
+        scales = k_scale.shape
+        if v.shape != shape or row != (dim + 31) // 32 * 16 or scales != (pages, heads, page_tokens, (dim + 63) // 64 * 4) or v_scale.shape != scales:
             raise ValueError("codes and scales do not fit one another and dim")
         requests, per = table.shape
         stride, one = table.stride()
@@ -294,9 +295,9 @@ class Kv4Cache:
             raise ValueError("a request needs room for a page in the table")
         if not (k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()) or one != 1:
             raise ValueError("the cache's tensors are contiguous")
-        for t in (k_head, v_head):
-            if t is not None and (t.dtype is not _F32 or t.shape != (heads,) or not t.is_contiguous()):
-                raise ValueError("k_head, v_head: contiguous fp32 [heads]")
+        if k_head is not None and (k_head.dtype is not _F32 or k_head.shape != (heads,) or not k_head.is_contiguous()) \
+                or v_head is not None and (v_head.dtype is not _F32 or v_head.shape != (heads,) or not v_head.is_contiguous()):
+            raise ValueError("k_head, v_head: contiguous fp32 [heads]")
         self.k, self.v, self.k_scale, self.v_scale, self.table, self.dim, self.k_head, self.v_head = k, v, k_scale, v_scale, table, dim, k_head, v_head
         self.struct = Kv4CacheStruct(_dev(k), _dev(v), _dev(k_scale), _dev(v_scale), _dev(k_head), _dev(v_head), _dev(table),
                                      stride if requests > 1 else per, pages, requests, heads, page_tokens, dim, per, 0)
@@ -311,13 +312,40 @@ class Kv4Cache:
 class RotaryTable:
     """Frequencies of rotary positions: fp32 [rotated / 2] on the device, radians per position (`rotary_frequencies` makes them), how a head's
     elements pair up, and the factor on cos and sin."""
-    __slots__ = ("freq", "rotated", "interleaved", "factor", "structs")
+    __slots__ = ("freq", "rotated", "interleaved", "factor", "_structs")
 
     def __init__(self, freq: torch.Tensor, interleaved: bool = False, factor: float = 1.0):
         if freq.dtype is not _F32 or freq.dim() != 1 or not freq.is_contiguous() or freq.numel() < 1:
             raise ValueError("freq: contiguous fp32 [rotated / 2]")
         self.freq, self.rotated, self.interleaved, self.factor = freq, 2 * freq.numel(), bool(interleaved), float(factor)
-        self.structs = tuple(RotaryTableStruct(_dev(freq), self.rotated, int(self.interleaved), inverse, self.factor) for inverse in (0, 1))
+        self._structs = [None, None]                                 # forward and inverse, made when they are used
+
+    def struct(self, inverse: bool = False) -> RotaryTableStruct:
+        s = self._structs[bool(inverse)]
+        if s is None:
+            s = self._structs[bool(inverse)] = RotaryTableStruct(_dev(self.freq), self.rotated, self.interleaved, bool(inverse), self.factor)
+        return s
+
+
+# sb_rotary_part as bytes: a third of the time that filling a ctypes structure takes
+_ROTARY_PART = struct.Struct("PqqPqqii")
+
+
+def _rotary_part(x: torch.Tensor, y: torch.Tensor, tokens: int, dim: int, dtype) -> bytes:
+    n, heads, d = shape = x.shape
+    xt, xh, one = x.stride()
+    if y is x:
+        yt, yh, two = xt, xh, one
+    else:
+        yt, yh, two = y.stride()
+        if y.shape != shape or y.dtype is not dtype:
+            raise ValueError("rotary: out has the shape and type of its input")
+    if n != tokens or d != dim or x.dtype is not dtype:
+        raise ValueError("rotary: tensors of one type, [tokens][heads][dim] with the same tokens and dim")
+    if one != 1 or two != 1:
+        raise ValueError("rotary: elements of a head are contiguous")
+    px = _dev(x)
+    return _ROTARY_PART.pack(px, xt, xh, px if y is x else _dev(y), yt, yh, heads, 0)
 
 
 class LoraAdapters:
@@ -812,43 +840,39 @@ class Context:
         """Turns q and, if given, k ([tokens][heads][dim], bf16 or fp32) by their positions: those of the requests' new tokens (starts, lens, max_new
         as in the cache calls), or `positions`, int32 [tokens].  In place, or into `out` (a tensor for each); inverse: the way
         back of gradients.  Returns (q, k) as written."""
-        xs = (q,) if k is None else (q, k)
-        ys = xs if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)[:len(xs)]
-        tokens, _, dim = q.shape
         dtype = q.dtype
         if dtype is not _BF16 and dtype is not _F32:
             raise TypeError("rotary: bf16 or fp32 tensors")
-        if len(ys) != len(xs):
-            raise ValueError("out: a tensor for q and, where it is given, one for k")
-        parts = (RotaryPartStruct * len(xs))()
-        for p, x, y in zip(parts, xs, ys):
-            n, heads, d = shape = x.shape
-            if n != tokens or d != dim or y.shape != shape or x.dtype is not dtype or y.dtype is not dtype:
-                raise ValueError("rotary: tensors of one type, [tokens][heads][dim] with the same tokens and dim, and out like them")
-            xt, xh, one = x.stride()
-            yt, yh, two = y.stride()
-            if one != 1 or two != 1:
-                raise ValueError("rotary: elements of a head are contiguous")
-            p.x, p.x_token_stride, p.x_head_stride = _dev(x), xt, xh
-            p.y, p.y_token_stride, p.y_head_stride = _dev(y), yt, yh
-            p.heads = heads
-        requests, at, s, n = 0, None, None, None
-        if positions is not None:
-            if starts is not None or lens is not None:
-                raise ValueError("rotary: positions, or starts and lens")
-            if positions.dtype is not _I32 or positions.shape != (tokens,) or not positions.is_contiguous():
-                raise ValueError("positions: contiguous int32 [tokens]")
-            at = _dev(positions)
+        if out is None:
+            yq, yk = q, k
+        elif isinstance(out, torch.Tensor):
+            yq, yk = out, None
         else:
+            yq, yk = out[0], out[1] if len(out) > 1 else None
+        if (k is None) != (yk is None):
+            if k is not None:
+                raise ValueError("out: a tensor for q and, where it is given, one for k")
+            yk = None
+        tokens, _, dim = q.shape
+        parts = _rotary_part(q, yq, tokens, dim, dtype)
+        if k is not None:
+            parts += _rotary_part(k, yk, tokens, dim, dtype)
+        if positions is None:
             if starts is None or lens is None:
                 raise ValueError("rotary: positions, or starts and lens")
             requests = lens.numel()
             if starts.dtype is not _I32 or lens.dtype is not _I32 or starts.numel() != requests + 1 or not starts.is_contiguous() or not lens.is_contiguous():
                 raise ValueError("starts: contiguous int32 [requests + 1], lens: contiguous int32 [requests]")
-            s, n = _dev(starts), _dev(lens)
-        self._check(lib().sb_rotary(self._h, table.structs[1 if inverse else 0], parts, len(xs), dim, int(dtype is _F32), tokens, at, s, n,
+            at, s, n = None, _dev(starts), _dev(lens)
+        else:
+            if starts is not None or lens is not None:
+                raise ValueError("rotary: positions, or starts and lens")
+            if positions.dtype is not _I32 or positions.shape != (tokens,) or not positions.is_contiguous():
+                raise ValueError("positions: contiguous int32 [tokens]")
+            requests, at, s, n = 0, _dev(positions), None, None
+        self._check(lib().sb_rotary(self._h, table.struct(inverse), parts, 1 if k is None else 2, dim, dtype is _F32, tokens, at, s, n,
                                     requests, max_new))
-        return (ys[0], ys[1] if len(ys) > 1 else None)
+        return yq, yk
 
     # ---- low-rank adapters ------------------------------------------------------------------
     def lora_add(self, adapters: LoraAdapters, X: torch.Tensor, base: torch.Tensor, ids: torch.Tensor, starts: torch.Tensor, max_new: int,

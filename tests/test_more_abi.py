@@ -69,7 +69,10 @@ def test_what_the_4_bit_cache_refuses(on_cpu):
 
 def test_rotary_tables_and_adapters(on_cpu):
     t = binding.RotaryTable(torch.ones(20), True, 1.5)
-    assert (t.rotated, t.structs[0].rotated, t.structs[0].interleaved, t.structs[0].inverse, t.structs[1].inverse, t.structs[1].factor) == (40, 40, 1, 0, 1, 1.5)
+    assert (t.rotated, t.struct().rotated, t.struct().interleaved, t.struct().inverse, t.struct(True).inverse, t.struct(True).factor) == (40, 40, 1, 0, 1, 1.5)
+    assert binding._ROTARY_PART.size == ctypes.sizeof(binding.RotaryPartStruct)
+    got = binding.RotaryPartStruct.from_buffer_copy(binding._ROTARY_PART.pack(1, 2, 3, 4, 5, 6, 7, 8))
+    assert [getattr(got, f) for f, _ in got._fields_] == [1, 2, 3, 4, 5, 6, 7, 8]
     for bad in (torch.ones(20).double(), torch.ones(2, 10), torch.ones(40)[::2], torch.ones(0)):
         with pytest.raises(ValueError):
             binding.RotaryTable(bad)
