@@ -508,7 +508,7 @@ extern "C" sb_status sb_kv4_attention(sb_ctx* ctx, const sb_kv4_cache* cache, co
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;
-    if (max_new * a.group > K4_PROMPT_FROM && cache->dim <= 128) return kv8_prompt(ctx, a, AT_E2M1, max_new, max_len);
+    if (max_new * a.group > K4_PROMPT_FROM) return kv8_prompt(ctx, a, AT_E2M1, max_new, max_len);
     return cache->dim <= 64 ? rows_by_count<64>(ctx, a, max_new, max_len)
          : cache->dim <= 128 ? rows_by_count<128>(ctx, a, max_new, max_len) : rows_by_count<256>(ctx, a, max_new, max_len);
 }

@@ -52,20 +52,23 @@ constexpr int PR_LEAST = 4;              // units of a share at least: one reque
 constexpr float PR_LIMIT4 = 16384.f;     // and over the 4-bit cache: 2^AT4_FAR
 constexpr float PR_LIMIT = 256.f;        // 2^AT_SLACK: largest sum of a half tile's weights before the row's reference moves
 
+// Heads of more than 128 (of the 4-bit cache, whose raw tiles are small enough): one row tile, and rings as long as fits.
 template <int DP>
 struct PrShape {
+    static constexpr int TILES = DP == 256 ? 1 : 2, ROWS = TILES * PR_ROWS;      // row tiles and rows of an item
     static constexpr int PANELS = DP / 64;                          // 128-byte columns of an operand row
     static constexpr int PANEL = 128 * 128;                         // bytes: 128 rows x 128
     static constexpr int OPERAND = PANELS * PANEL;
-    static constexpr int RING = 3, RAW_RING = 4;                    // converted and raw tiles: K, V, K, V, ...
-    static constexpr int RAW = PR_KEYS * DP;
-    static constexpr int Q_AT = 0, T_AT = 2 * OPERAND, RAW_AT = T_AT + RING * OPERAND;
+    static constexpr int RING = DP == 256 ? 2 : 3, RAW_RING = DP == 256 ? 1 : 4;      // converted and raw tiles: K, V, K, V, ...
+    static constexpr int RAW = DP == 256 ? PR_KEYS * (DP / 2 + DP / 16) : PR_KEYS * DP;
+    static constexpr int Q_AT = 0, T_AT = TILES * OPERAND, RAW_AT = T_AT + RING * OPERAND;
     static constexpr int SC_AT = RAW_AT + RAW_RING * RAW;           // scales of four tiles: 8 of K, 8 of V
     static constexpr int F_AT = SC_AT + 4 * 64;                      // score factor of a row, fp32
     static constexpr int BAR_AT = F_AT + 2 * PR_ROWS * 4;
     static constexpr int SMEM = BAR_AT + 304 + 1024;
     // tensor memory: S (and P) of the two tiles, then O of the two tiles
-    static constexpr int S_COL = 0, O_COL = 256, TMEM = DP == 64 ? 512 : 512;
+    static constexpr int S_COL = 0, O_COL = 256, TMEM = 512;
+    static_assert(SMEM <= 227 * 1024 && O_COL + TILES * DP <= TMEM, "");
 };
 
 __device__ __forceinline__ void pr_st16(unsigned taddr, const uint32_t (&r)[16]) {
@@ -200,18 +203,19 @@ __device__ __forceinline__ float pr_weights4(unsigned ts, unsigned (&s)[PR_SUB /
     return lo + hi;
 }
 
-// The plan of the shares (items: 256 query rows), written by a kernel of its own.
+// The plan of the shares (items: a CTA's query rows), written by a kernel of its own.
 struct PrWork {
     long long* prefix;           // [row tiles of all requests + 1] units of one head before the row tile
     int4* start;                 // [ctas] (row tile of all requests, head, unit) a share starts with; x < 0: no share
     long long* share;            // units of a share; units in all
     int ctas;
 };
-using PrWalk = AtWalk<2 * PR_ROWS, PR_KEYS, PR_EXTRA>;
+template <int ROWS>
 __device__ __forceinline__ int pr_units(const AtArgs& a, int row_tile) {
-    const int steps = at_item<2 * PR_ROWS, PR_KEYS>(a, row_tile).steps;
+    const int steps = at_item<ROWS, PR_KEYS>(a, row_tile).steps;
     return steps ? steps + PR_EXTRA : 0;
 }
+template <int ROWS>
 __global__ void __launch_bounds__(1024)
 kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     __shared__ long long warp_sum_at[32], total_at;
@@ -220,7 +224,7 @@ kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     long long before = 0;
     for (int base = 0; base < n; base += 1024) {
         const int i = base + threadIdx.x;
-        const long long mine = i < n ? pr_units(a, i) : 0;
+        const long long mine = i < n ? pr_units<ROWS>(a, i) : 0;
         long long x = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -281,7 +285,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int D = a.g.dim;
     const int pitch = TYPE == AT_E2M1 ? kv4_code_pitch(D) : D, spitch = kv4_scale_pitch(D);        // bytes of a token's codes and scales
-    PrWalk wk;
+    AtWalk<S::ROWS, PR_KEYS, PR_EXTRA> wk;
     at_after_previous();
     at_let_next();                           // its blocks find room when these end, and wait for that
     {
@@ -355,26 +359,30 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 unsigned char* q0 = smem + S::Q_AT + qt * S::OPERAND + (c >> 3) * S::PANEL;
                 const int tok0 = a.by_group.quot(it.r0), head0 = it.r0 - tok0 * a.group;
                 const __nv_bfloat16* src = a.q + (int64_t)(it.rq.row0 + tok0) * a.q_token_stride + (int64_t)wk.head * a.group * a.q_head_stride + 8 * c;
-                uint4 x[NI];
+                constexpr int CH = NI < 16 ? NI : 16;                  // of them side by side
+#pragma unroll 1
+                for (int i0 = 0; i0 < NI; i0 += CH) {
+                    uint4 x[CH];
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const int rr = qt * PR_ROWS + (warp & 3) * 32 + i * RPI + sub, at = head0 + rr;
-                    const int tok = a.by_group.quot(at);
-                    x[i] = make_uint4(0, 0, 0, 0);
-                    if (rr < it.nrow && 8 * c < D)
-                        x[i] = *reinterpret_cast<const uint4*>(src + tok * a.q_token_stride + (at - tok * a.group) * a.q_head_stride);
-                }
+                    for (int i = 0; i < CH; ++i) {
+                        const int rr = qt * PR_ROWS + (warp & 3) * 32 + (i0 + i) * RPI + sub, at = head0 + rr;
+                        const int tok = a.by_group.quot(at);
+                        x[i] = make_uint4(0, 0, 0, 0);
+                        if (rr < it.nrow && 8 * c < D)
+                            x[i] = *reinterpret_cast<const uint4*>(src + tok * a.q_token_stride + (at - tok * a.group) * a.q_head_stride);
+                    }
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    uint32_t m = __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+                    for (int i = 0; i < CH; ++i) {
+                        uint32_t m = __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
 #pragma unroll
-                    for (int o = 1; o < LANES; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    const float up = at_query_scale(max(m & 0xffffu, m >> 16)), by = at_signed(up, a.scale_log2);
-                    const int rr = (warp & 3) * 32 + i * RPI + sub;
-                    if (c == 0) factor[rr] = up;
-                    *reinterpret_cast<uint4*>(q0 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
-                        make_uint4(at_half2(bf16lo(x[i].x) * by, bf16hi(x[i].x) * by), at_half2(bf16lo(x[i].y) * by, bf16hi(x[i].y) * by),
-                                   at_half2(bf16lo(x[i].z) * by, bf16hi(x[i].z) * by), at_half2(bf16lo(x[i].w) * by, bf16hi(x[i].w) * by));
+                        for (int o = 1; o < LANES; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                        const float up = at_query_scale(max(m & 0xffffu, m >> 16)), by = at_signed(up, a.scale_log2);
+                        const int rr = (warp & 3) * 32 + (i0 + i) * RPI + sub;
+                        if (c == 0) factor[rr] = up;
+                        *reinterpret_cast<uint4*>(q0 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) =
+                            make_uint4(at_half2(bf16lo(x[i].x) * by, bf16hi(x[i].x) * by), at_half2(bf16lo(x[i].y) * by, bf16hi(x[i].y) * by),
+                                       at_half2(bf16lo(x[i].z) * by, bf16hi(x[i].z) * by), at_half2(bf16lo(x[i].w) * by, bf16hi(x[i].w) * by));
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -517,7 +525,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
                         if (c + i < D)
-                            *reinterpret_cast<float4*>(a.part + ((slot * (D / 4) + (c + i) / 4) * (2 * PR_ROWS) + r) * 4) =
+                            *reinterpret_cast<float4*>(a.part + ((slot * (D / 4) + (c + i) / 4) * S::ROWS + r) * 4) =
                                 make_float4(__uint_as_float(o[i]) * norm, __uint_as_float(o[i + 1]) * norm,
                                             __uint_as_float(o[i + 2]) * norm, __uint_as_float(o[i + 3]) * norm);
                 } else {
@@ -548,7 +556,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 }
                 __syncwarp();
                 if (real && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
-            } else if (real) a.part_ml[slot * (2 * PR_ROWS) + r] = make_float2(m, l);
+            } else if (real) a.part_ml[slot * S::ROWS + r] = make_float2(m, l);
             t5_fence_before();                                       // the sums are read before the next piece's products
         }
     } else if (warp < 12) {
@@ -699,7 +707,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                         // no such page: zeros, where a scale that was left there could be no number
                         unsigned char* raw = smem + S::RAW_AT + rs * S::RAW;
                         for (unsigned i = 0; i < bytes; i += 16) *reinterpret_cast<uint4*>(raw + lane * bytes + i) = make_uint4(0, 0, 0, 0);
-                        for (unsigned i = 0; i < sbytes; i += 16) *reinterpret_cast<uint4*>(raw + PR_KEYS * DP / 2 + lane * sbytes + i) = make_uint4(0, 0, 0, 0);
+                        for (int i = 0; i < (int)sbytes; i += 16) *reinterpret_cast<uint4*>(raw + PR_KEYS * DP / 2 + lane * sbytes + i) = make_uint4(0, 0, 0, 0);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     __syncwarp();
@@ -803,7 +811,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
 template <int DP>
 __global__ void __launch_bounds__(256)
 kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
-    constexpr int NQ = DP / 32;
+    constexpr int NQ = DP / 32, ROWS = PrShape<DP>::ROWS;
     const int c = blockIdx.x + 1, D = a.g.dim;
     const int4 s = w.start[c];
     const long long share = w.share[0], from = c * share - s.z;      // the item's first unit of all
@@ -812,7 +820,7 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
     const int c0 = mine ? (int)((from + PR_EXTRA) / share) : 0;      // the share with its first tile
     mine = mine && c == c0 + 1;
     AtItem it{};
-    if (mine) it = at_item<2 * PR_ROWS, PR_KEYS>(a, s.x);
+    if (mine) it = at_item<ROWS, PR_KEYS>(a, s.x);
     const int r = 32 * blockIdx.y + threadIdx.x / 8, quad0 = threadIdx.x % 8;
     at_after_previous();
     if (!mine || r >= it.nrow) return;
@@ -824,13 +832,13 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
     for (int x = c0; x <= c1; ++x) {
         // the first piece of that share, unless the item starts inside the share
         const int64_t slot = 2 * (int64_t)x + (from > x * share ? 1 : 0);
-        const float2 ml = a.part_ml[slot * (2 * PR_ROWS) + r];
+        const float2 ml = a.part_ml[slot * ROWS + r];
         float4 y[NQ];
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (4 * (quad0 + 8 * q) < D)
-                y[q] = *reinterpret_cast<const float4*>(a.part + ((slot * (D / 4) + quad0 + 8 * q) * (2 * PR_ROWS) + r) * 4);
+                y[q] = *reinterpret_cast<const float4*>(a.part + ((slot * (D / 4) + quad0 + 8 * q) * ROWS + r) * 4);
         }
         const float mn = fmaxf(m, ml.x);
         const float f = m == -INFINITY ? 0.f : at_exp2(m - mn), h = ml.x == -INFINITY ? 0.f : at_exp2(ml.x - mn);
@@ -859,7 +867,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     using S = PrShape<DP>;
     auto* kernel = kv8_prompt_kernel<TYPE, DP>;
     SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    const int64_t row_tiles = (max_new * a.group + 2 * PR_ROWS - 1) / (2 * PR_ROWS), n = row_tiles * a.g.requests;
+    const int64_t row_tiles = (max_new * a.group + S::ROWS - 1) / S::ROWS, n = row_tiles * a.g.requests;
     if (n >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
     int64_t keys = max_len;
     if (a.window > 0 && keys > a.window + max_new + PR_KEYS) keys = a.window + max_new + PR_KEYS;
@@ -869,7 +877,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     w.ctas = (int)(most < ctx->sm_count ? most : ctx->sm_count);
     a.row_tiles = (int)row_tiles;
     a.by_row_tiles = KvDiv(a.row_tiles);
-    const size_t rows = (size_t)w.ctas * 2 * (2 * PR_ROWS);
+    const size_t rows = (size_t)w.ctas * 2 * S::ROWS;
     void* arena;
     const sb_status s = sb_scratch(ctx, Carver::need({((size_t)n + 1) * 8, (size_t)w.ctas * 16, 16, rows * a.g.dim * 4, rows * 8}), &arena);
     if (s != SB_OK) return s;
@@ -879,7 +887,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     w.share = cv.take<long long>(2);
     a.part = cv.take<float>(rows * a.g.dim);
     a.part_ml = cv.take<float2>(rows);
-    kv8_prompt_plan_kernel<<<1, 1024, 0, ctx->stream>>>(a, w);
+    kv8_prompt_plan_kernel<S::ROWS><<<1, 1024, 0, ctx->stream>>>(a, w);
     SB_LAUNCHED(ctx);
     // The other two are sent off while the kernel before them still runs and wait on the device for its
     // end (at_after_previous), which hides their launches.
@@ -896,7 +904,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, a, w));
     SB_LAUNCHED(ctx);
     if (w.ctas > 1) {
-        cfg.gridDim = dim3((unsigned)(w.ctas - 1), 2 * PR_ROWS / 32);
+        cfg.gridDim = dim3((unsigned)(w.ctas - 1), S::ROWS / 32);
         cfg.blockDim = dim3(256);
         cfg.dynamicSmemBytes = 0;
         SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kv8_prompt_sum_kernel<DP>, a, w));
@@ -908,7 +916,9 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
 }  // namespace
 
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len) {
-    if (type == AT_E2M1) return a.g.dim <= 64 ? prompt_launch<AT_E2M1, 64>(ctx, a, max_new, max_len) : prompt_launch<AT_E2M1, 128>(ctx, a, max_new, max_len);
+    if (type == AT_E2M1)
+        return a.g.dim <= 64 ? prompt_launch<AT_E2M1, 64>(ctx, a, max_new, max_len)
+             : a.g.dim <= 128 ? prompt_launch<AT_E2M1, 128>(ctx, a, max_new, max_len) : prompt_launch<AT_E2M1, 256>(ctx, a, max_new, max_len);
     if (type == SB_KV_INT8)
         return a.g.dim <= 64 ? prompt_launch<SB_KV_INT8, 64>(ctx, a, max_new, max_len) : prompt_launch<SB_KV_INT8, 128>(ctx, a, max_new, max_len);
     return a.g.dim <= 64 ? prompt_launch<SB_KV_E4M3, 64>(ctx, a, max_new, max_len) : prompt_launch<SB_KV_E4M3, 128>(ctx, a, max_new, max_len);

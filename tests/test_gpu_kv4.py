@@ -247,7 +247,8 @@ def test_one_token_per_request(ctx, past, new, heads, group, page, dim):
 @pytest.mark.parametrize("past,new,heads,group,page,dim", [
     ([40, 3], [5, 2], 2, 4, 16, 128), ([0], [33], 1, 2, 16, 64), ([17, 0, 64], [40, 70, 0], 2, 3, 32, 128), ([30], [20], 1, 7, 48, 256),
     ([0, 100], [130, 1], 1, 4, 64, 96), ([5], [150], 1, 8, 16, 128), ([0, 257], [300, 129], 2, 1, 64, 128), ([9], [60], 1, 3, 16, 16),
-    ([9, 50], [60, 33], 1, 3, 16, 48), ([9], [60], 1, 3, 16, 112)])
+    ([9, 50], [60, 33], 1, 3, 16, 48), ([9], [60], 1, 3, 16, 112), ([9], [60], 1, 3, 16, 144),
+    ([0, 33], [130, 1], 1, 2, 64, 208)])
 def test_drafts_and_prompts(ctx, past, new, heads, group, page, dim):
     _attend(ctx, past, new, heads, group, page, dim)
 
@@ -265,7 +266,8 @@ def test_long_cache_in_many_chunks(ctx, dim):
 
 @pytest.mark.parametrize("past,new,heads,group,dim,window", [
     ([3000], [70], 1, 4, 128, 0), ([2500, 10], [33, 65], 2, 3, 64, 0), ([1500], [257], 1, 1, 96, 0), ([4000, 0], [40, 64], 1, 4, 80, 700),
-    ([0], [129], 1, 2, 128, 0), ([1111, 0, 127], [20, 0, 40], 2, 5, 128, 0)])
+    ([0], [129], 1, 2, 128, 0), ([1111, 0, 127], [20, 0, 40], 2, 5, 128, 0),
+    ([1900, 40], [50, 90], 2, 4, 256, 0), ([700], [64], 1, 4, 240, 300), ([0, 1000], [128, 129], 1, 1, 256, 0)])
 def test_chunks_of_prompts_behind_a_long_past(ctx, past, new, heads, group, dim, window):
     _attend(ctx, past, new, heads, group, 16, dim, window=window)
 
