@@ -22,7 +22,12 @@
 namespace {
 
 constexpr float K4_LIMIT = 16384.f;      // 2^AT4_FAR
-constexpr int K4_PROMPT_FROM = 24;       // more query rows than this per cache head go to the tcgen05 kernel
+// More query rows than this per cache head go to the tcgen05 kernel. Four query rows a token; here and there, us: heads of 64, 16
+// requests in 2000 tokens, 64 rows 37 and 41, 96 rows 48 and 41, one in 30000 45 and 50, 50 and 50; heads of 128, 32 rows, one in
+// 2000 28 and 22, 4 29 and 26, 16 40 and 49, one in 30000 68 and 50; heads of 256, 4 in 2000, 64 rows 42 and 48, 96 rows 49 and
+// 49, 16 108 and 97, 157 and 97, one in 30000 108 and 119, 125 and 119. The number of requests would decide too: the limits
+// are near where many of them change sides.
+__host__ __device__ constexpr int k4_prompt_from(int dim) { return dim <= 64 ? 80 : dim <= 128 ? 24 : 64; }
 
 template <int BYTES>
 __device__ __forceinline__ void k4_copy(unsigned dst, const void* src) {
@@ -508,7 +513,7 @@ extern "C" sb_status sb_kv4_attention(sb_ctx* ctx, const sb_kv4_cache* cache, co
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.window = window >= (1ll << 30) ? 0 : (int)window;
     a.st = ctx->dstate;
-    if (max_new * a.group > K4_PROMPT_FROM) return kv8_prompt(ctx, a, AT_E2M1, max_new, max_len);
+    if (max_new * a.group > k4_prompt_from(cache->dim)) return kv8_prompt(ctx, a, AT_E2M1, max_new, max_len);
     return cache->dim <= 64 ? rows_by_count<64>(ctx, a, max_new, max_len)
          : cache->dim <= 128 ? rows_by_count<128>(ctx, a, max_new, max_len) : rows_by_count<256>(ctx, a, max_new, max_len);
 }

@@ -160,9 +160,16 @@ template <> struct LoOut<__nv_bfloat16> {
     uint4 v;
     // from shared memory: 16 bytes (fp32: and 16 more)
     __device__ __forceinline__ void take(unsigned at, unsigned) { v = lo_lds16(at); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool wide) {
-        if (wide && left >= 8) v = *reinterpret_cast<const uint4*>(p);
-        else {
+    // `wide`: the bytes that bases and rows are aligned to, 16 at most
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, int wide) {
+        if (wide == 16 && left >= 8) v = *reinterpret_cast<const uint4*>(p);
+        else if (wide == 8 && left >= 8) {
+            const uint2 x = *reinterpret_cast<const uint2*>(p), y = *reinterpret_cast<const uint2*>(p + 4);
+            v = make_uint4(x.x, x.y, y.x, y.y);
+        } else if (wide == 4 && left >= 8) {
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+            v = make_uint4(q[0], q[1], q[2], q[3]);
+        } else {
             const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
             uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -177,9 +184,15 @@ template <> struct LoOut<__nv_bfloat16> {
         for (int i = 0; i < 4; ++i) w[i] = u32(__floats2bfloat162_rn(fmaf(x[2 * i], f, bf16lo(w[i])), fmaf(x[2 * i + 1], f, bf16hi(w[i]))));
         v = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ __forceinline__ void store(__nv_bfloat16* p, int left, bool wide) const {
-        if (wide && left >= 8) *reinterpret_cast<uint4*>(p) = v;
-        else {
+    __device__ __forceinline__ void store(__nv_bfloat16* p, int left, int wide) const {
+        if (wide == 16 && left >= 8) *reinterpret_cast<uint4*>(p) = v;
+        else if (wide == 8 && left >= 8) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(v.x, v.y);
+            *reinterpret_cast<uint2*>(p + 4) = make_uint2(v.z, v.w);
+        } else if (wide == 4 && left >= 8) {
+            uint32_t* q = reinterpret_cast<uint32_t*>(p);
+            q[0] = v.x; q[1] = v.y; q[2] = v.z; q[3] = v.w;
+        } else {
             uint16_t* q = reinterpret_cast<uint16_t*>(p);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -195,8 +208,8 @@ template <> struct LoOut<float> {
         v[0] = __uint_as_float(p.x); v[1] = __uint_as_float(p.y); v[2] = __uint_as_float(p.z); v[3] = __uint_as_float(p.w);
         v[4] = __uint_as_float(q.x); v[5] = __uint_as_float(q.y); v[6] = __uint_as_float(q.z); v[7] = __uint_as_float(q.w);
     }
-    __device__ __forceinline__ void load(const float* p, int left, bool wide) {
-        if (wide && left >= 8) {
+    __device__ __forceinline__ void load(const float* p, int left, int wide) {
+        if (wide == 16 && left >= 8) {
             const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
             v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
         } else {
@@ -208,8 +221,8 @@ template <> struct LoOut<float> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(x[i], f, v[i]);
     }
-    __device__ __forceinline__ void store(float* p, int left, bool wide) const {
-        if (wide && left >= 8) {
+    __device__ __forceinline__ void store(float* p, int left, int wide) const {
+        if (wide == 16 && left >= 8) {
             *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
         } else {
@@ -313,7 +326,7 @@ lora_few_kernel(const LoArgs a, const int wide) {
                 const bool take = c + row < c1 && 8 * piece < a.rank;
                 lo_copy16(dst + lm_b_at<RP>(row, piece), take ? b + (c + row) * a.rank + 8 * piece : a.b, take);
             }
-            if (wide) {
+            if (wide == 16) {
                 constexpr int PT = 2 * (int)sizeof(T), PE = 16 / (int)sizeof(T);      // pieces of a row of base, elements of one
 #pragma unroll
                 for (int i = 0; i < PT / 2; ++i) {
@@ -420,8 +433,8 @@ lora_few_kernel(const LoArgs a, const int wide) {
             const int r = g + 8 * e;
             if (left <= 0 || r >= tile.rows) continue;
             LoOut<T> o;
-            if (wide && left == 8) o.take(at + S::B + lf_base_at<T>(r, (int)sizeof(T) / 2 * t), at + S::B + lf_base_at<T>(r, 2 * t + 1));
-            else o.load(base + r * a.ld_base + col, left, false);
+            if (wide == 16 && left == 8) o.take(at + S::B + lf_base_at<T>(r, (int)sizeof(T) / 2 * t), at + S::B + lf_base_at<T>(r, 2 * t + 1));
+            else o.load(base + r * a.ld_base + col, left, wide);
             const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
                                 acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
             o.add(x, scale);
@@ -585,7 +598,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
                 const bool take = c + row < c1 && 8 * piece < a.rank;
                 lo_copy16(dst + lm_b_at<RP>(row, piece), take ? w + (c + row) * a.rank + 8 * piece : a.b, take);
             }
-            if (wide) {
+            if (wide == 16) {
                 constexpr int PT = LM_COLS * (int)sizeof(T) / 16, PE = 16 / (int)sizeof(T);
 #pragma unroll
                 for (int i = 0; i < LM_ROWS * PT; i += 256) {
@@ -640,9 +653,9 @@ lora_up_kernel(const LoArgs a, const int wide) {
             const int r = 16 * rg + g + 8 * e;
             if (left <= 0 || r >= tile.rows) continue;
             LoOut<T> o;
-            if (wide && left == 8)
+            if (wide == 16 && left == 8)
                 o.take(at + S::B + lm_base_at<T>(r, (int)sizeof(T) / 2 * (4 * cg + t)), at + S::B + lm_base_at<T>(r, (int)sizeof(T) / 2 * (4 * cg + t) + 1));
-            else o.load(base + r * a.ld_base + col, left, false);
+            else o.load(base + r * a.ld_base + col, left, wide);
             const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
                                 acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
             o.add(x, scale);
@@ -715,7 +728,9 @@ extern "C" sb_status sb_lora_add(sb_ctx* ctx, const sb_lora_adapters* ad, const 
     a.ldx = ldx; a.ld_base = ld_base; a.ldy = ldy; a.in = ad->in; a.out = ad->out; a.total = total;
     a.starts = starts; a.ids = ids; a.requests = requests; a.adapters = ad->adapters; a.rank = ad->rank;
     a.max_new = (int)max_new; a.st = ctx->dstate;
-    const int wide = (ends & 15) == 0 && (total == 1 || ((ld_base * size) % 16 == 0 && (ldy * size) % 16 == 0));
+    uintptr_t bits = ends | 16;
+    if (total > 1) bits |= (uintptr_t)((ld_base | ldy) * size);
+    const int wide = (int)(bits & (~bits + 1));
     return ad->rank <= 16 ? lo_by_type<16>(ctx, a, f32, wide) : ad->rank <= 32 ? lo_by_type<32>(ctx, a, f32, wide)
          : ad->rank <= 64 ? lo_by_type<64>(ctx, a, f32, wide) : lo_by_type<128>(ctx, a, f32, wide);
 }
