@@ -42,67 +42,59 @@ __device__ __forceinline__ void lo_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
 __device__ __forceinline__ uint4 lo_ld16(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 
 struct LoTile { int64_t row0; int rows, adapter; };
-// The rows of a request; none (and the status latched) where its numbers do not fit.
-__device__ __forceinline__ int lo_rows(const LoArgs& a, int b, int64_t& row0) {
-    row0 = a.starts[b];
-    const int64_t n = (int64_t)a.starts[b + 1] - row0;
-    if (row0 >= 0 && n >= 0 && n <= a.max_new && row0 + n <= a.total) return (int)n;
-    sb_latch(a.st, SB_ERR_INVALID, SBK_LORA);
-    return 0;
-}
-// Tile number `tile`; all threads of the block take part. rows = 0: there is no such tile.
-template <int TM, int THREADS>
-__device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
-    LoTile t{0, 0, -1};
-    int b = tile;
-    int64_t row0;
-    if (a.direct) {
-        t.rows = lo_rows(a, b, row0);
-        t.row0 = row0;
-    } else {
-        __shared__ int sums[THREADS / 32], found[2];
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        if (threadIdx.x == 0) found[0] = -1;
-        int before = 0;
-        for (int base = 0; base < a.requests; base += THREADS) {
-            const int r = base + threadIdx.x;
-            const int mine = r < a.requests ? (lo_rows(a, r, row0) + TM - 1) / TM : 0;
-            int x = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            __syncthreads();
-            if (lane == 31) sums[warp] = x;
-            __syncthreads();
-            int all = 0, below = before;
-#pragma unroll
-            for (int w = 0; w < THREADS / 32; ++w) {
-                if (w < warp) below += sums[w];
-                all += sums[w];
-            }
-            const int lo = below + x - mine;
-            if (tile >= lo && tile < lo + mine) {
-                found[0] = r;
-                found[1] = tile - lo;
-            }
-            before += all;
-            if (tile < before) break;
-        }
-        __syncthreads();
-        b = found[0];
-        if (b < 0) return t;
-        const int n = lo_rows(a, b, row0);
-        t.row0 = row0 + (int64_t)found[1] * TM;
-        t.rows = min(TM, n - found[1] * TM);
-    }
+// The rows of a request and its adapter; no rows (and the status latched) where its numbers do not fit.
+__device__ __forceinline__ LoTile lo_request(const LoArgs& a, int b) {
+    LoTile t;
+    t.row0 = a.starts[b];
     t.adapter = a.ids[b];
-    if (t.adapter < -1 || t.adapter >= a.adapters) {
+    const int64_t n = (int64_t)a.starts[b + 1] - t.row0;
+    const bool fits = t.row0 >= 0 && n >= 0 && n <= a.max_new && t.row0 + n <= a.total;
+    t.rows = fits ? (int)n : 0;
+    if (!fits || t.adapter < -1 || t.adapter >= a.adapters) {
         sb_latch(a.st, SB_ERR_INVALID, SBK_LORA);
         t.adapter = -1;
     }
     return t;
+}
+// Tile number `tile`; all threads of the block take part. rows = 0: there is no such tile.
+template <int TM, int THREADS>
+__device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
+    if (a.direct) return lo_request(a, tile);
+    __shared__ int sums[THREADS / 32];
+    __shared__ LoTile found;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) found.rows = 0;
+    int before = 0;
+    for (int base = 0; base < a.requests; base += THREADS) {
+        LoTile t{0, 0, -1};
+        if (base + threadIdx.x < a.requests) t = lo_request(a, base + threadIdx.x);
+        const int mine = (t.rows + TM - 1) / TM;
+        int x = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) sums[warp] = x;
+        __syncthreads();
+        int all = 0, below = before;
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) below += sums[w];
+            all += sums[w];
+        }
+        const int lo = below + x - mine;
+        if (tile >= lo && tile < lo + mine) {
+            t.row0 += (int64_t)(tile - lo) * TM;
+            t.rows = min(TM, t.rows - (tile - lo) * TM);
+            found = t;
+        }
+        before += all;
+        if (tile < before) break;
+    }
+    __syncthreads();
+    return found;
 }
 
 __device__ __forceinline__ unsigned lo_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -233,6 +225,27 @@ template <> struct LoOut<float> {
     }
 };
 
+// A tile of base, ROWS x COLS from p on, into shared memory by THREADS threads; `at`: place of a 16-byte piece of a row. Not where elements
+// are not aligned to 4 bytes.
+template <typename T, int BYTES, int ROWS, int COLS, int THREADS, typename At>
+__device__ __forceinline__ void lo_copy_pieces(unsigned dst, const T* p, int64_t ld, int rows, int64_t left, int tid, const At& at) {
+    constexpr int PT = COLS * (int)sizeof(T) / BYTES, PE = BYTES / (int)sizeof(T);         // pieces of a row, elements of one
+#pragma unroll(BYTES == 16 ? ROWS * PT / THREADS : 1)
+    for (int i = tid; i < ROWS * PT; i += THREADS) {
+        const int row = i / PT, piece = i % PT;
+        if (row >= rows || PE * (piece + 1) > left) continue;
+        const unsigned to = dst + at(row, piece * BYTES / 16) + (unsigned)(piece * BYTES % 16);
+        if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p + row * ld + PE * piece) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p + row * ld + PE * piece), "n"(BYTES) : "memory");
+    }
+}
+template <typename T, int ROWS, int COLS, int THREADS, typename At>
+__device__ __forceinline__ void lo_copy_base(unsigned dst, const T* p, int64_t ld, int rows, int64_t left, int wide, int tid, const At& at) {
+    if (wide == 16) lo_copy_pieces<T, 16, ROWS, COLS, THREADS>(dst, p, ld, rows, left, tid, at);
+    else if (wide == 8) lo_copy_pieces<T, 8, ROWS, COLS, THREADS>(dst, p, ld, rows, left, tid, at);
+    else if (wide == 4) lo_copy_pieces<T, 4, ROWS, COLS, THREADS>(dst, p, ld, rows, left, tid, at);
+}
+
 // Rows without an adapter: base as it is, columns c0 to c1.
 template <typename T>
 __device__ __forceinline__ void lo_pass(const LoArgs& a, const LoTile& tile, int64_t c0, int64_t c1, int wide) {
@@ -326,15 +339,9 @@ lora_few_kernel(const LoArgs a, const int wide) {
                 const bool take = c + row < c1 && 8 * piece < a.rank;
                 lo_copy16(dst + lm_b_at<RP>(row, piece), take ? b + (c + row) * a.rank + 8 * piece : a.b, take);
             }
-            if (wide == 16) {
-                constexpr int PT = 2 * (int)sizeof(T), PE = 16 / (int)sizeof(T);      // pieces of a row of base, elements of one
-#pragma unroll
-                for (int i = 0; i < PT / 2; ++i) {
-                    const int row = (32 * i + lane) / PT, piece = (32 * i + lane) % PT;
-                    const bool take = row < tile.rows && c + PE * (piece + 1) <= c1;
-                    lo_copy16(dst + S::B + lf_base_at<T>(row, piece), take ? static_cast<const void*>(base + row * a.ld_base + c + PE * piece) : a.b, take);
-                }
-            }
+            // base, in pieces as wide as its rows are aligned
+            const auto at = [](int row, int piece) { return lf_base_at<T>(row, piece); };
+            lo_copy_base<T, 16, 32, 32>(dst + S::B, base + c, a.ld_base, tile.rows, c1 - c, wide, lane, at);
         }
         lo_commit();
     };
@@ -433,7 +440,7 @@ lora_few_kernel(const LoArgs a, const int wide) {
             const int r = g + 8 * e;
             if (left <= 0 || r >= tile.rows) continue;
             LoOut<T> o;
-            if (wide == 16 && left == 8) o.take(at + S::B + lf_base_at<T>(r, (int)sizeof(T) / 2 * t), at + S::B + lf_base_at<T>(r, 2 * t + 1));
+            if (wide >= 4 && left == 8) o.take(at + S::B + lf_base_at<T>(r, (int)sizeof(T) / 2 * t), at + S::B + lf_base_at<T>(r, 2 * t + 1));
             else o.load(base + r * a.ld_base + col, left, wide);
             const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
                                 acc[2][2 * e], acc[2][2 * e + 1], acc[3][2 * e], acc[3][2 * e + 1]};
@@ -598,15 +605,8 @@ lora_up_kernel(const LoArgs a, const int wide) {
                 const bool take = c + row < c1 && 8 * piece < a.rank;
                 lo_copy16(dst + lm_b_at<RP>(row, piece), take ? w + (c + row) * a.rank + 8 * piece : a.b, take);
             }
-            if (wide == 16) {
-                constexpr int PT = LM_COLS * (int)sizeof(T) / 16, PE = 16 / (int)sizeof(T);
-#pragma unroll
-                for (int i = 0; i < LM_ROWS * PT; i += 256) {
-                    const int row = (i + (int)threadIdx.x) / PT, piece = (i + (int)threadIdx.x) % PT;
-                    const bool take = row < tile.rows && c + PE * (piece + 1) <= c1;
-                    lo_copy16(dst + S::B + lm_base_at<T>(row, piece), take ? static_cast<const void*>(base + row * a.ld_base + c + PE * piece) : a.b, take);
-                }
-            }
+            const auto place = [](int row, int piece) { return lm_base_at<T>(row, piece); };
+            lo_copy_base<T, LM_ROWS, LM_COLS, 256>(dst + S::B, base + c, a.ld_base, tile.rows, c1 - c, wide, threadIdx.x, place);
         }
         lo_commit();
     };
@@ -653,7 +653,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
             const int r = 16 * rg + g + 8 * e;
             if (left <= 0 || r >= tile.rows) continue;
             LoOut<T> o;
-            if (wide == 16 && left == 8)
+            if (wide >= 4 && left == 8)
                 o.take(at + S::B + lm_base_at<T>(r, (int)sizeof(T) / 2 * (4 * cg + t)), at + S::B + lm_base_at<T>(r, (int)sizeof(T) / 2 * (4 * cg + t) + 1));
             else o.load(base + r * a.ld_base + col, left, wide);
             const float x[8] = {acc[0][2 * e], acc[0][2 * e + 1], acc[1][2 * e], acc[1][2 * e + 1],
@@ -678,8 +678,8 @@ sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
         return sb_launch(ctx, lora_few_kernel<RP, T>, dim3((unsigned)(a.requests * a.splits)), 256, LfShape<RP, T>::SMEM, a.splits, true, a, wide);
     }
     const int64_t tiles = (a.total + LM_ROWS - 1) / LM_ROWS + a.requests, full = (a.total + LM_ROWS - 1) / LM_ROWS;
-    // parts of `in`: two blocks a multiprocessor, but 512 each at least
-    int64_t want = cut(2 * ctx->sm_count / full, 16), most = cut((a.in + 511) / 512, 16);
+    // parts of `in`: four blocks a multiprocessor, but 256 each at least
+    int64_t want = cut(4 * ctx->sm_count / full, 16), most = cut((a.in + 255) / 256, 16);
     if (want > most) want = most;
     for (a.splits = 1; 2 * a.splits <= want;) a.splits *= 2;
     if (tiles * a.splits >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "lora: too many rows");
