@@ -565,7 +565,8 @@ constexpr int LM_COLS = 64;
 template <int RP, typename T>
 struct LmUp {
     static constexpr int B = LM_COLS * RP * 2, BASE = LM_ROWS * LM_COLS * (int)sizeof(T), STAGE = B + BASE;
-    static constexpr int STAGES = STAGE <= 16384 ? 4 : 3;
+    static constexpr int STAGES = RP == 64 || STAGE > 16384 ? 3 : 4;
+    static constexpr int CTAS = RP == 64 ? 3 : 2;                    // at rank 64, 80 registers and three blocks a multiprocessor: 6 x 2048 rows 69 us -> 64
     static constexpr int SMEM = STAGES * STAGE;
 };
 template <typename T>
@@ -574,7 +575,7 @@ __device__ __forceinline__ unsigned lm_base_at(int row, int piece) {
 }
 // 8 warps: 4 groups of 16 rows, 2 of 32 columns.
 template <int RP, typename T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, LmUp<RP, T>::CTAS)
 lora_up_kernel(const LoArgs a, const int wide) {
     using S = LmUp<RP, T>;
     constexpr int KS = RP / 16, KW = RP / 8;
@@ -690,9 +691,11 @@ sb_status lo_run(sb_ctx* ctx, LoArgs& a, int wide) {
     a.h = Carver(arena).take<uint16_t>(2 * n);
     s = sb_launch(ctx, lora_down_kernel<RP>, dim3((unsigned)(tiles * a.splits)), 256, LmDown<RP>::SMEM, a.splits, true, a);
     if (s != SB_OK) return s;
-    // columns of a block of the second kernel: eight blocks a multiprocessor, four tiles each at least
-    most = (a.out + 4 * LM_COLS - 1) / (4 * LM_COLS);
-    const int64_t parts = cut(8 * ctx->sm_count / full, most < 65535 ? most : 65535), each = (a.out + LM_COLS - 1) / LM_COLS;
+    // Columns of a block of the second kernel: six or eight blocks a multiprocessor, four tiles each at least; with few rows, one block a
+    // multiprocessor of one tile each at least (2 tiles of rows, 144 columns, f32: 17 us in one part, 9.5 in three).
+    const int64_t each = (a.out + LM_COLS - 1) / LM_COLS, long_parts = cut((RP == 64 ? 6 : 8) * ctx->sm_count / full, (each + 3) / 4);
+    const int64_t short_parts = cut(ctx->sm_count / full, each);
+    const int64_t parts = cut(long_parts > short_parts ? long_parts : short_parts, 65535);
     a.columns = (each + parts - 1) / parts * LM_COLS;
     return sb_launch(ctx, lora_up_kernel<RP, T>, dim3((unsigned)tiles, (unsigned)((a.out + a.columns - 1) / a.columns)), 256, LmUp<RP, T>::SMEM, 1, true, a, wide);
 }
