@@ -490,7 +490,7 @@ sb_status sb_kv4_append(sb_ctx* ctx, const sb_kv4_cache* cache, const void* K_bf
                         int64_t k_head_stride, const void* V_bf16, int64_t v_token_stride, int64_t v_head_stride,
                         int64_t total, const int32_t* starts, const int32_t* lens, int64_t max_new);
 /* The values of the last n tokens of every request, rounded to bf16: K, V [total][heads][dim].
- * Rows of no request are left as they were.                                                     */
+ * Rows of no request are left as they were.  K and V must not overlap.                          */
 sb_status sb_kv4_read(sb_ctx* ctx, const sb_kv4_cache* cache, int64_t total, const int32_t* starts,
                       const int32_t* lens, int64_t max_new, void* K_bf16, void* V_bf16);
 /* Attention of the new tokens over the cache: the formula, arguments and limits of sb_kv8_attention.
@@ -519,7 +519,7 @@ typedef struct {                /* host struct, read during the call            
 typedef struct {                /* one tensor of rows: element (row, head, d) at row * token_stride + head * head_stride + d */
     const void* x;
     int64_t x_token_stride, x_head_stride;
-    void* y;                    /* may be x with x's strides; must not overlap it otherwise      */
+    void* y;                    /* may be x with x's strides; overlaps nothing of the call otherwise */
     int64_t y_token_stride, y_head_stride;
     int32_t heads, reserved;
 } sb_rotary_part;
@@ -527,7 +527,8 @@ typedef struct {                /* one tensor of rows: element (row, head, d) at
  * their type; 16-byte aligned rows are fastest.  dim: even, 2 .. 1024.
  * Positions: `positions` device int32 [total], any sign, one per row; or NULL and starts, lens as for the
  * caches: row starts[b] + i is at lens[b] - n + i (lens[b] is any number from n on).  Rows of no request are left as
- * they were; a request whose numbers do not fit is skipped and SB_ERR_INVALID is latched.       */
+ * they were; a request whose numbers do not fit is skipped and SB_ERR_INVALID is latched (where starts go down, so
+ * may its neighbours be).                                                                        */
 sb_status sb_rotary(sb_ctx* ctx, const sb_rotary_table* table, const sb_rotary_part* parts, int n_parts, int dim, int f32,
                     int64_t total, const int32_t* positions, const int32_t* starts, const int32_t* lens, int requests,
                     int64_t max_new);
@@ -537,7 +538,7 @@ sb_status sb_rotary(sb_ctx* ctx, const sb_rotary_table* table, const sb_rotary_p
  * (starts[b] .. starts[b + 1], at most max_new) and its adapter a = ids[b]:
  *   Y[t] = base[t] + scale[a] B_a (A_a x[t])         (a = -1: Y[t] = base[t])
  * An id outside -1 .. adapters - 1 counts as -1 and latches SB_ERR_INVALID, as a request does whose rows do not fit
- * (it is skipped).  Rows of no request are left as they were.
+ * (it is skipped, and where starts go down its neighbours may be).  Rows of no request are left as they were.
  * Products of bf16 numbers are summed in fp32; A_a x is held for the second product as the sum of two bf16
  * numbers (2^-17 of it); the result is rounded once.  The sums of a call are always taken in the same order.  */
 typedef struct {                /* host struct, read during the call                             */

@@ -170,7 +170,7 @@ extern "C" sb_status sb_kv4_read(sb_ctx* ctx, const sb_kv4_cache* cache, int64_t
     const sb_status s = kv4_check(ctx, "kv4 read", cache, total, starts, lens, max_new);
     if (s != SB_OK) return s;
     if (total == 0 || max_new == 0) return SB_OK;
-    if (!K || !V) return sb_fail(ctx, SB_ERR_INVALID, "kv4 read: null");
+    if (!K || !V || K == V) return sb_fail(ctx, SB_ERR_INVALID, "kv4 read: null, or one output for both");
     if (!kv8_aligned16(K) || !kv8_aligned16(V)) return sb_fail(ctx, SB_ERR_SHAPE, "kv4 read: 16-byte aligned outputs");
     const int blocks = cache->dim / 16;
     dim3 grid;

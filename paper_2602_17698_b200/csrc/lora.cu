@@ -64,7 +64,7 @@ __device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
     __shared__ LoTile found;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) found.rows = 0;
-    int before = 0;
+    int64_t before = 0;                                              // 64 bits: starts that go down may count rows more than once
     for (int base = 0; base < a.requests; base += THREADS) {
         LoTile t{0, 0, -1};
         if (base + threadIdx.x < a.requests) t = lo_request(a, base + threadIdx.x);
@@ -78,16 +78,16 @@ __device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
         __syncthreads();
         if (lane == 31) sums[warp] = x;
         __syncthreads();
-        int all = 0, below = before;
+        int64_t all = 0, below = before;
 #pragma unroll
         for (int w = 0; w < THREADS / 32; ++w) {
             if (w < warp) below += sums[w];
             all += sums[w];
         }
-        const int lo = below + x - mine;
+        const int64_t lo = below + x - mine;
         if (tile >= lo && tile < lo + mine) {
-            t.row0 += (int64_t)(tile - lo) * TM;
-            t.rows = min(TM, t.rows - (tile - lo) * TM);
+            t.row0 += (tile - lo) * TM;
+            t.rows = (int)min((int64_t)TM, t.rows - (tile - lo) * TM);
             found = t;
         }
         before += all;
@@ -723,6 +723,7 @@ extern "C" sb_status sb_lora_add(sb_ctx* ctx, const sb_lora_adapters* ad, const 
     if (total > 1 && (ldx < ad->in || ld_base < ad->out || ldy < ad->out)) return sb_fail(ctx, SB_ERR_SHAPE, "lora: rows longer than their leading dimension");
     if (!kv8_aligned16(X) || !kv8_aligned16(ad->a) || !kv8_aligned16(ad->b) || (total > 1 && ldx % 8) || (ends & (size - 1)))
         return sb_fail(ctx, SB_ERR_SHAPE, "lora: 16-byte aligned X, a and b, ldx a multiple of 8, base and Y aligned to their type");
+    if (Y == X) return sb_fail(ctx, SB_ERR_INVALID, "lora: Y is X");
     if (Y == base && total > 1 && ldy != ld_base) return sb_fail(ctx, SB_ERR_SHAPE, "lora: in place with another leading dimension");
     SB_CUDA(ctx, cudaSetDevice(ctx->device));
     LoArgs a{};

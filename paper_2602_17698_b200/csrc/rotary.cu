@@ -284,6 +284,10 @@ extern "C" sb_status sb_rotary(sb_ctx* ctx, const sb_rotary_table* table, const 
             return sb_fail(ctx, SB_ERR_SHAPE, "rotary: a base that is not aligned to its type");
         if (p.x == p.y && ((total > 1 && p.x_token_stride != p.y_token_stride) || (p.heads > 1 && p.x_head_stride != p.y_head_stride)))
             return sb_fail(ctx, SB_ERR_SHAPE, "rotary: in place with other strides");
+        if ((total > 1 && p.y_token_stride == 0) || (p.heads > 1 && p.y_head_stride == 0))
+            return sb_fail(ctx, SB_ERR_SHAPE, "rotary: an output whose rows lie on one another");
+        if (i == 1 && (p.y == parts[0].y || p.y == parts[0].x || p.x == parts[0].y))
+            return sb_fail(ctx, SB_ERR_INVALID, "rotary: the output of one part is the other part");
         a.part[i] = {p.x, p.y, p.x_token_stride, p.x_head_stride, p.y_token_stride, p.y_head_stride, p.heads};
         a.heads += p.heads;
         bits |= reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.y);

@@ -435,6 +435,8 @@ def test_refusals(ctx):
              (SB_ERR_INVALID, attend(good, max_new=-1)), (SB_ERR_SHAPE, attend(good, q=_device(_tokens(2, 3, 64, rng)))),
              (SB_ERR_SHAPE, attend(good, q=odd[1:513].view(2, 4, 64))),
              (SB_ERR_SHAPE, lambda: ctx.kv4_append(good, odd[1:257].view(2, 2, 64), x, starts, lens, 1))]
+    both = torch.empty_like(x)
+    calls.append((SB_ERR_INVALID, lambda: ctx.kv4_read(good, starts, lens, 1, out=(both, both))))
     for field, value, status in (("page_tokens", 24, SB_ERR_SHAPE), ("dim", 72, SB_ERR_SHAPE), ("dim", 272, SB_ERR_SHAPE), ("heads", 0, SB_ERR_INVALID),
                                  ("pages", 0, SB_ERR_INVALID), ("table", None, SB_ERR_INVALID), ("k", good.k.data_ptr() + 8, SB_ERR_SHAPE),
                                  ("v_scale", good.v_scale.data_ptr() + 4, SB_ERR_SHAPE), ("requests", 70000, SB_ERR_SHAPE),

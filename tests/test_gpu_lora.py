@@ -174,13 +174,14 @@ def test_requests_and_ids_that_do_not_fit(ctx):
                 assert torch.equal(out[third], case.base[third])
 
 
-def test_same_sums_every_time_and_in_a_graph(ctx):
+@pytest.mark.parametrize("new", [1, 40])
+def test_same_sums_every_time_and_in_a_graph(ctx, new):
     """A captured step serves requests whose adapters change."""
     from paper_2602_17698_b200.binding import Context
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
         c = Context(stream=side)
-        case = Case([1] * 12, [i % 5 for i in range(12)], 4096, 256, 16, 5)
+        case = Case([new] * 12, [i % 5 for i in range(12)], 4096, 256, 16, 5)
         x, out = _device(case.x), torch.empty_like(case.base)
         ids, starts, n = case.args
         c.lora_add(case.adapters, x, case.base, ids, starts, n, out=out)
@@ -200,6 +201,24 @@ def test_same_sums_every_time_and_in_a_graph(ctx):
         c.close()
 
 
+def test_two_contexts_at_once():
+    """Each with its own stream and scratch; the sums are those of a call alone."""
+    from paper_2602_17698_b200.binding import Context
+    runs = []
+    for new in ([90, 5, 70], [3, 1, 2], [400, 0, 33]):
+        case = Case(new, [1, 0, 1], 2048, 1000, 64, 2)
+        runs.append((case, Context(stream=torch.cuda.Stream()), _device(case.x), [torch.empty_like(case.base) for _ in range(6)]))
+    torch.cuda.synchronize()
+    for i in range(6):
+        for case, c, x, outs in runs:
+            c.lora_add(case.adapters, x, case.base, *case.args, out=outs[i])
+    for case, c, x, outs in runs:
+        c.sync()
+        case.check(outs[0])
+        assert all(torch.equal(o, outs[0]) for o in outs)
+        c.close()
+
+
 def test_nothing_to_do_and_refusals(ctx):
     from paper_2602_17698_b200.binding import SB_ERR_INVALID, SB_ERR_SHAPE, LoraAdapters, SbError, lib
     case = Case([2, 1], [0, 1], 64, 40, 8, 2)
@@ -211,7 +230,7 @@ def test_nothing_to_do_and_refusals(ctx):
                                                     starts.data_ptr(), ids.data_ptr(), 2, max_new))
     calls = [(SB_ERR_SHAPE, direct(ldx=60)), (SB_ERR_SHAPE, direct(ldx=68)), (SB_ERR_SHAPE, direct(xp=x.data_ptr() + 2)), (SB_ERR_SHAPE, direct(ldb=39)),
              (SB_ERR_SHAPE, direct(ldy=41)), (SB_ERR_SHAPE, direct(y=case.base.data_ptr() + 1)), (SB_ERR_INVALID, direct(f32=2)),
-             (SB_ERR_INVALID, direct(max_new=-1))]
+             (SB_ERR_INVALID, direct(max_new=-1)), (SB_ERR_INVALID, direct(y=x.data_ptr()))]
     for field, value, status in (("rank", 4, SB_ERR_SHAPE), ("rank", 136, SB_ERR_SHAPE), ("in_", 60, SB_ERR_SHAPE), ("adapters", 0, SB_ERR_INVALID),
                                  ("a", None, SB_ERR_INVALID), ("b", case.adapters.b.data_ptr() + 8, SB_ERR_SHAPE), ("out", 0, SB_ERR_INVALID)):
         ad = LoraAdapters(case.adapters.a, case.adapters.b)

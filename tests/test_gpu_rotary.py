@@ -189,12 +189,19 @@ def test_refusals(ctx):
     wide, _ = _table(66, False)
     pos = _ints([0, 1, 2, 3])
     back = RotaryTable(table.freq, factor=float("inf"))
+    other = torch.zeros_like(x)
     alias = torch.zeros(4 * 2 * 128, dtype=torch.bfloat16, device=DEV)
     for status, call in [(SB_ERR_SHAPE, lambda: ctx.rotary(wide, x, positions=pos)), (SB_ERR_INVALID, lambda: ctx.rotary(back, x, positions=pos)),
                          (SB_ERR_SHAPE, lambda: ctx.rotary(table, torch.zeros(4, 1, 65, dtype=torch.bfloat16, device=DEV), positions=pos)),
                          (SB_ERR_SHAPE, lambda: ctx.rotary(table, torch.zeros(4, 1, 1026, dtype=torch.bfloat16, device=DEV), positions=pos)),
                          (SB_ERR_INVALID, lambda: ctx.rotary(table, x, starts=_ints([0, 4]), lens=_ints([4]), max_new=-1)),
-                         (SB_ERR_SHAPE, lambda: ctx.rotary(table, alias[:512].view(4, 2, 64), positions=pos, out=alias.view(4, 4, 64)[:, ::2]))]:
+                         (SB_ERR_SHAPE, lambda: ctx.rotary(table, alias[:512].view(4, 2, 64), positions=pos, out=alias.view(4, 4, 64)[:, ::2])),
+                         # outputs on one another, on the other part, on themselves
+                         (SB_ERR_INVALID, lambda: ctx.rotary(table, x, x, positions=pos)), (SB_ERR_INVALID, lambda: ctx.rotary(table, x, other, positions=pos, out=(other, x))),
+                         (SB_ERR_INVALID, lambda: ctx.rotary(table, x, other, positions=pos, out=(alias[:512].view(4, 2, 64), alias[:512].view(4, 2, 64)))),
+                         (SB_ERR_INVALID, lambda: ctx.rotary(table, x, other, positions=pos, out=(alias[:512].view(4, 2, 64), x))),
+                         (SB_ERR_SHAPE, lambda: ctx.rotary(table, x[:, :1].expand(4, 2, 64), positions=pos)),
+                         (SB_ERR_SHAPE, lambda: ctx.rotary(table, x, positions=pos, out=other[:1].expand(4, 2, 64)))]:
         with pytest.raises(SbError) as e:
             call()
         assert e.value.status == status
