@@ -62,6 +62,7 @@ struct K4Shape {
     static constexpr int STAGE = 2 * CODES + 2 * SCALES;             // a step: codes of K and V, scales of K and V
     static constexpr int WARP_RING = STAGES * STAGE;
     static constexpr int ROWS = 8 * NR;
+    static constexpr int DIRECT = 33;                                // steps of an item that gets a CTA of its own
     static constexpr int OPITCH = DP + 4;                            // floats of a row of a warp's sums
     static constexpr int SUMS = AT_WARPS * ROWS * (OPITCH + 2) * 4, WEIGHTS = CTAS * 160 * ROWS * 4 + AT_WARPS * 32 * 16;
     static constexpr int RING_NEED = AT_WARPS * WARP_RING > SUMS ? AT_WARPS * WARP_RING : SUMS;
@@ -84,8 +85,8 @@ __device__ __forceinline__ unsigned k4_at(int row, int piece) {
     return (unsigned)(row * 128 + ((piece ^ ((row & 3) << 1) ^ (row & 4)) << 4));
 }
 
-// FULL: a head has DP elements, so a token's bytes are known here.
-template <int DP, int NR, bool FULL>
+// FULL: a head has DP elements, so a token's bytes are known here. DIRECT: a CTA an item.
+template <int DP, int NR, bool FULL, bool DIRECT>
 __global__ void __launch_bounds__(AT_WARPS * 32, K4Shape<DP, NR>::CTAS)
 kv4_rows_kernel(const AtArgs a) {
     using S = K4Shape<DP, NR>;
@@ -103,8 +104,8 @@ kv4_rows_kernel(const AtArgs a) {
     sb_after_previous();
     AtWalk<S::ROWS, AT_STEP, AT_EXTRA> wk;
     long long share;
-    if (!at_share<S>(a, smem, wk, share)) return;
-    for (bool more = true; more; more = wk.next(a)) {
+    if (!at_share<S, DIRECT>(a, smem, wk, share)) return;
+    for (bool more = true; more; more = !DIRECT && wk.next(a)) {
         const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
         const Kv8Request rq = wk.it.rq;
         const int i0 = a.by_group.quot(r0), i1 = a.by_group.quot(r0 + nrow - 1);
@@ -458,7 +459,7 @@ kv4_rows_kernel(const AtArgs a) {
                 }
             }
         __syncthreads();
-        at_finish<S, DP>(a, smem, wk, share);
+        at_finish<S, DP, DIRECT>(a, smem, wk, share);
         __syncthreads();                                                 // the next piece's copies go where the sums were
     }
 }
@@ -466,10 +467,11 @@ kv4_rows_kernel(const AtArgs a) {
 template <int DP, int NR>
 sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = K4Shape<DP, NR>;
-    auto* kernel = a.g.dim == DP ? kv4_rows_kernel<DP, NR, true> : kv4_rows_kernel<DP, NR, false>;
     int64_t ctas;
     const sb_status s = at_rows_plan<S>(ctx, "kv4 attention", a, max_new, max_len, ctas);
     if (s != SB_OK) return s;
+    auto* kernel = a.direct ? (a.g.dim == DP ? kv4_rows_kernel<DP, NR, true, true> : kv4_rows_kernel<DP, NR, false, true>)
+                            : a.g.dim == DP ? kv4_rows_kernel<DP, NR, true, false> : kv4_rows_kernel<DP, NR, false, false>;
     return sb_launch(ctx, kernel, dim3((unsigned)ctas), AT_WARPS * 32, S::SMEM, 1, true, a);
 }
 template <int DP>

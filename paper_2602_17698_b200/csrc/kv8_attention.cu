@@ -52,6 +52,7 @@ struct AtShape {
     static constexpr int SIDE = AT_STEP * DP;                      // bytes of a step's keys
     static constexpr int RING = AT_WARPS * STAGES * 2 * SIDE;
     static constexpr int ROWS = 8 * NR;
+    static constexpr int DIRECT = 17;                                // steps of an item that gets a CTA of its own
     static constexpr int QPITCH = 2 * DP + 16;                     // bytes of a query row
     static constexpr int Q_AT = RING;
     static constexpr int F_AT = Q_AT + ROWS * QPITCH;              // score factor of a row, fp32
@@ -63,7 +64,7 @@ struct AtShape {
     static constexpr bool QREGS = NR * DP <= 256;                  // query operands stay in registers
 };
 
-template <int TYPE, int DP, int NR>
+template <int TYPE, int DP, int NR, bool DIRECT>
 __global__ void __launch_bounds__(AT_WARPS * 32, AtShape<DP, NR>::CTAS)
 kv8_rows_kernel(const AtArgs a) {
     using S = AtShape<DP, NR>;
@@ -76,8 +77,8 @@ kv8_rows_kernel(const AtArgs a) {
     const int D = a.g.dim;
     AtWalk<S::ROWS, AT_STEP, AT_EXTRA> wk;
     long long share;
-    if (!at_share<S>(a, smem, wk, share)) return;
-    for (bool more = true; more; more = wk.next(a)) {
+    if (!at_share<S, DIRECT>(a, smem, wk, share)) return;
+    for (bool more = true; more; more = !DIRECT && wk.next(a)) {
         const int head = wk.head, b = wk.it.b, r0 = wk.it.r0, nrow = wk.it.nrow;
         const Kv8Request rq = wk.it.rq;
         const int i0 = a.by_group.quot(r0), i1 = a.by_group.quot(r0 + nrow - 1);
@@ -411,7 +412,7 @@ kv8_rows_kernel(const AtArgs a) {
                 }
             }
         __syncthreads();
-        at_finish<S, DP>(a, smem, wk, share);
+        at_finish<S, DP, DIRECT>(a, smem, wk, share);
         __syncthreads();                                                 // the next piece's copies go where the sums were
     }
 }
@@ -419,11 +420,11 @@ kv8_rows_kernel(const AtArgs a) {
 template <int TYPE, int DP, int NR>
 sb_status rows_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = AtShape<DP, NR>;
-    auto* kernel = kv8_rows_kernel<TYPE, DP, NR>;
-    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     int64_t ctas;
     const sb_status s = at_rows_plan<S>(ctx, "kv8 attention", a, max_new, max_len, ctas);
     if (s != SB_OK) return s;
+    auto* kernel = a.direct ? kv8_rows_kernel<TYPE, DP, NR, true> : kv8_rows_kernel<TYPE, DP, NR, false>;
+    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     kernel<<<(unsigned)ctas, AT_WARPS * 32, S::SMEM, ctx->stream>>>(a);
     SB_LAUNCHED(ctx);
     return SB_OK;

@@ -24,6 +24,7 @@ struct AtArgs {
     float2* part_ml;             // and its rows' (reference, sum of weights)
     unsigned* done;              // per item: pieces finished
     int least;                   // units of a share at least
+    int direct;                  // a CTA an item: no shares, no pieces
     SbDeviceState* st;
 };
 

@@ -30,10 +30,16 @@ __device__ __forceinline__ uint32_t at_transpose(uint32_t x) {
     return y;
 }
 
-// Where this CTA's share of all items' units starts and how long it is; false: there is none.
-template <class S>
+// Where this CTA's share of all items' units starts and how long it is; false: there is none. DIRECT: it has an item of its own.
+template <class S, bool DIRECT>
 __device__ __forceinline__ bool at_share(const AtArgs& a, unsigned char* smem, AtWalk<S::ROWS, AT_STEP, AT_EXTRA>& wk, long long& share) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (DIRECT) {
+        const int row_tile = blockIdx.x / a.g.heads;
+        const AtItem it = at_item<S::ROWS, AT_STEP>(a, row_tile);
+        share = it.steps + AT_EXTRA;
+        return it.steps && wk.begin(a, it, row_tile, (int)blockIdx.x - row_tile * a.g.heads, 0, 0, share);
+    }
     // units of one head before each row tile of all requests, 128 at a time
     struct Found {
         AtItem it;
@@ -103,14 +109,14 @@ __device__ __forceinline__ bool at_share(const AtArgs& a, unsigned char* smem, A
 
 // The warps' sums of a piece (osm [warp][row][OPITCH] and, behind it, their references and sums of weights) become results, or where
 // the item has other pieces an entry in scratch; the last piece to finish adds those.
-template <class S, int DP>
+template <class S, int DP, bool DIRECT>
 __device__ __forceinline__ void at_finish(const AtArgs& a, unsigned char* smem, const AtWalk<S::ROWS, AT_STEP, AT_EXTRA>& wk, long long share) {
     const int lane = threadIdx.x & 31;
     const int D = a.g.dim, head = wk.head, r0 = wk.it.r0, nrow = wk.it.nrow;
     const Kv8Request rq = wk.it.rq;
     const float* osm = reinterpret_cast<const float*>(smem);
     const float2* mlsm = reinterpret_cast<const float2*>(smem + (size_t)AT_WARPS * S::ROWS * S::OPITCH * 4);
-    const bool whole = wk.count == wk.it.steps;
+    const bool whole = DIRECT || wk.count == wk.it.steps;
     const int quads = D / 4;
     auto store = [&](int r, int d, float4 v, float mm, float sum) {
         const int row = r0 + r;
@@ -266,6 +272,15 @@ sb_status at_rows_plan(sb_ctx* ctx, const char* what, AtArgs& a, int64_t max_new
     int64_t keys = max_len;
     if (a.window > 0 && keys > a.window + S::ROWS + SB_KV8_BLOCK) keys = a.window + S::ROWS + SB_KV8_BLOCK;
     const int64_t steps = (keys + AT_STEP - 1) / AT_STEP + 1;
+    a.row_tiles = (int)row_tiles;
+    a.by_row_tiles = KvDiv(a.row_tiles);
+    // Short items: a CTA each, without the search for a share, scratch and the sum of pieces. Heads of 128, us, in shares and so, 4 and
+    // 8 bits: 22 requests of 20 rows in 70 tokens 13.9 and 7.8, 15.4 and 9.3; 1 of 4 rows and 8 heads in 200 8.7 and 5.0, 9.3 and
+    // 6.3; in 500 9.5 and 6.5, 10.2 and 8.4; in 900 9.7 and 9.6, 10.4 and 13.0; 48 in 900 21.9 and 15.6, 25.2 and 19.3; in
+    // 1500 28 and 22, 34 and 28; 60 in 1500 (a few items more than fit at once) 32.5 and 32, 40 and 48.
+    a.direct = steps <= S::DIRECT;
+    ctas = tiles;
+    if (a.direct) return SB_OK;
     // Units of a share at least. A step takes a share about 0.22 us, and every piece of an item 0.22 us per
     // eight rows when they are added: u units a share cost u + steps NR / u. Fixed shares of 6, 16 and
     // 28 took 12, 16 and 18 us for one request in 2000 (8 rows), 43, 35 and 31 for one in 8192 (16 rows).
@@ -273,8 +288,6 @@ sb_status at_rows_plan(sb_ctx* ctx, const char* what, AtArgs& a, int64_t max_new
     while ((int64_t)a.least * a.least < steps * (S::ROWS / 8)) ++a.least;
     const int64_t most = (tiles * (steps + AT_EXTRA) + a.least - 1) / a.least;
     ctas = most < (int64_t)S::CTAS * ctx->sm_count ? most : (int64_t)S::CTAS * ctx->sm_count;
-    a.row_tiles = (int)row_tiles;
-    a.by_row_tiles = KvDiv(a.row_tiles);
     const size_t n = (size_t)ctas * 2 * S::ROWS;
     void* arena;
     const sb_status s = sb_scratch(ctx, Carver::need({n * a.g.dim * 4, n * 8}), &arena);
