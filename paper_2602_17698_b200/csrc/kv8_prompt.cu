@@ -19,7 +19,7 @@
 //
 // A step first takes the weights by the reference there is and looks at their sum: where that is small no
 // maximum is needed (287 -> 273 us in the case below). The work is cut into equal shares (see
-// kv8_attention.cuh); a sum kernel adds the pieces of items that several shares hold.
+// kv8_attention.cuh); a sum kernel adds the pieces of items that several shares hold. Short items have a CTA each (pr_direct).
 //
 // What bounds it: per 128 keys of 256 rows the products need 2560 cycles (the scores, both operands from
 // shared memory in halves of 64 keys, 1536 of them) and the exponentials 2048 (16 per cycle and SM); the kernel
@@ -288,7 +288,12 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     AtWalk<S::ROWS, PR_KEYS, PR_EXTRA> wk;
     at_after_previous();
     at_let_next();                           // its blocks find room when these end, and wait for that
-    {
+    if (a.direct) {
+        // an item of its own, the requests' last row tiles, which have the most keys, first
+        const int i = blockIdx.x / a.g.heads, before = i / a.g.requests, row_tile = (i - before * a.g.requests + 1) * a.row_tiles - 1 - before;
+        const AtItem it = at_item<S::ROWS, PR_KEYS>(a, row_tile);
+        if (!it.steps || !wk.begin(a, it, row_tile, (int)blockIdx.x - i * a.g.heads, 0, 0, it.steps + PR_EXTRA)) return;
+    } else {
         const int4 s = work.start[blockIdx.x];
         const long long share = work.share[0], at = blockIdx.x * share;
         if (s.x < 0 || !wk.begin(a, s.x, s.y, s.z, at, min(share, work.share[1] - at))) return;
@@ -862,6 +867,25 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
     if (quad0 == 0 && a.lse) a.lse[tok * (a.g.heads * a.group) + h] = at_lse(m, l);
 }
 
+// Whether every item has a CTA of its own, without plan, pieces and their sum. Always where items are short (128-key tiles); up to 32
+// tiles where the CTAs end about together, the longest first: what equal shares would win is less than what plan and sum take, 10
+// tiles. Heads of 128, query heads four times the cache's 8, us, in shares and so, 4 and 8 bits: 1 request of 200 tokens 20.1 and
+// 16.4, 20.3 and 16.9; 8 of 400 67 and 59, 72 and 60; 1 of 1500 58 and 40, 61 and 42; 8 of 900 166 and 140, 182 and 146; 1 of 4000 183 and
+// 167, 198 and 180; 1 of 512 behind 1500 45 and 47, 47 and 51; 4 of 1024 behind 4000 329 and 350, 360 and 383.
+template <int ROWS>
+bool pr_direct(const sb_ctx* ctx, const AtArgs& a, int64_t items, int64_t max_new, int64_t max_len) {
+    if (items >= (1ll << 31)) return false;
+    int64_t keys = max_len;
+    if (a.window > 0 && keys > a.window + ROWS / a.group + 1 + SB_KV8_BLOCK) keys = a.window + ROWS / a.group + 1 + SB_KV8_BLOCK;
+    const int64_t steps = (keys + PR_KEYS - 1) / PR_KEYS;
+    if (steps <= 8 || steps > 32) return steps <= 8;
+    // the first row tiles of prompts have fewer keys than the last
+    const int64_t less = a.window > 0 ? 0 : max_new / PR_KEYS, least = (steps > less ? steps - less : 0) + PR_EXTRA;
+    const double rounds = (double)items / ctx->sm_count, even = rounds * (double)(steps + PR_EXTRA + least) / 2;
+    const double last = (double)((items + ctx->sm_count - 1) / ctx->sm_count) - rounds;            // of a round that is empty
+    return even + last * (double)least <= even + 10 && (double)(steps + PR_EXTRA) <= even + 10;
+}
+
 template <int TYPE, int DP>
 sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = PrShape<DP>;
@@ -877,6 +901,22 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     w.ctas = (int)(most < ctx->sm_count ? most : ctx->sm_count);
     a.row_tiles = (int)row_tiles;
     a.by_row_tiles = KvDiv(a.row_tiles);
+    a.direct = pr_direct<S::ROWS>(ctx, a, n * a.g.heads, max_new, max_len);
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.stream = ctx->stream;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)(a.direct ? n * a.g.heads : w.ctas));
+    cfg.blockDim = dim3(PR_THREADS);
+    cfg.dynamicSmemBytes = S::SMEM;
+    if (a.direct) {
+        SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, a, w));
+        SB_LAUNCHED(ctx);
+        return SB_OK;
+    }
     const size_t rows = (size_t)w.ctas * 2 * S::ROWS;
     void* arena;
     const sb_status s = sb_scratch(ctx, Carver::need({((size_t)n + 1) * 8, (size_t)w.ctas * 16, 16, rows * a.g.dim * 4, rows * 8}), &arena);
@@ -891,16 +931,6 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     SB_LAUNCHED(ctx);
     // The other two are sent off while the kernel before them still runs and wait on the device for its
     // end (at_after_previous), which hides their launches.
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.stream = ctx->stream;
-    cfg.attrs = &early;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)w.ctas);
-    cfg.blockDim = dim3(PR_THREADS);
-    cfg.dynamicSmemBytes = S::SMEM;
     SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, a, w));
     SB_LAUNCHED(ctx);
     if (w.ctas > 1) {
