@@ -266,7 +266,7 @@ kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     }
 }
 
-template <int TYPE, int DP>
+template <int TYPE, int DP, bool DIRECT>
 __global__ void __launch_bounds__(PR_THREADS, 1)
 kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     using S = PrShape<DP>;
@@ -288,7 +288,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     AtWalk<S::ROWS, PR_KEYS, PR_EXTRA> wk;
     at_after_previous();
     at_let_next();                           // its blocks find room when these end, and wait for that
-    if (a.direct) {
+    if (DIRECT) {
         // an item of its own, the requests' last row tiles, which have the most keys, first
         const int i = blockIdx.x / a.g.heads, before = i / a.g.requests, row_tile = (i - before * a.g.requests + 1) * a.row_tiles - 1 - before;
         const AtItem it = at_item<S::ROWS, PR_KEYS>(a, row_tile);
@@ -342,7 +342,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         const unsigned ts = tmem + lanes + S::S_COL + qt * 128, to = tmem + lanes + S::O_COL + qt * DP;
         int tiles_all = 0, tiles_mine = 0, pieces = 0;               // key tiles and pieces so far (of this row tile)
         bool ok = true, skipped = false;
-        for (bool more = true; more && ok; more = wk.next(a), ++tiles_all) {
+        for (bool more = true; more && ok; more = !DIRECT && wk.next(a), ++tiles_all) {
             const AtItem& it = wk.it;
             const int count = wk.count;
             tiles_all += count - 1;
@@ -513,7 +513,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             t5_fence_after();
             tiles_mine += count;
             ++pieces;
-            const bool whole = count == it.steps;
+            const bool whole = DIRECT || count == it.steps;
             const int h0 = wk.head * a.group;
             const int64_t tok = it.rq.row0 + a.by_group.quot(row);
             const int h = h0 + a.by_group.rem(row);
@@ -646,7 +646,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         const bool brings = TYPE != AT_E2M1 && warp == 8 && lane < 2 * PR_BLOCKS;
         bool ok = true;
         int n = 0;                                                   // converted tiles so far
-        for (bool more = true; more && ok; more = wk.next(a)) {
+        for (bool more = true; more && ok; more = !DIRECT && wk.next(a)) {
             const int k0 = wk.it.lo + wk.step0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
             const int limit = min(wk.it.rq.len, (k1 + SB_KV8_BLOCK - 1) / SB_KV8_BLOCK * SB_KV8_BLOCK) - k0;
             auto entry_of = [&](int j) -> int {
@@ -687,7 +687,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         const unsigned bytes = (unsigned)(SB_KV8_BLOCK * pitch), sbytes = TYPE == AT_E2M1 ? (unsigned)(SB_KV8_BLOCK * spitch) : 0u;
         bool ok = true;
         int issued = 0;
-        for (bool more = true; more && ok; more = wk.next(a)) {
+        for (bool more = true; more && ok; more = !DIRECT && wk.next(a)) {
             const int k0 = wk.it.lo + wk.step0 * PR_KEYS, k1 = min(wk.it.hi, k0 + wk.count * PR_KEYS);
             auto entry_of = [&](int j) -> int {
                 const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
@@ -756,7 +756,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         auto done = [&](int tile) { pr_commit(one, t5_smem(empty + tile % S::RING)); };
         bool ok = true;
         int t = 0, mine = 0, pieces = 0;                             // converted tiles (keys: even), this row tile's halves, pieces
-        for (bool more = true; more && ok; more = wk.next(a)) {
+        for (bool more = true; more && ok; more = !DIRECT && wk.next(a)) {
             const int halves = 2 * wk.count;
             if (wk.it.nrow <= qt * PR_ROWS) {                        // no rows: lets the tiles go as they come
                 for (int i = 0; ok && i < halves; ++i, ++t) {
@@ -889,8 +889,6 @@ bool pr_direct(const sb_ctx* ctx, const AtArgs& a, int64_t items, int64_t max_ne
 template <int TYPE, int DP>
 sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = PrShape<DP>;
-    auto* kernel = kv8_prompt_kernel<TYPE, DP>;
-    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     const int64_t row_tiles = (max_new * a.group + S::ROWS - 1) / S::ROWS, n = row_tiles * a.g.requests;
     if (n >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
     int64_t keys = max_len;
@@ -902,6 +900,8 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     a.row_tiles = (int)row_tiles;
     a.by_row_tiles = KvDiv(a.row_tiles);
     a.direct = pr_direct<S::ROWS>(ctx, a, n * a.g.heads, max_new, max_len);
+    auto* kernel = a.direct ? kv8_prompt_kernel<TYPE, DP, true> : kv8_prompt_kernel<TYPE, DP, false>;
+    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     cudaLaunchAttribute early{};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
