@@ -15,6 +15,11 @@
 // k4_at says, neither load has bank conflicts.
 //
 // Precision: as kv8_attention.cu, but a weight is held in fp16 relative to 2^-6 of the row's largest so far.
+//
+// Measured (heads of 128, four query heads per cache head, 8 cache heads): 64 requests in 8192 67 us, 4.3 TB/s: conversions, multiplications
+// by the scales and softmax fill 56 % of the issue slots, the copies' rate would allow 43 us; one in 100000 36 us, of which 15
+// are the start and the sum of the pieces; 16 x 5 tokens in a window of 4096 (20 rows) 43 us: 255 registers leave two warps a
+// scheduler, and their latencies bound it (three CTAs with spilled registers: 55 us).
 #include "kv_rows.cuh"
 #include "kv4.cuh"
 #include "launch.cuh"

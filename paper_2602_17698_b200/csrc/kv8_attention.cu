@@ -27,13 +27,13 @@
 // fp32 (0.0008 of their norm for 64 requests in 8192; both are 0.0017 from 64 bits, bf16's rounding).
 //
 // The work of all requests is cut into equal shares (see kv8_attention.cuh), which every CTA finds by
-// itself from the requests' lengths. Of an item that several shares hold, each leaves unnormalised sums,
+// itself from the requests' lengths; short items have a CTA each (at_rows_plan). Of an item that several shares hold, each leaves unnormalised sums,
 // and the last of them to finish (a counter) adds them in their order: the result does not depend on
 // which one that is.
 //
-// Measured (heads of 128, four query heads per cache head, 8 cache heads): 64 requests in 8192 88 us, 5.7 TB/s, 0.88
-// of a plain copy's rate; one in 100000 47 us, of which 35 stream at 5.9 TB/s and the rest is the start and the
-// sum of the pieces; 16 x 5 tokens in a window of 4096 (20 rows) 58 us: 251 registers leave two warps a scheduler,
+// Measured (heads of 128, four query heads per cache head, 8 cache heads): 64 requests in 8192 85 us, 5.9 TB/s, 0.91
+// of a plain copy's rate; one in 100000 45 us, of which 35 stream at 5.9 TB/s and the rest is the start and the
+// sum of the pieces; 16 x 5 tokens in a window of 4096 (20 rows) 53 us: 251 registers leave two warps a scheduler,
 // and their latencies bound it.
 #include "kv_rows.cuh"
 

@@ -26,8 +26,10 @@
 // takes 4400, because a row tile's scores, softmax, weights, sums and next scores wait for one
 // another. Half tiles and two row tiles overlap these chains; whole tiles per step were slower (339 us against
 // 287), and so was a warp of its own for the scores (344).
-// 4 requests of up to 1024 tokens behind up to 8192, 32 query heads of 128 over 8, e4m3: 255 us,
-// 761 TFLOP/s, tensor pipe 54 % active; heads of 64 231 us, of 80 and 96 252.
+// 4 requests of up to 1024 tokens behind up to 8192, 32 query heads of 128 over 8, e4m3: 250 us,
+// 776 TFLOP/s, tensor pipe 54 % active; heads of 64 231 us, of 80 and 96 252. Over the 4-bit cache 231 us, 841 TFLOP/s: half the bytes
+// to copy, and no value scales in the softmax. 4 of up to 1024 behind 4096 with heads of 256 (one row tile, so every key tile is
+// converted for 128 rows only): 0.88 ms, a third of the products' rate.
 #include "kv8_attention.cuh"
 #include "kv4.cuh"
 #include "tensor5.cuh"
@@ -870,8 +872,9 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
 // Whether every item has a CTA of its own, without plan, pieces and their sum. Always where items are short (128-key tiles); up to 32
 // tiles where the CTAs end about together, the longest first: what equal shares would win is less than what plan and sum take, 10
 // tiles. Heads of 128, query heads four times the cache's 8, us, in shares and so, 4 and 8 bits: 1 request of 200 tokens 20.1 and
-// 16.4, 20.3 and 16.9; 8 of 400 67 and 59, 72 and 60; 1 of 1500 58 and 40, 61 and 42; 8 of 900 166 and 140, 182 and 146; 1 of 4000 183 and
-// 167, 198 and 180; 1 of 512 behind 1500 45 and 47, 47 and 51; 4 of 1024 behind 4000 329 and 350, 360 and 383.
+// 15.4, 20.3 and 15.9; 8 of 400 67 and 55, 72 and 57; 1 of 1500 58 and 37, 61 and 39; 8 of 900 166 and 131, 182 and 137; 1 of 4000 183 and
+// 154, 198 and 166; 1 of 512 behind 1500 45 and 47, 47 and 51; 4 of 1024 behind 4000 329 and 350, 360 and 383 (the last two with the
+// kernel's first form).
 template <int ROWS>
 bool pr_direct(const sb_ctx* ctx, const AtArgs& a, int64_t items, int64_t max_new, int64_t max_len) {
     if (items >= (1ll << 31)) return false;

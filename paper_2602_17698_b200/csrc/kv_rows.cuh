@@ -275,8 +275,8 @@ sb_status at_rows_plan(sb_ctx* ctx, const char* what, AtArgs& a, int64_t max_new
     a.row_tiles = (int)row_tiles;
     a.by_row_tiles = KvDiv(a.row_tiles);
     // Short items: a CTA each, without the search for a share, scratch and the sum of pieces. Heads of 128, us, in shares and so, 4 and
-    // 8 bits: 22 requests of 20 rows in 70 tokens 13.9 and 7.8, 15.4 and 9.3; 1 of 4 rows and 8 heads in 200 8.7 and 5.0, 9.3 and
-    // 6.3; in 500 9.5 and 6.5, 10.2 and 8.4; in 900 9.7 and 9.6, 10.4 and 13.0; 48 in 900 21.9 and 15.6, 25.2 and 19.3; in
+    // 8 bits: 22 requests of 20 rows in 70 tokens 13.9 and 7.2, 15.4 and 9.1; 1 of 4 rows and 8 heads in 200 8.7 and 4.6, 9.3 and
+    // 5.8; in 500 9.5 and 6.1, 10.2 and 8.0; in 900 9.7 and 9.6, 10.4 and 13.0; 48 in 900 21.9 and 15.6, 25.2 and 19.3; in
     // 1500 28 and 22, 34 and 28; 60 in 1500 (a few items more than fit at once) 32.5 and 32, 40 and 48.
     a.direct = steps <= S::DIRECT;
     ctas = tiles;
