@@ -212,7 +212,7 @@ kv4_rows_kernel(const AtArgs a) {
         for (int j = 0; j < S::STAGES - 1; ++j) issue(j);
 
         // ---- queries: fp16 rows, each scaled by a power of two ----
-        const float by_head = a.k_head ? __ldg(a.k_head + head) : 1.f;
+        const float by_head = a.k_head ? a.k_head[head] : 1.f;
 #pragma unroll
         for (int i = 0; i < QR; ++i) {
             const int r = warp + AT_WARPS * i;
@@ -442,7 +442,7 @@ kv4_rows_kernel(const AtArgs a) {
         __syncthreads();
 
         // ---- the warps' sums side by side where the ring was ----
-        const float back = a.v_head ? __ldg(a.v_head + head) : 1.f;
+        const float back = a.v_head ? a.v_head[head] : 1.f;
         float* osm = reinterpret_cast<float*>(smem);                     // [warp][row][OPITCH]
         float2* mlsm = reinterpret_cast<float2*>(smem + (size_t)AT_WARPS * S::ROWS * S::OPITCH * 4);      // [warp][row]
 #pragma unroll

@@ -93,10 +93,10 @@ kv4_append_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvD
         for (int k = 0; k < 2; ++k) {
             const Kv4Side& sd = k ? vs : ks;
             const __nv_bfloat16* x = sd.x + (int64_t)(rq.row0 + i) * sd.token_stride + (int64_t)head * sd.head_stride + 16 * j;
-            const uint4 a = ld_stream16(x), c = ld_stream16(x + 8);
+            const uint4 a = ld_once16(x), c = ld_once16(x + 8);
             w[k][0] = a.x; w[k][1] = a.y; w[k][2] = a.z; w[k][3] = a.w;
             w[k][4] = c.x; w[k][5] = c.y; w[k][6] = c.z; w[k][7] = c.w;
-            by[k] = sd.head ? __ldg(sd.head + head) : 1.f;
+            by[k] = sd.head ? sd.head[head] : 1.f;
         }
     }
     const bool there = page >= 0 && page < g.pages;
@@ -155,7 +155,7 @@ kv4_read_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvDiv
     const int pitch = kv4_code_pitch(g.dim), spitch = kv4_scale_pitch(g.dim);
     Kv4Walk walk;
     walk.begin(g, b, rq.past + ROWS * group);
-    const float by[2] = {ks.head ? __ldg(ks.head + head) : 1.f, vs.head ? __ldg(vs.head + head) : 1.f};
+    const float by[2] = {ks.head ? ks.head[head] : 1.f, vs.head ? vs.head[head] : 1.f};
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const int i = ROWS * group + r;

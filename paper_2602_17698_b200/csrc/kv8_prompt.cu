@@ -396,7 +396,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 if (lane == 0) t5_bar_arrive(t5_smem(qready + qt));
             }
             const float fq = __fdiv_rn(fabsf(a.scale_log2), reinterpret_cast<const float*>(smem + S::F_AT)[r]) *
-                             (TYPE == AT_E2M1 && a.k_head ? __ldg(a.k_head + wk.head) : 1.f);
+                             (TYPE == AT_E2M1 && a.k_head ? a.k_head[wk.head] : 1.f);
             // (a thread without a row has queries of zeros, and its results go nowhere)
             const int pos = it.rq.past + a.by_group.quot(row);
             // positions of the tile's first and last row decide which key tiles need a mask
@@ -519,7 +519,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
             const int h0 = wk.head * a.group;
             const int64_t tok = it.rq.row0 + a.by_group.quot(row);
             const int h = h0 + a.by_group.rem(row);
-            const float back = TYPE != AT_E2M1 ? at_power_inv(inv) : a.v_head ? __ldg(a.v_head + wk.head) : 1.f, norm = whole ? at_norm(l) * back : back;
+            const float back = TYPE != AT_E2M1 ? at_power_inv(inv) : a.v_head ? a.v_head[wk.head] : 1.f, norm = whole ? at_norm(l) * back : back;
             const int64_t slot = 2 * (int64_t)blockIdx.x + (wk.first ? 0 : 1);
             // this warp's rows in bf16 where its queries were, in the same order
             unsigned char* o0 = smem + S::Q_AT + qt * S::OPERAND + (warp & 3) * 32 * 128;

@@ -3,7 +3,9 @@
 #include "common.cuh"
 
 // `early`: the kernel's blocks may become resident before the one ahead of it in the stream has ended, so they call sb_after_previous
-// before they touch memory that another kernel writes, or writes that another reads. cluster: blocks along x.
+// before they touch memory that another kernel writes, or writes that another reads, and do not read such memory by .nc or __ldg, which
+// want it unchanged for as long as the kernel is there. A kernel that reads before its own wait (lora_up_kernel) has to be let in by one
+// that calls sb_after_previous BEFORE sb_let_next (lora_down_kernel). cluster: blocks along x.
 template <typename... P>
 sb_status sb_launch(sb_ctx* ctx, void (*kernel)(P...), dim3 grid, unsigned threads, int smem, int cluster, bool early, P... args) {
     if (smem > 40 * 1024) SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);

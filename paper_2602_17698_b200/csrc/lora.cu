@@ -43,15 +43,15 @@ __device__ __forceinline__ void lo_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint4 lo_ld16(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ uint4 lo_ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
 struct LoTile { int64_t row0; int rows, adapter; };
 // The rows of a request and its adapter; no rows (and the status latched) where its numbers do not fit.
 __device__ __forceinline__ LoTile lo_request(const LoArgs& a, int b) {
     LoTile t;
-    t.row0 = a.starts[b];
-    t.adapter = a.ids[b];
-    const int64_t n = (int64_t)a.starts[b + 1] - t.row0;
+    t.row0 = __ldcg(a.starts + b);
+    t.adapter = __ldcg(a.ids + b);
+    const int64_t n = (int64_t)__ldcg(a.starts + b + 1) - t.row0;
     const bool fits = t.row0 >= 0 && n >= 0 && n <= a.max_new && t.row0 + n <= a.total;
     t.rows = fits ? (int)n : 0;
     if (!fits || t.adapter < -1 || t.adapter >= a.adapters) {
@@ -418,7 +418,7 @@ lora_few_kernel(const LoArgs a, const int wide) {
 #pragma unroll
             for (int i = 0; i < KW; ++i) h[k][e][i] = p[i];
         }
-    const float scale = a.scale ? __ldg(a.scale + tile.adapter) : 1.f;
+    const float scale = a.scale ? a.scale[tile.adapter] : 1.f;
     int n = 0;
     for (int64_t c = first; c < c1; c += 256, ++n) {
         lo_wait<S::STAGES - 2>();
@@ -584,6 +584,9 @@ lora_up_kernel(const LoArgs a, const int wide) {
     using S = LmUp<RP, T>;
     constexpr int KS = RP / 16, KW = RP / 8;
     extern __shared__ __align__(128) unsigned char lm_smem[];
+    // starts, ids, B and base are read before this kernel's own wait: lora_down_kernel, which lets it in, has waited for whoever wrote
+    // them. They come by way of L2 (.cg); base in narrower pieces can only be copied by way of L1, and waits.
+    if (wide < 16) sb_after_previous();
     const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x);
     const int64_t c0 = (int64_t)blockIdx.y * a.columns, c1 = min(a.out, c0 + a.columns);
     if (tile.rows <= 0 || tile.adapter < 0) {
@@ -632,7 +635,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
                 h[k][e][i + 1] = r < tile.rows ? x.y : 0u;
             }
         }
-    const float scale = a.scale ? __ldg(a.scale + tile.adapter) : 1.f;
+    const float scale = a.scale ? a.scale[tile.adapter] : 1.f;
     for (int n = 0; n < tiles; ++n) {
         lo_wait<S::STAGES - 2>();
         __syncthreads();

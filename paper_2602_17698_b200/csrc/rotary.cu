@@ -180,7 +180,7 @@ rotary_kernel(const RoArgs a) {
         if (!pos[a.rows + r]) continue;
         const int p = pos[r];
         __syncwarp();
-        for (int i = lane; i < half; i += 32) table[i] = ro_turn(p, __ldg(a.freq + i), a.factor, a.back);
+        for (int i = lane; i < half; i += 32) table[i] = ro_turn(p, a.freq[i], a.factor, a.back);
         __syncwarp();
         if (!works) continue;
         for (int slot = slot0; slot < a.slots; slot += 32) {
