@@ -403,7 +403,8 @@ lora_few_kernel(const LoArgs a, const int wide) {
     } else __syncthreads();
     for (int i = 4 * threadIdx.x; i < 16 * RP; i += 1024) {
         uint2 hi = make_uint2(0, 0), lo = hi;
-        if (i < tile.rows * RP) lo_total(lo_sums + i, a.splits, hi, lo);
+        // behind the rank there are zeros of A, of which an infinity of X makes NaN: zeros here, which meet zeros of B
+        if (i < tile.rows * RP && i % RP < a.rank) lo_total(lo_sums + i, a.splits, hi, lo);
         *reinterpret_cast<uint2*>(held + i / RP * (RP + 8) + i % RP) = hi;
         *reinterpret_cast<uint2*>(held + (16 + i / RP) * (RP + 8) + i % RP) = lo;
     }
@@ -552,8 +553,8 @@ lora_down_kernel(const LoArgs a) {
     // a part of the rows for every block
     const int r0 = tile.rows * part / a.splits, r1 = tile.rows * (part + 1) / a.splits;
     for (int i = r0 * RP + 4 * threadIdx.x; i < r1 * RP; i += 1024) {
-        uint2 hi, lo;
-        lo_total(sums + i, a.splits, hi, lo);
+        uint2 hi = make_uint2(0, 0), lo = hi;
+        if (i % RP < a.rank) lo_total(sums + i, a.splits, hi, lo);       // (as in lora_few_kernel)
         uint16_t* h = a.h + tile.row0 * RP + i;
         *reinterpret_cast<uint2*>(h) = hi;
         *reinterpret_cast<uint2*>(h + a.total * RP) = lo;
