@@ -408,8 +408,8 @@ sb_status sb_fp4_gemm(sb_ctx* ctx, const uint8_t* a_codes, const uint8_t* a_scal
  *   call's own: rows starts[b] .. of its dense arguments.  max_new: at least every n.  Token p of
  *   request b lives in page table[b][p / page_tokens], slot p % page_tokens.
  * A request whose numbers do not fit (n < 0 or > max_new, rows outside the dense arguments, lens
- * < n, more tokens than its table row has pages, a page number outside the cache) is skipped as
- * far as they do not fit and SB_ERR_INVALID is latched.                                         */
+ * < n, more tokens than its table row has pages or than 2^31 - 65536, a page number outside the
+ * cache) is skipped as far as they do not fit and SB_ERR_INVALID is latched.                    */
 enum { SB_KV_INT8 = 0, SB_KV_E4M3 = 1, SB_KV8_BLOCK = 16 };
 typedef struct {                /* host struct, read during the call                             */
     void *k, *v;                /* device codes [pages][heads][page_tokens][dim], 16-byte aligned */

@@ -501,7 +501,7 @@ extern "C" sb_status sb_kv4_attention(sb_ctx* ctx, const sb_kv4_cache* cache, co
     if (q_heads <= 0 || q_heads % cache->heads) return sb_fail(ctx, SB_ERR_SHAPE, "kv4 attention: q_heads must be a multiple of the cache's heads");
     if (max_len < 1 || window < 0 || !(scale == scale))
         return sb_fail(ctx, SB_ERR_INVALID, "kv4 attention: max_len below 1, negative window or scale not a number");
-    const int64_t most = kv4_table_pages(cache) * cache->page_tokens;
+    const int64_t most = std::min(kv4_table_pages(cache) * cache->page_tokens, KV_MOST);
     if (max_len > most) max_len = most;
     if (!kv8_aligned16(Q) || !kv8_aligned16(O) || q_token_stride % 8 || q_head_stride % 8 || o_token_stride % 8 || o_head_stride % 8)
         return sb_fail(ctx, SB_ERR_SHAPE, "kv4 attention: strides that are multiples of 8 and 16-byte aligned bases");
@@ -518,7 +518,7 @@ extern "C" sb_status sb_kv4_attention(sb_ctx* ctx, const sb_kv4_cache* cache, co
     a.group = q_heads / cache->heads;
     a.by_group = KvDiv(a.group);
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    a.window = window >= (1ll << 30) ? 0 : (int)window;
+    a.window = window >= KV_MOST ? 0 : (int)window;
     a.st = ctx->dstate;
     if (max_new * a.group > k4_prompt_from(cache->dim)) return kv8_prompt(ctx, a, AT_E2M1, max_new, max_len);
     return cache->dim <= 64 ? rows_by_count<64>(ctx, a, max_new, max_len)

@@ -1,5 +1,6 @@
 // The 8-bit key/value cache: layout, argument checks, conversions.
 #pragma once
+#include <algorithm>
 #include "common.cuh"
 
 // Quotients of 31-bit numbers by a divisor that the host knows: with m = ceil(2^64 / d),
@@ -19,13 +20,17 @@ struct Kv8Geom {                 // the parts of sb_kv8_cache that kernels read
     const int32_t* table;
     int64_t table_stride, pages;
     int requests, heads, page_tokens, dim;
-    int most;                    // tokens a request may have: what its pages hold
+    int most;                    // tokens a request may have: what its pages hold, at most KV_MOST
     const int32_t* starts;
     const int32_t* lens;
     int64_t total;               // rows of the call's dense arguments
     int max_new;
     KvDiv page;                  // by page_tokens
 };
+
+// Tokens a request may have whatever its table holds, and windows that hide nothing: kernels look up to 12544 keys (two batches of
+// 16 steps of 4 warps, 32 keys each) past a request's last in 31 bits.
+constexpr int64_t KV_MOST = (1ll << 31) - (1 << 16);
 
 inline bool kv8_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -53,7 +58,7 @@ inline Kv8Geom kv8_geom(const sb_kv8_cache* c, int64_t total, const int32_t* sta
     g.requests = c->requests; g.heads = c->heads; g.page_tokens = c->page_tokens; g.dim = c->dim;
     g.starts = starts; g.lens = lens; g.total = total; g.max_new = (int)max_new;
     g.page = KvDiv(c->page_tokens);
-    g.most = (int)(kv8_table_pages(c) * c->page_tokens);
+    g.most = (int)std::min(kv8_table_pages(c) * c->page_tokens, KV_MOST);
     return g;
 }
 

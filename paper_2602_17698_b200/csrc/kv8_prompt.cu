@@ -882,7 +882,7 @@ bool pr_direct(const sb_ctx* ctx, const AtArgs& a, int64_t items, int64_t max_ne
     const int64_t full = (a.g.total * a.group / ROWS + a.g.requests) * a.g.heads, real = items < full ? items : full;
     if (items >= (1ll << 31) || items - real > 16 * (int64_t)ctx->sm_count) return false;
     int64_t keys = max_len;
-    if (a.window > 0 && keys > a.window + ROWS / a.group + 1 + SB_KV8_BLOCK) keys = a.window + ROWS / a.group + 1 + SB_KV8_BLOCK;
+    if (a.window > 0 && keys > (int64_t)a.window + ROWS / a.group + 1 + SB_KV8_BLOCK) keys = (int64_t)a.window + ROWS / a.group + 1 + SB_KV8_BLOCK;
     const int64_t steps = (keys + PR_KEYS - 1) / PR_KEYS;
     if (steps <= 8 || steps > 32) return steps <= 8;
     // the first row tiles of prompts have fewer keys than the last

@@ -270,7 +270,7 @@ sb_status at_rows_plan(sb_ctx* ctx, const char* what, AtArgs& a, int64_t max_new
     if (tiles >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "%s: too many query rows", what);
     // a share per resident CTA, fewer if there cannot be so many shares
     int64_t keys = max_len;
-    if (a.window > 0 && keys > a.window + S::ROWS + SB_KV8_BLOCK) keys = a.window + S::ROWS + SB_KV8_BLOCK;
+    if (a.window > 0 && keys > (int64_t)a.window + S::ROWS + SB_KV8_BLOCK) keys = (int64_t)a.window + S::ROWS + SB_KV8_BLOCK;
     const int64_t steps = (keys + AT_STEP - 1) / AT_STEP + 1;
     a.row_tiles = (int)row_tiles;
     a.by_row_tiles = KvDiv(a.row_tiles);
