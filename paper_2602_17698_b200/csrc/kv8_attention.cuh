@@ -38,6 +38,12 @@ constexpr float AT4_UP = 6.f, AT4_FAR = 14.f;
 // kv8_prompt.cu: many rows of one cache head on the tensor cores of the fifth generation, dim <= 128
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len);
 
+// Items of `rows` query rows that can have any, of all that the numbers of the call make: a request has a token at least, or none.
+inline int64_t at_real(const AtArgs& a, int rows, int64_t items) {
+    const int64_t most = (a.g.total * a.group / rows + std::min<int64_t>(a.g.requests, a.g.total)) * a.g.heads;
+    return items < most ? items : most;
+}
+
 #ifdef __CUDACC__
 // ---- who does what -------------------------------------------------------------------------------
 // An item is a tile of query rows (new tokens x query heads of one cache head) of a request and a

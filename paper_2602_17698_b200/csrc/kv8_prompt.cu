@@ -879,7 +879,7 @@ template <int ROWS>
 bool pr_direct(const sb_ctx* ctx, const AtArgs& a, int64_t items, int64_t max_new, int64_t max_len) {
     // Where most requests have fewer rows than the longest, most of these CTAs find nothing, a round of them in about 1 us: 63 requests of one
     // token and one of 900 (7000 such CTAs) 104 us and in shares 84, 15 and one of 500 (800) 38 and 47.
-    const int64_t full = (a.g.total * a.group / ROWS + a.g.requests) * a.g.heads, real = items < full ? items : full;
+    const int64_t real = at_real(a, ROWS, items);
     if (items >= (1ll << 31) || items - real > 16 * (int64_t)ctx->sm_count) return false;
     int64_t keys = max_len;
     if (a.window > 0 && keys > (int64_t)a.window + ROWS / a.group + 1 + SB_KV8_BLOCK) keys = (int64_t)a.window + ROWS / a.group + 1 + SB_KV8_BLOCK;
