@@ -223,7 +223,7 @@ def _library():
     """The library's context of the current stream, made once as a program does."""
     from paper_2602_17698_b200 import binding
     stream = torch.cuda.current_stream()
-    key = stream.cuda_stream
+    key = stream.device_index, stream.cuda_stream
     if key not in _contexts:
         _contexts[key] = binding.Context(stream=stream)
     return _contexts[key], binding
