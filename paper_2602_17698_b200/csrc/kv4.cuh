@@ -29,7 +29,7 @@ inline Kv8Geom kv4_geom(const sb_kv4_cache* c, int64_t total, const int32_t* sta
     g.table = c->table; g.table_stride = c->table_stride; g.pages = c->pages;
     g.requests = c->requests; g.heads = c->heads; g.page_tokens = c->page_tokens; g.dim = c->dim;
     g.starts = starts; g.lens = lens; g.total = total; g.max_new = (int)max_new;
-    g.page = KvDiv(c->page_tokens);
+    g.page = KvDiv(c->page_tokens); g.family = SBK_KV4;
     g.most = (int)std::min(kv4_table_pages(c) * c->page_tokens, KV_MOST);
     return g;
 }

@@ -144,7 +144,7 @@ kv4_rows_kernel(const AtArgs a) {
             const int key = block_key(batch);
             if (key >= k1) return -1;
             if (entry < 0 || entry >= a.g.pages) {
-                sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
+                sb_latch(a.st, SB_ERR_INVALID, SBK_KV4);
                 return -1;
             }
             return ((int64_t)entry * a.g.heads + head) * a.g.page_tokens + a.g.page.rem(key);

@@ -100,7 +100,7 @@ kv4_append_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvD
         }
     }
     const bool there = page >= 0 && page < g.pages;
-    if (!there) sb_latch(st, SB_ERR_INVALID, SBK_KV8);
+    if (!there) sb_latch(st, SB_ERR_INVALID, SBK_KV4);
     const int64_t at = (page * g.heads + head) * g.page_tokens + g.page.rem(tok);
     const int pitch = kv4_code_pitch(g.dim);
 #pragma unroll
@@ -108,7 +108,7 @@ kv4_append_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvD
         const Kv4Side& sd = k ? vs : ks;
         uint32_t scale = 0;
         uint2 codes = make_uint2(0, 0);
-        if (inside && !kv4_codes(w[k], by[k], codes, scale)) sb_latch(st, SB_ERR_NONFINITE, SBK_KV8);
+        if (inside && !kv4_codes(w[k], by[k], codes, scale)) sb_latch(st, SB_ERR_NONFINITE, SBK_KV4);
         uint32_t word = scale;
         word |= __shfl_down_sync(four, scale, 1) << 8;
         word |= __shfl_down_sync(four, word, 2) << 16;
@@ -162,7 +162,7 @@ kv4_read_kernel(const Kv8Geom g, const Kv4Side ks, const Kv4Side vs, const KvDiv
         if (i >= rq.n) break;
         if (r > 0) walk.next(g, b);
         if (!walk.there(g)) {
-            sb_latch(st, SB_ERR_INVALID, SBK_KV8);
+            sb_latch(st, SB_ERR_INVALID, SBK_KV4);
             continue;
         }
         const int64_t at = walk.at(g, head), to = ((int64_t)(rq.row0 + i) * g.heads + head) * g.dim + 8 * j;

@@ -26,6 +26,7 @@ struct Kv8Geom {                 // the parts of sb_kv8_cache that kernels read
     int64_t total;               // rows of the call's dense arguments
     int max_new;
     KvDiv page;                  // by page_tokens
+    int family;                  // SBK_KV8 or SBK_KV4: who latches
 };
 
 // Tokens a request may have whatever its table holds, and windows that hide nothing: kernels look up to 12544 keys (two batches of
@@ -57,7 +58,7 @@ inline Kv8Geom kv8_geom(const sb_kv8_cache* c, int64_t total, const int32_t* sta
     g.table = c->table; g.table_stride = c->table_stride; g.pages = c->pages;
     g.requests = c->requests; g.heads = c->heads; g.page_tokens = c->page_tokens; g.dim = c->dim;
     g.starts = starts; g.lens = lens; g.total = total; g.max_new = (int)max_new;
-    g.page = KvDiv(c->page_tokens);
+    g.page = KvDiv(c->page_tokens); g.family = SBK_KV8;
     g.most = (int)std::min(kv8_table_pages(c) * c->page_tokens, KV_MOST);
     return g;
 }
@@ -73,14 +74,14 @@ __device__ __forceinline__ bool kv8_request(const Kv8Geom& g, int b, Kv8Request&
     r.past = r.len - r.n;
     const bool ok = r.row0 >= 0 && n >= 0 && n <= g.max_new && r.row0 + n <= g.total && r.len >= n &&
                     r.len <= g.most;
-    if (!ok) sb_latch(st, SB_ERR_INVALID, SBK_KV8);
+    if (!ok) sb_latch(st, SB_ERR_INVALID, g.family);
     return ok;
 }
 // Page of a request's token block; false (and the status latched) where it lies outside the cache.
 __device__ __forceinline__ bool kv8_page(const Kv8Geom& g, int b, int page_index, int64_t& page, SbDeviceState* st) {
     page = g.table[(int64_t)b * g.table_stride + page_index];
     if (page >= 0 && page < g.pages) return true;
-    sb_latch(st, SB_ERR_INVALID, SBK_KV8);
+    sb_latch(st, SB_ERR_INVALID, g.family);
     return false;
 }
 

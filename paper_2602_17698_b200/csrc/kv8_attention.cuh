@@ -35,7 +35,8 @@ constexpr int AT_E2M1 = 2;
 // be above the reference before that moves (below 2^15)
 constexpr float AT4_UP = 6.f, AT4_FAR = 14.f;
 
-// kv8_prompt.cu: many rows of one cache head on the tensor cores of the fifth generation, dim <= 128
+// kv8_prompt.cu: many rows of one cache head on the tensor cores of the fifth generation; dim at most 128 over the 8-bit cache, 256 over
+// the 4-bit one
 sb_status kv8_prompt(sb_ctx* ctx, AtArgs a, int type, int64_t max_new, int64_t max_len);
 
 // Items of `rows` query rows that can have any, of all that the numbers of the call make: a request has a token at least, or none.

@@ -700,7 +700,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
                 const int key = k0 + j * PR_KEYS + SB_KV8_BLOCK * lane;
                 const int slot = a.g.page.rem(key);
                 const bool inside = lane < PR_BLOCKS && key < k1, fine = inside && entry >= 0 && entry < a.g.pages;
-                if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, SBK_KV8);
+                if (inside && !fine) sb_latch(a.st, SB_ERR_INVALID, a.g.family);
                 const int64_t at = ((int64_t)entry * a.g.heads + wk.head) * a.g.page_tokens + slot;
                 const unsigned blocks = (unsigned)__popc(__ballot_sync(0xffffffffu, fine));
                 entry = entry_of(j + 1);
@@ -807,7 +807,7 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
         t5_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM) : "memory");
     }
-    if (threadIdx.x == 0 && *abort_flag) sb_latch(a.st, SB_ERR_TIMEOUT, SBK_KV8);
+    if (threadIdx.x == 0 && *abort_flag) sb_latch(a.st, SB_ERR_TIMEOUT, a.g.family);
 }
 
 // The pieces of an item that lies in several shares, in their order. Block (c, y): the item that the
@@ -896,7 +896,7 @@ template <int TYPE, int DP>
 sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len) {
     using S = PrShape<DP>;
     const int64_t row_tiles = (max_new * a.group + S::ROWS - 1) / S::ROWS, n = row_tiles * a.g.requests;
-    if (n >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "kv8 attention: too many query rows");
+    if (n >= (1ll << 31)) return sb_fail(ctx, SB_ERR_SHAPE, "%s attention: too many query rows", TYPE == AT_E2M1 ? "kv4" : "kv8");
     int64_t keys = max_len;
     if (a.window > 0 && keys > a.window + max_new + PR_KEYS) keys = a.window + max_new + PR_KEYS;
     // one share per SM, fewer if there cannot be so many shares
