@@ -836,9 +836,9 @@ class Context:
 
     # ---- rotary positions -------------------------------------------------------------------
     def rotary(self, table: RotaryTable, q: torch.Tensor, k: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
-               lens: Optional[torch.Tensor] = None, max_new: int = 0, positions: Optional[torch.Tensor] = None, inverse: bool = False, out=None):
+               lens: Optional[torch.Tensor] = None, max_new: Optional[int] = None, positions: Optional[torch.Tensor] = None, inverse: bool = False, out=None):
         """Turns q and, if given, k ([tokens][heads][dim], bf16 or fp32) by their positions: those of the requests' new tokens (starts, lens, max_new
-        as in the cache calls), or `positions`, int32 [tokens].  In place, or into `out` (a tensor for each); inverse: the way
+        as in the cache calls; max_new None: any number of q's rows), or `positions`, int32 [tokens].  In place, or into `out` (a tensor for each); inverse: the way
         back of gradients.  Returns (q, k) as written."""
         dtype = q.dtype
         if dtype is not _BF16 and dtype is not _F32:
@@ -864,12 +864,16 @@ class Context:
             if starts.dtype is not _I32 or lens.dtype is not _I32 or starts.numel() != requests + 1 or not starts.is_contiguous() or not lens.is_contiguous():
                 raise ValueError("starts: contiguous int32 [requests + 1], lens: contiguous int32 [requests]")
             at, s, n = None, _dev(starts), _dev(lens)
+            if max_new is None:
+                max_new = tokens
         else:
             if starts is not None or lens is not None:
                 raise ValueError("rotary: positions, or starts and lens")
             if positions.dtype is not _I32 or positions.shape != (tokens,) or not positions.is_contiguous():
                 raise ValueError("positions: contiguous int32 [tokens]")
             requests, at, s, n = 0, _dev(positions), None, None
+            if max_new is None:
+                max_new = 0
         self._check(lib().sb_rotary(self._h, table.struct(inverse), parts, 1 if k is None else 2, dim, dtype is _F32, tokens, at, s, n,
                                     requests, max_new))
         return yq, yk
