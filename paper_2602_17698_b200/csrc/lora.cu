@@ -46,12 +46,16 @@ __device__ __forceinline__ void lo_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
 __device__ __forceinline__ uint4 lo_ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
 struct LoTile { int64_t row0; int rows, adapter; };
-// The rows of a request and its adapter; no rows (and the status latched) where its numbers do not fit.
+// The rows of a request and its adapter; no rows (and the status latched) where its numbers do not fit. L2: by way of L2, as a kernel
+// has to that reads before its own wait. With few rows a block's warps find in L1 what the first has read (64 requests of one row 9.4 us
+// and so 8.7); lora_down_kernel was faster by way of L2 (6 x 1500 rows of rank 16 74.7 us and 69.7, both kernels).
+template <bool L2>
 __device__ __forceinline__ LoTile lo_request(const LoArgs& a, int b) {
+    auto number = [](const int32_t* p) -> int { return L2 ? __ldcg(p) : *p; };
     LoTile t;
-    t.row0 = __ldcg(a.starts + b);
-    t.adapter = __ldcg(a.ids + b);
-    const int64_t n = (int64_t)__ldcg(a.starts + b + 1) - t.row0;
+    t.row0 = number(a.starts + b);
+    t.adapter = number(a.ids + b);
+    const int64_t n = (int64_t)number(a.starts + b + 1) - t.row0;
     const bool fits = t.row0 >= 0 && n >= 0 && n <= a.max_new && t.row0 + n <= a.total;
     t.rows = fits ? (int)n : 0;
     if (!fits || t.adapter < -1 || t.adapter >= a.adapters) {
@@ -61,9 +65,9 @@ __device__ __forceinline__ LoTile lo_request(const LoArgs& a, int b) {
     return t;
 }
 // Tile number `tile`; all threads of the block take part. rows = 0: there is no such tile.
-template <int TM, int THREADS>
+template <int TM, int THREADS, bool L2>
 __device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
-    if (a.direct) return lo_request(a, tile);
+    if (a.direct) return lo_request<L2>(a, tile);
     __shared__ int sums[THREADS / 32];
     __shared__ LoTile found;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -71,7 +75,7 @@ __device__ __forceinline__ LoTile lo_tile(const LoArgs& a, int tile) {
     int64_t before = 0;                                              // 64 bits: starts that go down may count rows more than once
     for (int base = 0; base < a.requests; base += THREADS) {
         LoTile t{0, 0, -1};
-        if (base + threadIdx.x < a.requests) t = lo_request(a, base + threadIdx.x);
+        if (base + threadIdx.x < a.requests) t = lo_request<L2>(a, base + threadIdx.x);
         const int mine = (t.rows + TM - 1) / TM;
         int x = mine;
 #pragma unroll
@@ -318,7 +322,7 @@ lora_few_kernel(const LoArgs a, const int wide) {
     uint16_t* held = reinterpret_cast<uint16_t*>(lm_smem + S::RING + S::SUMS);     // H: [hi, lo][16][RP + 8]
     sb_let_next();
     sb_after_previous();
-    const LoTile tile = lo_tile<16, 256>(a, blockIdx.x / a.splits);
+    const LoTile tile = lo_tile<16, 256, false>(a, blockIdx.x / a.splits);
     const int rank = blockIdx.x % a.splits;                          // of the block in its cluster
     if (tile.rows <= 0) return;
     const int64_t c0 = min(a.out, rank * a.columns), c1 = min(a.out, c0 + a.columns);
@@ -476,7 +480,7 @@ lora_down_kernel(const LoArgs a) {
     // in this order: what the next kernel reads before this one's end (all but H) is there
     sb_after_previous();
     sb_let_next();
-    const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x / a.splits);
+    const LoTile tile = lo_tile<LM_ROWS, 256, true>(a, blockIdx.x / a.splits);
     const int part = blockIdx.x % a.splits;
     if (tile.rows <= 0 || tile.adapter < 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -588,7 +592,7 @@ lora_up_kernel(const LoArgs a, const int wide) {
     // starts, ids, B and base are read before this kernel's own wait: lora_down_kernel, which lets it in, has waited for whoever wrote
     // them. They come by way of L2 (.cg); base in narrower pieces can only be copied by way of L1, and waits.
     if (wide < 16) sb_after_previous();
-    const LoTile tile = lo_tile<LM_ROWS, 256>(a, blockIdx.x);
+    const LoTile tile = lo_tile<LM_ROWS, 256, true>(a, blockIdx.x);
     const int64_t c0 = (int64_t)blockIdx.y * a.columns, c1 = min(a.out, c0 + a.columns);
     if (tile.rows <= 0 || tile.adapter < 0) {
         sb_after_previous();
