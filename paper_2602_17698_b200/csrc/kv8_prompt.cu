@@ -873,8 +873,9 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
 // tiles where the CTAs end about together, the longest first: what equal shares would win is less than what plan and sum take, 10
 // tiles. Heads of 128, query heads four times the cache's 8, us, in shares and so, 4 and 8 bits: 1 request of 200 tokens 20.1 and
 // 15.4, 20.3 and 15.9; 8 of 400 67 and 55, 72 and 57; 1 of 1500 58 and 37, 61 and 39; 8 of 900 166 and 131, 182 and 137; 1 of 4000 183 and
-// 154, 198 and 166; 1 of 512 behind 1500 45 and 47, 47 and 51; 4 of 1024 behind 4000 329 and 350, 360 and 383 (the last two with the
-// kernel's first form).
+// 154, 198 and 166; 1 of 512 behind 1500 (in shares by this rule) 45 and 44, 48 and 48; 4 of 1024 behind 4000 (the same) 325 and 318, 365 and 351.
+// Heads of 64: 1 of 1500 47 and 34, 51 and 34; 8 of 900 128 and 118, 145 and 112; 1 of 4000 153 and 141, 172 and 144; 1 of 512 behind 1500
+// 37 and 42, 39 and 43. Heads of 256, 4 bits: 1 of 200 25 and 19, 1 of 1500 137 and 95, 8 of 900 481 and 334.
 template <int ROWS>
 bool pr_direct(const sb_ctx* ctx, const AtArgs& a, int64_t items, int64_t max_new, int64_t max_len) {
     // Where most requests have fewer rows than the longest, most of these CTAs find nothing, a round of them in about 1 us: 63 requests of one

@@ -277,7 +277,10 @@ sb_status at_rows_plan(sb_ctx* ctx, const char* what, AtArgs& a, int64_t max_new
     // Short items: a CTA each, without the search for a share, scratch and the sum of pieces. Heads of 128, us, in shares and so, 4 and
     // 8 bits: 22 requests of 20 rows in 70 tokens 13.9 and 7.2, 15.4 and 9.1; 1 of 4 rows and 8 heads in 200 8.7 and 4.6, 9.3 and
     // 5.8; in 500 9.5 and 6.1, 10.2 and 8.0; in 900 9.7 and 9.6, 10.4 and 13.0; 48 in 900 21.9 and 15.6, 25.2 and 19.3; in
-    // 1500 28 and 22, 34 and 28; 60 in 1500 (a few items more than fit at once) 32.5 and 32, 40 and 48.
+    // 1500 28 and 22, 34 and 28; 60 in 1500 (a few items more than fit at once) 32.5 and 32, 40 and 48. Heads of other sizes, 4 rows and 8
+    // heads: 1 in 500 of 64 8.5 and 5.2, 9.7 and 7.0, of 80 9.4 and 6.9, 10.5 and 9.2, of 208 11.9 and 10.0, 13.5 and 13.1, of 256 11.9 and
+    // 8.6, 12.8 and 11.1; 4 bits, 1 in 1000 of 64 8.9 and 7.5, of 80 9.5 and 10.8, of 208 13.8 and 15.8, of 256 13.8 and 13.3, 48 in 1000
+    // 18.6 and 13.6, 25.6 and 18.8, 52.7 and 36.8, 45.7 and 31.2.
     // Not where most of very many CTAs would find nothing (slots without a request's tokens; us in shares and so): heads of 128, 8 cache
     // heads, one of 512 slots in 60 tokens 6.6 and 5.7, 7.7 and 6.0, in 500 11.3 and 6.5, 11.8 and 8.6; one of 1024 in 60 7.9 and 10.3, 9.0
     // and 10.4, in 500 12.7 and 10.4, 13.2 and 10.6; one of 4096 in 60 15.6 and 38, 17 and 37, in 500 20 and 38, 21 and 38.

@@ -4,8 +4,8 @@
 
 // `early`: the kernel's blocks may become resident before the one ahead of it in the stream has ended, so they call sb_after_previous
 // before they touch memory that another kernel writes, or writes that another reads, and do not read such memory by .nc or __ldg, which
-// want it unchanged for as long as the kernel is there. A kernel that reads before its own wait (lora_up_kernel) has to be let in by one
-// that calls sb_after_previous BEFORE sb_let_next (lora_down_kernel). cluster: blocks along x.
+// want it unchanged for as long as the kernel is there. A kernel that reads before its own wait what that one does not write (lora_up_kernel,
+// kv8_prompt_sum_kernel) has to be let in by one that waits BEFORE it lets the next in (lora_down_kernel, kv8_prompt_kernel). cluster: blocks along x.
 template <typename... P>
 sb_status sb_launch(sb_ctx* ctx, void (*kernel)(P...), dim3 grid, unsigned threads, int smem, int cluster, bool early, P... args) {
     if (smem > 40 * 1024) SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);

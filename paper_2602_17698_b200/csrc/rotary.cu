@@ -6,8 +6,8 @@
 // them side by side. One read and one write an element. An angle is position times frequency in
 // 64 bits, with the products' rounding errors by fma: exact to fp32 for every 32-bit position. The bytes bound large calls, the
 // chain of dependent reads small ones, so the first heads are fetched before the positions are known. Measured, bf16, 32 query and 8
-// key heads of 128: 6 requests of up to 2048 tokens 41 us, 5.2 TB/s (a plain copy of as much: 33); 64 single tokens 4.3 us. 8 of up to
-// 700 tokens, 16 + 16 heads of 80, neighbouring pairs backwards, 12 us, where the blocks of one round still start and end apart.
+// key heads of 128: 6 requests of up to 2048 tokens 41 us, 5.2 TB/s (a plain copy of as much: 33); 64 single tokens 4.2 us, where a form
+// whose blocks shared one row's angles took 3.3 (and 18 in the next case, 40 in the first). 8 of up to 700 tokens, 16 + 16 heads of 80, neighbouring pairs backwards, 12 us, where the blocks of one round still start and end apart.
 #include "kv8.cuh"
 #include "launch.cuh"
 
