@@ -79,3 +79,81 @@ def test_adapters_behind_rotary_in_place(ctx, new, columns, dtype):
         ctx.sync()
         assert torch.equal(*got)
         got.clear()
+
+
+@pytest.mark.parametrize("ahead", ["kernel", "copy", "fill", "two streams"])
+def test_captured_behind_other_streams(ahead):
+    """A graph in which the context's stream follows others' kernels, copies and fills, and others follow it, against the same calls one by one."""
+    from paper_2602_17698_b200.binding import Context, Kv4Cache, LoraAdapters
+    torch.cuda.set_device(0)
+    main, other, side = (torch.cuda.Stream() for _ in range(3))
+    T, heads, dim, R = 300, 2, 64, 3
+    starts, lens, ids = _ints([0, 130, 131, T]), _ints([200, 31, 169]), _ints([1, -1, 0])
+    table = torch.arange(3 * 13, dtype=torch.int32, device=DEV).view(3, 13)
+    turn = _turn(dim)
+    adapters = LoraAdapters(torch.randn(2, 24, heads * dim, device=DEV).bfloat16(), torch.randn(2, 70, 24, device=DEV).bfloat16())
+    source, plus = torch.empty(T, heads, dim, dtype=torch.bfloat16, device=DEV), torch.empty(T, heads, dim, dtype=torch.bfloat16, device=DEV)
+
+    class Run:
+        def __init__(self):
+            self.ctx = Context(stream=side)
+            self.x = torch.empty_like(source)
+            self.base = torch.zeros(T, 70, dtype=torch.bfloat16, device=DEV)
+            self.cache = Kv4Cache.empty(39, heads, 16, dim, table)
+            self.out, self.sum = torch.empty_like(source), torch.empty_like(source)
+
+        def step(self):
+            main.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(main):
+                if ahead == "fill":
+                    self.x.zero_()
+                else:
+                    self.x.copy_(source)
+                if ahead == "kernel":
+                    self.x.mul_(2)
+            if ahead == "two streams":
+                other.wait_stream(main)
+                with torch.cuda.stream(other):
+                    self.x[100:].add_(plus[100:])
+                with torch.cuda.stream(main):
+                    self.x[:100].mul_(3)
+                side.wait_stream(other)
+            side.wait_stream(main)
+            with torch.cuda.stream(side):
+                c = self.ctx
+                c.rotary(turn, self.x, None, starts, lens, 200)
+                c.kv4_append(self.cache, self.x, self.x, starts, lens, 200)
+                c.kv4_attention(self.cache, self.x, starts, lens, 200, 200, out=self.out)
+                c.lora_add(adapters, self.x.flatten(1), self.base, ids, starts, 200)
+            main.wait_stream(side)
+            with torch.cuda.stream(main):
+                torch.add(self.out, self.x, out=self.sum)
+            torch.cuda.current_stream().wait_stream(main)
+
+    def new():
+        source.copy_(torch.randn(source.shape, device=DEV))
+        plus.copy_(torch.randn(source.shape, device=DEV))
+
+    plain, captured = Run(), Run()
+    new()
+    torch.cuda.synchronize()
+    captured.step()
+    torch.cuda.synchronize()
+    captured.base.zero_()
+    graph, at = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=at):
+        captured.step()
+    for _ in range(8):
+        new()
+        torch.cuda.synchronize()
+        plain.step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in ("x", "base", "out", "sum"):
+            assert torch.equal(getattr(plain, name), getattr(captured, name)), name
+        assert torch.equal(plain.cache.k, captured.cache.k) and torch.equal(plain.cache.v_scale, captured.cache.v_scale)
+    del graph
+    for r in (plain, captured):
+        r.ctx.sync()
+        r.ctx.close()
