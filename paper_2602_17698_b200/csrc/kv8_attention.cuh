@@ -137,10 +137,6 @@ __device__ __forceinline__ uint2 at_lds64(unsigned a) {
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
-// Of a kernel that was launched before the one ahead of it in the stream has ended: waits for that
-// end (all blocks do, so that no later kernel passes either); lets the next such kernel be launched.
-__device__ __forceinline__ void at_after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void at_let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ float at_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

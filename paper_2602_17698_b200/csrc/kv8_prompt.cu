@@ -32,6 +32,7 @@
 // converted for 128 rows only): 0.88 ms, a third of the products' rate.
 #include "kv8_attention.cuh"
 #include "kv4.cuh"
+#include "launch.cuh"
 #include "tensor5.cuh"
 
 namespace {
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(1024)
 kv8_prompt_plan_kernel(const AtArgs a, const PrWork w) {
     __shared__ long long warp_sum_at[32], total_at;
     const int n = a.row_tiles * a.g.requests, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    at_let_next();
+    sb_let_next();
     long long before = 0;
     for (int base = 0; base < n; base += 1024) {
         const int i = base + threadIdx.x;
@@ -288,8 +289,8 @@ kv8_prompt_kernel(const AtArgs a, const PrWork work) {
     const int D = a.g.dim;
     const int pitch = TYPE == AT_E2M1 ? kv4_code_pitch(D) : D, spitch = kv4_scale_pitch(D);        // bytes of a token's codes and scales
     AtWalk<S::ROWS, PR_KEYS, PR_EXTRA> wk;
-    at_after_previous();
-    at_let_next();                           // its blocks find room when these end, and wait for that
+    sb_after_previous();
+    sb_let_next();                           // its blocks find room when these end, and wait for that
     if (DIRECT) {
         // an item of its own, the requests' last row tiles, which have the most keys, first
         const int i = blockIdx.x / a.g.heads, before = i / a.g.requests, row_tile = (i - before * a.g.requests + 1) * a.row_tiles - 1 - before;
@@ -829,7 +830,7 @@ kv8_prompt_sum_kernel(const AtArgs a, const PrWork w) {
     AtItem it{};
     if (mine) it = at_item<ROWS, PR_KEYS>(a, s.x);
     const int r = 32 * blockIdx.y + threadIdx.x / 8, quad0 = threadIdx.x % 8;
-    at_after_previous();
+    sb_after_previous();
     if (!mine || r >= it.nrow) return;
     const int c1 = (int)((from + it.steps + PR_EXTRA - 1) / share);
     float m = -INFINITY, l = 0.f;
@@ -908,22 +909,7 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     a.by_row_tiles = KvDiv(a.row_tiles);
     a.direct = pr_direct<S::ROWS>(ctx, a, n * a.g.heads, max_new, max_len);
     auto* kernel = a.direct ? kv8_prompt_kernel<TYPE, DP, true> : kv8_prompt_kernel<TYPE, DP, false>;
-    SB_FUNC_ATTR(ctx, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.stream = ctx->stream;
-    cfg.attrs = &early;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)(a.direct ? n * a.g.heads : w.ctas));
-    cfg.blockDim = dim3(PR_THREADS);
-    cfg.dynamicSmemBytes = S::SMEM;
-    if (a.direct) {
-        SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, a, w));
-        SB_LAUNCHED(ctx);
-        return SB_OK;
-    }
+    if (a.direct) return sb_launch(ctx, kernel, dim3((unsigned)(n * a.g.heads)), PR_THREADS, S::SMEM, 1, true, a, w);
     const size_t rows = (size_t)w.ctas * 2 * S::ROWS;
     void* arena;
     const sb_status s = sb_scratch(ctx, Carver::need({((size_t)n + 1) * 8, (size_t)w.ctas * 16, 16, rows * a.g.dim * 4, rows * 8}), &arena);
@@ -937,17 +923,10 @@ sb_status prompt_launch(sb_ctx* ctx, AtArgs a, int64_t max_new, int64_t max_len)
     kv8_prompt_plan_kernel<S::ROWS><<<1, 1024, 0, ctx->stream>>>(a, w);
     SB_LAUNCHED(ctx);
     // The other two are sent off while the kernel before them still runs and wait on the device for its
-    // end (at_after_previous), which hides their launches.
-    SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, a, w));
-    SB_LAUNCHED(ctx);
-    if (w.ctas > 1) {
-        cfg.gridDim = dim3((unsigned)(w.ctas - 1), S::ROWS / 32);
-        cfg.blockDim = dim3(256);
-        cfg.dynamicSmemBytes = 0;
-        SB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kv8_prompt_sum_kernel<DP>, a, w));
-        SB_LAUNCHED(ctx);
-    }
-    return SB_OK;
+    // end, which hides their launches.
+    const sb_status t = sb_launch(ctx, kernel, dim3((unsigned)w.ctas), PR_THREADS, S::SMEM, 1, true, a, w);
+    if (t != SB_OK || w.ctas <= 1) return t;
+    return sb_launch(ctx, kv8_prompt_sum_kernel<DP>, dim3((unsigned)(w.ctas - 1), S::ROWS / 32), 256, 0, 1, true, a, w);
 }
 
 }  // namespace
